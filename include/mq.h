@@ -665,6 +665,140 @@ mq_status mq_transpose_i8(const int8_t* x, int64_t rows, int64_t cols, int64_t l
                           int8_t* y, void* stream);
 
 /*
+ * Text generation over a key/value cache in pages.  The cache holds, for
+ * each of `pages` pages of `page` token slots, the keys of G heads as rows of
+ * D int8 codes and the values transposed, so that the codes of one channel
+ * over a page's tokens are contiguous (the layout of mq_transpose_i8, which
+ * the products with the probabilities read):
+ *   k  device int8 [pages][G][page][D]     v  device int8 [pages][G][D][page]
+ * A sequence's key position p lies in slot p % page of the page that entry
+ * p / page of its page list names.
+ *   0 <= pages < 2^31; page a power of two in [16, 1024]; 1 <= G <= 1024; D a
+ *   multiple of 16 in [16, 256]; k and v 16-byte aligned.
+ */
+typedef struct mq_kv_cache {
+    int8_t* k;
+    int8_t* v;
+    int64_t pages;
+    int32_t page;
+    int32_t G;
+    int32_t D;
+} mq_kv_cache;
+
+/*
+ * mq_kv_batch -- the sequences of a call, B of them: one new token each in
+ * generation, a chunk of a prompt, or a mixture.  Sequence b owns the token
+ * rows [starts[b], starts[b+1]) of the call's T rows (starts[0] = 0; rows
+ * from starts[B] on belong to nobody and are left as they were), and lens[b]
+ * is its length with these tokens in it, so row t has the position
+ *   pos(t) = lens[b] - (starts[b+1] - t).
+ *   starts  device int32 [B + 1], ascending
+ *   lens    device int32 [B]
+ *   table   device int32 [B][ld], page indices; entries past the sequence's
+ *           last page are not read as long as lens[b] <= ld * page
+ *   0 <= B < 2^26, 0 <= ld <= 2^31, B * ld < 2^40
+ * These arrays are read on the device, so their contents cannot be refused:
+ * a position that is negative, past the list (>= ld * page) or on a page
+ * index outside [0, pages) is no place in the cache -- nothing is written
+ * there and no query sees it.
+ */
+typedef struct mq_kv_batch {
+    const int32_t* starts;
+    const int32_t* lens;
+    const int32_t* table;
+    int64_t B;
+    int64_t ld;
+} mq_kv_batch;
+
+/*
+ * mq_rope_append -- what a decoder block does with its projections before
+ * attending over a cache: the query and key codes of T new tokens are rotated
+ * by the angles of their positions, the keys (8-bit codes) and the values
+ * written to their places in the cache.  Rotation and requantization are
+ * those of mq_rope_apply, bit for bit, with each token's own position:
+ *   u = a (x - z) of the head's dimension i, w of i + D/2,
+ *   y_i = u cos - w sin,  y_{i+D/2} = w cos + u sin
+ *   q      device int16, row t at q + t * ldq: H heads of D
+ *   k      device int16, row t at k + t * ldk: G heads of D
+ *   v      device int8,  row t at v + t * ldv: G heads of D, copied
+ *   angles device fp64 [positions][D/2][2], cos and sin per position and
+ *          pair (mq_rope_table with pos0 = 0), or NULL: no rotation, the
+ *          codes are only requantized
+ *   positions  rows of angles (ignored when NULL); a token at a position
+ *          outside [0, positions) is left out altogether
+ *   q_out  device int16, row t at q_out + t * ldo (16-bit codes); may be q
+ *          itself with ldo == ldq
+ *   aq, zq / aqo, zqo  format of q and q_out (int16 zero-points)
+ *   ak, zk / ako, zko  format of k (int16) and of the cached keys (int8)
+ *   0 <= T < 2^26; H a multiple of G, H <= 1024, (T + B) (H + G) D < 2^36;
+ *   ldq, ldo >= H * D; ldk, ldv >= G * D, all < 2^40; two tokens must not share a place in the cache.
+ * Any alignment of q, k, v and q_out is taken; rows of whole 16-byte chunks
+ * are the faster ones.
+ */
+mq_status mq_rope_append(const int16_t* q, int64_t ldq, const int16_t* k, int64_t ldk,
+                         const int8_t* v, int64_t ldv, int64_t T, int32_t H, float aq, int32_t zq,
+                         float aqo, int32_t zqo, float ak, int32_t zk, float ako, int32_t zko,
+                         const double* angles, int64_t positions, const mq_kv_cache* cache,
+                         const mq_kv_batch* batch, int16_t* q_out, int64_t ldo, void* stream);
+
+/* Key positions per block of mq_paged_attn, and the weight of a block's
+ * largest logit. */
+#define MQ_ATTN_BLOCK 128
+#define MQ_ATTN_ONE 32512
+
+/*
+ * mq_paged_attn -- attention of the new tokens of each sequence over its
+ * cached keys and values (the new tokens' own among them: append first), in
+ * one pass, scores and probabilities never in memory.  Query head h reads
+ * head h / (H / G) of the cache.  The row at position pos sees the keys
+ *   j <= pos  and, with a sliding window, (j > pos - window or j < sinks)
+ * that have a place in the cache.  With q's codes in format (q_scale, q_zp),
+ *   c_j   = sum_d (q_d - q_zp) * k_jd          exact (a key zero-point would
+ *           add the same to every key of a row and drops out)
+ *   sigma = q_scale * k_scale * logit_scale    (fp64)
+ *   in every aligned block of MQ_ATTN_BLOCK positions, m = max c_j over the
+ *   keys seen there:
+ *     W_j = rint(MQ_ATTN_ONE * exp(sigma * (c_j - m)))
+ *     S_d = sum_j W_j * (v_jd - v_zp),  Z = sum_j W_j     exact
+ *   over the blocks, M = the largest m, f = exp(sigma * (m - M)), fp64:
+ *     y_d = v_scale * (sum f S_d) / (sum f Z)
+ *   and the output is y's code, clamp(rint(y / out_scale) + out_zp).
+ * Weights are integers of 15 bits relative to their block, as the paper
+ * keeps non-linear operators' activations at 16 bits; relative to a block
+ * rather than the row, long flat rows keep them.  exp and the fp64 sums are
+ * evaluated within 2^-46, so a weight or code that lies nearer than that to
+ * a rounding tie may fall on either side of it; nothing else depends on how
+ * the work is divided.  A row that sees nothing gets the code of 0.
+ *   q      device int16, row t at q + t * ldq: H heads of D
+ *   y      device int8 or int16 (out_bits 8 or 16), row t at y + t * ldy;
+ *          must not overlap q or the cache
+ *   window 0: none, else >= 1; sinks >= 0 (without a window not used)
+ *   max_len  the longest sequence as far as the host knows, or 0 (ld * page):
+ *          how many parts the keys are split into goes by it, results do not
+ *   workspace  device, 256-byte aligned, any contents, overwritten; calls
+ *          that may run at the same time must not share it.  With fewer
+ *          than mq_paged_attn_workspace_bytes bytes (or NULL) the keys are
+ *          split into fewer parts.
+ *   0 <= T < 2^26; H a multiple of G, H <= 1024, (T + B) (H + G) D < 2^36;
+ *   ldq, ldy >= H * D, < 2^40;
+ *   scales finite and > 0, sigma <= 1024; q_zp int16, v_zp int8, out_zp in
+ *   out_bits' range; window, sinks, max_len, workspace_bytes >= 0.
+ */
+mq_status mq_paged_attn(const int16_t* q, int64_t ldq, int64_t T, int32_t H, float q_scale,
+                        int32_t q_zp, const mq_kv_cache* cache, float k_scale, float v_scale,
+                        int32_t v_zp, const mq_kv_batch* batch, float logit_scale, int64_t window,
+                        int64_t sinks, float out_scale, int32_t out_zp, int32_t out_bits, void* y,
+                        int64_t ldy, int64_t max_len, void* workspace, int64_t workspace_bytes,
+                        void* stream);
+
+/* Workspace bytes mq_paged_attn can use for these sizes (0: the keys are not
+ * split; -1: invalid arguments).  Depends on the arguments alone and is at
+ * most MQ_ATTN_MAX_WORKSPACE. */
+#define MQ_ATTN_MAX_WORKSPACE (64 << 20)
+int64_t mq_paged_attn_workspace_bytes(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D,
+                                      int64_t max_len);
+
+/*
  * mq_dequant -- inverse of Eq.(4): y = alpha * (float)(q - zp), one exact
  * integer subtraction and one fp32 multiply.
  *   q      device int8 (bits 8) or int16 (bits 16) [numel]

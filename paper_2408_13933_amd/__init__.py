@@ -22,6 +22,8 @@ __all__ = [
     "PATH_AUTO", "PATH_DECODE", "PATH_PREFILL", "PATH_GENERIC", "MAX_K",
     "PATH_PREFILL_TILE0", "PREFILL_TILES", "prefill_tile_path", "mq_probe_read",
     "mq_qlinear_group", "MAX_GROUP", "QLinearOut", "mq_qlinear_dequant",
+    "mq_rope_append", "mq_paged_attn", "mq_paged_attn_workspace_bytes", "KVCache", "KVBatch",
+    "ATTN_BLOCK", "ATTN_ONE",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -69,6 +71,21 @@ class QLinearOut(ctypes.Structure):
                 ("w_zp", ctypes.c_void_p), ("w_colsum", ctypes.c_void_p),
                 ("bias", ctypes.c_void_p), ("N", ctypes.c_int64), ("out_scale", ctypes.c_float),
                 ("out_zp", ctypes.c_int32), ("y_q", ctypes.c_void_p)]
+
+
+ATTN_BLOCK, ATTN_ONE = 128, 32512  # MQ_ATTN_BLOCK, MQ_ATTN_ONE
+
+
+class KVCache(ctypes.Structure):
+    """mq_kv_cache of mq.h: a paged key/value cache."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("pages", ctypes.c_int64),
+                ("page", ctypes.c_int32), ("G", ctypes.c_int32), ("D", ctypes.c_int32)]
+
+
+class KVBatch(ctypes.Structure):
+    """mq_kv_batch of mq.h: the sequences of a call."""
+    _fields_ = [("starts", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("table", ctypes.c_void_p), ("B", ctypes.c_int64), ("ld", ctypes.c_int64)]
 
 
 def lib():
@@ -144,7 +161,16 @@ def lib():
                                      c_i32, c_p]
     L.mq_qlinear_group.argtypes = [c_p, c_p, c_i64, c_i64, c_i32, c_f, c_i32, c_i32,
                                    ctypes.POINTER(QLinearOut), c_i32, c_i32, c_p]
-    for name in ("mq_qlinear_dequant", "mq_qlinear_group", "mq_probe_read", "mq_attn_matmul", "mq_transpose_i8", "mq_act_params", "mq_fold_weights", "mq_fold_acts", "mq_quantize_act",
+    L.mq_rope_append.argtypes = [c_p, c_i64, c_p, c_i64, c_p, c_i64, c_i64, c_i32, c_f, c_i32, c_f,
+                                 c_i32, c_f, c_i32, c_f, c_i32, c_p, c_i64,
+                                 ctypes.POINTER(KVCache), ctypes.POINTER(KVBatch), c_p, c_i64,
+                                 c_p]
+    L.mq_paged_attn_workspace_bytes.argtypes = [c_i64, c_i64, c_i32, c_i32, c_i32, c_i64]
+    L.mq_paged_attn_workspace_bytes.restype = c_i64
+    L.mq_paged_attn.argtypes = [c_p, c_i64, c_i64, c_i32, c_f, c_i32, ctypes.POINTER(KVCache), c_f,
+                                c_f, c_i32, ctypes.POINTER(KVBatch), c_f, c_i64, c_i64, c_f, c_i32,
+                                c_i32, c_p, c_i64, c_i64, c_p, c_i64, c_p]
+    for name in ("mq_rope_append", "mq_paged_attn", "mq_qlinear_dequant", "mq_qlinear_group", "mq_probe_read", "mq_attn_matmul", "mq_transpose_i8", "mq_act_params", "mq_fold_weights", "mq_fold_acts", "mq_quantize_act",
                  "mq_pack_weights", "mq_qlinear", "mq_qlinear_ex", "mq_qlinear_ws", "mq_dequant",
                  "mq_qlinear_noalloc",
                  "mq_pack_weights_asym", "mq_act_rowsum", "mq_quantize_act_rowsum",
@@ -840,6 +866,113 @@ def mq_probe_read(buf, blocks: int, waves: int, unroll: int = 8, sink=None, stre
                                                      (blocks * waves,)),
                                _stream_ptr(stream)), "mq_probe_read")
     return sink
+
+
+def _rows(t, dtype, name, shape=None):
+    """Pointer and row stride (elements) of a [rows][cols] view whose rows are
+    contiguous."""
+    if not isinstance(t, (_torch_mod or _torch()).Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a 2-d view with contiguous rows")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+    rows, cols = t.shape
+    ld = t.stride(0) if rows > 1 else cols
+    if ld < cols:
+        raise ValueError(f"{name} must have rows that do not overlap")
+    return t.data_ptr(), ld
+
+
+def _kv_args(k_cache, v_cache, starts, lens, pages):
+    """(KVCache, KVBatch) of the cache tensors k [pages][G][page][D], v
+    [pages][G][D][page] and the batch's int32 tensors."""
+    torch = _torch_mod or _torch()
+    if k_cache.dim() != 4 or lens.dim() != 1 or pages.dim() != 2:
+        raise ValueError("k_cache must be [pages][G][page][D], lens [B], pages [B][entries]")
+    n, G, page, D = k_cache.shape
+    B = lens.shape[0]
+    c = KVCache(_dev_ptr(k_cache, torch.int8, "k_cache"),
+                _dev_ptr(v_cache, torch.int8, "v_cache", (n, G, D, page)), n, page, G, D)
+    b = KVBatch(_dev_ptr(starts, torch.int32, "starts", (B + 1,)),
+                _dev_ptr(lens, torch.int32, "lens"),
+                _dev_ptr(pages, torch.int32, "pages", (B, pages.shape[1])), B, pages.shape[1])
+    return c, b
+
+
+def mq_rope_append(q, k, v, aq: float, zq: int, aqo: float, zqo: int, ak: float, zk: int,
+                   ako: float, zko: int, k_cache, v_cache, starts, lens, pages, table=None,
+                   out=None, stream=None):
+    """Rotates the new tokens' query codes q [T][H * D] (returned, int16) and
+    key codes k [T][G * D] (int16) by their positions and writes the keys
+    (int8) and the value codes v [T][G * D] (int8) to the cache's pages.
+
+    k_cache [pages][G][page][D] and v_cache [pages][G][D][page] are updated in
+    place; rows [starts[b], starts[b+1]) belong to sequence b of length lens[b]
+    (these tokens included) with page list pages[b].  table: fp64 angles of
+    mq_rope_table from position 0 on (positions * D values), or None for no
+    rotation."""
+    torch = _torch_mod or _torch()
+    c, b = _kv_args(k_cache, v_cache, starts, lens, pages)
+    T, HD = q.shape
+    D = c.D
+    H = HD // D
+    if H * D != HD:
+        raise ValueError("q's row length must be heads * D")
+    out = torch.empty((T, HD), dtype=torch.int16, device=q.device) if out is None else out
+    pq, ldq = _rows(q, torch.int16, "q")
+    pk, ldk = _rows(k, torch.int16, "k", (T, c.G * D))
+    pv, ldv = _rows(v, torch.int8, "v", (T, c.G * D))
+    po, ldo = _rows(out, torch.int16, "out", (T, HD))
+    ptab = None if table is None else _dev_ptr(table, torch.float64, "table")
+    positions = 0 if table is None else table.numel() // D
+    _check(lib().mq_rope_append(pq, ldq, pk, ldk, pv, ldv, T, H, aq, zq, aqo, zqo, ak, zk, ako,
+                                zko, ptab, positions, ctypes.byref(c), ctypes.byref(b), po, ldo,
+                                _stream_ptr(stream)), "mq_rope_append")
+    return out
+
+
+def mq_paged_attn_workspace_bytes(T: int, B: int, H: int, G: int, D: int, max_len: int) -> int:
+    """Workspace bytes mq_paged_attn can use for these sizes (0: none)."""
+    n = lib().mq_paged_attn_workspace_bytes(T, B, H, G, D, max_len)
+    if n < 0:
+        raise ValueError(f"mq_paged_attn_workspace_bytes: invalid sizes {(T, B, H, G, D, max_len)}")
+    return n
+
+
+def mq_paged_attn(q, q_scale: float, q_zp: int, k_cache, k_scale: float, v_cache, v_scale: float,
+                  v_zp: int, starts, lens, pages, logit_scale: float, out_scale: float,
+                  out_zp: int, out_bits: int = 8, window: int = 0, sinks: int = 0,
+                  max_len: int = 0, out=None, workspace=None, stream=None):
+    """Attention of the new tokens' query codes q [T][H * D] over their
+    sequences' cached keys and values: the context codes [T][H * D].
+
+    Each row sees the keys at or before its position, with ``window`` > 0 only
+    the last ``window`` of them and the first ``sinks``.  max_len: the longest
+    sequence as far as the caller knows (0: what the page list holds).
+    workspace: a uint8 tensor kept by the caller (allocated here if None)."""
+    torch = _torch_mod or _torch()
+    c, b = _kv_args(k_cache, v_cache, starts, lens, pages)
+    T, HD = q.shape
+    D = c.D
+    H = HD // D
+    if H * D != HD:
+        raise ValueError("q's row length must be heads * D")
+    odt = _act_dtype(out_bits)
+    out = torch.empty((T, HD), dtype=odt, device=q.device) if out is None else out
+    pq, ldq = _rows(q, torch.int16, "q")
+    po, ldo = _rows(out, odt, "out", (T, HD))
+    if workspace is None:
+        n = lib().mq_paged_attn_workspace_bytes(T, b.B, H, c.G, D, max_len or b.ld * c.page)
+        workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n > 0 else None
+    ws, ws_bytes = _workspace_args(workspace)
+    _check(lib().mq_paged_attn(pq, ldq, T, H, q_scale, q_zp, ctypes.byref(c), k_scale, v_scale,
+                               v_zp, ctypes.byref(b), logit_scale, window, sinks, out_scale,
+                               out_zp, out_bits, po, ldo, max_len, ws, ws_bytes,
+                               _stream_ptr(stream)), "mq_paged_attn")
+    return out
 
 
 def mq_dequant(q, alpha: float, zp: int, out=None, stream=None):

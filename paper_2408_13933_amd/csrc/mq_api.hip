@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstdint>
 
+#include "kvcache.h"
 #include "mq.h"
 #include "mq_internal.h"
 
@@ -27,6 +28,42 @@ hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 
 // largest element count the grid-stride kernels index with int64 safely
 constexpr int64_t kMaxElems = (int64_t)1 << 46;
+
+// Sizes and pointers of a paged cache and a batch of sequences with T token
+// rows of H query heads; fills the kernels' form.
+mq_status kv_validate(const mq_kv_cache* c, const mq_kv_batch* b, int64_t T, int32_t H,
+                      mq::KvArgs* out)
+{
+    if (!c || !b) return MQ_ERR_INVALID_ARG;
+    if (c->page < 16 || c->page > 1024 || (c->page & (c->page - 1)) != 0)
+        return MQ_ERR_INVALID_ARG;
+    if (c->G < 1 || c->G > 1024 || H < 1 || H > 1024 || H % c->G != 0) return MQ_ERR_INVALID_ARG;
+    if (c->D < 16 || c->D > 256 || c->D % 16 != 0) return MQ_ERR_INVALID_ARG;
+    if (c->pages < 0 || c->pages > 0x7FFFFFFF) return MQ_ERR_INVALID_ARG;
+    if (T < 0 || T >= (1 << 26) || b->B < 0 || b->B >= (1 << 26)) return MQ_ERR_INVALID_ARG;
+    if ((T + b->B) * (H + c->G) >= ((int64_t)1 << 36) / c->D) return MQ_ERR_INVALID_ARG;
+    if (b->ld < 0 || b->ld > ((int64_t)1 << 31) || b->B * b->ld >= ((int64_t)1 << 40))
+        return MQ_ERR_INVALID_ARG;
+    if (T > 0 && b->B > 0) {
+        if (!b->starts || !b->lens || (b->ld > 0 && !b->table)) return MQ_ERR_INVALID_ARG;
+        if (c->pages > 0 && (!c->k || !c->v)) return MQ_ERR_INVALID_ARG;
+        if ((uintptr_t)c->k % 16 != 0 || (uintptr_t)c->v % 16 != 0) return MQ_ERR_INVALID_ARG;
+    }
+    out->k = c->k;
+    out->v = c->v;
+    out->pages = c->pages;
+    out->starts = b->starts;
+    out->lens = b->lens;
+    out->table = b->table;
+    out->ld = b->ld;
+    out->B = (int32_t)b->B;
+    out->G = c->G;
+    out->D = c->D;
+    out->shift = __builtin_ctz((unsigned)c->page);
+    return MQ_OK;
+}
+
+bool row_stride_ok(int64_t ld, int64_t row) { return ld >= row && ld < ((int64_t)1 << 40); }
 
 }  // namespace
 
@@ -716,6 +753,69 @@ mq_status mq_transpose_i8(const int8_t* x, int64_t rows, int64_t cols, int64_t l
     if (rows == 0 || cols == 0) return MQ_OK;
     if (!x || !y) return MQ_ERR_INVALID_ARG;
     return from_hip(mq::launch_transpose_i8(x, rows, cols, ldx, y, as_stream(stream)));
+}
+
+mq_status mq_rope_append(const int16_t* q, int64_t ldq, const int16_t* k, int64_t ldk,
+                         const int8_t* v, int64_t ldv, int64_t T, int32_t H, float aq, int32_t zq,
+                         float aqo, int32_t zqo, float ak, int32_t zk, float ako, int32_t zko,
+                         const double* angles, int64_t positions, const mq_kv_cache* cache,
+                         const mq_kv_batch* batch, int16_t* q_out, int64_t ldo, void* stream)
+{
+    mq::KvArgs kv;
+    const mq_status st = kv_validate(cache, batch, T, H, &kv);
+    if (st != MQ_OK) return st;
+    const int64_t hd = (int64_t)H * kv.D, gd = (int64_t)kv.G * kv.D;
+    if (!row_stride_ok(ldq, hd) || !row_stride_ok(ldo, hd) || !row_stride_ok(ldk, gd) ||
+        !row_stride_ok(ldv, gd))
+        return MQ_ERR_INVALID_ARG;
+    if (!finite_pos(aq) || !finite_pos(aqo) || !finite_pos(ak) || !finite_pos(ako))
+        return MQ_ERR_INVALID_ARG;
+    if (!zp_ok(zq, 16) || !zp_ok(zqo, 16) || !zp_ok(zk, 16) || !zp_ok(zko, 8))
+        return MQ_ERR_INVALID_ARG;
+    if (angles && (positions < 0 || positions > ((int64_t)1 << 40))) return MQ_ERR_INVALID_ARG;
+    if (T == 0 || batch->B == 0) return MQ_OK;
+    if (!q || !k || !v || !q_out) return MQ_ERR_INVALID_ARG;
+    return from_hip(mq::launch_rope_append(kv, q, ldq, k, ldk, v, ldv, T, H, aq, zq, aqo, zqo, ak,
+                                           zk, ako, zko, angles, positions, q_out, ldo,
+                                           as_stream(stream)));
+}
+
+int64_t mq_paged_attn_workspace_bytes(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D,
+                                      int64_t max_len)
+{
+    if (T < 0 || T >= (1 << 26) || B < 0 || B >= (1 << 26) || G < 1 || G > 1024 || H < 1 ||
+        H > 1024 || H % G != 0 || D < 16 || D > 256 || D % 16 != 0 || max_len < 0)
+        return -1;
+    return mq::paged_attn_workspace(T, B, H, G, D, max_len);
+}
+
+mq_status mq_paged_attn(const int16_t* q, int64_t ldq, int64_t T, int32_t H, float q_scale,
+                        int32_t q_zp, const mq_kv_cache* cache, float k_scale, float v_scale,
+                        int32_t v_zp, const mq_kv_batch* batch, float logit_scale, int64_t window,
+                        int64_t sinks, float out_scale, int32_t out_zp, int32_t out_bits, void* y,
+                        int64_t ldy, int64_t max_len, void* workspace, int64_t workspace_bytes,
+                        void* stream)
+{
+    mq::KvArgs kv;
+    const mq_status st = kv_validate(cache, batch, T, H, &kv);
+    if (st != MQ_OK) return st;
+    const int64_t hd = (int64_t)H * kv.D;
+    if (!row_stride_ok(ldq, hd) || !row_stride_ok(ldy, hd)) return MQ_ERR_INVALID_ARG;
+    if (!act_bits_ok(out_bits) || !finite_pos(q_scale) || !finite_pos(k_scale) ||
+        !finite_pos(v_scale) || !finite_pos(logit_scale) || !finite_pos(out_scale))
+        return MQ_ERR_INVALID_ARG;
+    if (!((double)q_scale * (double)k_scale * (double)logit_scale <= 1024.0))
+        return MQ_ERR_INVALID_ARG;
+    if (!zp_ok(q_zp, 16) || !zp_ok(v_zp, 8) || !zp_ok(out_zp, out_bits)) return MQ_ERR_INVALID_ARG;
+    if (window < 0 || sinks < 0 || max_len < 0 || workspace_bytes < 0) return MQ_ERR_INVALID_ARG;
+    if (workspace && (uintptr_t)workspace % 256 != 0) return MQ_ERR_INVALID_ARG;
+    if (T == 0 || batch->B == 0) return MQ_OK;
+    if (!q || !y) return MQ_ERR_INVALID_ARG;
+    if (max_len == 0) max_len = batch->ld << kv.shift;
+    return from_hip(mq::launch_paged_attn(kv, q, ldq, T, H, q_scale, q_zp, k_scale, v_scale, v_zp,
+                                          logit_scale, window, sinks, out_scale, out_zp, out_bits,
+                                          y, ldy, max_len, workspace, workspace_bytes,
+                                          as_stream(stream)));
 }
 
 }  // extern "C"

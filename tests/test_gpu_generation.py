@@ -1,0 +1,283 @@
+"""GPU parity of the paged key/value cache and the attention over it with the
+plain forms of generation.py (64-bit, numpy): rotation and append bit for
+bit, attention codes equal but at a rounding tie."""
+import numpy as np
+import pytest
+
+from tests import generation as gen
+
+pytestmark = pytest.mark.gpu
+
+QF, KF = (3.1e-4, 700), (2.4e-4, -1500)
+QO, KO = (3.3e-4, -1600), (0.0667, -7)
+
+
+def _mq():
+    import paper_2408_13933_amd as mq
+    return mq
+
+
+def _dev(*arrays):
+    import torch
+    return [None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
+            for a in arrays]
+
+
+def _angles(n, D, base=10000.0):
+    ang = np.arange(n)[:, None] * base ** (-np.arange(0, D, 2) / D)
+    return np.stack((np.cos(ang), np.sin(ang)), 2)
+
+
+def _append_case(rng, H, G, D, page, new, lens, positions=None, extra=0, **kw):
+    """Runs mq_rope_append on random codes and checks every output against the
+    plain form; returns what a caller may want to look at."""
+    mq = _mq()
+    import torch
+    starts, lens, pages, pool = gen.batch(rng, new, lens, page)
+    edit = kw.pop("edit", None)
+    if edit:
+        edit(pages, lens, pool)
+    T = int(starts[-1]) + extra
+    q = rng.integers(-32768, 32768, (T, H * D)).astype(np.int16)
+    k = rng.integers(-32768, 32768, (T, G * D)).astype(np.int16)
+    v = rng.integers(-128, 128, (T, G * D)).astype(np.int8)
+    kc = rng.integers(-128, 128, (pool, G, page, D)).astype(np.int8)
+    vc = rng.integers(-128, 128, (pool, G, D, page)).astype(np.int8)
+    out = rng.integers(-32768, 32768, (T, H * D)).astype(np.int16)
+    angles = None if positions == 0 else _angles(positions or int(max(lens.max(), 1)), D)
+    gq, gk, gv, gkc, gvc, gout, gst, gle, gpg = _dev(q, k, v, kc, vc, out, starts, lens, pages)
+    gtab = None if angles is None else torch.from_numpy(angles).cuda().reshape(-1)
+    shift = kw.pop("shift", 0)
+    if shift:  # rows that do not start at whole 16-byte chunks
+        def wide(x):
+            w = torch.zeros((x.shape[0], x.shape[1] + shift + 2), dtype=x.dtype, device="cuda")
+            w[:, shift:shift + x.shape[1]] = x
+            return w[:, shift:shift + x.shape[1]]
+        gq, gk, gv, gout = (wide(x) for x in (gq, gk, gv, gout))
+    if kw.pop("in_place", False):
+        gout, out = gq, q.copy()
+    got = mq.mq_rope_append(gq, gk, gv, *QF, *QO, *KF, *KO, gkc, gvc, gst, gle, gpg, table=gtab,
+                            out=gout)
+    torch.cuda.synchronize()
+    gen.rope_append(q.copy(), k, v, QF, QO, KF, KO, kc, vc, starts, lens, pages, angles, out)
+    assert np.array_equal(got.cpu().numpy(), out)
+    assert np.array_equal(gkc.cpu().numpy(), kc)
+    assert np.array_equal(gvc.cpu().numpy(), vc)
+
+
+@pytest.mark.parametrize("H,G,D", [(32, 4, 64), (8, 1, 256), (3, 3, 80), (6, 2, 16), (5, 1, 48),
+                                   (4, 4, 128)])
+@pytest.mark.parametrize("page", [16, 64, 1024])
+def test_append(H, G, D, page):
+    rng = np.random.default_rng(H * D + page)
+    # one token at the start, in the middle and at a page's last slot; chunks
+    # that begin and end inside pages and 16-slot groups; no new token
+    new = [1, 1, 1, 37, 0, 16, 70, 2]
+    lens = [1, 100, page, 37, 9, 16 + 5, 70 + 3 * page - 1, 2 + 15]
+    _append_case(rng, H, G, D, page, new, lens)
+
+
+@pytest.mark.parametrize("shift", [1, 3, 8])
+def test_append_strided_rows(shift):
+    rng = np.random.default_rng(shift)
+    _append_case(rng, 4, 2, 64, 16, [20, 1, 3], [20, 40, 30], shift=shift)
+
+
+def test_append_without_angles_in_place():
+    rng = np.random.default_rng(5)
+    _append_case(rng, 4, 2, 64, 32, [20, 1, 3], [20, 40, 30], positions=0)
+    _append_case(rng, 4, 2, 64, 32, [20, 1, 3], [20, 40, 30], in_place=True)
+
+
+def test_append_leaves_out_what_has_no_place():
+    """Positions before 0, past the angles and past the page list, page
+    indices outside the pool, rows behind the last sequence."""
+    rng = np.random.default_rng(6)
+
+    def edit(pages, lens, pool):
+        pages[0, 1] = -1
+        pages[1, 0] = pool
+        lens[2] = 3                              # five new tokens: two before 0
+        lens[3] = pages.shape[1] * 16 + 4        # four past the list
+
+    _append_case(rng, 4, 2, 32, 16, [40, 10, 5, 30], [40, 10, 5, 60], positions=50, extra=7,
+                 edit=edit)
+
+
+def test_append_many_sequences():
+    """More sequences than one round of the search probes, most without a new
+    token."""
+    rng = np.random.default_rng(7)
+    B = 5000
+    new = (rng.random(B) < 0.1).astype(int)
+    _append_case(rng, 2, 1, 16, 16, list(new), list(rng.integers(1, 20, B)))
+
+
+def test_append_equals_rope_apply():
+    """A prompt's rotation is mq_rope_apply's, bit for bit."""
+    mq = _mq()
+    import torch
+    T, H, G, D, page = 200, 8, 2, 64, 64
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q = torch.randint(-32768, 32768, (T, H * D), generator=g, device="cuda", dtype=torch.int16)
+    k = torch.randint(-32768, 32768, (T, G * D), generator=g, device="cuda", dtype=torch.int16)
+    v = torch.randint(-128, 128, (T, G * D), generator=g, device="cuda", dtype=torch.int8)
+    table = mq.mq_rope_table(T, D)
+    n = -(-T // page)
+    kc = torch.zeros((n, G, page, D), dtype=torch.int8, device="cuda")
+    vc = torch.zeros((n, G, D, page), dtype=torch.int8, device="cuda")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    out = mq.mq_rope_append(q, k, v, *QF, *QO, *KF, *KO, kc, vc, torch.tensor([0, T], **i32),
+                            torch.tensor([T], **i32), torch.arange(n, **i32)[None], table=table)
+    assert torch.equal(out, mq.mq_rope_apply(q, H, *QF, *QO, table, 16))
+    kr = mq.mq_rope_apply(k, G, *KF, *KO, table, 8)
+    assert torch.equal(kc.permute(0, 2, 1, 3).reshape(n * page, G * D)[:T], kr)
+    vt = vc.permute(1, 2, 0, 3).reshape(G * D, n * page)[:, :T]
+    assert torch.equal(vt, mq.mq_transpose_i8(v))
+
+
+# ---------------------------------------------------------------------------
+
+VF = (0.031, 5)
+
+
+def _attn_case(rng, H, G, D, page, new, lens, out_bits=16, q_zp=321, window=0, sinks=0, q_std=3000,
+               k_std=30, logit_scale=None, k_scale=0.05, extra=0, edit=None, shift=0,
+               workspace=None, max_len=0, out_scale=None):
+    mq = _mq()
+    import torch
+    starts, lens, pages, pool = gen.batch(rng, new, lens, page)
+    if edit:
+        edit(pages, lens, pool)
+    T = int(starts[-1]) + extra
+    fq = (4.0e-4, q_zp)
+    q = np.clip(np.rint(rng.standard_normal((T, H * D)) * q_std) + q_zp, -32768, 32767)
+    q = q.astype(np.int16)
+    kc = np.clip(np.rint(rng.standard_normal((pool, G, page, D)) * k_std) + 9, -128, 127)
+    kc = kc.astype(np.int8)
+    vc = rng.integers(-128, 128, (pool, G, D, page)).astype(np.int8)
+    logit_scale = D ** -0.5 if logit_scale is None else logit_scale
+    out_scale = (0.03 if out_bits == 8 else 1.2e-4) if out_scale is None else out_scale
+    out_zp = -11
+    odt = torch.int8 if out_bits == 8 else torch.int16
+    gq, gkc, gvc, gst, gle, gpg = _dev(q, kc, vc, starts, lens, pages)
+    gout = torch.full((T, H * D), 77, dtype=odt, device="cuda")
+    if shift:
+        w = torch.zeros((T, H * D + shift + 2), dtype=torch.int16, device="cuda")
+        w[:, shift:shift + H * D] = gq
+        gq = w[:, shift:shift + H * D]
+        gout = torch.full((T, H * D + 5), 77, dtype=odt, device="cuda")[:, 3:3 + H * D]
+    ws = None if workspace is None else torch.empty(workspace, dtype=torch.uint8, device="cuda")
+    mq.mq_paged_attn(gq, *fq, gkc, k_scale, gvc, *VF, gst, gle, gpg, logit_scale, out_scale,
+                     out_zp, out_bits, window=window, sinks=sinks, out=gout, workspace=ws,
+                     max_len=max_len)
+    torch.cuda.synchronize()
+    real = gen.paged_attn(q, fq, kc, k_scale, vc, VF, starts, lens, pages, logit_scale, window,
+                          sinks)
+    n = int(starts[-1])
+    got = gout.cpu().numpy()
+    # a weight at a tie moves the sums by one value step of at most 255 over a
+    # weight sum of at least ONE
+    slack = 255 * VF[0] / gen.ONE / out_scale + 1e-9
+    gen.assert_codes(got[:n], real[:n], out_scale, out_zp, out_bits, slack)
+    assert (got[n:] == 77).all()
+    return got
+
+
+@pytest.mark.parametrize("H,G,D", [(32, 4, 64), (8, 1, 256), (3, 3, 80), (6, 2, 16), (5, 1, 48),
+                                   (8, 2, 128), (7, 1, 192), (40, 1, 32)])
+@pytest.mark.parametrize("page", [16, 128, 512])
+def test_attend_generation(H, G, D, page):
+    """One token of each sequence, lengths from one to several blocks, at and
+    off the borders of pages and blocks."""
+    rng = np.random.default_rng(H * D + page)
+    lens = [1, 2, 15, 16, 17, 127, 128, 129, 300, 777]
+    _attn_case(rng, H, G, D, page, [1] * len(lens), lens)
+
+
+@pytest.mark.parametrize("out_bits", [8, 16])
+@pytest.mark.parametrize("H,G,D,page", [(8, 2, 64, 16), (3, 1, 128, 64), (2, 2, 256, 256)])
+def test_attend_chunks(H, G, D, page, out_bits):
+    """Prompts, later chunks and single tokens in one call."""
+    rng = np.random.default_rng(D + out_bits)
+    new = [130, 1, 0, 33, 64, 5]
+    lens = [130, 260, 50, 33 + 100, 64 + 128, 6]
+    _attn_case(rng, H, G, D, page, new, lens, out_bits=out_bits, extra=4)
+
+
+@pytest.mark.parametrize("q_zp", [-32768, -900, 0, 128, 32767])
+def test_attend_query_zero_points(q_zp):
+    """Codes over the whole 16-bit range around any zero-point: differences
+    that fit two bytes and ones that do not."""
+    rng = np.random.default_rng(abs(q_zp))
+    _attn_case(rng, 4, 2, 64, 16, [3, 1], [200, 140], q_zp=q_zp, q_std=25000,
+               logit_scale=0.01)
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (5, 3), (128, 4), (130, 0), (200, 140),
+                                          (1000, 2), (64, 1000)])
+@pytest.mark.parametrize("page", [16, 128])
+def test_attend_window_and_sinks(window, sinks, page):
+    rng = np.random.default_rng(window + sinks)
+    _attn_case(rng, 4, 2, 64, page, [1, 40, 3, 1], [700, 500, 3, 129], window=window, sinks=sinks)
+
+
+def test_attend_rows_that_see_nothing():
+    """Positions before 0, sequences of length 0, pages that do not exist: the
+    code of 0; holes in the page list are not seen."""
+    rng = np.random.default_rng(3)
+
+    def edit(pages, lens, pool):
+        lens[0] = 2                  # five new tokens, three before 0
+        lens[1] = 0
+        pages[2, :] = pool           # nowhere
+        pages[3, 2] = -5             # a hole
+        pages[3, 9:11] = pool + 7
+        lens[4] = pages.shape[1] * 16 + 40   # past the list
+        lens[5] = -3
+
+    got = _attn_case(rng, 4, 2, 64, 16, [5, 1, 2, 20, 50, 1], [5, 1, 30, 300, 310, 1], edit=edit)
+    assert (got[0:3] == -11).all() and (got[5:8] == -11).all() and (got[-1] == -11).all()
+
+
+def test_attend_extreme_codes_and_scales():
+    """The largest logits that the formats allow (sums at the ends of 32
+    bits), one dominant key, equal keys, tiny and large logit scales."""
+    rng = np.random.default_rng(4)
+    for q_zp in (-32768, 32767):
+        _attn_case(rng, 2, 1, 256, 16, [2, 1], [150, 140], q_zp=q_zp, q_std=1e6, k_std=1e6,
+                   logit_scale=1e-5)
+    _attn_case(rng, 2, 1, 64, 16, [2], [300], k_std=1e6, logit_scale=50.0)
+    _attn_case(rng, 2, 1, 64, 16, [2], [300], logit_scale=1e-30)
+    _attn_case(rng, 2, 1, 64, 16, [2], [300], q_std=0)        # flat: every key alike
+    _attn_case(rng, 2, 1, 64, 16, [2], [300], out_scale=1e-30)  # saturates
+    # one integer step of the logits is thousands of powers of two
+    _attn_case(rng, 2, 1, 16, 16, [2], [300], k_scale=1e5, logit_scale=20.0)
+
+
+@pytest.mark.parametrize("shift", [1, 4, 8])
+def test_attend_strided_rows(shift):
+    rng = np.random.default_rng(shift)
+    for ob in (8, 16):
+        _attn_case(rng, 4, 2, 80, 16, [20, 1], [150, 260], shift=shift, out_bits=ob)
+
+
+def test_attend_splits_give_the_same_codes():
+    """The keys in one part, in as many as the workspace allows and in as many
+    as a wrong guess of the longest sequence gives."""
+    mq = _mq()
+    need = mq.mq_paged_attn_workspace_bytes(2, 2, 8, 2, 64, 5000)
+    assert need > 0 and need % 16 == 0
+    got = []
+    for ws, max_len in ((0, 0), (need // 2, 5000), (need, 5000), (need, 1), (need, 100000)):
+        rng = np.random.default_rng(9)
+        got.append(_attn_case(rng, 8, 2, 64, 16, [1, 1], [5000, 700], workspace=ws,
+                              max_len=max_len))
+    for g in got[1:]:
+        assert np.array_equal(g, got[0])
+
+
+def test_attend_long_rows():
+    """A long sequence of nearly equal logits: the weights keep their bits."""
+    rng = np.random.default_rng(10)
+    _attn_case(rng, 2, 1, 64, 64, [2], [70001], q_std=300, out_scale=1e-5)
