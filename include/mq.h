@@ -798,6 +798,50 @@ mq_status mq_paged_attn(const int16_t* q, int64_t ldq, int64_t T, int32_t H, flo
 int64_t mq_paged_attn_workspace_bytes(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D,
                                       int64_t max_len);
 
+/* Most words of an mq_sample row, and the bound of its workspace. */
+#define MQ_SAMPLE_MAX_V (1 << 22)
+#define MQ_SAMPLE_MAX_WORKSPACE (64 << 20)
+
+/*
+ * mq_sample -- draws the next token of every row of logits with given random
+ * numbers.  For row m with the largest logit X and temperature t:
+ *   w_i = rint(2^40 * exp((x_i - X) / t))        (2^40 for x_i = X)
+ * integers, so that all sums are exact.  In the order of descending logits,
+ * ties by ascending index, the row keeps
+ *   top_k: its first k words (k <= 0: all of them);
+ *   top_p: of these, the shortest prefix whose weights sum to at least p
+ *          times the sum of all of these, the first word always (p >= 1: all);
+ *   min_p: of these, the words with w_i >= min_p * 2^40 (min_p <= 0: all; the
+ *          words as likely as the first always).
+ * With R the sum of the kept weights, r = min(floor(u * R), R - 1) (fp64), the
+ * token is the first word in index order at which the running sum of kept
+ * weights exceeds r.  exp is evaluated within 2^-46.  A row with t <= 0 (or
+ * NaN) takes the first word of the order.  Logits that are NaN or -infinity
+ * are never drawn; a row of nothing else gives -1.  With +infinity logits
+ * only these have weight.
+ *   logits  bits 32: device fp32; bits 16: device int16 codes of format
+ *           (alpha, zp), x = alpha * (q - zp) exactly (mq_qlinear's 16-bit
+ *           outputs, without a dequantization pass); row m at logits + m * ld
+ *   temperature, top_p, min_p  device fp32 [M]; top_k device int32 [M]; each
+ *           may be NULL: 1, off, off, off
+ *   u       device fp32 [M], in [0, 1) (others are limited to [0, 1], NaN: 0)
+ *   tokens  device int32 [M], written
+ *   workspace  device, 256-byte aligned, any contents, overwritten; at least
+ *           mq_sample_workspace_bytes(1, V) bytes; with fewer than for all
+ *           rows, they are done in several turns.  Calls that may run at the
+ *           same time must not share it.
+ *   0 <= M < 2^31; 1 <= V <= MQ_SAMPLE_MAX_V; V <= ld < 2^40; alpha finite
+ *   and > 0, zp int16 (bits 16; else not used).
+ */
+mq_status mq_sample(const void* logits, int32_t bits, int64_t M, int64_t V, int64_t ld, float alpha,
+                    int32_t zp, const float* temperature, const int32_t* top_k, const float* top_p,
+                    const float* min_p, const float* u, int32_t* tokens, void* workspace,
+                    int64_t workspace_bytes, void* stream);
+
+/* Workspace bytes with which mq_sample does M rows at once, within
+ * MQ_SAMPLE_MAX_WORKSPACE or one row's need (-1: invalid sizes). */
+int64_t mq_sample_workspace_bytes(int64_t M, int64_t V);
+
 /*
  * mq_dequant -- inverse of Eq.(4): y = alpha * (float)(q - zp), one exact
  * integer subtraction and one fp32 multiply.

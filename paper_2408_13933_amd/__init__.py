@@ -23,7 +23,7 @@ __all__ = [
     "PATH_PREFILL_TILE0", "PREFILL_TILES", "prefill_tile_path", "mq_probe_read",
     "mq_qlinear_group", "MAX_GROUP", "QLinearOut", "mq_qlinear_dequant",
     "mq_rope_append", "mq_paged_attn", "mq_paged_attn_workspace_bytes", "KVCache", "KVBatch",
-    "ATTN_BLOCK", "ATTN_ONE",
+    "ATTN_BLOCK", "ATTN_ONE", "mq_sample", "mq_sample_workspace_bytes",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -170,7 +170,11 @@ def lib():
     L.mq_paged_attn.argtypes = [c_p, c_i64, c_i64, c_i32, c_f, c_i32, ctypes.POINTER(KVCache), c_f,
                                 c_f, c_i32, ctypes.POINTER(KVBatch), c_f, c_i64, c_i64, c_f, c_i32,
                                 c_i32, c_p, c_i64, c_i64, c_p, c_i64, c_p]
-    for name in ("mq_rope_append", "mq_paged_attn", "mq_qlinear_dequant", "mq_qlinear_group", "mq_probe_read", "mq_attn_matmul", "mq_transpose_i8", "mq_act_params", "mq_fold_weights", "mq_fold_acts", "mq_quantize_act",
+    L.mq_sample_workspace_bytes.argtypes = [c_i64, c_i64]
+    L.mq_sample_workspace_bytes.restype = c_i64
+    L.mq_sample.argtypes = [c_p, c_i32, c_i64, c_i64, c_i64, c_f, c_i32, c_p, c_p, c_p, c_p, c_p,
+                            c_p, c_p, c_i64, c_p]
+    for name in ("mq_sample", "mq_rope_append", "mq_paged_attn", "mq_qlinear_dequant", "mq_qlinear_group", "mq_probe_read", "mq_attn_matmul", "mq_transpose_i8", "mq_act_params", "mq_fold_weights", "mq_fold_acts", "mq_quantize_act",
                  "mq_pack_weights", "mq_qlinear", "mq_qlinear_ex", "mq_qlinear_ws", "mq_dequant",
                  "mq_qlinear_noalloc",
                  "mq_pack_weights_asym", "mq_act_rowsum", "mq_quantize_act_rowsum",
@@ -972,6 +976,42 @@ def mq_paged_attn(q, q_scale: float, q_zp: int, k_cache, k_scale: float, v_cache
                                v_zp, ctypes.byref(b), logit_scale, window, sinks, out_scale,
                                out_zp, out_bits, po, ldo, max_len, ws, ws_bytes,
                                _stream_ptr(stream)), "mq_paged_attn")
+    return out
+
+
+def mq_sample_workspace_bytes(M: int, V: int) -> int:
+    """Workspace bytes with which mq_sample does M rows of V words at once."""
+    n = lib().mq_sample_workspace_bytes(M, V)
+    if n < 0:
+        raise ValueError(f"mq_sample_workspace_bytes: invalid sizes {(M, V)}")
+    return n
+
+
+def mq_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, alpha: float = 1.0,
+              zp: int = 0, out=None, workspace=None, stream=None):
+    """Next tokens int32 [M] from logits [M][V] (fp32, or int16 codes of
+    format (alpha, zp)) and random numbers u fp32 [M] in [0, 1), with
+    per-row settings (fp32 [M], top_k int32 [M]) or None for off.
+    workspace: a uint8 tensor kept by the caller (allocated here if None)."""
+    torch = _torch_mod or _torch()
+    bits = {torch.float32: 32, torch.int16: 16}.get(getattr(logits, "dtype", None))
+    if bits is None:
+        raise ValueError("logits must be float32 or int16")
+    pl, ld = _rows(logits, logits.dtype, "logits")
+    M, V = logits.shape
+    f32 = torch.float32
+    opt = [None if t is None else _dev_ptr(t, dt, name, (M,))
+           for t, dt, name in ((temperature, f32, "temperature"), (top_k, torch.int32, "top_k"),
+                               (top_p, f32, "top_p"), (min_p, f32, "min_p"))]
+    pu = _dev_ptr(u, f32, "u", (M,))
+    out = torch.empty(M, dtype=torch.int32, device=logits.device) if out is None else out
+    po = _dev_ptr(out, torch.int32, "out", (M,))
+    if workspace is None:
+        workspace = torch.empty(mq_sample_workspace_bytes(M, V), dtype=torch.uint8,
+                                device=logits.device)
+    ws, ws_bytes = _workspace_args(workspace)
+    _check(lib().mq_sample(pl, bits, M, V, ld, alpha, zp, *opt, pu, po, ws, ws_bytes,
+                           _stream_ptr(stream)), "mq_sample")
     return out
 
 

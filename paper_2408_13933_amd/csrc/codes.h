@@ -22,6 +22,27 @@ __device__ inline int32_t rint_low(double shifted)
     return (int32_t)(uint32_t)__double_as_longlong(shifted);
 }
 
+// 2^x for -2^30 < x < 1024 (to 0 far below -1022): rint by the 1.5 * 2^52 shift, a
+// polynomial of degree 10 through the Chebyshev nodes of [-1/2, 1/2] (within
+// 3e-16 of 2^f), the exponent added.
+__device__ inline double exp2_poly(double x)
+{
+    const double t = x + kRintShift;
+    const double f = x - (t - kRintShift);
+    double p = 0x1.e6063f7217bc6p-28;
+    p = __builtin_fma(p, f, 0x1.b675bca4eeebbp-24);
+    p = __builtin_fma(p, f, 0x1.62bfd47773353p-20);
+    p = __builtin_fma(p, f, 0x1.ffcb54062e698p-17);
+    p = __builtin_fma(p, f, 0x1.430913096fd9fp-13);
+    p = __builtin_fma(p, f, 0x1.5d87fe9d7a584p-10);
+    p = __builtin_fma(p, f, 0x1.3b2ab6fba1ddap-7);
+    p = __builtin_fma(p, f, 0x1.c6b08d703ce49p-5);
+    p = __builtin_fma(p, f, 0x1.ebfbdff82c598p-3);
+    p = __builtin_fma(p, f, 0x1.62e42fefa3a19p-1);
+    p = __builtin_fma(p, f, 1.0);
+    return __builtin_amdgcn_ldexp(p, rint_low(t));
+}
+
 template <int BITS>
 __device__ inline int32_t clamp_code(int32_t q)
 {

@@ -818,4 +818,28 @@ mq_status mq_paged_attn(const int16_t* q, int64_t ldq, int64_t T, int32_t H, flo
                                           as_stream(stream)));
 }
 
+int64_t mq_sample_workspace_bytes(int64_t M, int64_t V)
+{
+    if (M < 0 || M > 0x7FFFFFFF || V < 1 || V > MQ_SAMPLE_MAX_V) return -1;
+    return M == 0 ? 0 : mq::sample_workspace(M, V, false);
+}
+
+mq_status mq_sample(const void* logits, int32_t bits, int64_t M, int64_t V, int64_t ld, float alpha,
+                    int32_t zp, const float* temperature, const int32_t* top_k, const float* top_p,
+                    const float* min_p, const float* u, int32_t* tokens, void* workspace,
+                    int64_t workspace_bytes, void* stream)
+{
+    if (bits != 32 && bits != 16) return MQ_ERR_INVALID_ARG;
+    if (M < 0 || M > 0x7FFFFFFF || V < 1 || V > MQ_SAMPLE_MAX_V || !row_stride_ok(ld, V))
+        return MQ_ERR_INVALID_ARG;
+    if (bits == 16 && (!finite_pos(alpha) || !zp_ok(zp, 16))) return MQ_ERR_INVALID_ARG;
+    if (M == 0) return MQ_OK;
+    if (!logits || !u || !tokens || !workspace) return MQ_ERR_INVALID_ARG;
+    if ((uintptr_t)workspace % 256 != 0 || workspace_bytes < mq::sample_workspace(M, V, true))
+        return MQ_ERR_INVALID_ARG;
+    return from_hip(mq::launch_sample(logits, bits, M, V, ld, alpha, zp, temperature, top_k, top_p,
+                                      min_p, u, tokens, workspace, workspace_bytes,
+                                      as_stream(stream)));
+}
+
 }  // extern "C"

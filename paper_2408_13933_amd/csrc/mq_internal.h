@@ -209,6 +209,13 @@ hipError_t launch_paged_attn(const KvArgs& kv, const int16_t* q, int64_t ldq, in
 int64_t paged_attn_workspace(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D,
                              int64_t max_len);
 
+// Workspace of launch_sample: for all rows (within its bound), or the least.
+int64_t sample_workspace(int64_t M, int64_t V, bool least);
+hipError_t launch_sample(const void* x, int32_t bits, int64_t M, int64_t V, int64_t ld, float alpha,
+                         int32_t zp, const float* temperature, const int32_t* top_k,
+                         const float* top_p, const float* min_p, const float* u, int32_t* tokens,
+                         void* ws, int64_t ws_bytes, hipStream_t s);
+
 hipError_t launch_qlinear_generic(const QLinearArgs& p, hipStream_t s);
 hipError_t launch_qlinear_decode(const QLinearArgs& p, hipStream_t s);
 // one token (M = 1, 8-bit codes): the vector-ALU GEMV the decode path takes

@@ -110,3 +110,41 @@ def batch(rng, new, lens, page, spare=3, first=0):
         at += n
     starts = np.concatenate(([0], np.cumsum(new))).astype(np.int32)
     return starts, np.array(lens, np.int32), pages, pool
+
+
+def sample_row(x, u, t=1.0, k=0, p=1.0, floor=0.0):
+    """One row's token: x real logits (fp64), the settings as in mq_sample;
+    Python integers for the weights and their sums."""
+    idx = [i for i in range(len(x)) if x[i] > -np.inf]
+    if not idx:
+        return -1
+    order = sorted(idx, key=lambda i: (-x[i], i))
+    top = x[order[0]]
+    if not t > 0:
+        return order[0]
+    if 0 < k < len(order):
+        order = order[:k]
+
+    def weight(i):
+        if x[i] == top:
+            return 1 << 40
+        return 0 if np.isinf(top) else int(np.rint(np.exp((x[i] - top) / t) * 2.0 ** 40))
+
+    w = {i: weight(i) for i in order}
+    if p < 1:
+        total, before, kept = float(sum(w.values())), 0, []
+        for i in order:
+            if kept and not float(before) < p * total:
+                break
+            kept.append(i)
+            before += w[i]
+        order = kept
+    if floor > 0:
+        order = [i for i in order if float(w[i]) >= min(floor, 1.0) * 2.0 ** 40]
+    total = sum(w[i] for i in order)
+    r = min(int(np.floor(min(max(u, 0.0), 1.0) * float(total))) if u == u else 0, total - 1)
+    run = 0
+    for i in sorted(order):
+        run += w[i]
+        if run > r:
+            return i

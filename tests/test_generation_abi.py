@@ -1,5 +1,5 @@
 """Refusals of the text-generation entry points (paged key/value cache,
-attention over it): every invalid argument is turned away on the host before
+attention over it, sampling): every invalid argument is turned away on the host before
 anything is enqueued.  No GPU is touched: the pointers are never read."""
 import ctypes
 
@@ -109,6 +109,37 @@ def test_attention_workspace_is_bounded():
                              (4096, 1, 32, 4, 64, 4096), (1, 1, 8, 1, 256, 100), (0, 0, 8, 1, 64, 9)]:
         n = mq.mq_paged_attn_workspace_bytes(T, B, H, G, D, L)
         assert 0 <= n <= 64 << 20
+
+
+def sample(**kw):
+    a = dict(x=NZ, bits=32, M=4, V=1000, ld=1000, alpha=0.1, zp=0, t=NZ, k=NZ, p=NZ, mp=NZ, u=NZ,
+             y=NZ, ws=NZ, wsb=1 << 20)
+    a.update(kw)
+    return mq.lib().mq_sample(a["x"], a["bits"], a["M"], a["V"], a["ld"], a["alpha"], a["zp"],
+                              a["t"], a["k"], a["p"], a["mp"], a["u"], a["y"], a["ws"], a["wsb"],
+                              None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(x=None), dict(u=None), dict(y=None), dict(ws=None), dict(ws=NZ + 8), dict(wsb=0),
+    dict(wsb=-1), dict(wsb=500), dict(bits=8), dict(bits=0), dict(M=-1), dict(M=1 << 31), dict(V=0),
+    dict(V=-3), dict(V=(1 << 22) + 1, ld=1 << 23), dict(ld=999), dict(ld=1 << 40),
+    dict(bits=16, alpha=0.0), dict(bits=16, alpha=float("nan")), dict(bits=16, zp=40000),
+])
+def test_sample_refuses(kw):
+    assert sample(**kw) == INVALID
+
+
+def test_sample_nothing_to_do_and_workspace():
+    assert sample(M=0, x=None, u=None, y=None, ws=None, wsb=0) == 0
+    for args in ((-1, 10), (1, 0), (1, (1 << 22) + 1), (1 << 31, 10)):
+        assert mq.lib().mq_sample_workspace_bytes(*args) == -1
+        with pytest.raises(ValueError):
+            mq.mq_sample_workspace_bytes(*args)
+    assert mq.mq_sample_workspace_bytes(0, 10) == 0
+    one = mq.mq_sample_workspace_bytes(1, 256000)
+    assert 0 < one <= mq.mq_sample_workspace_bytes(512, 256000) <= 64 << 20
+    assert sample(V=256000, ld=256000, M=3, wsb=one - 1) == INVALID
 
 
 def test_binding_checks_tensors():
