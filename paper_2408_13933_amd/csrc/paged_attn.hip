@@ -20,11 +20,17 @@
 #include "mq_internal.h"
 #include "requant.h"
 
+#define MQ_LDS __attribute__((address_space(3)))
+#define MQ_GLOBAL __attribute__((address_space(1)))
+
 namespace mq {
 namespace {
 
 constexpr int kBlk = MQ_ATTN_BLOCK;
-constexpr int kRows = 16;   // rows per wave
+constexpr int kRows = 16;             // rows per wave
+constexpr int kWaves = 4;             // waves per work-group
+constexpr int kTile = kRows * kWaves; // rows per work-group where the waves share keys
+constexpr int kMaxSplits = 256;
 constexpr int32_t kNone = INT32_MIN;  // no key seen (|c| <= 65535 * 128 * 256 < 2^31)
 
 struct AttnArgs {
@@ -38,23 +44,64 @@ struct AttnArgs {
     double v_scale, out_scale;
     uint32_t d_cut;       // logit distances from here on weigh nothing
     int64_t window, sinks;
-    int32_t vec;          // 16-byte aligned query rows
+    int32_t vec_q, vec_y; // query rows in 16-byte chunks, output rows in fours of codes
     int32_t splits;
-    double* part;         // [splits][T * H][D + 2] when splits > 1
+    double* mz;           // [T * H][splits][2]: maximum and weight sum of a part
+    double* sums;         // [T * H][splits][D]
 };
-
-constexpr double kLog2One = 0x1.dfa34e1177c23p+3;  // log2(MQ_ATTN_ONE)
 
 // factor between two block maxima, 2^(-tau (hi - lo)), hi >= lo
 __device__ inline double factor(const AttnArgs& p, int32_t hi, int32_t lo)
 {
-    return exp2_poly(fmax(-p.tau * ((double)hi - (double)lo), -1100.0));
+    return exp2_poly(fmax(-p.tau * ((double)hi - (double)lo), -1000.0));
 }
 
 __device__ inline v4i mfma(v4i a, v4i b, v4i c)
 {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }
+
+// The larger of a value's copies in the four lanes of one row.
+__device__ inline int32_t row_max(int32_t m)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap((uint32_t)m, (uint32_t)m, false, false);
+    m = max((int32_t)a[0], (int32_t)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap((uint32_t)m, (uint32_t)m, false, false);
+    return max((int32_t)b[0], (int32_t)b[1]);
+}
+
+// rint(MQ_ATTN_ONE 2^(-tau d)) for 0 <= tau d < 1000: tau d to the next 1/64
+// by the 1.5 * 2^46 shift, 2^(j/64) from the table that the wave's lanes hold
+// (lane j), a polynomial of degree 4 on the rest (|f| <= 1/128, within
+// 2.5e-15) and the last product added to 1.5 * 2^52, whose low word is then
+// the rounded weight.  14 vector instructions; the polynomial over all of
+// [-1/2, 1/2] (degree 10) took 18.
+struct WeightTable {
+    int lo, hi;  // MQ_ATTN_ONE * 2^(lane/64)
+    __device__ void init()
+    {
+        const double e = (double)MQ_ATTN_ONE * exp2_poly((double)(threadIdx.x & 63) / 64.0);
+        lo = (int)(uint32_t)__double_as_longlong(e);
+        hi = (int)(__double_as_longlong(e) >> 32);
+    }
+    __device__ int32_t weight(double tau, uint32_t d) const
+    {
+        constexpr double kShift = 105553116266496.0;  // 1.5 * 2^46
+        const double x = (double)d;
+        const double t = __builtin_fma(-tau, x, kShift);
+        const double f = __builtin_fma(-tau, x, -(t - kShift));
+        const int32_t k = rint_low(t);
+        const int tl = __builtin_amdgcn_ds_bpermute(k << 2, lo);
+        const int th = __builtin_amdgcn_ds_bpermute(k << 2, hi) + ((k & ~63) << 14);
+        const double e = __longlong_as_double(((int64_t)th << 32) | (uint32_t)tl);
+        double q = 0x1.3b2ad0385b409p-7;
+        q = __builtin_fma(q, f, 0x1.c6b0c40d8c4e9p-5);
+        q = __builtin_fma(q, f, 0x1.ebfbdff82ac52p-3);
+        q = __builtin_fma(q, f, 0x1.62e42fefa0352p-1);
+        q = __builtin_fma(q, f, 1.0);
+        return rint_low(__builtin_fma(q, e, kRintShift));
+    }
+};
 
 // The weights of four scores as the two byte planes of 32-bit words: w =
 // 256 hi + lo with both bytes signed (w <= 127 * 256).
@@ -70,11 +117,22 @@ __device__ inline void pack_weights4(const int32_t* w, int& hi, int& lo)
 }
 
 // The state of a wave's 16 rows.
-template <int KS>
+template <int KS, int ND>
 struct Rows {
-    double acc[4 * KS][4];  // output channels 16 dt + 4 (lane >> 4) + i of row lane & 15
+    v4i qh[KS], ql[KS];     // byte planes of the queries
+    int32_t cz;
+    double acc[ND][4];      // output channels 16 dt + 4 (lane >> 4) + i of row lane & 15
     double z;
     int32_t m;
+    __device__ void clear()
+    {
+        m = kNone;
+        z = 0.0;
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[dt][i] = 0.0;
+    }
 };
 
 template <int KS>
@@ -90,7 +148,7 @@ __device__ inline void load_queries(const AttnArgs& p, int64_t t, int32_t head, 
         const int d = 64 * s + 16 * g;
         int32_t c[16];
         if (have && d < p.kv.D) {
-            if (p.vec) {
+            if (p.vec_q) {
                 raw[s][0] = *reinterpret_cast<const v4i*>(x + d);
                 raw[s][1] = *reinterpret_cast<const v4i*>(x + d + 8);
             } else {
@@ -135,72 +193,213 @@ __device__ inline void load_queries(const AttnArgs& p, int64_t t, int32_t head, 
     }
 }
 
-// One block of 128 positions for the wave's rows.  lo, hi: the row's
-// positions (lo, hi] without the sinks; sinks: positions below it are seen too
-// (window only).
-template <int KS>
-__device__ inline void attend_block(const AttnArgs& p, Rows<KS>& st, const v4i (&qh)[KS],
-                                    const v4i (&ql)[KS], int32_t cz, int32_t b, int32_t g0,
-                                    int64_t blk, int64_t lo, int64_t hi, bool full)
+// What one row sees: positions (lo, hi], and below the sinks.
+struct Sees {
+    int64_t lo, hi;
+};
+
+// The page list's entries for a block's eight 16-key groups, in the lanes' low
+// three bits, as they are (looked at when the block's turn comes, so that the
+// load can be under way until then).  Blocks past the list are never asked for.
+__device__ inline int32_t load_pages(const AttnArgs& p, int32_t b, int64_t blk)
+{
+    const int64_t e = (blk * kBlk + 16 * (threadIdx.x & 7)) >> p.kv.shift;
+    return p.kv.table[(int64_t)b * p.kv.ld + min(e, p.kv.ld - 1)];
+}
+// Those that are a place in the cache, else -1.
+__device__ inline int32_t valid_pages(const AttnArgs& p, int64_t blk, int32_t pages)
+{
+    const int64_t e = (blk * kBlk + 16 * (threadIdx.x & 7)) >> p.kv.shift;
+    return e < p.kv.ld && pages >= 0 && (int64_t)pages < p.kv.pages ? pages : -1;
+}
+
+// Offsets of a block's keys and values for this lane: of half h, the key row
+// 16 (r >> 2) + (r & 3) of tile 0 (tile j: 4 j rows on) from channel 16 g on,
+// and 16 values of channel r from key 16 g on.  Groups without a place get
+// page 0's (they are masked).
+__device__ inline int64_t key_offset(const AttnArgs& p, int32_t g0, int64_t blk, int32_t pages,
+                                     int h)
+{
+    const int lane = threadIdx.x & 63, r = lane & 15;
+    const int64_t at = blk * kBlk + 64 * h + 16 * (r >> 2);
+    const int64_t pg = max(__shfl(pages, 4 * h + (r >> 2)), 0);
+    return ((((pg * p.kv.G + g0) << p.kv.shift) + (at & (((int64_t)1 << p.kv.shift) - 1))) +
+            (r & 3)) * p.kv.D;
+}
+__device__ inline int64_t value_offset(const AttnArgs& p, int32_t g0, int64_t blk, int32_t pages,
+                                       int h)
 {
     const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-    const int32_t D = p.kv.D, shift = p.kv.shift;
-    const int64_t base = blk * kBlk, psz = (int64_t)1 << shift;
-    // pages of the 16-key groups this lane reads keys of (group r >> 2 of each
-    // 64) and values of (group g)
-    int64_t kp[2], vp[2];
-    uint32_t seen = 0xffffffffu;  // keys 64 (i / 16) + 16 g + i % 16 of row r
-    bool placed = true;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int64_t ka = base + 64 * h + 16 * (r >> 2), va = base + 64 * h + 16 * g;
-        const int64_t kg = kv_page(p.kv, b, ka >> shift), vg = kv_page(p.kv, b, va >> shift);
-        if (vg < 0) {
-            seen &= ~(0xffffu << (16 * h));
-            placed = false;
-        }
-        kp[h] = ((((kg < 0 ? 0 : kg) * p.kv.G + g0) << shift) + (ka & (psz - 1))) * D;
-        vp[h] = ((((vg < 0 ? 0 : vg) * p.kv.G + g0) * D) << shift) + (va & (psz - 1));
-    }
-    const bool mask = !full || __ballot(!placed) != 0;
-    if (mask) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const int64_t j = base + 64 * (i >> 4) + 16 * g + (i & 15);
-            if (!(j <= hi && (j > lo || j < p.sinks))) seen &= ~(1u << i);
-        }
-    }
+    const int64_t at = blk * kBlk + 64 * h + 16 * g;
+    const int64_t pg = max(__shfl(pages, 4 * h + g), 0);
+    return ((((pg * p.kv.G + g0) * p.kv.D) + r) << p.kv.shift) +
+           (at & (((int64_t)1 << p.kv.shift) - 1));
+}
 
-    // scores
-    v4i c[2][4];
+// Channels are taken in steps of 64 (KS of them) by the scores and in tiles of
+// 16 (ND, an even number) by the outputs; what is past the head dimension
+// there reads the head's first channels.  For the scores the query planes are
+// neutral there, the outputs of such a tile are dropped.
+
+// Channel offset of the lane's chunk of a key row in 64-channel step s.
+__device__ inline int32_t key_chunk(const AttnArgs& p, int s)
+{
+    const int32_t d = 64 * s + 16 * ((threadIdx.x & 63) >> 4);
+    return d < p.kv.D ? d : 0;
+}
+// Offset of output tile dt's values from tile 0's.
+__device__ inline int64_t value_tile(const AttnArgs& p, int dt)
+{
+    return 16 * dt < p.kv.D ? (int64_t)(16 * dt) << p.kv.shift : 0;
+}
+
+// Fragments of a block straight from the cache.
+template <int KS>
+struct FromCache {
+    const MQ_GLOBAL int8_t* k[2];
+    const MQ_GLOBAL int8_t* v[2];
+    int32_t chunk[KS];
+    const AttnArgs& p;
+    __device__ FromCache(const AttnArgs& a, int32_t g0, int64_t blk, int32_t pages) : p(a)
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            k[h] = (const MQ_GLOBAL int8_t*)p.kv.k + key_offset(p, g0, blk, pages, h);
+            v[h] = (const MQ_GLOBAL int8_t*)p.kv.v + value_offset(p, g0, blk, pages, h);
+        }
+#pragma unroll
+        for (int s = 0; s < KS; ++s) chunk[s] = key_chunk(p, s);
+    }
+    // The same fragments, to be read anew (their registers are not kept).
+    __device__ FromCache again() const
+    {
+        FromCache o = *this;
+        asm volatile("" : "+v"(o.k[0]), "+v"(o.k[1]));
+        return o;
+    }
+    __device__ v4i key(int h, int j, int s) const
+    {
+        return *reinterpret_cast<const MQ_GLOBAL v4i*>(k[h] + 4 * j * p.kv.D + chunk[s]);
+    }
+    __device__ v4i value(int h, int dt) const
+    {
+        return *reinterpret_cast<const MQ_GLOBAL v4i*>(v[h] + value_tile(p, dt));
+    }
+};
+
+// Fragments staged in LDS in the order of the lanes: 1 KB each, keys (h, j, s)
+// then values (h, dt).
+template <int KS, int ND>
+struct FromLds {
+    const MQ_LDS int8_t* at;  // of this lane
+    __device__ FromLds again() const
+    {
+        FromLds o = *this;
+        asm volatile("" : "+v"(o.at));
+        return o;
+    }
+    __device__ v4i key(int h, int j, int s) const
+    {
+        return *reinterpret_cast<const MQ_LDS v4i*>(at + ((4 * h + j) * KS + s) * 1024);
+    }
+    __device__ v4i value(int h, int dt) const
+    {
+        return *reinterpret_cast<const MQ_LDS v4i*>(at + (8 * KS + ND * h + dt) * 1024);
+    }
+};
+template <int KS, int ND>
+constexpr int kStage = (8 * KS + 2 * ND) * 1024;
+
+// The wave's own copies into LDS have landed (they count as vector memory).
+__device__ inline void wait_staged()
+{
+    __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // vmcnt(0), the others left alone
+}
+
+// The wave's share of a block into a stage: two of the eight key tiles and
+// half of one half's values.
+template <int KS, int ND>
+__device__ inline void stage_block(const AttnArgs& p, int32_t g0, int64_t blk, int32_t pages,
+                                   int wave, MQ_LDS int8_t* stage)
+{
+    const int kh = wave >> 1, vh = wave & 1;
+    const int8_t* k = p.kv.k + key_offset(p, g0, blk, pages, kh);
+    const int8_t* v = p.kv.v + value_offset(p, g0, blk, pages, vh);
+#pragma unroll
+    for (int jj = 0; jj < 2; ++jj) {
+        const int j = 2 * (wave & 1) + jj;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+            __builtin_amdgcn_global_load_lds(
+                (const MQ_GLOBAL void*)(k + 4 * j * p.kv.D + key_chunk(p, s)),
+                (MQ_LDS void*)(stage + ((4 * kh + j) * KS + s) * 1024), 16, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < ND / 2; ++i) {
+        const int dt = 2 * i + (wave >> 1);
+        __builtin_amdgcn_global_load_lds(
+            (const MQ_GLOBAL void*)(v + value_tile(p, dt)),
+            (MQ_LDS void*)(stage + (8 * KS + ND * vh + dt) * 1024), 16, 0, 0);
+    }
+}
+
+// One block of 128 positions for the wave's rows.  pages: of its groups;
+// full: every row sees all of its positions that have a place.
+template <int KS, int ND, class Source>
+__device__ inline void attend_block(const AttnArgs& p, const WeightTable& table, Rows<KS, ND>& st,
+                                    const Source& src, int32_t pages, int64_t blk,
+                                    const Sees& sees, bool full)
+{
+    const int lane = threadIdx.x & 63, g = lane >> 4;
     const v4i zero = {0, 0, 0, 0};
+    const v4i ones = {0x01010101, 0x01010101, 0x01010101, 0x01010101};
+
+    // scores of keys 64 h + 16 g + 4 j + i
+    v4i c[2][4];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int8_t* kr = p.kv.k + kp[h] + (4 * j + (r & 3)) * D + 16 * g;
-            v4i kf[KS];
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-                kf[s] = 64 * s + 16 * g < D ? *reinterpret_cast<const v4i*>(kr + 64 * s) : zero;
             v4i a = zero;
 #pragma unroll
-            for (int s = 0; s < KS; ++s) a = mfma(kf[s], qh[s], a);
+            for (int s = 0; s < KS; ++s) a = mfma(src.key(h, j, s), st.qh[s], a);
 #pragma unroll
             for (int i = 0; i < 4; ++i) a[i] = (int)((uint32_t)a[i] << 8);
-            if (cz != 0) {
-                const v4i ones = {0x01010101, 0x01010101, 0x01010101, 0x01010101};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) a = mfma(src.key(h, j, s), st.ql[s], a);
+            c[h][j] = a;
+            if (j & 1) __builtin_amdgcn_sched_barrier(0);  // bounds the registers
+        }
+    if (st.cz != 0) {
+        const Source again = src.again();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
                 v4i k1 = zero;
 #pragma unroll
-                for (int s = 0; s < KS; ++s) k1 = mfma(kf[s], ones, k1);
+                for (int s = 0; s < KS; ++s) k1 = mfma(again.key(h, j, s), ones, k1);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) a[i] += __mul24(k1[i], cz);
+                for (int i = 0; i < 4; ++i) c[h][j][i] += __mul24(k1[i], st.cz);
             }
-#pragma unroll
-            for (int s = 0; s < KS; ++s) a = mfma(kf[s], ql[s], a);
-            c[h][j] = a;
-        }
+    }
+
+    // the largest that the row sees, without what has no place
+    const uint32_t placed = (uint32_t)__ballot(pages >= 0) & 0xff;
+    const bool mask = !full || placed != 0xff;
+    uint32_t seen = 0xffffffffu;  // bit 16 h + 4 j + i
     if (mask) {
+        const int64_t first = blk * kBlk + 16 * g;
+        const int32_t hi = (int32_t)max(min(sees.hi - first, (int64_t)1000), (int64_t)-1);
+        const int32_t lo = (int32_t)max(min(sees.lo - first, (int64_t)1000), (int64_t)-1);
+        const int32_t sink = (int32_t)max(min(p.sinks - first, (int64_t)1000), (int64_t)0);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const int at = 64 * (i >> 4) + (i & 15);
+            if (!(at <= hi && (at > lo || at < sink))) seen &= ~(1u << i);
+        }
+        if (!((placed >> g) & 1)) seen &= 0xffff0000u;
+        if (!((placed >> (4 + g)) & 1)) seen &= 0x0000ffffu;
 #pragma unroll
         for (int i = 0; i < 32; ++i)
             if (!((seen >> i) & 1)) c[i >> 4][(i >> 2) & 3][i & 3] = kNone;
@@ -208,8 +407,7 @@ __device__ inline void attend_block(const AttnArgs& p, Rows<KS>& st, const v4i (
     int32_t m = kNone;
 #pragma unroll
     for (int i = 0; i < 32; ++i) m = max(m, c[i >> 4][(i >> 2) & 3][i & 3]);
-    m = max(m, __shfl_xor(m, 16));
-    m = max(m, __shfl_xor(m, 32));
+    m = row_max(m);
 
     // weights
     v4i wh[2], wl[2];
@@ -219,16 +417,30 @@ __device__ inline void attend_block(const AttnArgs& p, Rows<KS>& st, const v4i (
         for (int j = 0; j < 4; ++j) {
             int32_t w[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t d = min((uint32_t)m - (uint32_t)c[h][j][i], p.d_cut);
-                w[i] = rint_low(exp2_poly(__builtin_fma(-p.tau, (double)d, kLog2One)) + kRintShift);
-                if (mask && !((seen >> (16 * h + 4 * j + i)) & 1)) w[i] = 0;
-            }
+            for (int i = 0; i < 4; ++i)
+                w[i] = table.weight(p.tau, min((uint32_t)m - (uint32_t)c[h][j][i], p.d_cut));
             int hi4, lo4;
             pack_weights4(w, hi4, lo4);
+            // here and not after all of the table's reads, whose results
+            // would be kept until then
+            asm volatile("" : "+v"(hi4), "+v"(lo4));
             wh[h][j] = hi4;
             wl[h][j] = lo4;
+            if (j & 1) __builtin_amdgcn_sched_barrier(0);
         }
+
+    if (mask) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                // four bits to four bytes
+                const uint32_t bits = (seen >> (16 * h + 4 * j)) & 15;
+                const int keep = (int)(((bits * 0x00204081u) & 0x01010101u) * 255u);
+                wh[h][j] &= keep;
+                wl[h][j] &= keep;
+            }
+    }
 
     // the block joins the rows' state
     const int32_t m_new = max(st.m, m);
@@ -237,13 +449,12 @@ __device__ inline void attend_block(const AttnArgs& p, Rows<KS>& st, const v4i (
         const double rs = factor(p, m_new, st.m);
         st.z *= rs;
 #pragma unroll
-        for (int dt = 0; dt < 4 * KS; ++dt)
+        for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) st.acc[dt][i] *= rs;
         st.m = m_new;
     }
     {
-        const v4i ones = {0x01010101, 0x01010101, 0x01010101, 0x01010101};
         v4i s = mfma(ones, wh[1], mfma(ones, wh[0], zero));
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[i] = (int)((uint32_t)s[i] << 8);
@@ -251,11 +462,8 @@ __device__ inline void attend_block(const AttnArgs& p, Rows<KS>& st, const v4i (
         st.z = __builtin_fma(f, (double)s[0], st.z);
     }
 #pragma unroll
-    for (int dt = 0; dt < 4 * KS; ++dt) {
-        if (16 * dt >= D) break;
-        const int64_t col = (int64_t)(16 * dt + r) << shift;
-        const v4i v0 = *reinterpret_cast<const v4i*>(p.kv.v + vp[0] + col);
-        const v4i v1 = *reinterpret_cast<const v4i*>(p.kv.v + vp[1] + col);
+    for (int dt = 0; dt < ND; ++dt) {
+        const v4i v0 = src.value(0, dt), v1 = src.value(1, dt);
         v4i s = mfma(v1, wh[1], mfma(v0, wh[0], zero));
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[i] = (int)((uint32_t)s[i] << 8);
@@ -263,6 +471,7 @@ __device__ inline void attend_block(const AttnArgs& p, Rows<KS>& st, const v4i (
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             st.acc[dt][i] = __builtin_fma(f, (double)s[i], st.acc[dt][i]);
+        if (dt & 1) __builtin_amdgcn_sched_barrier(0);
     }
 }
 
@@ -282,144 +491,336 @@ __device__ inline void store_out(const AttnArgs& p, int64_t t, int32_t head, int
     else static_cast<int16_t*>(p.y)[at] = (int16_t)q;
 }
 
-// grid (row tiles, G, splits); four waves share a tile's 16 rows and take
-// every fourth block of the split.
-template <int KS>
-__global__ __launch_bounds__(256, 1) void paged_attn_kernel(AttnArgs p)
+// A tile of rows of one sequence and the blocks that its rows see.
+struct Tile {
+    int32_t b;
+    int64_t s0, pos0;        // the sequence's first token row and its position
+    int64_t row0, rows;      // first row (token, head of the group) and the sequence's rows
+    int64_t n, skip0, skip1; // blocks to walk: n, without those in [skip0, skip1)
+    int64_t hi_min, hi_max;  // positions of the first and last token
+    __device__ int64_t block(int64_t i) const { return i < skip0 ? i : i + (skip1 - skip0); }
+    // Every row sees all positions of the block.
+    __device__ bool full(const AttnArgs& p, int64_t blk) const
+    {
+        return (blk + 1) * kBlk - 1 <= hi_min && (p.window == 0 || blk * kBlk > hi_max - p.window);
+    }
+};
+
+// The tile's index counts from floor(starts[b] grp / R) + b for sequence b: an
+// upper bound of the tiles before it that needs no scan.
+template <int R>
+__device__ inline bool find_tile(const AttnArgs& p, int64_t index, Tile& t)
 {
-    __shared__ double lds[4][4][64];
-    __shared__ double lz[4][kRows];
-    __shared__ int32_t lm[4][kRows];
-    const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t* starts = p.kv.starts;
     const int32_t grp = p.grp;
-    const int64_t tile = blockIdx.x;
-    const int32_t b = find_seq(p.kv.B, tile, [=](int32_t i) {
-        return (int64_t)starts[i] * grp / kRows + i;
-    });
-    const int64_t s0 = starts[b], s1 = starts[b + 1], len = p.kv.lens[b];
-    if (s0 < 0 || s1 > p.T || s0 >= s1) return;
-    const int64_t row0 = (tile - (s0 * grp / kRows + b)) * kRows, rows = (s1 - s0) * grp;
-    if (row0 < 0 || row0 >= rows) return;
-    const int32_t g0 = blockIdx.y;
-    const bool have = row0 + r < rows;
-    const int64_t row = have ? row0 + r : rows - 1;
-    const int64_t t = s0 + row / grp;
-    const int32_t head = g0 * grp + (int32_t)(row % grp);
-    // positions seen: (lo, hi], and with a window those below the sinks
-    const int64_t hi = len - s1 + t, lo = p.window > 0 ? hi - p.window : -1;
-
-    // blocks that some row of the tile sees: up to the last row's position,
-    // with a window from the first row's on, and the sinks'
-    const int64_t hi_max = len - s1 + s0 + (min(row0 + kRows, rows) - 1) / grp;
-    const int64_t hi_min = len - s1 + s0 + row0 / grp;
+    t.b = find_seq(p.kv.B, index, [=](int32_t i) { return (int64_t)starts[i] * grp / R + i; });
+    t.s0 = starts[t.b];
+    const int64_t s1 = starts[t.b + 1], len = p.kv.lens[t.b];
+    if (t.s0 < 0 || s1 > p.T || t.s0 >= s1) return false;
+    t.row0 = (index - (t.s0 * grp / R + t.b)) * R;
+    t.rows = (s1 - t.s0) * grp;
+    if (t.row0 < 0 || t.row0 >= t.rows) return false;
+    t.pos0 = len - (s1 - t.s0);
+    t.hi_max = t.pos0 + (min(t.row0 + R, t.rows) - 1) / grp;
+    t.hi_min = t.pos0 + t.row0 / grp;
     const int64_t list = ((p.kv.ld << p.kv.shift) + kBlk - 1) / kBlk;  // blocks with places
-    const int64_t end = hi_max < 0 ? 0 : min(hi_max / kBlk + 1, list);
-    int64_t skip0 = 0, skip1 = 0;  // blocks [skip0, skip1) are seen by none
+    const int64_t end = t.hi_max < 0 ? 0 : min(t.hi_max / kBlk + 1, list);
+    t.skip0 = t.skip1 = 0;
     if (p.window > 0) {
-        skip1 = hi_min - p.window + 1 > 0 ? min((hi_min - p.window + 1) / kBlk, end) : 0;
-        skip0 = min((p.sinks + kBlk - 1) / kBlk, skip1);
+        t.skip1 = t.hi_min - p.window + 1 > 0 ? min((t.hi_min - p.window + 1) / kBlk, end) : 0;
+        t.skip0 = min((p.sinks + kBlk - 1) / kBlk, t.skip1);
     }
-    const int64_t n = end - (skip1 - skip0);
-    const int64_t per = (n + p.splits - 1) / p.splits;
-    const int64_t i0 = per * blockIdx.z, i1 = min(i0 + per, n);
+    t.n = end - (t.skip1 - t.skip0);
+    return true;
+}
 
-    Rows<KS> st;
-    st.m = kNone;
-    st.z = 0.0;
-#pragma unroll
-    for (int dt = 0; dt < 4 * KS; ++dt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) st.acc[dt][i] = 0.0;
-    if (i0 < i1) {
-        v4i qh[KS], ql[KS];
-        int32_t cz;
-        load_queries<KS>(p, t, head, have, qh, ql, cz);
-        for (int64_t i = i0 + wave; i < i1; i += 4) {
-            const int64_t blk = i < skip0 ? i : i + (skip1 - skip0);
-            // every row sees all of the block
-            const bool full = (blk + 1) * kBlk - 1 <= hi_min &&
-                              (p.window == 0 || blk * kBlk > hi_max - p.window);
-            attend_block<KS>(p, st, qh, ql, cz, b, g0, blk, lo, hi, full);
+// Row lane & 15 of the 16 from `first` on: token row, query head, what it sees.
+struct RowAt {
+    bool have;
+    int64_t t;
+    int32_t head;
+    Sees sees;
+    __device__ RowAt(const AttnArgs& p, const Tile& tile, int64_t first, int32_t g0)
+    {
+        const int64_t x = first + (threadIdx.x & 15);
+        have = x < tile.rows;
+        const uint32_t row = (uint32_t)(have ? x : tile.rows - 1);  // rows < 2^26 * 2^10 / G
+        const uint32_t tok = row / (uint32_t)p.grp;
+        t = tile.s0 + tok;
+        head = g0 * p.grp + (int32_t)(row - tok * (uint32_t)p.grp);
+        sees.hi = tile.pos0 + tok;
+        sees.lo = p.window > 0 ? sees.hi - p.window : -1;
+    }
+};
+
+// Four waves share 16 rows and take every fourth block of [i0, i1); their
+// states are joined through LDS.
+template <int KS, int ND>
+__device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g0, int64_t i0,
+                                  int64_t i1, int split, double* lds)
+{
+    const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const RowAt row(p, tile, tile.row0, g0);
+    Rows<KS, ND> st;
+    st.clear();
+    int64_t i = i0 + wave;
+    if (i < i1) {
+        WeightTable table;
+        table.init();
+        int32_t pages = load_pages(p, tile.b, tile.block(i));
+        load_queries<KS>(p, row.t, row.head, row.have, st.qh, st.ql, st.cz);
+        for (; i < i1; i += kWaves) {
+            const int64_t blk = tile.block(i);
+            pages = valid_pages(p, blk, pages);
+            const FromCache<KS> src(p, g0, blk, pages);
+            const int32_t next = load_pages(p, tile.b, tile.block(min(i + kWaves, i1 - 1)));
+            attend_block<KS, ND>(p, table, st, src, pages, blk, row.sees, tile.full(p, blk));
+            pages = next;
         }
     }
 
-    // the four waves' states joined
+    double* lz = lds + kWaves * 4 * 64;                                  // [wave][row]
+    int32_t* lm = reinterpret_cast<int32_t*>(lz + kWaves * kRows);       // [wave][row]
     if (g == 0) {
-        lm[wave][r] = st.m;
-        lz[wave][r] = st.z;
+        lm[wave * kRows + r] = st.m;
+        lz[wave * kRows + r] = st.z;
     }
     __syncthreads();
-    const int32_t m = max(max(lm[0][r], lm[1][r]), max(lm[2][r], lm[3][r]));
+    int32_t m = kNone;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) m = max(m, lm[w * kRows + r]);
     double z = 0.0;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) z = __builtin_fma(factor(p, m, lm[w][r]), lz[w][r], z);
+    for (int w = 0; w < kWaves; ++w)
+        z = __builtin_fma(factor(p, m, lm[w * kRows + r]), lz[w * kRows + r], z);
     const double f = factor(p, m, st.m);
-    const int64_t at = (int64_t)blockIdx.z * p.T * p.H + t * p.H + head;
-    double* part = p.splits > 1 ? p.part + at * (p.kv.D + 2) : nullptr;
-    if (part && have && wave == 0 && g == 0) {
-        part[p.kv.D] = z;
-        part[p.kv.D + 1] = (double)m;
+    const int64_t at = (row.t * p.H + row.head) * p.splits + split;
+    if (p.splits > 1 && row.have && wave == 0 && g == 0) {
+        p.mz[2 * at] = (double)m;
+        p.mz[2 * at + 1] = z;
     }
 #pragma unroll
-    for (int dt = 0; dt < 4 * KS; ++dt) {
+    for (int dt = 0; dt < ND; ++dt) {
         if (16 * dt >= p.kv.D) break;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) lds[wave][i][lane] = f * st.acc[dt][i];
+        for (int i = 0; i < 4; ++i) lds[(wave * 4 + i) * 64 + lane] = f * st.acc[dt][i];
         __syncthreads();
-        const double s = (lds[0][wave][lane] + lds[1][wave][lane]) +
-                         (lds[2][wave][lane] + lds[3][wave][lane]);
-        if (!have) continue;
+        double s = 0.0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) s += lds[(w * 4 + wave) * 64 + lane];
+        if (!row.have) continue;
         const int32_t d = 16 * dt + 4 * g + wave;
-        if (part) part[d] = s;
-        else store_out(p, t, head, d, out_code(p, s, z));
+        if (p.splits > 1) p.sums[at * p.kv.D + d] = s;
+        else store_out(p, row.t, row.head, d, out_code(p, s, z));
     }
 }
 
-// One wave per row joins the splits.
-__global__ __launch_bounds__(256) void paged_attn_join_kernel(AttnArgs p)
+// Every wave has 16 rows of its own; all walk over blocks [i0, i1), staged in
+// LDS by the four together, the next block on its way during this one.
+template <int KS, int ND>
+__device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g0, int64_t i0,
+                                  int64_t i1, int split, MQ_LDS int8_t* lds)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= p.T * p.H) return;
-    const int64_t t = row / p.H;
-    const int32_t b = find_seq(p.kv.B, t, [=](int32_t i) { return (int64_t)p.kv.starts[i]; });
-    if (t < p.kv.starts[b] || t >= p.kv.starts[b + 1]) return;
-    const int32_t D = p.kv.D;
-    const int64_t step = p.T * p.H * (D + 2);
-    const double* part = p.part + row * (D + 2);
-    double m = (double)kNone;
-    for (int s = 0; s < p.splits; ++s) m = fmax(m, part[s * step + D + 1]);
-    double z = 0.0, acc[4] = {0.0, 0.0, 0.0, 0.0};
-    for (int s = 0; s < p.splits; ++s) {
-        const double* x = part + s * step;
-        const double f = exp2_poly(fmax(-p.tau * (m - x[D + 1]), -1100.0));
-        z = __builtin_fma(f, x[D], z);
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const RowAt row(p, tile, tile.row0 + kRows * wave, g0);
+    Rows<KS, ND> st;
+    st.clear();
+    if (i0 < i1) {
+        WeightTable table;
+        table.init();
+        int32_t pages = valid_pages(p, tile.block(i0), load_pages(p, tile.b, tile.block(i0)));
+        stage_block<KS, ND>(p, g0, tile.block(i0), pages, wave, lds);
+        int32_t next = load_pages(p, tile.b, tile.block(min(i0 + 1, i1 - 1)));
+        load_queries<KS>(p, row.t, row.head, row.have, st.qh, st.ql, st.cz);
+        wait_staged();
+        __syncthreads();
+        for (int64_t i = i0; i < i1; ++i) {
+            const int64_t blk = tile.block(i);
+            const int buf = (int)(i - i0) & 1;
+            const int64_t blk1 = tile.block(min(i + 1, i1 - 1));
+            next = valid_pages(p, blk1, next);
+            if (i + 1 < i1)
+                stage_block<KS, ND>(p, g0, blk1, next, wave, lds + (buf ^ 1) * kStage<KS, ND>);
+            const int32_t after = load_pages(p, tile.b, tile.block(min(i + 2, i1 - 1)));
+            const FromLds<KS, ND> src{lds + buf * kStage<KS, ND> + lane * 16};
+            attend_block<KS, ND>(p, table, st, src, pages, blk, row.sees, tile.full(p, blk));
+            pages = next;
+            next = after;
+            wait_staged();
+            __syncthreads();
+        }
+    }
+    if (!row.have) return;
+    if (p.splits > 1) {
+        const int64_t at = (row.t * p.H + row.head) * p.splits + split;
+        if (g == 0) {
+            p.mz[2 * at] = (double)st.m;
+            p.mz[2 * at + 1] = st.z;
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (lane + 64 * i < D) acc[i] = __builtin_fma(f, x[lane + 64 * i], acc[i]);
+        for (int dt = 0; dt < ND; ++dt) {
+            if (16 * dt >= p.kv.D) break;
+            double* s = p.sums + at * p.kv.D + 16 * dt + 4 * g;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] = st.acc[dt][i];
+        }
+        return;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (lane + 64 * i < D)
-            store_out(p, t, (int32_t)(row % p.H), lane + 64 * i, out_code(p, acc[i], z));
+    for (int dt = 0; dt < ND; ++dt) {
+        if (16 * dt >= p.kv.D) break;
+        int32_t q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = out_code(p, st.acc[dt][i], st.z);
+        const int32_t d = 16 * dt + 4 * g;
+        const int64_t at = row.t * p.ldy + (int64_t)row.head * p.kv.D + d;
+        if (!p.vec_y) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) store_out(p, row.t, row.head, d + i, q[i]);
+        } else if (p.out_bits == 8) {
+            *reinterpret_cast<uint32_t*>(static_cast<int8_t*>(p.y) + at) =
+                (uint32_t)(uint8_t)q[0] | ((uint32_t)(uint8_t)q[1] << 8) |
+                ((uint32_t)(uint8_t)q[2] << 16) | ((uint32_t)(uint8_t)q[3] << 24);
+        } else {
+            *reinterpret_cast<uint2*>(static_cast<int16_t*>(p.y) + at) =
+                make_uint2((uint32_t)(uint16_t)q[0] | ((uint32_t)(uint16_t)q[1] << 16),
+                           (uint32_t)(uint16_t)q[2] | ((uint32_t)(uint16_t)q[3] << 16));
+        }
+    }
+}
+
+// The split's blocks [i0, i1) of the tile.
+__device__ inline void split_range(const AttnArgs& p, const Tile& t, int split, int64_t& i0,
+                                   int64_t& i1)
+{
+    const int64_t per = (t.n + p.splits - 1) / p.splits;
+    i0 = per * split;
+    i1 = min(i0 + per, t.n);
+}
+
+// grid (tiles of 16 rows, G, splits)
+template <int KS, int ND>
+__global__ __launch_bounds__(256, KS <= 2 ? 2 : 1) void paged_attn_split_kernel(AttnArgs p)
+{
+    __shared__ double lds[kWaves * 4 * 64 + kWaves * kRows * 3 / 2];
+    Tile tile;
+    if (!find_tile<kRows>(p, blockIdx.x, tile)) return;
+    int64_t i0, i1;
+    split_range(p, tile, blockIdx.z, i0, i1);
+    split_rows<KS, ND>(p, tile, blockIdx.y, i0, i1, blockIdx.z, lds);
+}
+
+// grid (tiles of 64 rows, G, splits); a sequence's last 16 rows or fewer are
+// split among the waves.
+template <int KS, int ND>
+__global__ __launch_bounds__(256, KS <= 2 ? 2 : 1) void paged_attn_tile_kernel(AttnArgs p)
+{
+    __shared__ __attribute__((aligned(1024))) int8_t lds[2 * kStage<KS, ND>];
+    Tile tile;
+    // the last tiles of a prompt see the most keys: they go first
+    if (!find_tile<kTile>(p, gridDim.x - 1 - blockIdx.x, tile)) return;
+    int64_t i0, i1;
+    split_range(p, tile, blockIdx.z, i0, i1);
+    if (tile.rows - tile.row0 <= kRows)
+        split_rows<KS, ND>(p, tile, blockIdx.y, i0, i1, blockIdx.z, reinterpret_cast<double*>(lds));
+    else
+        share_keys<KS, ND>(p, tile, blockIdx.y, i0, i1, blockIdx.z, (MQ_LDS int8_t*)lds);
+}
+
+// Joins the splits: NW waves per row and 64 channels, each every NW-th split.
+template <int NW>
+__global__ __launch_bounds__(NW < 4 ? 256 : 64 * NW) void paged_attn_join_kernel(AttnArgs p)
+{
+    __shared__ double lds[NW][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int units = NW < 4 ? 4 / NW : 1;
+    const int64_t row = (int64_t)blockIdx.x * units + wave / NW;
+    if (row >= p.T * p.H) return;
+    const int w = wave % NW;
+    const int64_t t = row / p.H;
+    const int32_t* starts = p.kv.starts;
+    const int32_t b = find_seq(p.kv.B, t, [=](int32_t i) { return (int64_t)starts[i]; });
+    if (t < starts[b] || t >= starts[b + 1]) return;
+    const double* mz = p.mz + row * p.splits * 2;
+    double m = (double)kNone, f[kMaxSplits / 64], z = 0.0;
+#pragma unroll
+    for (int i = 0; i < kMaxSplits / 64; ++i) {
+        f[i] = lane + 64 * i < p.splits ? mz[2 * (lane + 64 * i)] : (double)kNone;
+        m = fmax(m, f[i]);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmax(m, __shfl_xor(m, o));
+#pragma unroll
+    for (int i = 0; i < kMaxSplits / 64; ++i) {
+        f[i] = exp2_poly(fmax(-p.tau * (m - f[i]), -1000.0));
+        if (lane + 64 * i < p.splits) z = __builtin_fma(f[i], mz[2 * (lane + 64 * i) + 1], z);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o);
+    const int32_t d = blockIdx.y * 64 + lane;
+    const bool have = d < p.kv.D;
+    const double* x = p.sums + row * p.splits * p.kv.D + (have ? d : 0);
+    double acc = 0.0;
+#pragma unroll
+    for (int i = 0; i < kMaxSplits / 64; ++i) {
+        const int end = min(64, p.splits - 64 * i);
+        for (int s0 = w; s0 < end; s0 += 8 * NW) {  // eight loads in flight
+            double v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int s = min(s0 + u * NW, end - 1);
+                v[u] = x[(int64_t)(64 * i + s) * p.kv.D];
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const double fs = __shfl(f[i], (s0 + u * NW) & 63);
+                if (s0 + u * NW < end) acc = __builtin_fma(fs, v[u], acc);
+            }
+        }
+    }
+    if (NW > 1) {
+        lds[wave][lane] = acc;
+        __syncthreads();
+        if (w != 0) return;
+        acc = 0.0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) acc += lds[i][lane];
+    }
+    if (have) store_out(p, t, (int32_t)(row % p.H), d, out_code(p, acc, z));
 }
 
 // Row tiles of all sequences, at most.
-int64_t row_tiles(int64_t T, int64_t B, int32_t grp) { return T * grp / kRows + B; }
+int64_t row_tiles(int64_t T, int64_t B, int32_t grp, int R) { return T * grp / R + B; }
 
-// Parts the keys of every tile are split into: enough work-groups for the
-// chip, at least four blocks each.
+// Whether the sequences have more rows than a wave takes, on average.
+bool tiled(int64_t T, int64_t B, int32_t grp) { return T * grp > B * kRows; }
+
+// Parts the keys of every tile are split into: two work-groups per CU, at
+// least a block per wave in each.
 int64_t split_count(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D, int64_t max_len)
 {
-    const int64_t groups = row_tiles(T, B, H / G) * G;
-    int64_t s = 1024 / (groups > 0 ? groups : 1);
+    const int32_t grp = H / G;
+    const int R = tiled(T, B, grp) ? kTile : kRows;
+    const int64_t groups = std::max(T * grp / R, std::min(B, T)) * G;
+    int64_t s = 512 / std::max<int64_t>(groups, 1);
     const int64_t blocks = (max_len + kBlk - 1) / kBlk;
-    s = std::min(s, (blocks + 3) / 4);
+    s = std::min(s, (blocks + kWaves - 1) / kWaves);
     s = std::min<int64_t>(s, MQ_ATTN_MAX_WORKSPACE / (T * H * (D + 2) * 8));
-    return s < 1 ? 1 : s;
+    return std::max<int64_t>(1, std::min<int64_t>(s, kMaxSplits));
+}
+
+template <int ND>
+void launch_main(const AttnArgs& p, int64_t B, hipStream_t s)
+{
+    constexpr int KS = (ND + 3) / 4;
+    const bool t = tiled(p.T, B, p.grp);
+    const dim3 grid((unsigned)row_tiles(p.T, B, p.grp, t ? kTile : kRows), (unsigned)p.kv.G,
+                    (unsigned)p.splits);
+    if (t) paged_attn_tile_kernel<KS, ND><<<grid, 256, 0, s>>>(p);
+    else paged_attn_split_kernel<KS, ND><<<grid, 256, 0, s>>>(p);
 }
 
 }  // namespace
@@ -452,32 +853,48 @@ hipError_t launch_paged_attn(const KvArgs& kv, const int16_t* q, int64_t ldq, in
     p.out_zp = out_zp;
     p.out_bits = out_bits;
     const double sigma = (double)q_scale * (double)k_scale * (double)logit_scale;
-    p.tau = sigma * 1.4426950408889634;  // log2(e)
+    // (from 128 on only the largest logits of a block, and of the row, weigh
+    // anything, whatever the scale)
+    p.tau = std::min(sigma * 1.4426950408889634, 128.0);  // log2(e)
     p.v_scale = v_scale;
     p.out_scale = out_scale;
-    // a weight is 0 below 2^-1: from 2^-40 of the largest on, whatever the
-    // distance
+    // a weight is 0 below 1/2: from 2^-40 of the largest on whatever the
+    // distance (tau d_cut <= 40 + tau)
     const double cut = 40.0 / p.tau;
     p.d_cut = cut < 4294967295.0 ? (uint32_t)std::ceil(cut) : 0xFFFFFFFFu;
     p.window = window;
     p.sinks = window > 0 ? sinks : 0;
-    p.vec = ((uintptr_t)q % 16) == 0 && ldq % 8 == 0;
+    p.vec_q = ((uintptr_t)q % 16) == 0 && ldq % 8 == 0;
+    p.vec_y = ((uintptr_t)y % (out_bits / 2)) == 0 && ldy % 4 == 0;
+    // the blocks that a row of a windowed call walks over
+    if (window > 0 && window < max_len)
+        max_len = std::min(max_len, window + std::min(p.sinks, max_len) + 2 * kBlk);
     int64_t splits = split_count(T, kv.B, H, kv.G, kv.D, max_len);
     const int64_t one = T * H * (kv.D + 2) * 8;
-    if (!ws) splits = 1;
-    splits = std::min(splits, std::max<int64_t>(ws_bytes / one, 1));
+    splits = ws ? std::min(splits, std::max<int64_t>(ws_bytes / one, 1)) : 1;
     p.splits = (int32_t)splits;
-    p.part = static_cast<double*>(ws);
-    const dim3 grid((unsigned)row_tiles(T, kv.B, p.grp), (unsigned)kv.G, (unsigned)splits);
-    switch ((kv.D + 63) / 64) {
-    case 1: paged_attn_kernel<1><<<grid, 256, 0, s>>>(p); break;
-    case 2: paged_attn_kernel<2><<<grid, 256, 0, s>>>(p); break;
-    case 3: paged_attn_kernel<3><<<grid, 256, 0, s>>>(p); break;
-    default: paged_attn_kernel<4><<<grid, 256, 0, s>>>(p); break;
+    p.mz = static_cast<double*>(ws);
+    p.sums = p.mz + T * H * splits * 2;
+    switch ((kv.D + 31) / 32) {
+    case 1: launch_main<2>(p, kv.B, s); break;
+    case 2: launch_main<4>(p, kv.B, s); break;
+    case 3: launch_main<6>(p, kv.B, s); break;
+    case 4: launch_main<8>(p, kv.B, s); break;
+    case 5: launch_main<10>(p, kv.B, s); break;
+    case 6: launch_main<12>(p, kv.B, s); break;
+    case 7: launch_main<14>(p, kv.B, s); break;
+    default: launch_main<16>(p, kv.B, s); break;
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
-    paged_attn_join_kernel<<<(unsigned)((T * H + 3) / 4), 256, 0, s>>>(p);
+    const unsigned chunks = (unsigned)((kv.D + 63) / 64);
+    const int64_t rows = T * H;
+    if (splits <= 8)
+        paged_attn_join_kernel<1><<<dim3((unsigned)((rows + 3) / 4), chunks), 256, 0, s>>>(p);
+    else if (splits <= 64)
+        paged_attn_join_kernel<4><<<dim3((unsigned)rows, chunks), 256, 0, s>>>(p);
+    else
+        paged_attn_join_kernel<16><<<dim3((unsigned)rows, chunks), 1024, 0, s>>>(p);
     return hipGetLastError();
 }
 

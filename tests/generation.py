@@ -85,12 +85,13 @@ def paged_attn(q, fq, k_cache, k_scale, v_cache, fv, starts, lens, pages, logit_
 
 
 def assert_codes(got, real, scale, zp, bits, slack):
-    """Codes of real values: equal, but for one step where the value lies
-    within ``slack`` (in steps) of a rounding tie."""
+    """Codes of real values: equal, but for one step in at most one of a
+    thousand where the value lies within ``slack`` (in steps) of a rounding tie."""
     want = code(real, scale, zp, bits)
     bad = np.nonzero(got != want)
     if len(bad[0]) == 0:
         return
+    assert len(bad[0]) <= 1e-3 * want.size, (len(bad[0]), want.size)
     v = real[bad] / f32(scale)
     tie = np.abs(v - np.floor(v) - 0.5)
     assert (np.abs(got[bad].astype(np.int64) - want[bad]) <= 1).all() and (tie <= slack).all(), \
