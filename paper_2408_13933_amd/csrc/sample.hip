@@ -4,16 +4,19 @@
 // Weights are integers, w = rint(2^40 exp((x - max x) / temperature)), so a
 // sum is the same in whatever order it is made.  Logits are compared as
 // 32-bit keys that ascend with them (0: never drawn).  The kept words are a
-// prefix of the order (key descending, index ascending) in every setting: all
-// keys above some key and the first few words at it.
+// prefix of the order (key descending, index ascending) in every setting: a
+// cut is the last kept word's key and index.
 //
-// 1. scan: a wave reads 2048 logits, notes their largest key and lists the
-//    few words whose key is at least its 24th largest lane maximum.  Together
-//    the lists hold every word of the row above the largest of these bounds.
-// 2. sums (only rows that need the weight of all words): the weights of each
-//    2048 words added.
-// 3. draw: a block per row, on the listed words in LDS wherever the kept ones
-//    are among them, else on the whole row.
+// 1. scan: a wave reads 2048 logits, notes the largest and lists the few words
+//    at or above a bound that 24 of its lanes' maxima reach.  Together the
+//    lists hold every word of the row above the largest of these bounds.
+// 2. sums (rows without top_k): the weights of all words, added per 2048 words
+//    or, for top_p, per bin of logit distance from the largest.
+// 3. gather (top_p rows whose cut is below what the lists hold): the words of
+//    the cut's bin, and the weights above it per 2048 words.
+// 4. draw: a block per row finds the cut among the listed or gathered words,
+//    then the word; rows that neither serves (a top_k larger than the lists
+//    hold, thousands of equal logits at the cut) walk over the whole row.
 #include <algorithm>
 
 #include "codes.h"
@@ -22,13 +25,24 @@
 namespace mq {
 namespace {
 
-constexpr int kSeg = 2048;       // words per wave of the first two kernels
+constexpr int kSeg = 2048;       // words per wave of the first three kernels
 constexpr int kList = 64;        // places in a wave's list
 constexpr int kRank = 24;        // lane maxima at or above a list's bound
+constexpr int kBins = 1024;
+constexpr double kBinScale = 24.0;  // bins per factor of two: weights past the last are 0
 constexpr int kDrawThreads = 512, kDrawWaves = kDrawThreads / 64;
-constexpr int kBins = 2 * kDrawThreads, kBinBits = 10;
-constexpr int kEntries = 8192;   // listed words that the draw takes into LDS
+constexpr int kEntries = 4096;   // listed words that the draw takes into LDS
+constexpr int kGather = 2048;    // gathered words of a row
+constexpr int kNear = 512;       // words of the cut's bin among the listed ones
 constexpr double kOne = 1099511627776.0;  // 2^40
+
+// A row's part of the workspace beyond its segments'.
+struct RowWork {
+    unsigned long long mass[kBins];
+    uint2 near[kGather];  // key, index of the words in the cut's bin
+    uint32_t found;       // how many there are (also past the places)
+    uint32_t pad[3];
+};
 
 struct SampleArgs {
     const void* x;
@@ -45,25 +59,40 @@ struct SampleArgs {
     uint4* info;            // [rows][segs]: largest key, bound, listed words
     uint2* list;            // [rows][segs][kList]: key, index
     int64_t* sums;          // [rows][segs]
+    RowWork* work;          // [rows]
 };
 
+// Logits as they are compared: of_key(key(v)) == v for the values that occur.
 struct Fp32 {
     using T = float;
-    static __device__ uint32_t key(float x)
+    using V = float;
+    static constexpr int kTopBit = 31;
+    static constexpr uint32_t kLeast = 0x00800000u;  // of the least finite value
+    static __device__ V load(float x) { return x; }
+    static __device__ V none() { return -__builtin_inff(); }
+    static __device__ V larger(V a, V b) { return fmaxf(a, b); }  // the other one for NaN
+    static __device__ uint32_t key(V x)
     {
-        uint32_t b = __float_as_uint(x);
-        if (b == 0x80000000u) b = 0;           // -0 is 0
-        const uint32_t k = (b >> 31) ? ~b : b | 0x80000000u;
-        return !(x > -__builtin_inff()) ? 0 : k;  // NaN and -inf are never drawn
+        const uint32_t b = __float_as_uint(x + 0.0f);  // -0 is 0
+        const uint32_t k = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+        return x > -__builtin_inff() ? k : 0;  // NaN and -infinity are never drawn
     }
-    static __device__ double value(const SampleArgs&, uint32_t k)
+    static __device__ V of_key(uint32_t k)
     {
-        return (double)__uint_as_float((k >> 31) ? k & 0x7fffffffu : ~k);
+        return __uint_as_float((k >> 31) ? k & 0x7fffffffu : ~k);
     }
+    static __device__ double value(const SampleArgs&, uint32_t k) { return (double)of_key(k); }
 };
 struct Code16 {
     using T = int16_t;
-    static __device__ uint32_t key(int16_t q) { return (uint32_t)((int32_t)q + 32769); }
+    using V = int32_t;
+    static constexpr int kTopBit = 16;
+    static constexpr uint32_t kLeast = 1;
+    static __device__ V load(int16_t q) { return (int32_t)q + 32769; }
+    static __device__ V none() { return 0; }
+    static __device__ V larger(V a, V b) { return max(a, b); }
+    static __device__ uint32_t key(V v) { return (uint32_t)v; }
+    static __device__ V of_key(uint32_t k) { return (int32_t)k; }
     static __device__ double value(const SampleArgs& p, uint32_t k)
     {
         return p.alpha * (double)((int32_t)k - 32769 - p.zp);
@@ -110,8 +139,19 @@ __device__ inline int64_t weight(const SampleArgs& a, const Row& r, uint32_t k)
     return __double_as_longlong(w) - __double_as_longlong(kRintShift);
 }
 
-// Whether the row's draw needs the weights of all words.
+// The bin of a key's distance from the largest (0: the largest's; the same
+// for equal logits, never less for smaller ones).
+template <class F>
+__device__ inline int32_t bin_of(const SampleArgs& a, const Row& r, uint32_t k)
+{
+    if (k == r.kmax) return 0;
+    const double z = (r.max - F::value(a, k)) * r.scale;  // NaN with infinities: the last
+    return z * kBinScale < (double)(kBins - 1) ? (int32_t)(z * kBinScale) : kBins - 1;
+}
+
+// Rows without top_k need the weights of all words: with top_p per bin.
 __device__ inline bool needs_sums(const Row& r) { return r.k == 0; }
+__device__ inline bool needs_bins(const Row& r) { return r.k == 0 && r.p < 1.0; }
 
 template <class F>
 __global__ __launch_bounds__(256) void sample_scan_kernel(SampleArgs a, int64_t row0)
@@ -121,35 +161,46 @@ __global__ __launch_bounds__(256) void sample_scan_kernel(SampleArgs a, int64_t 
     if (seg >= a.segs) return;
     const int64_t m = blockIdx.y;
     const typename F::T* x = static_cast<const typename F::T*>(a.x) + (row0 + m) * a.ld;
+    // the row's bins and counter start at zero
+    RowWork& work = a.work[m];
+    for (int i = seg * 64 + lane; i < kBins; i += a.segs * 64) work.mass[i] = 0;
+    if (seg == 0 && lane == 0) work.found = 0;
+
     const int32_t i0 = seg * kSeg + lane;
-    uint32_t k[kSeg / 64];
-    uint32_t top = 0;
+    typename F::V k[kSeg / 64];
 #pragma unroll
-    for (int j = 0; j < kSeg / 64; ++j) k[j] = i0 + 64 * j < a.V ? F::key(x[i0 + 64 * j]) : 0;
+    for (int j = 0; j < kSeg / 64; ++j) k[j] = i0 + 64 * j < a.V ? F::load(x[i0 + 64 * j]) : F::none();
+    typename F::V most = F::none();
 #pragma unroll
-    for (int j = 0; j < kSeg / 64; ++j) top = max(top, k[j]);
-    // the largest bound that kRank lanes' maxima reach
+    for (int j = 0; j < kSeg / 64; ++j) most = F::larger(most, k[j]);
+    uint32_t top = F::key(most);
+    // the largest bound of 16 leading bits that kRank lanes' maxima reach
     uint32_t bound = 0;
-#pragma unroll 1
-    for (int bit = 31; bit >= 0; --bit) {
+#pragma unroll
+    for (int bit = F::kTopBit; bit > F::kTopBit - 16 && bit >= 0; --bit) {
         const uint32_t c = bound | (1u << bit);
         if (__popcll(__ballot(top >= c)) >= kRank) bound = c;
     }
-    bound = max(bound, 1u);  // key 0 is never listed
+    bound = max(bound, F::kLeast);
+    typename F::V at_least = F::of_key(bound);
     int n = 0;
 #pragma unroll
-    for (int j = 0; j < kSeg / 64; ++j) n += __popcll(__ballot(k[j] >= bound));
+    for (int j = 0; j < kSeg / 64; ++j) n += __popcll(__ballot(k[j] >= at_least));
     if (n > kList) {  // the smallest bound that leaves no more than the list holds
         uint32_t b = 0;
 #pragma unroll 1
-        for (int bit = 31; bit >= 0; --bit) {
+        for (int bit = F::kTopBit; bit >= 0; --bit) {
             const uint32_t c = b | (1u << bit);
+            const typename F::V v = F::of_key(c);
             int cnt = 0;
+            // (bounds that are no value: NaN above +infinity, none reach them;
+            // below the least, all do)
 #pragma unroll
-            for (int j = 0; j < kSeg / 64; ++j) cnt += __popcll(__ballot(k[j] >= c));
-            if (cnt > kList) b = c;
+            for (int j = 0; j < kSeg / 64; ++j) cnt += __popcll(__ballot(k[j] >= v));
+            if (c < F::kLeast || cnt > kList) b = c;
         }
-        bound = b + 1;  // b: the largest key that too many reach (b < 2^32 - 1)
+        bound = b + 1;  // b: the largest key that too many reach
+        at_least = F::of_key(bound);
     }
     const int64_t at = m * a.segs + seg;
     uint2* list = a.list + at * kList;
@@ -157,10 +208,11 @@ __global__ __launch_bounds__(256) void sample_scan_kernel(SampleArgs a, int64_t 
     const uint64_t below = ((uint64_t)1 << lane) - 1;
 #pragma unroll
     for (int j = 0; j < kSeg / 64; ++j) {
-        const uint64_t hit = __ballot(k[j] >= bound);
+        const uint64_t hit = __ballot(k[j] >= at_least);
         if (hit) {
-            if (k[j] >= bound)
-                list[pos + __popcll(hit & below)] = make_uint2(k[j], (uint32_t)(i0 + 64 * j));
+            if (k[j] >= at_least)
+                list[pos + __popcll(hit & below)] =
+                    make_uint2(F::key(k[j]), (uint32_t)(i0 + 64 * j));
             pos += __popcll(hit);
         }
     }
@@ -169,35 +221,175 @@ __global__ __launch_bounds__(256) void sample_scan_kernel(SampleArgs a, int64_t 
     if (lane == 0) a.info[at] = make_uint4(top, bound, (uint32_t)pos, 0);
 }
 
-// The row's largest key, from its segments (every lane of the wave).
-__device__ inline uint32_t row_max(const SampleArgs& a, int64_t m)
+// The row's largest key and the largest bound of its lists (every lane of the
+// wave).
+__device__ inline uint2 row_info(const SampleArgs& a, int64_t m)
 {
-    uint32_t top = 0;
-    for (int i = threadIdx.x & 63; i < a.segs; i += 64) top = max(top, a.info[m * a.segs + i].x);
+    uint32_t top = 0, bound = 1;
+    for (int i = threadIdx.x & 63; i < a.segs; i += 64) {
+        const uint4 v = a.info[m * a.segs + i];
+        top = max(top, v.x);
+        bound = max(bound, v.y);
+    }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-    return top;
+    for (int o = 32; o > 0; o >>= 1) {
+        top = max(top, (uint32_t)__shfl_xor((int)top, o));
+        bound = max(bound, (uint32_t)__shfl_xor((int)bound, o));
+    }
+    return make_uint2(top, bound);
 }
 
 template <class F>
 __global__ __launch_bounds__(256) void sample_sums_kernel(SampleArgs a, int64_t row0)
 {
+    __shared__ unsigned long long mass[kBins];
+    const int lane = threadIdx.x & 63;
+    const int seg = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t m = blockIdx.y;
+    const uint32_t kmax = row_info(a, m).x;
+    const Row r = row_of<F>(a, row0 + m, kmax);
+    if (!needs_sums(r) || kmax == 0) return;  // the same for the whole block
+    const typename F::T* x = static_cast<const typename F::T*>(a.x) + (row0 + m) * a.ld;
+    const int32_t i0 = seg * kSeg + lane, left = seg < a.segs ? a.V : 0;
+    const bool bins = needs_bins(r);
+    if (bins) {
+        for (int i = threadIdx.x; i < kBins; i += 256) mass[i] = 0;
+        __syncthreads();
+    }
+    int64_t s = 0;
+#pragma unroll 1
+    for (int j0 = 0; j0 < kSeg / 64; j0 += 8) {
+        uint32_t k[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int32_t i = i0 + 64 * (j0 + j);
+            k[j] = i < left ? F::key(F::load(x[i])) : 0;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int64_t w = weight<F>(a, r, k[j]);
+            if (bins) {
+                if (w) atomicAdd(&mass[bin_of<F>(a, r, k[j])], (unsigned long long)w);
+            } else {
+                s += (double)w >= r.floor ? w : 0;
+            }
+        }
+    }
+    if (bins) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < kBins; i += 256)
+            if (mass[i]) atomicAdd(&a.work[m].mass[i], mass[i]);
+        return;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    if (lane == 0 && left) a.sums[m * a.segs + seg] = s;
+}
+
+// What a search over bins finds: the first bin from the top that reaches the
+// target (else the last one that holds anything), and the words and mass of
+// the bins before it.
+struct Found {
+    int32_t bin;
+    int64_t count, mass;
+    int64_t total;  // mass of all bins
+};
+
+// One wave looks for the bin; lane l holds bins 16 l on.  reaches(count,
+// mass) of everything up to and with a bin.
+template <class Reaches>
+__device__ inline Found find_bin(const uint32_t* count, const unsigned long long* mass,
+                                 Reaches reaches)
+{
+    constexpr int per = kBins / 64;
+    const int lane = threadIdx.x & 63;
+    int64_t n = 0, w = 0;
+#pragma unroll
+    for (int i = 0; i < per; ++i) {
+        n += count ? count[lane * per + i] : 0;
+        w += (int64_t)mass[lane * per + i];
+    }
+    int64_t ns = n, wsum = w;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t t = __shfl_up(ns, o), v = __shfl_up(wsum, o);
+        if (lane >= o) {
+            ns += t;
+            wsum += v;
+        }
+    }
+    Found f;
+    f.total = __shfl(wsum, 63);
+    const uint64_t hit = __ballot(reaches(ns, wsum)), some = __ballot(n > 0 || w > 0);
+    const int l = hit ? __builtin_ctzll(hit) : some ? 63 - __builtin_clzll(some) : 0;
+    int64_t nb = __shfl(ns - n, l), mb = __shfl(wsum - w, l);
+    int32_t last = l * per;
+    f.count = nb;
+    f.mass = mb;
+    for (int i = 0; i < per; ++i) {  // the same in every lane
+        const int64_t c = count ? count[l * per + i] : 0, v = (int64_t)mass[l * per + i];
+        if (c == 0 && v == 0) continue;
+        last = l * per + i;
+        f.count = nb;
+        f.mass = mb;
+        nb += c;
+        mb += v;
+        if (hit && reaches(nb, mb)) break;
+    }
+    f.bin = last;
+    return f;
+}
+
+// The bin of a top_p row's cut, and whether the lists hold all of it.
+template <class F>
+__device__ inline Found find_mass_bin(const SampleArgs& a, const Row& r, int64_t m)
+{
+    int64_t total = 0;
+    const unsigned long long* mass = a.work[m].mass;
+    for (int i = threadIdx.x & 63; i < kBins; i += 64) total += (int64_t)mass[i];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
+    const double target = r.p * (double)total;
+    return find_bin(nullptr, mass, [=](int64_t, int64_t w) { return (double)w >= target; });
+}
+
+// Gathers the words of the cut's bin and adds the weights above it.
+template <class F>
+__global__ __launch_bounds__(256) void sample_gather_kernel(SampleArgs a, int64_t row0)
+{
     const int lane = threadIdx.x & 63;
     const int seg = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (seg >= a.segs) return;
     const int64_t m = blockIdx.y;
-    const uint32_t kmax = row_max(a, m);
-    const Row r = row_of<F>(a, row0 + m, kmax);
-    if (!needs_sums(r) || kmax == 0) return;
+    const uint2 info = row_info(a, m);
+    if (info.x == 0) return;
+    const Row r = row_of<F>(a, row0 + m, info.x);
+    if (!needs_bins(r)) return;
+    const Found f = find_mass_bin<F>(a, r, m);
+    if (f.bin < bin_of<F>(a, r, info.y)) return;  // the lists hold it
     const typename F::T* x = static_cast<const typename F::T*>(a.x) + (row0 + m) * a.ld;
     const int32_t i0 = seg * kSeg + lane;
-    // without top_p the floor alone decides what is kept
-    const double least = r.p < 1.0 ? 0.0 : r.floor;
+    RowWork& work = a.work[m];
     int64_t s = 0;
-#pragma unroll 4
-    for (int j = 0; j < kSeg / 64; ++j) {
-        const int64_t w = i0 + 64 * j < a.V ? weight<F>(a, r, F::key(x[i0 + 64 * j])) : 0;
-        s += (double)w >= least ? w : 0;
+#pragma unroll 1
+    for (int j0 = 0; j0 < kSeg / 64; j0 += 8) {
+        uint32_t k[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int32_t i = i0 + 64 * (j0 + j);
+            k[j] = i < a.V ? F::key(F::load(x[i])) : 0;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int32_t bin = k[j] ? bin_of<F>(a, r, k[j]) : kBins;
+            if (bin < f.bin) {
+                const int64_t w = weight<F>(a, r, k[j]);
+                s += (double)w >= r.floor ? w : 0;
+            } else if (bin == f.bin) {
+                const uint32_t n = atomicAdd(&work.found, 1u);
+                if (n < kGather) work.near[n] = make_uint2(k[j], (uint32_t)(i0 + 64 * (j0 + j)));
+            }
+        }
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
@@ -210,17 +402,18 @@ __global__ __launch_bounds__(256) void sample_sums_kernel(SampleArgs a, int64_t 
 struct DrawLds {
     uint32_t count[kBins];
     unsigned long long mass[kBins];
-    uint32_t key[kEntries];
-    uint32_t idx[kEntries];
+    // listed words, as order() has them; gathered ones and, past kGather, the
+    // same in order
+    uint64_t word[kEntries];
+    uint64_t near[2 * kNear];
     int64_t wave64[kDrawWaves];
     int32_t wave32[kDrawWaves];
     uint32_t sel[4];
-    int64_t sel64[2];
+    int64_t sel64[4];
 };
 
-// Sums of one value per thread over the block: the sum of the threads before
-// this one, and the total.
-__device__ inline int64_t block_scan(int64_t v, int64_t* total, int64_t* lds)
+// The sum of the values of the threads before this one, and of all.
+__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* total, int64_t* lds)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int64_t s = v;
@@ -241,6 +434,71 @@ __device__ inline int64_t block_scan(int64_t v, int64_t* total, int64_t* lds)
     return before + s - v;
 }
 
+// A word as one number that ascends along the order.
+__device__ __forceinline__ uint64_t order(uint32_t key, uint32_t idx)
+{
+    return ((uint64_t)~key << 32) | idx;
+}
+__device__ __forceinline__ uint32_t key_of(uint64_t w) { return ~(uint32_t)(w >> 32); }
+
+// The last kept word.
+struct Cut {
+    uint32_t key, idx;
+    int64_t mass;  // of it and all before it in the order
+    __device__ bool keeps(uint32_t k, uint32_t i) const { return k > key || (k == key && i <= idx); }
+};
+
+// n words in LDS put in order (dst): each counts those before it.
+__device__ __forceinline__ void order_words(const uint64_t* src, int n, uint64_t* dst)
+{
+    for (int e = threadIdx.x; e < n; e += kDrawThreads) {
+        const uint64_t w = src[e];
+        int rank = 0;
+#pragma unroll 8
+        for (int o = 0; o < n; ++o) rank += src[o] < w;
+        dst[rank] = w;
+    }
+}
+
+// The cut among n ordered words of one bin, by count (words of the bin kept)
+// or by mass; before: the mass of the bins before.  Wave 0 looks, all get it.
+template <class F, bool MASS>
+__device__ __forceinline__ Cut cut_in_order(const SampleArgs& a, const Row& r, DrawLds& lds,
+                                            const uint64_t* word, int n, int64_t before,
+                                            int64_t keep, double target)
+{
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        const int lane = threadIdx.x;
+        int64_t run = before;
+        for (int e0 = 0; e0 < n; e0 += 64) {
+            const uint64_t w = e0 + lane < n ? word[e0 + lane] : ~0ull;
+            int64_t c = weight<F>(a, r, key_of(w));
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int64_t v = __shfl_up(c, o);
+                if (lane >= o) c += v;
+            }
+            // the last word is kept in any case that gets that far
+            const bool here = MASS ? (double)(run + c) >= target : e0 + lane + 1 >= keep;
+            const uint64_t hit = __ballot(e0 + lane < n && (here || e0 + lane == n - 1));
+            if (hit) {
+                if (lane == __builtin_ctzll(hit)) {
+                    lds.sel[0] = key_of(w);
+                    lds.sel[1] = (uint32_t)w;
+                    lds.sel64[0] = run + c;
+                }
+                break;
+            }
+            run += __shfl(c, 63);
+        }
+    }
+    __syncthreads();
+    const Cut c{lds.sel[0], lds.sel[1], lds.sel64[0]};
+    __syncthreads();
+    return c;
+}
+
 // The words that a draw looks at: the listed ones in LDS or the whole row.
 template <class F>
 struct Words {
@@ -248,140 +506,165 @@ struct Words {
     const typename F::T* x;
     int32_t n;
     bool listed;
-    __device__ uint32_t key(int32_t i) const { return listed ? lds->key[i] : F::key(x[i]); }
-    __device__ uint32_t index(int32_t i) const { return listed ? lds->idx[i] : (uint32_t)i; }
+    __device__ uint32_t key(int32_t i) const
+    {
+        return listed ? key_of(lds->word[i]) : F::key(F::load(x[i]));
+    }
+    __device__ uint32_t index(int32_t i) const { return listed ? (uint32_t)lds->word[i] : (uint32_t)i; }
 };
 
-// The cut of the order where the count (MASS false) or the mass of the words
-// before reaches a target: keys above `key` are kept and the first `ties` at
-// it.  lo: least key that belongs to the set, lo_ties of it (the rest are
-// not in the set).
-struct Cut {
-    uint32_t key;
-    int64_t ties;
-    int64_t count, mass;  // of the words above key
-};
-
+// The cut over the listed words in LDS by their bins (count and mass there
+// already); false if its bin holds more words than there is room for.
 template <class F, bool MASS>
-__device__ Cut find_cut(const SampleArgs& a, const Row& r, const Words<F>& ws, DrawLds& lds,
-                        uint32_t lo, int64_t lo_ties, int64_t count, double mass)
+__device__ __forceinline__ bool cut_listed(const SampleArgs& a, const Row& r, DrawLds& lds, int n,
+                                  int64_t keep, double target, Cut& cut)
 {
-    const int tid = threadIdx.x;
-    uint32_t hi = r.kmax;
-    const uint32_t set_lo = lo;
-    Cut c;
-    c.count = 0;
-    c.mass = 0;
+    if (threadIdx.x < 64) {
+        const Found f = find_bin(lds.count, lds.mass, [=](int64_t c, int64_t w) {
+            return MASS ? (double)w >= target : c >= keep;
+        });
+        if (threadIdx.x == 0) {
+            lds.sel[0] = (uint32_t)f.bin;
+            lds.sel[1] = 0;
+            lds.sel64[0] = f.count;
+            lds.sel64[1] = f.mass;
+        }
+    }
+    __syncthreads();
+    const int32_t bin = (int32_t)lds.sel[0];
+    const int64_t count = lds.sel64[0], mass = lds.sel64[1];
+    const int near = (int)lds.count[bin];
+    if (near > kNear) return false;
+    for (int i = threadIdx.x; i < n; i += kDrawThreads)
+        if (bin_of<F>(a, r, key_of(lds.word[i])) == bin)
+            lds.near[atomicAdd(&lds.sel[1], 1u)] = lds.word[i];
+    __syncthreads();
+    order_words(lds.near, near, lds.near + kNear);
+    cut = cut_in_order<F, MASS>(a, r, lds, lds.near + kNear, near, mass, keep - count, target);
+    return true;
+}
+
+// The cut over the whole row, bit by bit of the keys from the top: the words
+// that have the leading bits found so far are counted by the next ten.
+template <class F, bool MASS>
+__device__ __forceinline__ Cut cut_row(const SampleArgs& a, const Row& r, const Words<F>& ws, DrawLds& lds,
+                       int64_t count, double target)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    uint32_t lo = 1, hi = r.kmax;
+    int64_t n0 = 0, m0 = 0;  // words and mass above hi
+    int64_t ties = 0;
     for (;;) {
         const uint32_t range = hi - lo;
         const int bits = range ? 32 - __builtin_clz(range) : 0;
-        const int shift = bits > kBinBits ? bits - kBinBits : 0;
+        const int shift = bits > 10 ? bits - 10 : 0;
         __syncthreads();
         for (int i = tid; i < kBins; i += kDrawThreads) {
             lds.count[i] = 0;
             lds.mass[i] = 0;
         }
-        if (tid == 0) lds.sel[0] = 0;
         __syncthreads();
-        for (int i = tid; i < ws.n; i += kDrawThreads) {
-            const uint32_t k = ws.key(i);
-            if (k < lo || k > hi) continue;
-            const uint32_t bin = (k - lo) >> shift;
-            atomicAdd(&lds.count[bin], 1u);
-            atomicAdd(&lds.mass[bin], (unsigned long long)weight<F>(a, r, k));
-        }
-        __syncthreads();
-        // from the top: thread t holds bins kBins - 1 - 2 t and the one below
-        const int b0 = kBins - 1 - 2 * tid, b1 = b0 - 1;
-        const int64_t n0 = lds.count[b0], n1 = lds.count[b1];
-        const int64_t m0 = (int64_t)lds.mass[b0], m1 = (int64_t)lds.mass[b1];
-        int64_t all;
-        const int64_t nb = c.count + block_scan(n0 + n1, &all, lds.wave64);
-        const int64_t mb = c.mass + block_scan(m0 + m1, &all, lds.wave64);
-        // the first bin from the top that reaches the target, else the last
-        // one with words
-        auto reaches = [&](int64_t n, int64_t m) {
-            return MASS ? (double)m >= mass : n >= count;
-        };
-        if (n0 && (reaches(nb + n0, mb + m0))) atomicMax(&lds.sel[0], (uint32_t)b0 + 4096);
-        if (n1 && (reaches(nb + n0 + n1, mb + m0 + m1))) atomicMax(&lds.sel[0], (uint32_t)b1 + 4096);
-        __syncthreads();
-        if (lds.sel[0] == 0) {  // none: the lowest bin with words
-            __syncthreads();
-            if (tid == 0) lds.sel[1] = kBins;
-            __syncthreads();
-            if (n1) atomicMin(&lds.sel[1], (uint32_t)b1);
-            else if (n0) atomicMin(&lds.sel[1], (uint32_t)b0);
-            __syncthreads();
-            if (tid == 0) lds.sel[0] = lds.sel[1] + 4096;
-            __syncthreads();
-        }
-        const uint32_t bin = lds.sel[0] - 4096;
-        if ((uint32_t)b0 == bin || (uint32_t)b1 == bin) {
-            lds.sel64[0] = (uint32_t)b0 == bin ? nb : nb + n0;
-            lds.sel64[1] = (uint32_t)b0 == bin ? mb : mb + m0;
-        }
-        __syncthreads();
-        c.count = lds.sel64[0];
-        c.mass = lds.sel64[1];
-        lo = lo + (bin << shift);
-        hi = min(hi, lo + ((1u << shift) - 1));
-        if (shift == 0) {
-            c.key = lo;
-            int64_t ties = lds.count[bin];
-            if (lo == set_lo) ties = min(ties, lo_ties);
-            int64_t keep = ties;
-            if (MASS) {
-                const int64_t w = weight<F>(a, r, lo);
-                // the fewest ties that reach the mass
-                int64_t l = 1, h = ties;
-                while (l < h) {
-                    const int64_t mid = (l + h) >> 1;
-                    if ((double)(c.mass + mid * w) >= mass) h = mid;
-                    else l = mid + 1;
-                }
-                keep = l;
-            } else {
-                keep = min(ties, count - c.count);
+        for (int i0 = tid; i0 < ws.n; i0 += 8 * kDrawThreads) {
+            uint32_t k[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int i = i0 + u * kDrawThreads;
+                k[u] = i < ws.n ? ws.key(i) : 0;
             }
-            c.ties = keep;
-            return c;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                if (k[u] < lo || k[u] > hi) continue;
+                const uint32_t bin = (hi - k[u]) >> shift;
+                atomicAdd(&lds.count[bin], 1u);
+                atomicAdd(&lds.mass[bin], (unsigned long long)weight<F>(a, r, k[u]));
+            }
+        }
+        __syncthreads();
+        if (tid < 64) {
+            const Found f = find_bin(lds.count, lds.mass, [=](int64_t c, int64_t w) {
+                return MASS ? (double)(m0 + w) >= target : n0 + c >= count;
+            });
+            if (tid == 0) {
+                lds.sel[0] = (uint32_t)f.bin;
+                lds.sel64[0] = n0 + f.count;
+                lds.sel64[1] = m0 + f.mass;
+            }
+        }
+        __syncthreads();
+        const uint32_t bin = lds.sel[0];
+        n0 = lds.sel64[0];
+        m0 = lds.sel64[1];
+        hi = hi - (bin << shift);
+        lo = max(lo, hi - ((1u << shift) - 1));
+        if (shift == 0) {
+            ties = lds.count[bin];
+            break;
         }
     }
+    // the words at key lo: how many are kept, and which is the last
+    const int64_t w = weight<F>(a, r, lo);
+    int64_t keep;
+    if (MASS) {
+        int64_t l = 1, h = ties;
+        while (l < h) {
+            const int64_t mid = (l + h) >> 1;
+            if ((double)(m0 + mid * w) >= target) h = mid;
+            else l = mid + 1;
+        }
+        keep = l;
+    } else {
+        keep = min(ties, count - n0);
+    }
+    const int32_t part = ((ws.n + kDrawWaves - 1) / kDrawWaves + 63) & ~63;
+    const int32_t i0 = min(wave * part, ws.n), i1 = min(i0 + part, ws.n);
+    int32_t t = 0;
+    for (int32_t i = i0; i < i1; i += 64)
+        t += __popcll(__ballot(i + lane < i1 && ws.key(i + lane) == lo));
+    __syncthreads();
+    if (lane == 0) lds.wave32[wave] = t;
+    __syncthreads();
+    int64_t seen = 0;
+    for (int v = 0; v < wave; ++v) seen += lds.wave32[v];
+    if (keep > seen && keep <= seen + t)
+        for (int32_t i = i0; i < i1; i += 64) {
+            const uint64_t tie = __ballot(i + lane < i1 && ws.key(i + lane) == lo);
+            const int32_t c = __popcll(tie);
+            if (keep <= seen + c) {
+                const bool last = ((tie >> lane) & 1) &&
+                                  seen + __popcll(tie & (((uint64_t)2 << lane) - 1)) == keep;
+                if (last) lds.sel[1] = ws.index(i + lane);
+                break;
+            }
+            seen += c;
+        }
+    __syncthreads();
+    const Cut c{lo, lds.sel[1], m0 + keep * w};
+    __syncthreads();
+    return c;
 }
 
 // The word at which the running weight of the kept ones, in index order,
 // passes u times their total; every wave walks a contiguous part.
 template <class F>
-__device__ int32_t draw_word(const SampleArgs& a, const Row& r, const Words<F>& ws, DrawLds& lds,
-                             uint32_t cut, int64_t ties, double u)
+__device__ __forceinline__ int32_t draw_word(const SampleArgs& a, const Row& r, const Words<F>& ws, DrawLds& lds,
+                             const Cut& cut, double u)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
     const int32_t part = ((ws.n + kDrawWaves - 1) / kDrawWaves + 63) & ~63;
     const int32_t i0 = min(wave * part, ws.n), i1 = min(i0 + part, ws.n);
-    int32_t t = 0;
-    for (int32_t i = i0; i < i1; i += 64)
-        t += __popcll(__ballot(i + lane < i1 && ws.key(i + lane) == cut));
-    __syncthreads();
-    if (lane == 0) lds.wave32[wave] = t;
-    __syncthreads();
-    int64_t first = 0;  // ties before this wave's part
-    for (int w = 0; w < wave; ++w) first += lds.wave32[w];
-
-    auto kept = [&](int32_t i, int64_t& seen) -> int64_t {
-        const uint32_t k = i < i1 ? ws.key(i) : 0;
-        const uint64_t tie = __ballot(k == cut && i < i1);
-        const int64_t rank = seen + __popcll(tie & below);
-        seen += __popcll(tie);
-        if (!(k > cut || (k == cut && rank < ties)) || i >= i1) return 0;
+    auto kept = [&](int32_t i) -> int64_t {
+        if (i >= i1) return 0;
+        const uint32_t k = ws.key(i);
+        if (!cut.keeps(k, ws.index(i))) return 0;
         const int64_t w = weight<F>(a, r, k);
         return (double)w >= r.floor ? w : 0;
     };
-    int64_t s = 0, seen = first;
-    for (int32_t i = i0; i < i1; i += 64) s += kept(i + lane, seen);
+    int64_t s = 0;
+#pragma unroll 4
+    for (int32_t i = i0; i < i1; i += 64) s += kept(i + lane);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    __syncthreads();
     if (lane == 0) lds.wave64[wave] = s;
     __syncthreads();
     int64_t total = 0, before = 0;
@@ -393,11 +676,9 @@ __device__ int32_t draw_word(const SampleArgs& a, const Row& r, const Words<F>& 
     if (threadIdx.x == 0) lds.sel[0] = 0;
     __syncthreads();
     if (target >= before && target < before + s) {
-        seen = first;
         int64_t run = before;
         for (int32_t i = i0; i < i1; i += 64) {
-            const int64_t w = kept(i + lane, seen);
-            int64_t c = w;
+            int64_t c = kept(i + lane);
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) {
                 const int64_t v = __shfl_up(c, o);
@@ -415,77 +696,46 @@ __device__ int32_t draw_word(const SampleArgs& a, const Row& r, const Words<F>& 
     return (int32_t)lds.sel[0];
 }
 
-template <class F>
-__global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a, int64_t row0)
+// The word from the kept weights of every segment: sum(i) of segment i, the
+// cut's own rule within the segment.
+template <class F, class Sum>
+__device__ __forceinline__ int32_t draw_by_segments(const SampleArgs& a, const Row& r, const typename F::T* x,
+                                    DrawLds& lds, const Cut& cut, double u, Sum sum)
 {
-    __shared__ DrawLds lds;
     const int tid = threadIdx.x, lane = tid & 63;
-    const int64_t m = blockIdx.x, row = row0 + m;
-    const uint4* info = a.info + m * a.segs;
-    const uint32_t kmax = row_max(a, m);
-    if (kmax == 0) {  // nothing can be drawn
-        if (tid == 0) a.tokens[row] = -1;
-        return;
-    }
-    const Row r = row_of<F>(a, row, kmax);
-    const double u0 = (double)a.u[row], u = u0 > 0.0 ? fmin(u0, 1.0) : 0.0;
-
-    // what all lists together hold without a gap: keys from the largest bound
-    uint32_t bound = 1;
-    for (int i = lane; i < a.segs; i += 64) bound = max(bound, info[i].y);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) bound = max(bound, (uint32_t)__shfl_xor((int)bound, o));
-
-    const typename F::T* x = static_cast<const typename F::T*>(a.x) + row * a.ld;
-    Words<F> ws{&lds, x, a.V, false};
-
-    // listed words into LDS, in index order; a thread per segment and turn
-    int64_t n = 0;
+    int64_t s = 0, all = 0, base = 0, total = 0;
+    for (int i = tid; i < a.segs; i += kDrawThreads) s += sum(i);
+    block_scan(s, &total, lds.wave64);
+    const int64_t target = min((int64_t)(u * (double)total), total - 1);
+    if (tid == 0) lds.sel[0] = 0;
+    __syncthreads();
     for (int s0 = 0; s0 < a.segs; s0 += kDrawThreads) {
-        const int s = s0 + tid;
-        const uint2* list = a.list + (m * a.segs + s) * kList;
-        const int cnt = s < a.segs ? (int)info[s].z : 0;
-        int mine = 0;
-        for (int i = 0; i < cnt; ++i) mine += list[i].x >= bound;
-        int64_t all;
-        int64_t at = n + block_scan(mine, &all, lds.wave64);
-        for (int i = 0; i < cnt; ++i)
-            if (list[i].x >= bound) {
-                if (at < kEntries) {
-                    lds.key[at] = list[i].x;
-                    lds.idx[at] = list[i].y;
-                }
-                ++at;
-            }
-        n += all;
+        const int i = s0 + tid;
+        const int64_t v = i < a.segs ? sum(i) : 0;
+        const int64_t before = base + block_scan(v, &all, lds.wave64);
+        if (target >= before && target < before + v) {
+            lds.sel[0] = (uint32_t)i;
+            lds.sel64[0] = before;
+        }
+        base += all;
     }
     __syncthreads();
-    const bool have_list = n > 0 && n <= kEntries;
-
-    if (needs_sums(r) && !(r.p < 1.0)) {
-        // no cut: the segment, then the word in it
-        int64_t s = 0, all = 0, base = 0, total = 0;
-        for (int i = tid; i < a.segs; i += kDrawThreads) s += a.sums[m * a.segs + i];
-        block_scan(s, &total, lds.wave64);
-        const int64_t target = min((int64_t)(u * (double)total), total - 1);
-        if (tid == 0) lds.sel[0] = 0;
-        __syncthreads();
-        for (int s0 = 0; s0 < a.segs; s0 += kDrawThreads) {
-            const int i = s0 + tid;
-            const int64_t v = i < a.segs ? a.sums[m * a.segs + i] : 0;
-            const int64_t before = base + block_scan(v, &all, lds.wave64);
-            if (target >= before && target < before + v) {
-                lds.sel[0] = (uint32_t)i;
-                lds.sel64[0] = before;
-            }
-            base += all;
+    const int32_t i0 = (int32_t)lds.sel[0] * kSeg;
+    int64_t run = lds.sel64[0];
+    __syncthreads();
+    if (tid < 64) {
+        uint32_t k[kSeg / 64];
+#pragma unroll
+        for (int j = 0; j < kSeg / 64; ++j) {
+            const int32_t i = i0 + 64 * j + lane;
+            k[j] = i < a.V ? F::key(F::load(x[i])) : 0;
         }
-        __syncthreads();
-        if (tid >= 64) return;
-        const int32_t i0 = (int32_t)lds.sel[0] * kSeg, i1 = min(i0 + kSeg, a.V);
-        int64_t run = lds.sel64[0];
-        for (int32_t i = i0; i < i1; i += 64) {
-            int64_t c = i + lane < i1 ? weight<F>(a, r, F::key(x[i + lane])) : 0;
+        bool done = false;
+#pragma unroll
+        for (int j = 0; j < kSeg / 64; ++j) {
+            if (done) continue;
+            const int32_t i = i0 + 64 * j + lane;
+            int64_t c = cut.keeps(k[j], (uint32_t)i) ? weight<F>(a, r, k[j]) : 0;
             if (!((double)c >= r.floor)) c = 0;
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) {
@@ -494,51 +744,157 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a,
             }
             const uint64_t hit = __ballot(run + c > target);
             if (hit) {
-                if (lane == __builtin_ctzll(hit)) a.tokens[row] = i + lane;
-                return;
+                if (lane == __builtin_ctzll(hit)) lds.sel[0] = (uint32_t)i;
+                done = true;
             }
             run += __shfl(c, 63);
         }
+    }
+    __syncthreads();
+    return (int32_t)lds.sel[0];
+}
+
+// The listed words from the bound on into LDS, in index order; how many there
+// are (more than kEntries: not all of them are there).
+__device__ __forceinline__ int64_t load_list(const SampleArgs& a, int64_t m, uint32_t bound, DrawLds& lds)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint4* info = a.info + m * a.segs;
+    const uint2* list = a.list + m * a.segs * kList;
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    constexpr int kTurn = 16;  // segments of a wave per turn, all loads under way
+    int64_t n = 0;
+    for (int s0 = 0; s0 < a.segs; s0 += kTurn * kDrawWaves) {
+        const int first = s0 + wave * kTurn;
+        uint2 e[kTurn];
+#pragma unroll
+        for (int i = 0; i < kTurn; ++i) {
+            const int s = first + i;
+            e[i] = make_uint2(0, 0);
+            if (s < a.segs && lane < (int)info[s].z) e[i] = list[(int64_t)s * kList + lane];
+        }
+        int mine = 0;
+#pragma unroll
+        for (int i = 0; i < kTurn; ++i) mine += __popcll(__ballot(e[i].x >= bound));
+        __syncthreads();
+        if (lane == 0) lds.wave32[wave] = mine;
+        __syncthreads();
+        int64_t at = n;
+        for (int w = 0; w < kDrawWaves; ++w) {
+            if (w < wave) at += lds.wave32[w];
+            n += lds.wave32[w];
+        }
+#pragma unroll
+        for (int i = 0; i < kTurn; ++i) {
+            const uint64_t hit = __ballot(e[i].x >= bound);
+            const int64_t to = at + __popcll(hit & below);
+            if (e[i].x >= bound && to < kEntries) lds.word[to] = order(e[i].x, e[i].y);
+            at += __popcll(hit);
+        }
+    }
+    __syncthreads();
+    return n;
+}
+
+template <class F>
+__global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a, int64_t row0)
+{
+    __shared__ DrawLds lds;
+    const int tid = threadIdx.x;
+    const int64_t m = blockIdx.x, row = row0 + m;
+    const uint2 info = row_info(a, m);
+    const uint32_t bound = info.y;
+    if (info.x == 0) {  // nothing can be drawn
+        if (tid == 0) a.tokens[row] = -1;
+        return;
+    }
+    const Row r = row_of<F>(a, row, info.x);
+    const double u0 = (double)a.u[row], u = u0 > 0.0 ? fmin(u0, 1.0) : 0.0;
+    const typename F::T* x = static_cast<const typename F::T*>(a.x) + row * a.ld;
+    const int64_t* sums = a.sums + m * a.segs;
+
+    if (needs_sums(r) && !needs_bins(r)) {  // no cut
+        const Cut all{1, 0xffffffffu, 0};
+        const int32_t tok = draw_by_segments<F>(a, r, x, lds, all, u, [&](int i) { return sums[i]; });
+        if (tid == 0) a.tokens[row] = tok;
         return;
     }
 
-    uint32_t cut = 1;
-    int64_t ties = INT64_MAX, total;
-    if (r.k > 0) {
-        ws.listed = have_list && n >= r.k;
-        ws.n = ws.listed ? (int32_t)n : a.V;
-        const Cut c = find_cut<F, false>(a, r, ws, lds, ws.listed ? bound : 1, INT64_MAX, r.k, 0.0);
-        cut = c.key;
-        ties = c.ties;
-        total = c.mass + c.ties * weight<F>(a, r, c.key);
-    } else {
-        int64_t s = 0;
-        for (int i = tid; i < a.segs; i += kDrawThreads) s += a.sums[m * a.segs + i];
-        block_scan(s, &total, lds.wave64);
-    }
-    if (r.p < 1.0) {
-        const double mass = r.p * (double)total;
-        if (r.k == 0 && have_list) {
-            // listed words hold the mass?
-            int64_t s = 0, all;
-            for (int i = tid; i < n; i += kDrawThreads) s += weight<F>(a, r, lds.key[i]);
-            block_scan(s, &all, lds.wave64);
-            ws.listed = (double)all >= mass;
-            ws.n = ws.listed ? (int32_t)n : a.V;
+    Cut cut{1, 0xffffffffu, 0};
+    double target = 0.0;
+    if (needs_bins(r)) {
+        const Found f = find_mass_bin<F>(a, r, m);
+        target = r.p * (double)f.total;
+        const RowWork& work = a.work[m];
+        const int n = (int)min(work.found, (uint32_t)0x7fffffff);
+        if (f.bin >= bin_of<F>(a, r, bound) && n <= kGather && a.segs <= kBins) {
+            for (int i = tid; i < n; i += kDrawThreads)
+                lds.word[i] = order(work.near[i].x, work.near[i].y);
+            for (int i = tid; i < a.segs; i += kDrawThreads)
+                lds.mass[i] = (unsigned long long)sums[i];
+            __syncthreads();
+            order_words(lds.word, n, lds.word + kGather);
+            cut = cut_in_order<F, true>(a, r, lds, lds.word + kGather, n, f.mass, 0, target);
+            // the kept words of the bin join their segments' sums
+            for (int i = tid; i < n; i += kDrawThreads) {
+                const uint32_t k = key_of(lds.word[i]), at = (uint32_t)lds.word[i];
+                if (!cut.keeps(k, at)) continue;
+                const int64_t w = weight<F>(a, r, k);
+                if ((double)w >= r.floor) atomicAdd(&lds.mass[at / kSeg], (unsigned long long)w);
+            }
+            __syncthreads();
+            const int32_t tok = draw_by_segments<F>(a, r, x, lds, cut, u,
+                                                    [&](int i) { return (int64_t)lds.mass[i]; });
+            if (tid == 0) a.tokens[row] = tok;
+            return;
         }
-        const uint32_t lo = r.k > 0 ? cut : ws.listed ? bound : 1;
-        const Cut c = find_cut<F, true>(a, r, ws, lds, lo, ties, 0, mass);
-        cut = c.key;
-        ties = c.ties;
     }
-    const int32_t tok = draw_word<F>(a, r, ws, lds, cut, ties, u);
+
+    const int64_t n = load_list(a, m, bound, lds);
+    bool listed = n > 0 && n <= kEntries && n >= r.k;
+    if (listed) {
+        for (int i = tid; i < kBins; i += kDrawThreads) {
+            lds.count[i] = 0;
+            lds.mass[i] = 0;
+        }
+        __syncthreads();
+        int64_t s = 0, all;
+        for (int i = tid; i < n; i += kDrawThreads) {
+            const uint32_t k = key_of(lds.word[i]);
+            const int32_t bin = bin_of<F>(a, r, k);
+            const int64_t w = weight<F>(a, r, k);
+            s += w;
+            atomicAdd(&lds.count[bin], 1u);
+            atomicAdd(&lds.mass[bin], (unsigned long long)w);
+        }
+        block_scan(s, &all, lds.wave64);
+        if (r.k > 0) {
+            listed = cut_listed<F, false>(a, r, lds, (int)n, r.k, 0.0, cut);
+            if (listed && r.p < 1.0)
+                listed = cut_listed<F, true>(a, r, lds, (int)n, 0, r.p * (double)cut.mass, cut);
+        } else {
+            listed = (double)all >= target && cut_listed<F, true>(a, r, lds, (int)n, 0, target, cut);
+        }
+    }
+    const Words<F> ws{&lds, x, listed ? (int32_t)n : a.V, listed};
+    if (!listed) {
+        if (r.k > 0) {
+            cut = cut_row<F, false>(a, r, ws, lds, r.k, 0.0);
+            target = r.p * (double)cut.mass;
+        }
+        if (r.p < 1.0) cut = cut_row<F, true>(a, r, ws, lds, 0, target);
+    }
+    const int32_t tok = draw_word<F>(a, r, ws, lds, cut, u);
     if (tid == 0) a.tokens[row] = tok;
 }
 
 int32_t segments(int64_t V) { return (int32_t)((V + kSeg - 1) / kSeg); }
 
-// Bytes per row of the three workspace parts.
-int64_t row_bytes(int64_t V) { return (int64_t)segments(V) * (16 + 8 * kList + 8); }
+// Bytes per row of the workspace: its segments', and its own.
+int64_t row_bytes(int64_t V)
+{
+    return (int64_t)segments(V) * (16 + 8 * kList + 8) + 8 + (int64_t)sizeof(RowWork);
+}
 
 template <class F>
 hipError_t launch(SampleArgs a, int64_t M, char* ws, int64_t ws_bytes, hipStream_t s)
@@ -546,12 +902,14 @@ hipError_t launch(SampleArgs a, int64_t M, char* ws, int64_t ws_bytes, hipStream
     const int64_t rows = std::min<int64_t>(ws_bytes / row_bytes(a.V), 65535);
     for (int64_t m0 = 0; m0 < M; m0 += rows) {
         const int64_t n = std::min(rows, M - m0);
-        a.info = reinterpret_cast<uint4*>(ws);
-        a.list = reinterpret_cast<uint2*>(ws + n * a.segs * 16);
-        a.sums = reinterpret_cast<int64_t*>(ws + n * a.segs * (16 + 8 * kList));
+        a.work = reinterpret_cast<RowWork*>(ws);
+        a.info = reinterpret_cast<uint4*>(ws + n * sizeof(RowWork));
+        a.list = reinterpret_cast<uint2*>(ws + n * (sizeof(RowWork) + a.segs * 16));
+        a.sums = reinterpret_cast<int64_t*>(ws + n * (sizeof(RowWork) + a.segs * (16 + 8 * kList)));
         const dim3 g((unsigned)((a.segs + 3) / 4), (unsigned)n);
         sample_scan_kernel<F><<<g, 256, 0, s>>>(a, m0);
         sample_sums_kernel<F><<<g, 256, 0, s>>>(a, m0);
+        if (a.top_p) sample_gather_kernel<F><<<g, 256, 0, s>>>(a, m0);
         sample_draw_kernel<F><<<(unsigned)n, kDrawThreads, 0, s>>>(a, m0);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
