@@ -25,7 +25,8 @@
 namespace mq {
 namespace {
 
-constexpr int kSeg = 2048;       // words per wave of the first three kernels
+constexpr int kSeg = 2048;       // words of a list and of a sum
+constexpr int kUnit = 512;       // words that a wave of the second and third kernel takes at once
 constexpr int kList = 64;        // places in a wave's list
 constexpr int kRank = 24;        // lane maxima at or above a list's bound
 constexpr int kBins = 1024;
@@ -39,6 +40,7 @@ constexpr double kOne = 1099511627776.0;  // 2^40
 // A row's part of the workspace beyond its segments'.
 struct RowWork {
     unsigned long long mass[kBins];
+    uint32_t count[kBins];
     uint2 near[kGather];  // key, index of the words in the cut's bin
     uint32_t found;       // how many there are (also past the places)
     uint32_t pad[3];
@@ -101,24 +103,27 @@ struct Code16 {
 
 // A row's settings.
 struct Row {
-    double max;      // its largest logit
     double scale;    // log2(e) / temperature
     double p, floor; // top_p (>= 1: off), least weight of the min_p rule
     int32_t k;       // 0: off
+    double max;      // its largest logit
     uint32_t kmax;
+    template <class F>
+    __device__ void set_max(const SampleArgs& a, uint32_t key)
+    {
+        kmax = key;
+        max = F::value(a, key);
+    }
 };
 
-template <class F>
-__device__ inline Row row_of(const SampleArgs& a, int64_t m, uint32_t kmax)
+__device__ inline Row row_of(const SampleArgs& a, int64_t m)
 {
     Row r;
-    r.kmax = kmax;
-    r.max = F::value(a, kmax);
     const double t = a.temperature ? (double)a.temperature[m] : 1.0;
     const int32_t k = a.top_k ? a.top_k[m] : 0;
     r.k = k > 0 && k < a.V ? k : 0;
     r.p = a.top_p ? (double)a.top_p[m] : 1.0;
-    if (!(r.p < 1.0)) r.p = 1.0;
+    r.p = r.p < 1.0 ? fmax(r.p, 0.0) : 1.0;  // NaN: off
     const double mp = a.min_p ? (double)a.min_p[m] : 0.0;
     r.floor = mp > 0.0 ? fmin(mp, 1.0) * kOne : 0.0;
     r.scale = 1.4426950408889634 / t;
@@ -129,29 +134,67 @@ __device__ inline Row row_of(const SampleArgs& a, int64_t m, uint32_t kmax)
     return r;
 }
 
+// The distance of a key's logit from the largest, in factors of two of its
+// weight, at most 100.  The same for equal logits, never less for smaller ones.
 template <class F>
-__device__ inline int64_t weight(const SampleArgs& a, const Row& r, uint32_t k)
+__device__ inline double distance(const SampleArgs& a, const Row& r, uint32_t k)
 {
-    if (k == r.kmax) return (int64_t)1 << 40;
-    if (k == 0 || r.max == (double)__builtin_inff()) return 0;
-    const double z = fmax((F::value(a, k) - r.max) * r.scale, -100.0);
-    const double w = exp2_poly(z + 40.0) + kRintShift;
-    return __double_as_longlong(w) - __double_as_longlong(kRintShift);
+    if (k == r.kmax) return 0.0;
+    return fmin((r.max - F::value(a, k)) * r.scale, 100.0);  // NaN (infinities): 100
 }
 
-// The bin of a key's distance from the largest (0: the largest's; the same
-// for equal logits, never less for smaller ones).
+// rint(2^40 2^-z): z to the next 1/64, 2^(j/64) from a table in LDS (2^40 of
+// it in entry j), a polynomial of degree 4 on the rest (within 2.5e-15); the
+// last product is added to 1.5 * 2^52, whose low bits are then the rounded
+// weight.
+__device__ inline void init_table(double* table)  // by the block, which waits afterwards
+{
+    if (threadIdx.x < 64) table[threadIdx.x] = kOne * exp2_poly((double)threadIdx.x / 64.0);
+}
+__device__ inline int64_t weight_at(const double* table, double z)
+{
+    constexpr double kShift = 105553116266496.0;  // 1.5 * 2^46
+    const double t = kShift - z;
+    const double f = (kShift - t) - z;
+    const int32_t k = rint_low(t);
+    int64_t e = __double_as_longlong(table[k & 63]);
+    e += (int64_t)(k & ~63) << 46;  // the exponent field, k / 64 lower
+    double q = 0x1.3b2ad0385b409p-7;
+    q = __builtin_fma(q, f, 0x1.c6b0c40d8c4e9p-5);
+    q = __builtin_fma(q, f, 0x1.ebfbdff82ac52p-3);
+    q = __builtin_fma(q, f, 0x1.62e42fefa0352p-1);
+    q = __builtin_fma(q, f, 1.0);
+    const double w = __builtin_fma(q, __longlong_as_double(e), kRintShift);
+    return __double_as_longlong(w) - __double_as_longlong(kRintShift);
+}
+template <class F>
+__device__ inline int64_t weight(const SampleArgs& a, const Row& r, const double* table, uint32_t k)
+{
+    return k ? weight_at(table, distance<F>(a, r, k)) : 0;
+}
+
+// The bin of a distance.
+__device__ inline int32_t bin_at(double z)
+{
+    return z * kBinScale < (double)(kBins - 1) ? max((int32_t)(z * kBinScale), 0) : kBins - 1;
+}
 template <class F>
 __device__ inline int32_t bin_of(const SampleArgs& a, const Row& r, uint32_t k)
 {
-    if (k == r.kmax) return 0;
-    const double z = (r.max - F::value(a, k)) * r.scale;  // NaN with infinities: the last
-    return z * kBinScale < (double)(kBins - 1) ? (int32_t)(z * kBinScale) : kBins - 1;
+    return bin_at(distance<F>(a, r, k));
 }
 
-// Rows without top_k need the weights of all words: with top_p per bin.
-__device__ inline bool needs_sums(const Row& r) { return r.k == 0; }
-__device__ inline bool needs_bins(const Row& r) { return r.k == 0 && r.p < 1.0; }
+// Rows without top_k need the weights of all words, with top_p per bin; so do
+// rows whose top_k is more than the lists are likely to hold (a list has at
+// least 24 words, some of them below the largest bound).
+__device__ inline bool needs_bins(const SampleArgs& a, const Row& r)
+{
+    return r.k == 0 ? r.p < 1.0 : r.k > 12 * a.segs + 12;
+}
+__device__ inline bool needs_sums(const SampleArgs& a, const Row& r)
+{
+    return r.k == 0 || needs_bins(a, r);
+}
 
 template <class F>
 __global__ __launch_bounds__(256) void sample_scan_kernel(SampleArgs a, int64_t row0)
@@ -161,11 +204,6 @@ __global__ __launch_bounds__(256) void sample_scan_kernel(SampleArgs a, int64_t 
     if (seg >= a.segs) return;
     const int64_t m = blockIdx.y;
     const typename F::T* x = static_cast<const typename F::T*>(a.x) + (row0 + m) * a.ld;
-    // the row's bins and counter start at zero
-    RowWork& work = a.work[m];
-    for (int i = seg * 64 + lane; i < kBins; i += a.segs * 64) work.mass[i] = 0;
-    if (seg == 0 && lane == 0) work.found = 0;
-
     const int32_t i0 = seg * kSeg + lane;
     typename F::V k[kSeg / 64];
 #pragma unroll
@@ -218,7 +256,18 @@ __global__ __launch_bounds__(256) void sample_scan_kernel(SampleArgs a, int64_t 
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-    if (lane == 0) a.info[at] = make_uint4(top, bound, (uint32_t)pos, 0);
+    if (lane == 0) {
+        a.info[at] = make_uint4(top, bound, (uint32_t)pos, 0);
+        a.sums[at] = 0;
+    }
+    // the row's bins and counter start at zero too (stores before the loads
+    // would be waited for with them)
+    RowWork& work = a.work[m];
+    for (int i = seg * 64 + lane; i < kBins; i += a.segs * 64) {
+        work.mass[i] = 0;
+        work.count[i] = 0;
+    }
+    if (seg == 0 && lane == 0) work.found = 0;
 }
 
 // The row's largest key and the largest bound of its lists (every lane of the
@@ -239,51 +288,99 @@ __device__ inline uint2 row_info(const SampleArgs& a, int64_t m)
     return make_uint2(top, bound);
 }
 
+// The sum of the values of the threads before this one, and of all.
+template <int WAVES>
+__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* total, int64_t* lds)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t s = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t t = __shfl_up(s, o);
+        if (lane >= o) s += t;
+    }
+    __syncthreads();
+    if (lane == 63) lds[wave] = s;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) before += lds[w];
+        all += lds[w];
+    }
+    *total = all;
+    return before + s - v;
+}
+
+// The keys of the unit's words, eight per lane (0 past the row).
 template <class F>
-__global__ __launch_bounds__(256) void sample_sums_kernel(SampleArgs a, int64_t row0)
+__device__ __forceinline__ void load_unit(const SampleArgs& a, const typename F::T* x, int32_t i0,
+                                          uint32_t (&k)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) k[j] = i0 + 64 * j < a.V ? F::key(F::load(x[i0 + 64 * j])) : 0;
+}
+
+// A wave takes `units` units of 512 words in a row.
+template <class F>
+__global__ __launch_bounds__(256) void sample_sums_kernel(SampleArgs a, int64_t row0, int units)
 {
     __shared__ unsigned long long mass[kBins];
+    __shared__ uint32_t count[kBins];
+    __shared__ double table[64];
     const int lane = threadIdx.x & 63;
-    const int seg = blockIdx.x * 4 + (threadIdx.x >> 6);
     const int64_t m = blockIdx.y;
+    Row r = row_of(a, row0 + m);
+    if (!needs_sums(a, r)) return;
     const uint32_t kmax = row_info(a, m).x;
-    const Row r = row_of<F>(a, row0 + m, kmax);
-    if (!needs_sums(r) || kmax == 0) return;  // the same for the whole block
+    if (kmax == 0) return;  // the same for the whole block
+    r.set_max<F>(a, kmax);
     const typename F::T* x = static_cast<const typename F::T*>(a.x) + (row0 + m) * a.ld;
-    const int32_t i0 = seg * kSeg + lane, left = seg < a.segs ? a.V : 0;
-    const bool bins = needs_bins(r);
-    if (bins) {
-        for (int i = threadIdx.x; i < kBins; i += 256) mass[i] = 0;
-        __syncthreads();
-    }
-    int64_t s = 0;
-#pragma unroll 1
-    for (int j0 = 0; j0 < kSeg / 64; j0 += 8) {
-        uint32_t k[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int32_t i = i0 + 64 * (j0 + j);
-            k[j] = i < left ? F::key(F::load(x[i])) : 0;
+    const int32_t first = (blockIdx.x * 4 + (threadIdx.x >> 6)) * units * kUnit;
+    const bool bins = needs_bins(a, r);
+    init_table(table);
+    if (bins)
+        for (int i = threadIdx.x; i < kBins; i += 256) {
+            mass[i] = 0;
+            count[i] = 0;
         }
+    __syncthreads();
+    uint32_t k[8], next[8];
+    load_unit<F>(a, x, first + lane, next);
+#pragma unroll 1
+    for (int n = 0; n < units; ++n) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) k[j] = next[j];
+        if (n + 1 < units) load_unit<F>(a, x, first + (n + 1) * kUnit + lane, next);
+        int64_t s = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int64_t w = weight<F>(a, r, k[j]);
+            const double z = distance<F>(a, r, k[j]);
+            const int64_t w = k[j] ? weight_at(table, z) : 0;
             if (bins) {
-                if (w) atomicAdd(&mass[bin_of<F>(a, r, k[j])], (unsigned long long)w);
+                if (w) {
+                    const int32_t bin = bin_at(z);
+                    atomicAdd(&mass[bin], (unsigned long long)w);
+                    if (r.k) atomicAdd(&count[bin], 1u);
+                }
             } else {
                 s += (double)w >= r.floor ? w : 0;
             }
         }
-    }
-    if (bins) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < kBins; i += 256)
-            if (mass[i]) atomicAdd(&a.work[m].mass[i], mass[i]);
-        return;
-    }
+        if (bins) continue;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
-    if (lane == 0 && left) a.sums[m * a.segs + seg] = s;
+        for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+        const int32_t at = first + n * kUnit;
+        if (lane == 0 && at < a.V)
+            atomicAdd(reinterpret_cast<unsigned long long*>(&a.sums[m * a.segs + at / kSeg]),
+                      (unsigned long long)s);
+    }
+    if (!bins) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += 256) {
+        if (mass[i]) atomicAdd(&a.work[m].mass[i], mass[i]);
+        if (count[i]) atomicAdd(&a.work[m].count[i], count[i]);
+    }
 }
 
 // What a search over bins finds: the first bin from the top that reaches the
@@ -304,9 +401,9 @@ __device__ inline Found find_bin(const uint32_t* count, const unsigned long long
     constexpr int per = kBins / 64;
     const int lane = threadIdx.x & 63;
     int64_t n = 0, w = 0;
-#pragma unroll
+#pragma unroll 4
     for (int i = 0; i < per; ++i) {
-        n += count ? count[lane * per + i] : 0;
+        n += count[lane * per + i];
         w += (int64_t)mass[lane * per + i];
     }
     int64_t ns = n, wsum = w;
@@ -327,7 +424,7 @@ __device__ inline Found find_bin(const uint32_t* count, const unsigned long long
     f.count = nb;
     f.mass = mb;
     for (int i = 0; i < per; ++i) {  // the same in every lane
-        const int64_t c = count ? count[l * per + i] : 0, v = (int64_t)mass[l * per + i];
+        const int64_t c = count[l * per + i], v = (int64_t)mass[l * per + i];
         if (c == 0 && v == 0) continue;
         last = l * per + i;
         f.count = nb;
@@ -340,60 +437,153 @@ __device__ inline Found find_bin(const uint32_t* count, const unsigned long long
     return f;
 }
 
-// The bin of a top_p row's cut, and whether the lists hold all of it.
-template <class F>
-__device__ inline Found find_mass_bin(const SampleArgs& a, const Row& r, int64_t m)
+// Where the cuts of a row lie in its bins.
+struct Cuts {
+    // top_k's cut is in bin k (kBins without top_k), after so many words and
+    // so much mass
+    int32_t k;
+    int64_t k_count, k_mass;
+    // top_p's is in one of bins [p0, p1], after that mass (without top_p the
+    // bin of top_k's cut): the mass it is a part of is known up to the words
+    // of bin k
+    int32_t p0, p1;
+    int64_t p_mass;
+    double target;  // without top_k
+};
+struct CutLds {
+    int64_t wave[16], k_count, k_mass, k_own, p_mass;
+    int32_t k, p0, p1;
+};
+// Thread t of the block looks at kBins / THREADS bins.
+template <int THREADS>
+__device__ __forceinline__ Cuts find_cuts(const SampleArgs& a, const Row& r, int64_t m, CutLds& lds)
 {
-    int64_t total = 0;
-    const unsigned long long* mass = a.work[m].mass;
-    for (int i = threadIdx.x & 63; i < kBins; i += 64) total += (int64_t)mass[i];
+    constexpr int per = kBins / THREADS;
+    const int b0 = threadIdx.x * per;
+    int64_t w[per], s = 0, total;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
-    const double target = r.p * (double)total;
-    return find_bin(nullptr, mass, [=](int64_t, int64_t w) { return (double)w >= target; });
+    for (int i = 0; i < per; ++i) {
+        w[i] = (int64_t)a.work[m].mass[b0 + i];
+        s += w[i];
+    }
+    const int64_t before = block_scan<THREADS / 64>(s, &total, lds.wave);
+    if (threadIdx.x == 0) {
+        lds.k = kBins;
+        lds.k_count = 0;
+        lds.k_mass = total;
+        lds.k_own = 0;
+        lds.p0 = lds.p1 = kBins;
+        lds.p_mass = total;
+    }
+    __syncthreads();
+    if (r.k > 0) {
+        int64_t c[per], n = 0, all;
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            c[i] = a.work[m].count[b0 + i];
+            n += c[i];
+        }
+        int64_t run = block_scan<THREADS / 64>(n, &all, lds.wave), mass = before;
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            if (run < r.k && run + c[i] >= r.k) {
+                lds.k = b0 + i;
+                lds.k_count = run;
+                lds.k_mass = mass;
+                lds.k_own = w[i];
+            }
+            run += c[i];
+            mass += w[i];
+        }
+        __syncthreads();
+    }
+    Cuts f{lds.k, lds.k_count, lds.k_mass, lds.k, lds.k, lds.k_mass, r.p * (double)total};
+    if (r.p < 1.0) {
+        // the first bins that reach the least and the most that top_p asks for
+        const double least = r.p * (double)lds.k_mass;
+        const double most = r.p * (double)(lds.k_mass + lds.k_own);
+        int64_t run = before;
+#pragma unroll
+        for (int i = 0; i < per; ++i) {
+            const bool first = b0 + i == 0;
+            if (w[i] && (first || (double)run < least) && (double)(run + w[i]) >= least) {
+                lds.p0 = b0 + i;
+                lds.p_mass = run;
+            }
+            if (w[i] && (first || (double)run < most) && (double)(run + w[i]) >= most)
+                lds.p1 = b0 + i;
+            run += w[i];
+        }
+        __syncthreads();
+        f.p0 = min(lds.p0, lds.k);
+        f.p1 = min(lds.p1, lds.k);
+        f.p_mass = lds.p0 <= lds.k ? lds.p_mass : lds.k_mass;
+    }
+    return f;
 }
 
-// Gathers the words of the cut's bin and adds the weights above it.
+// Gathers the words of the cuts' bins and adds the weights above them.
 template <class F>
-__global__ __launch_bounds__(256) void sample_gather_kernel(SampleArgs a, int64_t row0)
+__global__ __launch_bounds__(256) void sample_gather_kernel(SampleArgs a, int64_t row0, int units)
 {
+    __shared__ CutLds lds;
+    __shared__ double table[64];
     const int lane = threadIdx.x & 63;
-    const int seg = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (seg >= a.segs) return;
     const int64_t m = blockIdx.y;
+    Row r = row_of(a, row0 + m);
+    if (!needs_bins(a, r)) return;
     const uint2 info = row_info(a, m);
     if (info.x == 0) return;
-    const Row r = row_of<F>(a, row0 + m, info.x);
-    if (!needs_bins(r)) return;
-    const Found f = find_mass_bin<F>(a, r, m);
-    if (f.bin < bin_of<F>(a, r, info.y)) return;  // the lists hold it
+    r.set_max<F>(a, info.x);
+    init_table(table);
+    const Cuts f = find_cuts<256>(a, r, m, lds);
+    if (r.k == 0 && f.p1 < bin_of<F>(a, r, info.y)) return;  // the lists hold it
     const typename F::T* x = static_cast<const typename F::T*>(a.x) + (row0 + m) * a.ld;
-    const int32_t i0 = seg * kSeg + lane;
+    const int32_t first = (blockIdx.x * 4 + (threadIdx.x >> 6)) * units * kUnit;
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
     RowWork& work = a.work[m];
-    int64_t s = 0;
+    uint32_t k[8], next[8];
+    load_unit<F>(a, x, first + lane, next);
 #pragma unroll 1
-    for (int j0 = 0; j0 < kSeg / 64; j0 += 8) {
-        uint32_t k[8];
+    for (int n = 0; n < units; ++n) {
+        const int32_t i0 = first + n * kUnit;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) k[j] = next[j];
+        if (n + 1 < units) load_unit<F>(a, x, i0 + kUnit + lane, next);
+        int64_t s = 0;
+        uint32_t mine = 0;  // bit j: word j is in one of the bins
+        int cnt = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int32_t i = i0 + 64 * (j0 + j);
-            k[j] = i < a.V ? F::key(F::load(x[i])) : 0;
+            const double z = distance<F>(a, r, k[j]);
+            const int32_t bin = k[j] ? bin_at(z) : kBins + 1;
+            if (bin < f.p0) {
+                const int64_t w = weight_at(table, z);
+                s += (double)w >= r.floor ? w : 0;
+            }
+            const bool here = (bin >= f.p0 && bin <= f.p1) || bin == f.k;
+            mine |= (uint32_t)here << j;
+            cnt += __popcll(__ballot(here));
         }
 #pragma unroll
+        for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+        if (lane == 0 && s)
+            atomicAdd(reinterpret_cast<unsigned long long*>(&a.sums[m * a.segs + i0 / kSeg]),
+                      (unsigned long long)s);
+        if (cnt == 0) continue;
+        // places for all of the wave's at once
+        uint32_t at = 0;
+        if (lane == 0) at = atomicAdd(&work.found, (uint32_t)cnt);
+        at = __shfl((int)at, 0);
+#pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int32_t bin = k[j] ? bin_of<F>(a, r, k[j]) : kBins;
-            if (bin < f.bin) {
-                const int64_t w = weight<F>(a, r, k[j]);
-                s += (double)w >= r.floor ? w : 0;
-            } else if (bin == f.bin) {
-                const uint32_t n = atomicAdd(&work.found, 1u);
-                if (n < kGather) work.near[n] = make_uint2(k[j], (uint32_t)(i0 + 64 * (j0 + j)));
-            }
+            const uint64_t hit = __ballot((mine >> j) & 1);
+            const uint32_t to = at + __popcll(hit & below);
+            if (((mine >> j) & 1) && to < kGather)
+                work.near[to] = make_uint2(k[j], (uint32_t)(i0 + 64 * j + lane));
+            at += __popcll(hit);
         }
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
-    if (lane == 0) a.sums[m * a.segs + seg] = s;
 }
 
 // ---------------------------------------------------------------------------
@@ -408,31 +598,11 @@ struct DrawLds {
     uint64_t near[2 * kNear];
     int64_t wave64[kDrawWaves];
     int32_t wave32[kDrawWaves];
+    CutLds cuts;
+    double table[64];
     uint32_t sel[4];
     int64_t sel64[4];
 };
-
-// The sum of the values of the threads before this one, and of all.
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* total, int64_t* lds)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t s = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int64_t t = __shfl_up(s, o);
-        if (lane >= o) s += t;
-    }
-    __syncthreads();
-    if (lane == 63) lds[wave] = s;
-    __syncthreads();
-    int64_t before = 0, all = 0;
-    for (int w = 0; w < kDrawWaves; ++w) {
-        if (w < wave) before += lds[w];
-        all += lds[w];
-    }
-    *total = all;
-    return before + s - v;
-}
 
 // A word as one number that ascends along the order.
 __device__ __forceinline__ uint64_t order(uint32_t key, uint32_t idx)
@@ -473,7 +643,7 @@ __device__ __forceinline__ Cut cut_in_order(const SampleArgs& a, const Row& r, D
         int64_t run = before;
         for (int e0 = 0; e0 < n; e0 += 64) {
             const uint64_t w = e0 + lane < n ? word[e0 + lane] : ~0ull;
-            int64_t c = weight<F>(a, r, key_of(w));
+            int64_t c = weight<F>(a, r, lds.table, key_of(w));
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) {
                 const int64_t v = __shfl_up(c, o);
@@ -576,7 +746,7 @@ __device__ __forceinline__ Cut cut_row(const SampleArgs& a, const Row& r, const 
                 if (k[u] < lo || k[u] > hi) continue;
                 const uint32_t bin = (hi - k[u]) >> shift;
                 atomicAdd(&lds.count[bin], 1u);
-                atomicAdd(&lds.mass[bin], (unsigned long long)weight<F>(a, r, k[u]));
+                atomicAdd(&lds.mass[bin], (unsigned long long)weight<F>(a, r, lds.table, k[u]));
             }
         }
         __syncthreads();
@@ -602,7 +772,7 @@ __device__ __forceinline__ Cut cut_row(const SampleArgs& a, const Row& r, const 
         }
     }
     // the words at key lo: how many are kept, and which is the last
-    const int64_t w = weight<F>(a, r, lo);
+    const int64_t w = weight<F>(a, r, lds.table, lo);
     int64_t keep;
     if (MASS) {
         int64_t l = 1, h = ties;
@@ -656,7 +826,7 @@ __device__ __forceinline__ int32_t draw_word(const SampleArgs& a, const Row& r, 
         if (i >= i1) return 0;
         const uint32_t k = ws.key(i);
         if (!cut.keeps(k, ws.index(i))) return 0;
-        const int64_t w = weight<F>(a, r, k);
+        const int64_t w = weight<F>(a, r, lds.table, k);
         return (double)w >= r.floor ? w : 0;
     };
     int64_t s = 0;
@@ -705,14 +875,14 @@ __device__ __forceinline__ int32_t draw_by_segments(const SampleArgs& a, const R
     const int tid = threadIdx.x, lane = tid & 63;
     int64_t s = 0, all = 0, base = 0, total = 0;
     for (int i = tid; i < a.segs; i += kDrawThreads) s += sum(i);
-    block_scan(s, &total, lds.wave64);
+    block_scan<kDrawWaves>(s, &total, lds.wave64);
     const int64_t target = min((int64_t)(u * (double)total), total - 1);
     if (tid == 0) lds.sel[0] = 0;
     __syncthreads();
     for (int s0 = 0; s0 < a.segs; s0 += kDrawThreads) {
         const int i = s0 + tid;
         const int64_t v = i < a.segs ? sum(i) : 0;
-        const int64_t before = base + block_scan(v, &all, lds.wave64);
+        const int64_t before = base + block_scan<kDrawWaves>(v, &all, lds.wave64);
         if (target >= before && target < before + v) {
             lds.sel[0] = (uint32_t)i;
             lds.sel64[0] = before;
@@ -724,71 +894,83 @@ __device__ __forceinline__ int32_t draw_by_segments(const SampleArgs& a, const R
     int64_t run = lds.sel64[0];
     __syncthreads();
     if (tid < 64) {
-        uint32_t k[kSeg / 64];
-#pragma unroll
-        for (int j = 0; j < kSeg / 64; ++j) {
-            const int32_t i = i0 + 64 * j + lane;
-            k[j] = i < a.V ? F::key(F::load(x[i])) : 0;
-        }
         bool done = false;
+#pragma unroll 1
+        for (int j0 = 0; j0 < kSeg / 64 && !done; j0 += 8) {
+            uint32_t k[8];
+            load_unit<F>(a, x, i0 + 64 * j0 + lane, k);
 #pragma unroll
-        for (int j = 0; j < kSeg / 64; ++j) {
-            if (done) continue;
-            const int32_t i = i0 + 64 * j + lane;
-            int64_t c = cut.keeps(k[j], (uint32_t)i) ? weight<F>(a, r, k[j]) : 0;
-            if (!((double)c >= r.floor)) c = 0;
+            for (int j = 0; j < 8; ++j) {
+                if (done) continue;
+                const int32_t i = i0 + 64 * (j0 + j) + lane;
+                int64_t c = cut.keeps(k[j], (uint32_t)i) ? weight<F>(a, r, lds.table, k[j]) : 0;
+                if (!((double)c >= r.floor)) c = 0;
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int64_t v = __shfl_up(c, o);
-                if (lane >= o) c += v;
+                for (int o = 1; o < 64; o <<= 1) {
+                    const int64_t v = __shfl_up(c, o);
+                    if (lane >= o) c += v;
+                }
+                const uint64_t hit = __ballot(run + c > target);
+                if (hit) {
+                    if (lane == __builtin_ctzll(hit)) lds.sel[0] = (uint32_t)i;
+                    done = true;
+                }
+                run += __shfl(c, 63);
             }
-            const uint64_t hit = __ballot(run + c > target);
-            if (hit) {
-                if (lane == __builtin_ctzll(hit)) lds.sel[0] = (uint32_t)i;
-                done = true;
-            }
-            run += __shfl(c, 63);
         }
     }
     __syncthreads();
     return (int32_t)lds.sel[0];
 }
 
-// The listed words from the bound on into LDS, in index order; how many there
-// are (more than kEntries: not all of them are there).
-__device__ __forceinline__ int64_t load_list(const SampleArgs& a, int64_t m, uint32_t bound, DrawLds& lds)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint4* info = a.info + m * a.segs;
-    const uint2* list = a.list + m * a.segs * kList;
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    constexpr int kTurn = 16;  // segments of a wave per turn, all loads under way
-    int64_t n = 0;
-    for (int s0 = 0; s0 < a.segs; s0 += kTurn * kDrawWaves) {
-        const int first = s0 + wave * kTurn;
-        uint2 e[kTurn];
+// A wave's lists of one turn, all loads under way at once.
+constexpr int kTurn = 8;
+struct Lists {
+    uint2 e[kTurn];
+    uint32_t n[kTurn];
+    __device__ __forceinline__ void load(const SampleArgs& a, int64_t m, int s0)
+    {
+        const int lane = threadIdx.x & 63, first = s0 + (threadIdx.x >> 6) * kTurn;
 #pragma unroll
         for (int i = 0; i < kTurn; ++i) {
-            const int s = first + i;
-            e[i] = make_uint2(0, 0);
-            if (s < a.segs && lane < (int)info[s].z) e[i] = list[(int64_t)s * kList + lane];
+            const int64_t s = m * a.segs + min(first + i, a.segs - 1);
+            e[i] = a.list[s * kList + lane];  // places past the list's words: anything
+            n[i] = first + i < a.segs ? a.info[s].z : 0;
         }
+    }
+    __device__ __forceinline__ bool has(int i, uint32_t bound) const
+    {
+        return (threadIdx.x & 63) < n[i] && e[i].x >= bound;
+    }
+};
+
+// The listed words from the bound on into LDS, in index order; how many there
+// are (more than kEntries: not all of them are there).  t: the first turn.
+__device__ __forceinline__ int64_t store_lists(const SampleArgs& a, int64_t m, uint32_t bound,
+                                               Lists& t, DrawLds& lds)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    int64_t n = 0;
+    for (int s0 = 0; s0 < a.segs; s0 += kTurn * kDrawWaves) {
+        if (s0) t.load(a, m, s0);
         int mine = 0;
 #pragma unroll
-        for (int i = 0; i < kTurn; ++i) mine += __popcll(__ballot(e[i].x >= bound));
+        for (int i = 0; i < kTurn; ++i) mine += __popcll(__ballot(t.has(i, bound)));
         __syncthreads();
         if (lane == 0) lds.wave32[wave] = mine;
         __syncthreads();
         int64_t at = n;
+#pragma unroll
         for (int w = 0; w < kDrawWaves; ++w) {
             if (w < wave) at += lds.wave32[w];
             n += lds.wave32[w];
         }
 #pragma unroll
         for (int i = 0; i < kTurn; ++i) {
-            const uint64_t hit = __ballot(e[i].x >= bound);
+            const uint64_t hit = __ballot(t.has(i, bound));
             const int64_t to = at + __popcll(hit & below);
-            if (e[i].x >= bound && to < kEntries) lds.word[to] = order(e[i].x, e[i].y);
+            if (t.has(i, bound) && to < kEntries) lds.word[to] = order(t.e[i].x, t.e[i].y);
             at += __popcll(hit);
         }
     }
@@ -796,24 +978,58 @@ __device__ __forceinline__ int64_t load_list(const SampleArgs& a, int64_t m, uin
     return n;
 }
 
+// The draw from the n <= kDrawThreads first words of the order, unordered in
+// lds.near, which hold the kept ones: a thread per word.  mass: top_p's, or
+// negative: p of the sum of the first k.
 template <class F>
-__global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a, int64_t row0)
+__device__ __forceinline__ int32_t draw_few(const SampleArgs& a, const Row& r, DrawLds& lds, int n,
+                                            double mass, double u)
+{
+    const int e = threadIdx.x;
+    order_words(lds.near, n, lds.near + kNear);
+    __syncthreads();
+    const uint64_t word = e < n ? lds.near[kNear + e] : 0;
+    const int64_t w = e < n && (r.k == 0 || e < r.k) ? weight<F>(a, r, lds.table, key_of(word)) : 0;
+    int64_t total;
+    const int64_t before = block_scan<kDrawWaves>(w, &total, lds.wave64);
+    if (mass < 0.0) mass = r.p * (double)total;
+    const bool kept = (r.p >= 1.0 || e == 0 || (double)before < mass) && (double)w >= r.floor;
+    const int64_t kw = kept ? w : 0;
+    lds.mass[e] = (unsigned long long)kw;
+    block_scan<kDrawWaves>(kw, &total, lds.wave64);
+    const int64_t target = min((int64_t)(u * (double)total), total - 1);
+    // the kept weight of the words before this one in index order
+    int64_t run = 0;
+#pragma unroll 8
+    for (int o = 0; o < n; ++o)
+        run += (uint32_t)lds.near[kNear + o] < (uint32_t)word ? (int64_t)lds.mass[o] : 0;
+    if (kw > 0 && target >= run && target < run + kw) lds.sel[0] = (uint32_t)word;
+    __syncthreads();
+    return (int32_t)lds.sel[0];
+}
+
+template <class F>
+__global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs a, int64_t row0)
 {
     __shared__ DrawLds lds;
     const int tid = threadIdx.x;
     const int64_t m = blockIdx.x, row = row0 + m;
+    Row r = row_of(a, row);
+    const double u0 = (double)a.u[row], u = u0 > 0.0 ? fmin(u0, 1.0) : 0.0;
     const uint2 info = row_info(a, m);
     const uint32_t bound = info.y;
     if (info.x == 0) {  // nothing can be drawn
         if (tid == 0) a.tokens[row] = -1;
         return;
     }
-    const Row r = row_of<F>(a, row, info.x);
-    const double u0 = (double)a.u[row], u = u0 > 0.0 ? fmin(u0, 1.0) : 0.0;
+    r.set_max<F>(a, info.x);
+    init_table(lds.table);
+    __syncthreads();
     const typename F::T* x = static_cast<const typename F::T*>(a.x) + row * a.ld;
     const int64_t* sums = a.sums + m * a.segs;
+    const bool bins = needs_bins(a, r);
 
-    if (needs_sums(r) && !needs_bins(r)) {  // no cut
+    if (needs_sums(a, r) && !bins) {  // no cut
         const Cut all{1, 0xffffffffu, 0};
         const int32_t tok = draw_by_segments<F>(a, r, x, lds, all, u, [&](int i) { return sums[i]; });
         if (tid == 0) a.tokens[row] = tok;
@@ -822,24 +1038,41 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a,
 
     Cut cut{1, 0xffffffffu, 0};
     double target = 0.0;
-    if (needs_bins(r)) {
-        const Found f = find_mass_bin<F>(a, r, m);
-        target = r.p * (double)f.total;
+    if (bins) {
+        const Cuts f = find_cuts<kDrawThreads>(a, r, m, lds.cuts);
+        target = f.target;
         const RowWork& work = a.work[m];
         const int n = (int)min(work.found, (uint32_t)0x7fffffff);
-        if (f.bin >= bin_of<F>(a, r, bound) && n <= kGather && a.segs <= kBins) {
+        const bool gathered = r.k > 0 || f.p1 >= bin_of<F>(a, r, bound);
+        if (gathered && n <= kGather && a.segs <= kBins) {
             for (int i = tid; i < n; i += kDrawThreads)
                 lds.word[i] = order(work.near[i].x, work.near[i].y);
             for (int i = tid; i < a.segs; i += kDrawThreads)
                 lds.mass[i] = (unsigned long long)sums[i];
+            if (tid == 0) lds.sel[2] = 0;
             __syncthreads();
+            const uint64_t* sorted = lds.word + kGather;
             order_words(lds.word, n, lds.word + kGather);
-            cut = cut_in_order<F, true>(a, r, lds, lds.word + kGather, n, f.mass, 0, target);
-            // the kept words of the bin join their segments' sums
+            double mass = target;
+            if (r.k > 0 && f.k == kBins) {  // fewer than k have a weight
+                mass = r.p * (double)f.k_mass;
+            } else if (r.k > 0) {
+                // words of bin k come last
+                for (int i = tid; i < n; i += kDrawThreads)
+                    if (bin_of<F>(a, r, key_of(lds.word[i])) < f.k) atomicAdd(&lds.sel[2], 1u);
+                __syncthreads();
+                const int s = (int)lds.sel[2];
+                cut = cut_in_order<F, false>(a, r, lds, sorted + s, n - s, f.k_mass, r.k - f.k_count,
+                                             0.0);
+                mass = r.p * (double)cut.mass;
+            }
+            if (r.p < 1.0)
+                cut = cut_in_order<F, true>(a, r, lds, sorted, n, f.p_mass, 0, mass);
+            // the kept ones of these words join their segments' sums
             for (int i = tid; i < n; i += kDrawThreads) {
                 const uint32_t k = key_of(lds.word[i]), at = (uint32_t)lds.word[i];
                 if (!cut.keeps(k, at)) continue;
-                const int64_t w = weight<F>(a, r, k);
+                const int64_t w = weight<F>(a, r, lds.table, k);
                 if ((double)w >= r.floor) atomicAdd(&lds.mass[at / kSeg], (unsigned long long)w);
             }
             __syncthreads();
@@ -850,7 +1083,9 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a,
         }
     }
 
-    const int64_t n = load_list(a, m, bound, lds);
+    Lists lists;
+    lists.load(a, m, 0);
+    const int64_t n = store_lists(a, m, bound, lists, lds);
     bool listed = n > 0 && n <= kEntries && n >= r.k;
     if (listed) {
         for (int i = tid; i < kBins; i += kDrawThreads) {
@@ -862,18 +1097,46 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(SampleArgs a,
         for (int i = tid; i < n; i += kDrawThreads) {
             const uint32_t k = key_of(lds.word[i]);
             const int32_t bin = bin_of<F>(a, r, k);
-            const int64_t w = weight<F>(a, r, k);
+            const int64_t w = weight<F>(a, r, lds.table, k);
             s += w;
             atomicAdd(&lds.count[bin], 1u);
             atomicAdd(&lds.mass[bin], (unsigned long long)w);
         }
-        block_scan(s, &all, lds.wave64);
+        block_scan<kDrawWaves>(s, &all, lds.wave64);
+        listed = r.k > 0 || (double)all >= target;
+    }
+    if (listed) {
+        // the bin of top_k's cut, without top_k of top_p's
+        if (tid < 64) {
+            const Found f = find_bin(lds.count, lds.mass, [=](int64_t c, int64_t w) {
+                return r.k > 0 ? c >= r.k : (double)w >= target;
+            });
+            if (tid == 0) {
+                lds.sel[0] = (uint32_t)f.bin;
+                lds.sel[1] = 0;
+                lds.sel64[0] = f.count;
+                lds.sel64[1] = f.mass;
+            }
+        }
+        __syncthreads();
+        const int32_t bin = (int32_t)lds.sel[0];
+        const int64_t count = lds.sel64[0] + lds.count[bin];
+        if (count <= kNear) {
+            for (int i = tid; i < n; i += kDrawThreads)
+                if (bin_of<F>(a, r, key_of(lds.word[i])) <= bin)
+                    lds.near[atomicAdd(&lds.sel[1], 1u)] = lds.word[i];
+            __syncthreads();
+            const int32_t tok = draw_few<F>(a, r, lds, (int)count, r.k > 0 ? -1.0 : target, u);
+            if (tid == 0) a.tokens[row] = tok;
+            return;
+        }
+        __syncthreads();
         if (r.k > 0) {
             listed = cut_listed<F, false>(a, r, lds, (int)n, r.k, 0.0, cut);
             if (listed && r.p < 1.0)
                 listed = cut_listed<F, true>(a, r, lds, (int)n, 0, r.p * (double)cut.mass, cut);
         } else {
-            listed = (double)all >= target && cut_listed<F, true>(a, r, lds, (int)n, 0, target, cut);
+            listed = cut_listed<F, true>(a, r, lds, (int)n, 0, target, cut);
         }
     }
     const Words<F> ws{&lds, x, listed ? (int32_t)n : a.V, listed};
@@ -908,8 +1171,12 @@ hipError_t launch(SampleArgs a, int64_t M, char* ws, int64_t ws_bytes, hipStream
         a.sums = reinterpret_cast<int64_t*>(ws + n * (sizeof(RowWork) + a.segs * (16 + 8 * kList)));
         const dim3 g((unsigned)((a.segs + 3) / 4), (unsigned)n);
         sample_scan_kernel<F><<<g, 256, 0, s>>>(a, m0);
-        sample_sums_kernel<F><<<g, 256, 0, s>>>(a, m0);
-        if (a.top_p) sample_gather_kernel<F><<<g, 256, 0, s>>>(a, m0);
+        // a unit per wave, a segment or four of them where that fills the chip
+        // (each work-group adds its bins to the row's)
+        const int units = n * a.segs >= 32768 ? 4 * kSeg / kUnit : n * a.segs >= 8192 ? kSeg / kUnit : 1;
+        const dim3 gu((unsigned)((a.V + 4 * units * kUnit - 1) / (4 * units * kUnit)), (unsigned)n);
+        sample_sums_kernel<F><<<gu, 256, 0, s>>>(a, m0, units);
+        if (a.top_p || a.top_k) sample_gather_kernel<F><<<gu, 256, 0, s>>>(a, m0, units);
         sample_draw_kernel<F><<<(unsigned)n, kDrawThreads, 0, s>>>(a, m0);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
