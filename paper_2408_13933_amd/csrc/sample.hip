@@ -70,9 +70,9 @@ struct Fp32 {
     using V = float;
     static constexpr int kTopBit = 31;
     static constexpr uint32_t kLeast = 0x00800000u;  // of the least finite value
-    static __device__ V load(float x) { return x; }
+    static __device__ V load(float x) { return fmaxf(x, -__builtin_inff()); }  // no NaN
     static __device__ V none() { return -__builtin_inff(); }
-    static __device__ V larger(V a, V b) { return fmaxf(a, b); }  // the other one for NaN
+    static __device__ V larger(V a, V b) { return fmaxf(a, b); }
     static __device__ uint32_t key(V x)
     {
         const uint32_t b = __float_as_uint(x + 0.0f);  // -0 is 0
@@ -83,7 +83,6 @@ struct Fp32 {
     {
         return __uint_as_float((k >> 31) ? k & 0x7fffffffu : ~k);
     }
-    static __device__ double value(const SampleArgs&, uint32_t k) { return (double)of_key(k); }
 };
 struct Code16 {
     using T = int16_t;
@@ -95,24 +94,23 @@ struct Code16 {
     static __device__ V larger(V a, V b) { return max(a, b); }
     static __device__ uint32_t key(V v) { return (uint32_t)v; }
     static __device__ V of_key(uint32_t k) { return (int32_t)k; }
-    static __device__ double value(const SampleArgs& p, uint32_t k)
-    {
-        return p.alpha * (double)((int32_t)k - 32769 - p.zp);
-    }
 };
 
 // A row's settings.
 struct Row {
     double scale;    // log2(e) / temperature
-    double p, floor; // top_p (>= 1: off), least weight of the min_p rule
-    int32_t k;       // 0: off
-    double max;      // its largest logit
-    uint32_t kmax;
+    double p;        // top_p (1: off)
+    int64_t floor;   // least weight of the min_p rule
+    int32_t k;       // top_k (0: off)
+    uint32_t kmax;   // key of its largest logit
+    double max;      // that logit (fp32)
+    double step;     // distance of neighbouring codes (16 bits)
     template <class F>
     __device__ void set_max(const SampleArgs& a, uint32_t key)
     {
         kmax = key;
-        max = F::value(a, key);
+        max = (double)F::of_key(key);
+        step = a.alpha * scale;
     }
 };
 
@@ -125,8 +123,10 @@ __device__ inline Row row_of(const SampleArgs& a, int64_t m)
     r.p = a.top_p ? (double)a.top_p[m] : 1.0;
     r.p = r.p < 1.0 ? fmax(r.p, 0.0) : 1.0;  // NaN: off
     const double mp = a.min_p ? (double)a.min_p[m] : 0.0;
-    r.floor = mp > 0.0 ? fmin(mp, 1.0) * kOne : 0.0;
-    r.scale = 1.4426950408889634 / t;
+    r.floor = mp > 0.0 ? (int64_t)ceil(fmin(mp, 1.0) * kOne) : 0;
+    // finite (t >= 2^-149); not 0 even for an infinite t, so that an infinite
+    // distance stays one
+    r.scale = fmax(1.4426950408889634 / t, 1e-300);
     if (!(t > 0.0)) {  // greedy: the first of the largest
         r.k = 1;
         r.scale = 1.4426950408889634;
@@ -134,13 +134,16 @@ __device__ inline Row row_of(const SampleArgs& a, int64_t m)
     return r;
 }
 
-// The distance of a key's logit from the largest, in factors of two of its
-// weight, at most 100.  The same for equal logits, never less for smaller ones.
-template <class F>
-__device__ inline double distance(const SampleArgs& a, const Row& r, uint32_t k)
+// The distance of a logit from the row's largest, in factors of two of its
+// weight, at most 100.  The same for equal logits, never less for smaller
+// ones; 100 for -infinity, and next to +infinity for all but that.
+__device__ inline double distance(const Row& r, float v)
 {
-    if (k == r.kmax) return 0.0;
-    return fmin((r.max - F::value(a, k)) * r.scale, 100.0);  // NaN (infinities): 100
+    return fmin(fmax((r.max - (double)v) * r.scale, 0.0), 100.0);  // infinity - infinity: 0
+}
+__device__ inline double distance(const Row& r, int32_t v)
+{
+    return fmin((double)((int32_t)r.kmax - v) * r.step, 100.0);
 }
 
 // rint(2^40 2^-z): z to the next 1/64, 2^(j/64) from a table in LDS (2^40 of
@@ -157,31 +160,29 @@ __device__ inline int64_t weight_at(const double* table, double z)
     const double t = kShift - z;
     const double f = (kShift - t) - z;
     const int32_t k = rint_low(t);
-    int64_t e = __double_as_longlong(table[k & 63]);
-    e += (int64_t)(k & ~63) << 46;  // the exponent field, k / 64 lower
+    const int64_t e = __double_as_longlong(table[k & 63]);
+    const int32_t hi = (int32_t)(e >> 32) + ((k & ~63) << 14);  // the exponent, k / 64 lower
     double q = 0x1.3b2ad0385b409p-7;
     q = __builtin_fma(q, f, 0x1.c6b0c40d8c4e9p-5);
     q = __builtin_fma(q, f, 0x1.ebfbdff82ac52p-3);
     q = __builtin_fma(q, f, 0x1.62e42fefa0352p-1);
     q = __builtin_fma(q, f, 1.0);
-    const double w = __builtin_fma(q, __longlong_as_double(e), kRintShift);
+    const double w = __builtin_fma(
+        q, __longlong_as_double(((int64_t)hi << 32) | (uint32_t)e), kRintShift);
     return __double_as_longlong(w) - __double_as_longlong(kRintShift);
 }
 template <class F>
-__device__ inline int64_t weight(const SampleArgs& a, const Row& r, const double* table, uint32_t k)
+__device__ inline int64_t weight(const Row& r, const double* table, uint32_t k)
 {
-    return k ? weight_at(table, distance<F>(a, r, k)) : 0;
+    return k ? weight_at(table, distance(r, F::of_key(k))) : 0;
 }
 
 // The bin of a distance.
-__device__ inline int32_t bin_at(double z)
-{
-    return z * kBinScale < (double)(kBins - 1) ? max((int32_t)(z * kBinScale), 0) : kBins - 1;
-}
+__device__ inline int32_t bin_at(double z) { return min((int32_t)(z * kBinScale), kBins - 1); }
 template <class F>
-__device__ inline int32_t bin_of(const SampleArgs& a, const Row& r, uint32_t k)
+__device__ inline int32_t bin_of(const Row& r, uint32_t k)
 {
-    return bin_at(distance<F>(a, r, k));
+    return bin_at(distance(r, F::of_key(k)));
 }
 
 // Rows without top_k need the weights of all words, with top_p per bin; so do
@@ -196,6 +197,26 @@ __device__ inline bool needs_sums(const SampleArgs& a, const Row& r)
     return r.k == 0 || needs_bins(a, r);
 }
 
+// Words i0, i0 + 64, ... of a row, `none` past its end; first: the least of
+// them over the wave.  All loads are under way before the first is looked at.
+template <class F, int N>
+__device__ __forceinline__ void load_words(const SampleArgs& a, const typename F::T* x,
+                                           int32_t first, int32_t i0, typename F::V (&v)[N])
+{
+    typename F::T t[N];
+    if (first + 64 * N <= a.V) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) t[j] = x[i0 + 64 * j];
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = F::load(t[j]);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) t[j] = x[min(i0 + 64 * j, a.V - 1)];
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = i0 + 64 * j < a.V ? F::load(t[j]) : F::none();
+}
+
 template <class F>
 __global__ __launch_bounds__(256) void sample_scan_kernel(SampleArgs a, int64_t row0)
 {
@@ -206,8 +227,7 @@ __global__ __launch_bounds__(256) void sample_scan_kernel(SampleArgs a, int64_t 
     const typename F::T* x = static_cast<const typename F::T*>(a.x) + (row0 + m) * a.ld;
     const int32_t i0 = seg * kSeg + lane;
     typename F::V k[kSeg / 64];
-#pragma unroll
-    for (int j = 0; j < kSeg / 64; ++j) k[j] = i0 + 64 * j < a.V ? F::load(x[i0 + 64 * j]) : F::none();
+    load_words<F>(a, x, seg * kSeg, i0, k);
     typename F::V most = F::none();
 #pragma unroll
     for (int j = 0; j < kSeg / 64; ++j) most = F::larger(most, k[j]);
@@ -312,15 +332,6 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* total, int64_t
     return before + s - v;
 }
 
-// The keys of the unit's words, eight per lane (0 past the row).
-template <class F>
-__device__ __forceinline__ void load_unit(const SampleArgs& a, const typename F::T* x, int32_t i0,
-                                          uint32_t (&k)[8])
-{
-#pragma unroll
-    for (int j = 0; j < 8; ++j) k[j] = i0 + 64 * j < a.V ? F::key(F::load(x[i0 + 64 * j])) : 0;
-}
-
 // A wave takes `units` units of 512 words in a row.
 template <class F>
 __global__ __launch_bounds__(256) void sample_sums_kernel(SampleArgs a, int64_t row0, int units)
@@ -345,18 +356,19 @@ __global__ __launch_bounds__(256) void sample_sums_kernel(SampleArgs a, int64_t 
             count[i] = 0;
         }
     __syncthreads();
-    uint32_t k[8], next[8];
-    load_unit<F>(a, x, first + lane, next);
+    typename F::V v[8], next[8];
+    load_words<F>(a, x, first, first + lane, next);
 #pragma unroll 1
     for (int n = 0; n < units; ++n) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) k[j] = next[j];
-        if (n + 1 < units) load_unit<F>(a, x, first + (n + 1) * kUnit + lane, next);
+        for (int j = 0; j < 8; ++j) v[j] = next[j];
+        if (n + 1 < units)
+            load_words<F>(a, x, first + (n + 1) * kUnit, first + (n + 1) * kUnit + lane, next);
         int64_t s = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const double z = distance<F>(a, r, k[j]);
-            const int64_t w = k[j] ? weight_at(table, z) : 0;
+            const double z = distance(r, v[j]);
+            const int64_t w = v[j] != F::none() ? weight_at(table, z) : 0;
             if (bins) {
                 if (w) {
                     const int32_t bin = bin_at(z);
@@ -364,7 +376,7 @@ __global__ __launch_bounds__(256) void sample_sums_kernel(SampleArgs a, int64_t 
                     if (r.k) atomicAdd(&count[bin], 1u);
                 }
             } else {
-                s += (double)w >= r.floor ? w : 0;
+                s += w >= r.floor ? w : 0;
             }
         }
         if (bins) continue;
@@ -392,48 +404,52 @@ struct Found {
     int64_t total;  // mass of all bins
 };
 
+// Bins in LDS are kept so that the lanes that hold 16 neighbouring ones each
+// read next to each other.
+__device__ inline int32_t place_of(int32_t bin) { return (bin & 15) * 64 + (bin >> 4); }
+
 // One wave looks for the bin; lane l holds bins 16 l on.  reaches(count,
 // mass) of everything up to and with a bin.
 template <class Reaches>
 __device__ inline Found find_bin(const uint32_t* count, const unsigned long long* mass,
                                  Reaches reaches)
 {
-    constexpr int per = kBins / 64;
+    static_assert(kBins == 64 * 16, "16 bins per lane");
     const int lane = threadIdx.x & 63;
     int64_t n = 0, w = 0;
 #pragma unroll 4
-    for (int i = 0; i < per; ++i) {
-        n += count[lane * per + i];
-        w += (int64_t)mass[lane * per + i];
+    for (int i = 0; i < 16; ++i) {
+        n += count[64 * i + lane];
+        w += (int64_t)mass[64 * i + lane];
     }
-    int64_t ns = n, wsum = w;
+    auto scan = [=](int64_t& a, int64_t& b) {
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int64_t t = __shfl_up(ns, o), v = __shfl_up(wsum, o);
-        if (lane >= o) {
-            ns += t;
-            wsum += v;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int64_t t = __shfl_up(a, o), v = __shfl_up(b, o);
+            if (lane >= o) {
+                a += t;
+                b += v;
+            }
         }
-    }
+    };
+    int64_t ns = n, ws = w;
+    scan(ns, ws);
     Found f;
-    f.total = __shfl(wsum, 63);
-    const uint64_t hit = __ballot(reaches(ns, wsum)), some = __ballot(n > 0 || w > 0);
+    f.total = __shfl(ws, 63);
+    // the first lane that reaches the target, or the last with anything; then
+    // the same among its bins
+    const uint64_t hit = __ballot(reaches(ns, ws)), some = __ballot(n > 0);
     const int l = hit ? __builtin_ctzll(hit) : some ? 63 - __builtin_clzll(some) : 0;
-    int64_t nb = __shfl(ns - n, l), mb = __shfl(wsum - w, l);
-    int32_t last = l * per;
-    f.count = nb;
-    f.mass = mb;
-    for (int i = 0; i < per; ++i) {  // the same in every lane
-        const int64_t c = count[l * per + i], v = (int64_t)mass[l * per + i];
-        if (c == 0 && v == 0) continue;
-        last = l * per + i;
-        f.count = nb;
-        f.mass = mb;
-        nb += c;
-        mb += v;
-        if (hit && reaches(nb, mb)) break;
-    }
-    f.bin = last;
+    const int64_t nb = __shfl(ns - n, l), mb = __shfl(ws - w, l);
+    const int64_t c = lane < 16 ? count[64 * lane + l] : 0;
+    const int64_t v = lane < 16 ? (int64_t)mass[64 * lane + l] : 0;
+    int64_t cs = c, vs = v;
+    scan(cs, vs);
+    const uint64_t have = __ballot(c > 0), in = __ballot(c > 0 && reaches(nb + cs, mb + vs));
+    const int i = in ? __builtin_ctzll(in) : have ? 63 - __builtin_clzll(have) : 0;
+    f.bin = 16 * l + i;
+    f.count = nb + __shfl(cs - c, i);
+    f.mass = mb + __shfl(vs - v, i);
     return f;
 }
 
@@ -537,29 +553,29 @@ __global__ __launch_bounds__(256) void sample_gather_kernel(SampleArgs a, int64_
     r.set_max<F>(a, info.x);
     init_table(table);
     const Cuts f = find_cuts<256>(a, r, m, lds);
-    if (r.k == 0 && f.p1 < bin_of<F>(a, r, info.y)) return;  // the lists hold it
+    if (r.k == 0 && f.p1 < bin_of<F>(r, info.y)) return;  // the lists hold it
     const typename F::T* x = static_cast<const typename F::T*>(a.x) + (row0 + m) * a.ld;
     const int32_t first = (blockIdx.x * 4 + (threadIdx.x >> 6)) * units * kUnit;
     const uint64_t below = ((uint64_t)1 << lane) - 1;
     RowWork& work = a.work[m];
-    uint32_t k[8], next[8];
-    load_unit<F>(a, x, first + lane, next);
+    typename F::V v[8], next[8];
+    load_words<F>(a, x, first, first + lane, next);
 #pragma unroll 1
     for (int n = 0; n < units; ++n) {
         const int32_t i0 = first + n * kUnit;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) k[j] = next[j];
-        if (n + 1 < units) load_unit<F>(a, x, i0 + kUnit + lane, next);
+        for (int j = 0; j < 8; ++j) v[j] = next[j];
+        if (n + 1 < units) load_words<F>(a, x, i0 + kUnit, i0 + kUnit + lane, next);
         int64_t s = 0;
         uint32_t mine = 0;  // bit j: word j is in one of the bins
         int cnt = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const double z = distance<F>(a, r, k[j]);
-            const int32_t bin = k[j] ? bin_at(z) : kBins + 1;
+            const double z = distance(r, v[j]);
+            const int32_t bin = v[j] != F::none() ? bin_at(z) : kBins + 1;
             if (bin < f.p0) {
                 const int64_t w = weight_at(table, z);
-                s += (double)w >= r.floor ? w : 0;
+                s += w >= r.floor ? w : 0;
             }
             const bool here = (bin >= f.p0 && bin <= f.p1) || bin == f.k;
             mine |= (uint32_t)here << j;
@@ -580,7 +596,7 @@ __global__ __launch_bounds__(256) void sample_gather_kernel(SampleArgs a, int64_
             const uint64_t hit = __ballot((mine >> j) & 1);
             const uint32_t to = at + __popcll(hit & below);
             if (((mine >> j) & 1) && to < kGather)
-                work.near[to] = make_uint2(k[j], (uint32_t)(i0 + 64 * j + lane));
+                work.near[to] = make_uint2(F::key(v[j]), (uint32_t)(i0 + 64 * j + lane));
             at += __popcll(hit);
         }
     }
@@ -643,7 +659,7 @@ __device__ __forceinline__ Cut cut_in_order(const SampleArgs& a, const Row& r, D
         int64_t run = before;
         for (int e0 = 0; e0 < n; e0 += 64) {
             const uint64_t w = e0 + lane < n ? word[e0 + lane] : ~0ull;
-            int64_t c = weight<F>(a, r, lds.table, key_of(w));
+            int64_t c = weight<F>(r, lds.table, key_of(w));
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) {
                 const int64_t v = __shfl_up(c, o);
@@ -703,10 +719,10 @@ __device__ __forceinline__ bool cut_listed(const SampleArgs& a, const Row& r, Dr
     __syncthreads();
     const int32_t bin = (int32_t)lds.sel[0];
     const int64_t count = lds.sel64[0], mass = lds.sel64[1];
-    const int near = (int)lds.count[bin];
+    const int near = (int)lds.count[place_of(bin)];
     if (near > kNear) return false;
     for (int i = threadIdx.x; i < n; i += kDrawThreads)
-        if (bin_of<F>(a, r, key_of(lds.word[i])) == bin)
+        if (bin_of<F>(r, key_of(lds.word[i])) == bin)
             lds.near[atomicAdd(&lds.sel[1], 1u)] = lds.word[i];
     __syncthreads();
     order_words(lds.near, near, lds.near + kNear);
@@ -744,9 +760,9 @@ __device__ __forceinline__ Cut cut_row(const SampleArgs& a, const Row& r, const 
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 if (k[u] < lo || k[u] > hi) continue;
-                const uint32_t bin = (hi - k[u]) >> shift;
-                atomicAdd(&lds.count[bin], 1u);
-                atomicAdd(&lds.mass[bin], (unsigned long long)weight<F>(a, r, lds.table, k[u]));
+                const int32_t at = place_of((int32_t)((hi - k[u]) >> shift));
+                atomicAdd(&lds.count[at], 1u);
+                atomicAdd(&lds.mass[at], (unsigned long long)weight<F>(r, lds.table, k[u]));
             }
         }
         __syncthreads();
@@ -767,12 +783,12 @@ __device__ __forceinline__ Cut cut_row(const SampleArgs& a, const Row& r, const 
         hi = hi - (bin << shift);
         lo = max(lo, hi - ((1u << shift) - 1));
         if (shift == 0) {
-            ties = lds.count[bin];
+            ties = lds.count[place_of((int32_t)bin)];
             break;
         }
     }
     // the words at key lo: how many are kept, and which is the last
-    const int64_t w = weight<F>(a, r, lds.table, lo);
+    const int64_t w = weight<F>(r, lds.table, lo);
     int64_t keep;
     if (MASS) {
         int64_t l = 1, h = ties;
@@ -826,8 +842,8 @@ __device__ __forceinline__ int32_t draw_word(const SampleArgs& a, const Row& r, 
         if (i >= i1) return 0;
         const uint32_t k = ws.key(i);
         if (!cut.keeps(k, ws.index(i))) return 0;
-        const int64_t w = weight<F>(a, r, lds.table, k);
-        return (double)w >= r.floor ? w : 0;
+        const int64_t w = weight<F>(r, lds.table, k);
+        return w >= r.floor ? w : 0;
     };
     int64_t s = 0;
 #pragma unroll 4
@@ -897,14 +913,15 @@ __device__ __forceinline__ int32_t draw_by_segments(const SampleArgs& a, const R
         bool done = false;
 #pragma unroll 1
         for (int j0 = 0; j0 < kSeg / 64 && !done; j0 += 8) {
-            uint32_t k[8];
-            load_unit<F>(a, x, i0 + 64 * j0 + lane, k);
+            typename F::V v8[8];
+            load_words<F>(a, x, i0 + 64 * j0, i0 + 64 * j0 + lane, v8);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 if (done) continue;
                 const int32_t i = i0 + 64 * (j0 + j) + lane;
-                int64_t c = cut.keeps(k[j], (uint32_t)i) ? weight<F>(a, r, lds.table, k[j]) : 0;
-                if (!((double)c >= r.floor)) c = 0;
+                const uint32_t k = F::key(v8[j]);
+                int64_t c = cut.keeps(k, (uint32_t)i) ? weight<F>(r, lds.table, k) : 0;
+                if (c < r.floor) c = 0;
 #pragma unroll
                 for (int o = 1; o < 64; o <<= 1) {
                     const int64_t v = __shfl_up(c, o);
@@ -989,11 +1006,11 @@ __device__ __forceinline__ int32_t draw_few(const SampleArgs& a, const Row& r, D
     order_words(lds.near, n, lds.near + kNear);
     __syncthreads();
     const uint64_t word = e < n ? lds.near[kNear + e] : 0;
-    const int64_t w = e < n && (r.k == 0 || e < r.k) ? weight<F>(a, r, lds.table, key_of(word)) : 0;
+    const int64_t w = e < n && (r.k == 0 || e < r.k) ? weight<F>(r, lds.table, key_of(word)) : 0;
     int64_t total;
     const int64_t before = block_scan<kDrawWaves>(w, &total, lds.wave64);
     if (mass < 0.0) mass = r.p * (double)total;
-    const bool kept = (r.p >= 1.0 || e == 0 || (double)before < mass) && (double)w >= r.floor;
+    const bool kept = (r.p >= 1.0 || e == 0 || (double)before < mass) && w >= r.floor;
     const int64_t kw = kept ? w : 0;
     lds.mass[e] = (unsigned long long)kw;
     block_scan<kDrawWaves>(kw, &total, lds.wave64);
@@ -1014,6 +1031,8 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs
     __shared__ DrawLds lds;
     const int tid = threadIdx.x;
     const int64_t m = blockIdx.x, row = row0 + m;
+    Lists lists;  // under way from the start
+    lists.load(a, m, 0);
     Row r = row_of(a, row);
     const double u0 = (double)a.u[row], u = u0 > 0.0 ? fmin(u0, 1.0) : 0.0;
     const uint2 info = row_info(a, m);
@@ -1043,7 +1062,7 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs
         target = f.target;
         const RowWork& work = a.work[m];
         const int n = (int)min(work.found, (uint32_t)0x7fffffff);
-        const bool gathered = r.k > 0 || f.p1 >= bin_of<F>(a, r, bound);
+        const bool gathered = r.k > 0 || f.p1 >= bin_of<F>(r, bound);
         if (gathered && n <= kGather && a.segs <= kBins) {
             for (int i = tid; i < n; i += kDrawThreads)
                 lds.word[i] = order(work.near[i].x, work.near[i].y);
@@ -1059,7 +1078,7 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs
             } else if (r.k > 0) {
                 // words of bin k come last
                 for (int i = tid; i < n; i += kDrawThreads)
-                    if (bin_of<F>(a, r, key_of(lds.word[i])) < f.k) atomicAdd(&lds.sel[2], 1u);
+                    if (bin_of<F>(r, key_of(lds.word[i])) < f.k) atomicAdd(&lds.sel[2], 1u);
                 __syncthreads();
                 const int s = (int)lds.sel[2];
                 cut = cut_in_order<F, false>(a, r, lds, sorted + s, n - s, f.k_mass, r.k - f.k_count,
@@ -1072,8 +1091,8 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs
             for (int i = tid; i < n; i += kDrawThreads) {
                 const uint32_t k = key_of(lds.word[i]), at = (uint32_t)lds.word[i];
                 if (!cut.keeps(k, at)) continue;
-                const int64_t w = weight<F>(a, r, lds.table, k);
-                if ((double)w >= r.floor) atomicAdd(&lds.mass[at / kSeg], (unsigned long long)w);
+                const int64_t w = weight<F>(r, lds.table, k);
+                if (w >= r.floor) atomicAdd(&lds.mass[at / kSeg], (unsigned long long)w);
             }
             __syncthreads();
             const int32_t tok = draw_by_segments<F>(a, r, x, lds, cut, u,
@@ -1083,8 +1102,6 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs
         }
     }
 
-    Lists lists;
-    lists.load(a, m, 0);
     const int64_t n = store_lists(a, m, bound, lists, lds);
     bool listed = n > 0 && n <= kEntries && n >= r.k;
     if (listed) {
@@ -1096,11 +1113,11 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs
         int64_t s = 0, all;
         for (int i = tid; i < n; i += kDrawThreads) {
             const uint32_t k = key_of(lds.word[i]);
-            const int32_t bin = bin_of<F>(a, r, k);
-            const int64_t w = weight<F>(a, r, lds.table, k);
+            const int32_t at = place_of(bin_of<F>(r, k));
+            const int64_t w = weight<F>(r, lds.table, k);
             s += w;
-            atomicAdd(&lds.count[bin], 1u);
-            atomicAdd(&lds.mass[bin], (unsigned long long)w);
+            atomicAdd(&lds.count[at], 1u);
+            atomicAdd(&lds.mass[at], (unsigned long long)w);
         }
         block_scan<kDrawWaves>(s, &all, lds.wave64);
         listed = r.k > 0 || (double)all >= target;
@@ -1120,10 +1137,10 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs
         }
         __syncthreads();
         const int32_t bin = (int32_t)lds.sel[0];
-        const int64_t count = lds.sel64[0] + lds.count[bin];
+        const int64_t count = lds.sel64[0] + lds.count[place_of(bin)];
         if (count <= kNear) {
             for (int i = tid; i < n; i += kDrawThreads)
-                if (bin_of<F>(a, r, key_of(lds.word[i])) <= bin)
+                if (bin_of<F>(r, key_of(lds.word[i])) <= bin)
                     lds.near[atomicAdd(&lds.sel[1], 1u)] = lds.word[i];
             __syncthreads();
             const int32_t tok = draw_few<F>(a, r, lds, (int)count, r.k > 0 ? -1.0 : target, u);
