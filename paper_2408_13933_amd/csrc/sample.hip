@@ -21,6 +21,7 @@
 
 #include "codes.h"
 #include "mq_internal.h"
+#include "wave.h"
 
 namespace mq {
 namespace {
@@ -274,8 +275,7 @@ __global__ __launch_bounds__(256) void sample_scan_kernel(SampleArgs a, int64_t 
             pos += __popcll(hit);
         }
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    top = wave_max(top);
     if (lane == 0) {
         a.info[at] = make_uint4(top, bound, (uint32_t)pos, 0);
         a.sums[at] = 0;
@@ -300,12 +300,7 @@ __device__ inline uint2 row_info(const SampleArgs& a, int64_t m)
         top = max(top, v.x);
         bound = max(bound, v.y);
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        top = max(top, (uint32_t)__shfl_xor((int)top, o));
-        bound = max(bound, (uint32_t)__shfl_xor((int)bound, o));
-    }
-    return make_uint2(top, bound);
+    return make_uint2(wave_max(top), wave_max(bound));
 }
 
 // The sum of the values of the threads before this one, and of all.
@@ -313,12 +308,7 @@ template <int WAVES>
 __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* total, int64_t* lds)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t s = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int64_t t = __shfl_up(s, o);
-        if (lane >= o) s += t;
-    }
+    const int64_t s = wave_scan(v);
     __syncthreads();
     if (lane == 63) lds[wave] = s;
     __syncthreads();
@@ -380,8 +370,7 @@ __global__ __launch_bounds__(256) void sample_sums_kernel(SampleArgs a, int64_t 
             }
         }
         if (bins) continue;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+        s = wave_sum(s);
         const int32_t at = first + n * kUnit;
         if (lane == 0 && at < a.V)
             atomicAdd(reinterpret_cast<unsigned long long*>(&a.sums[m * a.segs + at / kSeg]),
@@ -422,34 +411,22 @@ __device__ inline Found find_bin(const uint32_t* count, const unsigned long long
         n += count[64 * i + lane];
         w += (int64_t)mass[64 * i + lane];
     }
-    auto scan = [=](int64_t& a, int64_t& b) {
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int64_t t = __shfl_up(a, o), v = __shfl_up(b, o);
-            if (lane >= o) {
-                a += t;
-                b += v;
-            }
-        }
-    };
-    int64_t ns = n, ws = w;
-    scan(ns, ws);
+    const int64_t ns = wave_scan(n), ws = wave_scan(w);
     Found f;
-    f.total = __shfl(ws, 63);
+    f.total = wave_read(ws, 63);
     // the first lane that reaches the target, or the last with anything; then
     // the same among its bins
     const uint64_t hit = __ballot(reaches(ns, ws)), some = __ballot(n > 0);
     const int l = hit ? __builtin_ctzll(hit) : some ? 63 - __builtin_clzll(some) : 0;
-    const int64_t nb = __shfl(ns - n, l), mb = __shfl(ws - w, l);
+    const int64_t nb = wave_read(ns - n, l), mb = wave_read(ws - w, l);
     const int64_t c = lane < 16 ? count[64 * lane + l] : 0;
     const int64_t v = lane < 16 ? (int64_t)mass[64 * lane + l] : 0;
-    int64_t cs = c, vs = v;
-    scan(cs, vs);
+    const int64_t cs = wave_scan(c), vs = wave_scan(v);
     const uint64_t have = __ballot(c > 0), in = __ballot(c > 0 && reaches(nb + cs, mb + vs));
     const int i = in ? __builtin_ctzll(in) : have ? 63 - __builtin_clzll(have) : 0;
     f.bin = 16 * l + i;
-    f.count = nb + __shfl(cs - c, i);
-    f.mass = mb + __shfl(vs - v, i);
+    f.count = nb + wave_read(cs - c, i);
+    f.mass = mb + wave_read(vs - v, i);
     return f;
 }
 
@@ -581,8 +558,7 @@ __global__ __launch_bounds__(256) void sample_gather_kernel(SampleArgs a, int64_
             mine |= (uint32_t)here << j;
             cnt += __popcll(__ballot(here));
         }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+        s = wave_sum(s);
         if (lane == 0 && s)
             atomicAdd(reinterpret_cast<unsigned long long*>(&a.sums[m * a.segs + i0 / kSeg]),
                       (unsigned long long)s);
@@ -660,11 +636,7 @@ __device__ __forceinline__ Cut cut_in_order(const SampleArgs& a, const Row& r, D
         for (int e0 = 0; e0 < n; e0 += 64) {
             const uint64_t w = e0 + lane < n ? word[e0 + lane] : ~0ull;
             int64_t c = weight<F>(r, lds.table, key_of(w));
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int64_t v = __shfl_up(c, o);
-                if (lane >= o) c += v;
-            }
+            c = wave_scan(c);
             // the last word is kept in any case that gets that far
             const bool here = MASS ? (double)(run + c) >= target : e0 + lane + 1 >= keep;
             const uint64_t hit = __ballot(e0 + lane < n && (here || e0 + lane == n - 1));
@@ -676,7 +648,7 @@ __device__ __forceinline__ Cut cut_in_order(const SampleArgs& a, const Row& r, D
                 }
                 break;
             }
-            run += __shfl(c, 63);
+            run += wave_read(c, 63);
         }
     }
     __syncthreads();
@@ -848,8 +820,7 @@ __device__ __forceinline__ int32_t draw_word(const SampleArgs& a, const Row& r, 
     int64_t s = 0;
 #pragma unroll 4
     for (int32_t i = i0; i < i1; i += 64) s += kept(i + lane);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    s = wave_sum(s);
     __syncthreads();
     if (lane == 0) lds.wave64[wave] = s;
     __syncthreads();
@@ -865,17 +836,13 @@ __device__ __forceinline__ int32_t draw_word(const SampleArgs& a, const Row& r, 
         int64_t run = before;
         for (int32_t i = i0; i < i1; i += 64) {
             int64_t c = kept(i + lane);
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int64_t v = __shfl_up(c, o);
-                if (lane >= o) c += v;
-            }
+            c = wave_scan(c);
             const uint64_t hit = __ballot(run + c > target);
             if (hit) {
                 if (lane == __builtin_ctzll(hit)) lds.sel[0] = ws.index(i + lane);
                 break;
             }
-            run += __shfl(c, 63);
+            run += wave_read(c, 63);
         }
     }
     __syncthreads();
@@ -922,17 +889,13 @@ __device__ __forceinline__ int32_t draw_by_segments(const SampleArgs& a, const R
                 const uint32_t k = F::key(v8[j]);
                 int64_t c = cut.keeps(k, (uint32_t)i) ? weight<F>(r, lds.table, k) : 0;
                 if (c < r.floor) c = 0;
-#pragma unroll
-                for (int o = 1; o < 64; o <<= 1) {
-                    const int64_t v = __shfl_up(c, o);
-                    if (lane >= o) c += v;
-                }
+                c = wave_scan(c);
                 const uint64_t hit = __ballot(run + c > target);
                 if (hit) {
                     if (lane == __builtin_ctzll(hit)) lds.sel[0] = (uint32_t)i;
                     done = true;
                 }
-                run += __shfl(c, 63);
+                run += wave_read(c, 63);
             }
         }
     }
@@ -941,7 +904,7 @@ __device__ __forceinline__ int32_t draw_by_segments(const SampleArgs& a, const R
 }
 
 // A wave's lists of one turn, all loads under way at once.
-constexpr int kTurn = 8;
+constexpr int kTurn = 16;
 struct Lists {
     uint2 e[kTurn];
     uint32_t n[kTurn];
@@ -1033,9 +996,9 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs
     const int64_t m = blockIdx.x, row = row0 + m;
     Lists lists;  // under way from the start
     lists.load(a, m, 0);
+    const uint2 info = row_info(a, m);
     Row r = row_of(a, row);
     const double u0 = (double)a.u[row], u = u0 > 0.0 ? fmin(u0, 1.0) : 0.0;
-    const uint2 info = row_info(a, m);
     const uint32_t bound = info.y;
     if (info.x == 0) {  // nothing can be drawn
         if (tid == 0) a.tokens[row] = -1;
