@@ -610,14 +610,21 @@ struct Cut {
     __device__ bool keeps(uint32_t k, uint32_t i) const { return k > key || (k == key && i <= idx); }
 };
 
-// n words in LDS put in order (dst): each counts those before it.
+// n words in LDS put in order (dst): each counts those before it, eight reads
+// under way at once.
 __device__ __forceinline__ void order_words(const uint64_t* src, int n, uint64_t* dst)
 {
     for (int e = threadIdx.x; e < n; e += kDrawThreads) {
         const uint64_t w = src[e];
-        int rank = 0;
-#pragma unroll 8
-        for (int o = 0; o < n; ++o) rank += src[o] < w;
+        int rank = 0, o = 0;
+        for (; o + 8 <= n; o += 8) {
+            uint64_t t[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = src[o + i];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rank += t[i] < w;
+        }
+        for (; o < n; ++o) rank += src[o] < w;
         dst[rank] = w;
     }
 }
@@ -907,20 +914,22 @@ __device__ __forceinline__ int32_t draw_by_segments(const SampleArgs& a, const R
 constexpr int kTurn = 16;
 struct Lists {
     uint2 e[kTurn];
-    uint32_t n[kTurn];
+    uint32_t n;  // lane i: of list i
     __device__ __forceinline__ void load(const SampleArgs& a, int64_t m, int s0)
     {
         const int lane = threadIdx.x & 63, first = s0 + (threadIdx.x >> 6) * kTurn;
+        n = a.info[m * a.segs + min(first + (lane & (kTurn - 1)), a.segs - 1)].z;
 #pragma unroll
         for (int i = 0; i < kTurn; ++i) {
             const int64_t s = m * a.segs + min(first + i, a.segs - 1);
             e[i] = a.list[s * kList + lane];  // places past the list's words: anything
-            n[i] = first + i < a.segs ? a.info[s].z : 0;
         }
+        if (first + (lane & (kTurn - 1)) >= a.segs) n = 0;
     }
     __device__ __forceinline__ bool has(int i, uint32_t bound) const
     {
-        return (threadIdx.x & 63) < n[i] && e[i].x >= bound;
+        return (threadIdx.x & 63) < (uint32_t)__builtin_amdgcn_readlane((int)n, i) &&
+               e[i].x >= bound;
     }
 };
 
@@ -980,9 +989,17 @@ __device__ __forceinline__ int32_t draw_few(const SampleArgs& a, const Row& r, D
     const int64_t target = min((int64_t)(u * (double)total), total - 1);
     // the kept weight of the words before this one in index order
     int64_t run = 0;
-#pragma unroll 8
-    for (int o = 0; o < n; ++o)
-        run += (uint32_t)lds.near[kNear + o] < (uint32_t)word ? (int64_t)lds.mass[o] : 0;
+    for (int o = 0; o < n; o += 8) {  // (past n the weights are 0)
+        uint32_t idx[8];
+        int64_t kw8[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            idx[i] = (uint32_t)lds.near[kNear + o + i];
+            kw8[i] = (int64_t)lds.mass[o + i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) run += idx[i] < (uint32_t)word ? kw8[i] : 0;
+    }
     if (kw > 0 && target >= run && target < run + kw) lds.sel[0] = (uint32_t)word;
     __syncthreads();
     return (int32_t)lds.sel[0];
