@@ -584,9 +584,7 @@ __global__ __launch_bounds__(256) void sample_gather_kernel(SampleArgs a, int64_
 struct DrawLds {
     uint32_t count[kBins];
     unsigned long long mass[kBins];
-    // listed words, as order() has them; gathered ones and, past kGather, the
-    // same in order
-    uint64_t word[kEntries];
+    uint64_t word[kEntries];  // listed or gathered words, as order() has them
     uint64_t near[2 * kNear];
     int64_t wave64[kDrawWaves];
     int32_t wave32[kDrawWaves];
@@ -706,6 +704,60 @@ __device__ __forceinline__ bool cut_listed(const SampleArgs& a, const Row& r, Dr
     __syncthreads();
     order_words(lds.near, near, lds.near + kNear);
     cut = cut_in_order<F, MASS>(a, r, lds, lds.near + kNear, near, mass, keep - count, target);
+    return true;
+}
+
+// The cut among n words in LDS that lie in bins [b0, b1], by finer bins; so
+// many words and so much mass come before them.  False if too many share the
+// finer bin.
+template <class F, bool MASS>
+__device__ __forceinline__ bool cut_gathered(const SampleArgs& a, const Row& r, DrawLds& lds, int n,
+                                             int b0, int b1, int64_t count, int64_t mass,
+                                             int64_t keep, double target, Cut& cut)
+{
+    const double fine = (double)kBins / (double)(b1 - b0 + 1);
+    // -1: not one of them
+    auto sub_bin = [&](uint32_t k) {
+        const double z = distance(r, F::of_key(k));
+        const int32_t b = bin_at(z);
+        if (b < b0 || b > b1) return -1;
+        return min(max((int32_t)((z * kBinScale - (double)b0) * fine), 0), kBins - 1);
+    };
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += kDrawThreads) {
+        lds.count[i] = 0;
+        lds.mass[i] = 0;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kDrawThreads) {
+        const uint32_t k = key_of(lds.word[i]);
+        const int32_t b = sub_bin(k);
+        if (b < 0) continue;
+        atomicAdd(&lds.count[place_of(b)], 1u);
+        atomicAdd(&lds.mass[place_of(b)], (unsigned long long)weight<F>(r, lds.table, k));
+    }
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        const Found f = find_bin(lds.count, lds.mass, [=](int64_t c, int64_t w) {
+            return MASS ? (double)(mass + w) >= target : count + c >= keep;
+        });
+        if (threadIdx.x == 0) {
+            lds.sel[0] = (uint32_t)f.bin;
+            lds.sel[1] = 0;
+            lds.sel64[0] = count + f.count;
+            lds.sel64[1] = mass + f.mass;
+        }
+    }
+    __syncthreads();
+    const int32_t bin = (int32_t)lds.sel[0];
+    const int64_t c0 = lds.sel64[0], m0 = lds.sel64[1];
+    const int near = (int)lds.count[place_of(bin)];
+    if (near > kNear) return false;
+    for (int i = threadIdx.x; i < n; i += kDrawThreads)
+        if (sub_bin(key_of(lds.word[i])) == bin) lds.near[atomicAdd(&lds.sel[1], 1u)] = lds.word[i];
+    __syncthreads();
+    order_words(lds.near, near, lds.near + kNear);
+    cut = cut_in_order<F, MASS>(a, r, lds, lds.near + kNear, near, m0, keep - c0, target);
     return true;
 }
 
@@ -1043,31 +1095,27 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs
         const RowWork& work = a.work[m];
         const int n = (int)min(work.found, (uint32_t)0x7fffffff);
         const bool gathered = r.k > 0 || f.p1 >= bin_of<F>(r, bound);
-        if (gathered && n <= kGather && a.segs <= kBins) {
+        bool found = gathered && n <= kGather && a.segs <= kBins;
+        if (found) {
             for (int i = tid; i < n; i += kDrawThreads)
                 lds.word[i] = order(work.near[i].x, work.near[i].y);
-            for (int i = tid; i < a.segs; i += kDrawThreads)
-                lds.mass[i] = (unsigned long long)sums[i];
-            if (tid == 0) lds.sel[2] = 0;
-            __syncthreads();
-            const uint64_t* sorted = lds.word + kGather;
-            order_words(lds.word, n, lds.word + kGather);
             double mass = target;
             if (r.k > 0 && f.k == kBins) {  // fewer than k have a weight
                 mass = r.p * (double)f.k_mass;
             } else if (r.k > 0) {
-                // words of bin k come last
-                for (int i = tid; i < n; i += kDrawThreads)
-                    if (bin_of<F>(r, key_of(lds.word[i])) < f.k) atomicAdd(&lds.sel[2], 1u);
-                __syncthreads();
-                const int s = (int)lds.sel[2];
-                cut = cut_in_order<F, false>(a, r, lds, sorted + s, n - s, f.k_mass, r.k - f.k_count,
-                                             0.0);
+                found = cut_gathered<F, false>(a, r, lds, n, f.k, f.k, f.k_count, f.k_mass, r.k, 0.0,
+                                               cut);
                 mass = r.p * (double)cut.mass;
             }
-            if (r.p < 1.0)
-                cut = cut_in_order<F, true>(a, r, lds, sorted, n, f.p_mass, 0, mass);
-            // the kept ones of these words join their segments' sums
+            if (found && r.p < 1.0)
+                found = cut_gathered<F, true>(a, r, lds, n, f.p0, f.p1, 0, f.p_mass, 0, mass, cut);
+        }
+        if (found) {
+            // the segments' sums, which the kept ones of these words join
+            __syncthreads();
+            for (int i = tid; i < a.segs; i += kDrawThreads)
+                lds.mass[i] = (unsigned long long)sums[i];
+            __syncthreads();
             for (int i = tid; i < n; i += kDrawThreads) {
                 const uint32_t k = key_of(lds.word[i]), at = (uint32_t)lds.word[i];
                 if (!cut.keeps(k, at)) continue;
@@ -1080,6 +1128,8 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs
             if (tid == 0) a.tokens[row] = tok;
             return;
         }
+        cut = Cut{1, 0xffffffffu, 0};
+        __syncthreads();
     }
 
     const int64_t n = store_lists(a, m, bound, lists, lds);
@@ -1168,9 +1218,10 @@ hipError_t launch(SampleArgs a, int64_t M, char* ws, int64_t ws_bytes, hipStream
         a.sums = reinterpret_cast<int64_t*>(ws + n * (sizeof(RowWork) + a.segs * (16 + 8 * kList)));
         const dim3 g((unsigned)((a.segs + 3) / 4), (unsigned)n);
         sample_scan_kernel<F><<<g, 256, 0, s>>>(a, m0);
-        // a unit per wave, a segment or four of them where that fills the chip
-        // (each work-group adds its bins to the row's)
-        const int units = n * a.segs >= 32768 ? 4 * kSeg / kUnit : n * a.segs >= 8192 ? kSeg / kUnit : 1;
+        // a wave per segment where that fills the chip (each work-group adds its
+        // bins to the row's), else per unit.  512 rows of 256000, a fifth of
+        // them with sums: 4 units 37 us, 8 45, 16 62
+        const int units = n * a.segs >= 8192 ? kSeg / kUnit : 1;
         const dim3 gu((unsigned)((a.V + 4 * units * kUnit - 1) / (4 * units * kUnit)), (unsigned)n);
         sample_sums_kernel<F><<<gu, 256, 0, s>>>(a, m0, units);
         if (a.top_p || a.top_k) sample_gather_kernel<F><<<gu, 256, 0, s>>>(a, m0, units);
