@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 __all__ = [
     "MQError", "lib", "lib_path", "mq_version", "mq_act_params", "mq_fold_weights",
@@ -22,7 +23,7 @@ __all__ = [
     "PATH_AUTO", "PATH_DECODE", "PATH_PREFILL", "PATH_GENERIC", "MAX_K",
     "PATH_PREFILL_TILE0", "PREFILL_TILES", "prefill_tile_path", "mq_probe_read",
     "mq_qlinear_group", "MAX_GROUP", "QLinearOut", "mq_qlinear_dequant",
-    "mq_rope_append", "mq_paged_attn", "mq_paged_attn_workspace_bytes", "KVCache", "KVBatch",
+    "mq_rope_append", "mq_paged_attn", "mq_paged_attn_workspace_bytes",
     "ATTN_BLOCK", "ATTN_ONE", "mq_sample", "mq_sample_workspace_bytes",
 ]
 
@@ -74,18 +75,6 @@ class QLinearOut(ctypes.Structure):
 
 
 ATTN_BLOCK, ATTN_ONE = 128, 32512  # MQ_ATTN_BLOCK, MQ_ATTN_ONE
-
-
-class KVCache(ctypes.Structure):
-    """mq_kv_cache of mq.h: a paged key/value cache."""
-    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("pages", ctypes.c_int64),
-                ("page", ctypes.c_int32), ("G", ctypes.c_int32), ("D", ctypes.c_int32)]
-
-
-class KVBatch(ctypes.Structure):
-    """mq_kv_batch of mq.h: the sequences of a call."""
-    _fields_ = [("starts", ctypes.c_void_p), ("lens", ctypes.c_void_p),
-                ("table", ctypes.c_void_p), ("B", ctypes.c_int64), ("ld", ctypes.c_int64)]
 
 
 def lib():
@@ -161,15 +150,15 @@ def lib():
                                      c_i32, c_p]
     L.mq_qlinear_group.argtypes = [c_p, c_p, c_i64, c_i64, c_i32, c_f, c_i32, c_i32,
                                    ctypes.POINTER(QLinearOut), c_i32, c_i32, c_p]
+    c_s = ctypes.c_char_p  # the bytes of mq_kv_cache and mq_kv_batch
     L.mq_rope_append.argtypes = [c_p, c_i64, c_p, c_i64, c_p, c_i64, c_i64, c_i32, c_f, c_i32, c_f,
-                                 c_i32, c_f, c_i32, c_f, c_i32, c_p, c_i64,
-                                 ctypes.POINTER(KVCache), ctypes.POINTER(KVBatch), c_p, c_i64,
+                                 c_i32, c_f, c_i32, c_f, c_i32, c_p, c_i64, c_s, c_s, c_p, c_i64,
                                  c_p]
     L.mq_paged_attn_workspace_bytes.argtypes = [c_i64, c_i64, c_i32, c_i32, c_i32, c_i64]
     L.mq_paged_attn_workspace_bytes.restype = c_i64
-    L.mq_paged_attn.argtypes = [c_p, c_i64, c_i64, c_i32, c_f, c_i32, ctypes.POINTER(KVCache), c_f,
-                                c_f, c_i32, ctypes.POINTER(KVBatch), c_f, c_i64, c_i64, c_f, c_i32,
-                                c_i32, c_p, c_i64, c_i64, c_p, c_i64, c_p]
+    L.mq_paged_attn.argtypes = [c_p, c_i64, c_i64, c_i32, c_f, c_i32, c_s, c_f, c_f, c_i32, c_s,
+                                c_f, c_i64, c_i64, c_f, c_i32, c_i32, c_p, c_i64, c_i64, c_p,
+                                c_i64, c_p]
     L.mq_sample_workspace_bytes.argtypes = [c_i64, c_i64]
     L.mq_sample_workspace_bytes.restype = c_i64
     L.mq_sample.argtypes = [c_p, c_i32, c_i64, c_i64, c_i64, c_f, c_i32, c_p, c_p, c_p, c_p, c_p,
@@ -872,38 +861,78 @@ def mq_probe_read(buf, blocks: int, waves: int, unroll: int = 8, sink=None, stre
     return sink
 
 
-def _rows(t, dtype, name, shape=None):
+# The calls of a generated token are as small as the kernels behind them, so
+# these helpers look at each tensor once and build no ctypes objects (append
+# for one token: 11.8 us on the host with them, 7 without; the launch alone
+# takes 4).
+_KV_CACHE, _KV_BATCH = struct.Struct("qqqiiixxxx"), struct.Struct("qqqqq")
+
+
+def _device_and_stream(t, name, stream):
+    """The device of the call's tensors, which has to be the current one, and
+    the handle of the stream to use."""
+    torch = _torch_mod or _torch()
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    dev = t.get_device()
+    if dev != torch.cuda.current_device() if _get_device is None else dev != _get_device():
+        raise ValueError(f"{name} must be on the current device")
+    if stream is None and _get_raw_stream is not None:
+        return dev, _get_raw_stream(dev)
+    if stream is not None and stream.device_index != dev:
+        raise ValueError("stream must be one of the tensors' device")
+    return dev, _stream_ptr(stream)
+
+
+def _flat(t, dtype, dev, name, shape):
+    """Pointer of a contiguous tensor of a shape on the call's device."""
+    if not isinstance(t, _torch_mod.Tensor) or t.get_device() != dev:
+        raise ValueError(f"{name} must be a GPU tensor on the same device")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _rows(t, dtype, dev, name, shape):
     """Pointer and row stride (elements) of a [rows][cols] view whose rows are
     contiguous."""
-    if not isinstance(t, (_torch_mod or _torch()).Tensor) or not t.is_cuda:
-        raise ValueError(f"{name} must be a GPU tensor")
-    if t.dtype != dtype:
+    if not isinstance(t, _torch_mod.Tensor) or t.get_device() != dev:
+        raise ValueError(f"{name} must be a GPU tensor on the same device")
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must be a 2-d view with contiguous rows")
-    if shape is not None and tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
-    rows, cols = t.shape
-    ld = t.stride(0) if rows > 1 else cols
-    if ld < cols:
-        raise ValueError(f"{name} must have rows that do not overlap")
+    rows, cols = shape
+    ld, step = t.stride()
+    if rows <= 1:
+        ld = cols
+    if (cols > 1 and step != 1) or ld < cols:
+        raise ValueError(f"{name} must be a view of contiguous rows that do not overlap")
     return t.data_ptr(), ld
 
 
-def _kv_args(k_cache, v_cache, starts, lens, pages):
-    """(KVCache, KVBatch) of the cache tensors k [pages][G][page][D], v
-    [pages][G][D][page] and the batch's int32 tensors."""
-    torch = _torch_mod or _torch()
-    if k_cache.dim() != 4 or lens.dim() != 1 or pages.dim() != 2:
-        raise ValueError("k_cache must be [pages][G][page][D], lens [B], pages [B][entries]")
+def _kv_args(dev, k_cache, v_cache, starts, lens, pages):
+    """The bytes of mq_kv_cache and mq_kv_batch for the cache tensors k
+    [pages][G][page][D], v [pages][G][D][page] and the batch's int32 tensors,
+    and (G, D, B, keys that a page list holds)."""
+    i8, i32 = _torch_mod.int8, _torch_mod.int32
     n, G, page, D = k_cache.shape
-    B = lens.shape[0]
-    c = KVCache(_dev_ptr(k_cache, torch.int8, "k_cache"),
-                _dev_ptr(v_cache, torch.int8, "v_cache", (n, G, D, page)), n, page, G, D)
-    b = KVBatch(_dev_ptr(starts, torch.int32, "starts", (B + 1,)),
-                _dev_ptr(lens, torch.int32, "lens"),
-                _dev_ptr(pages, torch.int32, "pages", (B, pages.shape[1])), B, pages.shape[1])
-    return c, b
+    B, ld = pages.shape
+    c = _KV_CACHE.pack(_flat(k_cache, i8, dev, "k_cache", (n, G, page, D)),
+                       _flat(v_cache, i8, dev, "v_cache", (n, G, D, page)), n, page, G, D)
+    b = _KV_BATCH.pack(_flat(starts, i32, dev, "starts", (B + 1,)),
+                       _flat(lens, i32, dev, "lens", (B,)),
+                       _flat(pages, i32, dev, "pages", (B, ld)), B, ld)
+    return c, b, (G, D, B, ld * page)
+
+
+def _kv_shapes(q, k_cache, pages):
+    if k_cache.dim() != 4 or pages.dim() != 2 or q.dim() != 2:
+        raise ValueError("k_cache must be [pages][G][page][D], pages [B][entries], q [T][H * D]")
 
 
 def mq_rope_append(q, k, v, aq: float, zq: int, aqo: float, zqo: int, ak: float, zk: int,
@@ -918,23 +947,24 @@ def mq_rope_append(q, k, v, aq: float, zq: int, aqo: float, zqo: int, ak: float,
     (these tokens included) with page list pages[b].  table: fp64 angles of
     mq_rope_table from position 0 on (positions * D values), or None for no
     rotation."""
-    torch = _torch_mod or _torch()
-    c, b = _kv_args(k_cache, v_cache, starts, lens, pages)
-    T, HD = q.shape
-    D = c.D
+    _kv_shapes(q, k_cache, pages)
+    dev, st = _device_and_stream(q, "q", stream)
+    torch = _torch_mod
+    c, b, (G, D, _, _) = _kv_args(dev, k_cache, v_cache, starts, lens, pages)
+    shape = T, HD = q.shape
     H = HD // D
     if H * D != HD:
         raise ValueError("q's row length must be heads * D")
-    out = torch.empty((T, HD), dtype=torch.int16, device=q.device) if out is None else out
-    pq, ldq = _rows(q, torch.int16, "q")
-    pk, ldk = _rows(k, torch.int16, "k", (T, c.G * D))
-    pv, ldv = _rows(v, torch.int8, "v", (T, c.G * D))
-    po, ldo = _rows(out, torch.int16, "out", (T, HD))
-    ptab = None if table is None else _dev_ptr(table, torch.float64, "table")
-    positions = 0 if table is None else table.numel() // D
-    _check(lib().mq_rope_append(pq, ldq, pk, ldk, pv, ldv, T, H, aq, zq, aqo, zqo, ak, zk, ako,
-                                zko, ptab, positions, ctypes.byref(c), ctypes.byref(b), po, ldo,
-                                _stream_ptr(stream)), "mq_rope_append")
+    i16 = torch.int16
+    out = torch.empty((T, HD), dtype=i16, device=q.device) if out is None else out
+    ptab, positions = None, 0
+    if table is not None:
+        positions = table.numel() // D
+        ptab = _flat(table, torch.float64, dev, "table", table.shape)
+    _check(lib().mq_rope_append(*_rows(q, i16, dev, "q", shape), *_rows(k, i16, dev, "k", (T, G * D)),
+                                *_rows(v, torch.int8, dev, "v", (T, G * D)), T, H, aq, zq, aqo, zqo,
+                                ak, zk, ako, zko, ptab, positions, c, b,
+                                *_rows(out, i16, dev, "out", shape), st), "mq_rope_append")
     return out
 
 
@@ -957,25 +987,25 @@ def mq_paged_attn(q, q_scale: float, q_zp: int, k_cache, k_scale: float, v_cache
     the last ``window`` of them and the first ``sinks``.  max_len: the longest
     sequence as far as the caller knows (0: what the page list holds).
     workspace: a uint8 tensor kept by the caller (allocated here if None)."""
-    torch = _torch_mod or _torch()
-    c, b = _kv_args(k_cache, v_cache, starts, lens, pages)
-    T, HD = q.shape
-    D = c.D
+    _kv_shapes(q, k_cache, pages)
+    dev, st = _device_and_stream(q, "q", stream)
+    torch = _torch_mod
+    c, b, (G, D, B, keys) = _kv_args(dev, k_cache, v_cache, starts, lens, pages)
+    shape = T, HD = q.shape
     H = HD // D
     if H * D != HD:
         raise ValueError("q's row length must be heads * D")
     odt = _act_dtype(out_bits)
     out = torch.empty((T, HD), dtype=odt, device=q.device) if out is None else out
-    pq, ldq = _rows(q, torch.int16, "q")
-    po, ldo = _rows(out, odt, "out", (T, HD))
     if workspace is None:
-        n = lib().mq_paged_attn_workspace_bytes(T, b.B, H, c.G, D, max_len or b.ld * c.page)
+        n = lib().mq_paged_attn_workspace_bytes(T, B, H, G, D, max_len or keys)
         workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n > 0 else None
-    ws, ws_bytes = _workspace_args(workspace)
-    _check(lib().mq_paged_attn(pq, ldq, T, H, q_scale, q_zp, ctypes.byref(c), k_scale, v_scale,
-                               v_zp, ctypes.byref(b), logit_scale, window, sinks, out_scale,
-                               out_zp, out_bits, po, ldo, max_len, ws, ws_bytes,
-                               _stream_ptr(stream)), "mq_paged_attn")
+    ws, ws_bytes = (None, 0) if workspace is None else \
+        (_flat(workspace, torch.uint8, dev, "workspace", workspace.shape), workspace.numel())
+    _check(lib().mq_paged_attn(*_rows(q, torch.int16, dev, "q", shape), T, H, q_scale, q_zp, c,
+                               k_scale, v_scale, v_zp, b, logit_scale, window, sinks, out_scale,
+                               out_zp, out_bits, *_rows(out, odt, dev, "out", shape), max_len, ws,
+                               ws_bytes, st), "mq_paged_attn")
     return out
 
 
@@ -993,25 +1023,28 @@ def mq_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, a
     format (alpha, zp)) and random numbers u fp32 [M] in [0, 1), with
     per-row settings (fp32 [M], top_k int32 [M]) or None for off.
     workspace: a uint8 tensor kept by the caller (allocated here if None)."""
-    torch = _torch_mod or _torch()
-    bits = {torch.float32: 32, torch.int16: 16}.get(getattr(logits, "dtype", None))
-    if bits is None:
-        raise ValueError("logits must be float32 or int16")
-    pl, ld = _rows(logits, logits.dtype, "logits")
-    M, V = logits.shape
-    f32 = torch.float32
-    opt = [None if t is None else _dev_ptr(t, dt, name, (M,))
-           for t, dt, name in ((temperature, f32, "temperature"), (top_k, torch.int32, "top_k"),
-                               (top_p, f32, "top_p"), (min_p, f32, "min_p"))]
-    pu = _dev_ptr(u, f32, "u", (M,))
-    out = torch.empty(M, dtype=torch.int32, device=logits.device) if out is None else out
-    po = _dev_ptr(out, torch.int32, "out", (M,))
+    dev, st = _device_and_stream(logits, "logits", stream)
+    torch = _torch_mod
+    f32, i32 = torch.float32, torch.int32
+    dt = logits.dtype
+    if (dt is not f32 and dt is not torch.int16) or logits.dim() != 2:
+        raise ValueError("logits must be a float32 or int16 tensor [M][V]")
+    M, V = shape = logits.shape
+    per_row = (M,)
+    out = torch.empty(M, dtype=i32, device=logits.device) if out is None else out
     if workspace is None:
         workspace = torch.empty(mq_sample_workspace_bytes(M, V), dtype=torch.uint8,
                                 device=logits.device)
-    ws, ws_bytes = _workspace_args(workspace)
-    _check(lib().mq_sample(pl, bits, M, V, ld, alpha, zp, *opt, pu, po, ws, ws_bytes,
-                           _stream_ptr(stream)), "mq_sample")
+    ptr, ld = _rows(logits, dt, dev, "logits", shape)
+    _check(lib().mq_sample(
+        ptr, 32 if dt is f32 else 16, M, V, ld, alpha, zp,
+        None if temperature is None else _flat(temperature, f32, dev, "temperature", per_row),
+        None if top_k is None else _flat(top_k, i32, dev, "top_k", per_row),
+        None if top_p is None else _flat(top_p, f32, dev, "top_p", per_row),
+        None if min_p is None else _flat(min_p, f32, dev, "min_p", per_row),
+        _flat(u, f32, dev, "u", per_row), _flat(out, i32, dev, "out", per_row),
+        _flat(workspace, torch.uint8, dev, "workspace", workspace.shape), workspace.numel(), st),
+        "mq_sample")
     return out
 
 

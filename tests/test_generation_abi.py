@@ -1,13 +1,12 @@
 """Refusals of the text-generation entry points (paged key/value cache,
 attention over it, sampling): every invalid argument is turned away on the host before
 anything is enqueued.  No GPU is touched: the pointers are never read."""
-import ctypes
+import struct
 
 import pytest
 
 import paper_2408_13933_amd as mq
 
-P = ctypes.c_void_p
 NZ = 256  # aligned, never dereferenced
 INVALID = 1
 
@@ -15,21 +14,21 @@ INVALID = 1
 def _cache(**kw):
     a = dict(k=NZ, v=NZ, pages=8, page=16, G=2, D=64)
     a.update(kw)
-    return mq.KVCache(a["k"], a["v"], a["pages"], a["page"], a["G"], a["D"])
+    return struct.pack("qqqiii4x", a["k"] or 0, a["v"] or 0, a["pages"], a["page"], a["G"], a["D"])
 
 
 def _batch(**kw):
     a = dict(starts=NZ, lens=NZ, table=NZ, B=3, ld=4)
     a.update(kw)
-    return mq.KVBatch(a["starts"], a["lens"], a["table"], a["B"], a["ld"])
+    return struct.pack("qqqqq", a["starts"] or 0, a["lens"] or 0, a["table"] or 0, a["B"], a["ld"])
 
 
 def append(cache=None, batch=None, no_cache=False, no_batch=False, **kw):
     a = dict(q=NZ, ldq=512, k=NZ, ldk=128, v=NZ, ldv=128, T=5, H=8, aq=0.1, zq=0, aqo=0.1, zqo=0,
              ak=0.1, zk=0, ako=0.1, zko=0, angles=NZ, positions=100, q_out=NZ, ldo=512)
     a.update(kw)
-    c = None if no_cache else ctypes.byref(cache or _cache())
-    b = None if no_batch else ctypes.byref(batch or _batch())
+    c = None if no_cache else cache or _cache()
+    b = None if no_batch else batch or _batch()
     return mq.lib().mq_rope_append(a["q"], a["ldq"], a["k"], a["ldk"], a["v"], a["ldv"], a["T"],
                                    a["H"], a["aq"], a["zq"], a["aqo"], a["zqo"], a["ak"], a["zk"],
                                    a["ako"], a["zko"], a["angles"], a["positions"], c, b,
@@ -40,8 +39,8 @@ def attend(cache=None, batch=None, no_cache=False, no_batch=False, **kw):
     a = dict(q=NZ, ldq=512, T=5, H=8, qs=0.1, qz=0, ks=0.1, vs=0.1, vz=0, ls=0.125, window=0,
              sinks=0, os=0.1, oz=0, ob=8, y=NZ, ldy=512, max_len=0, ws=NZ, wsb=0)
     a.update(kw)
-    c = None if no_cache else ctypes.byref(cache or _cache())
-    b = None if no_batch else ctypes.byref(batch or _batch())
+    c = None if no_cache else cache or _cache()
+    b = None if no_batch else batch or _batch()
     return mq.lib().mq_paged_attn(a["q"], a["ldq"], a["T"], a["H"], a["qs"], a["qz"], c, a["ks"],
                                   a["vs"], a["vz"], b, a["ls"], a["window"], a["sinks"], a["os"],
                                   a["oz"], a["ob"], a["y"], a["ldy"], a["max_len"], a["ws"],
