@@ -70,19 +70,23 @@ __device__ inline int32_t row_max(int32_t m)
     return max((int32_t)b[0], (int32_t)b[1]);
 }
 
-// rint(MQ_ATTN_ONE 2^(-tau d)) for 0 <= tau d < 1000: tau d to the next 1/64
-// by the 1.5 * 2^46 shift, 2^(j/64) from the table that the wave's lanes hold
-// (lane j), a polynomial of degree 4 on the rest (|f| <= 1/128, within
-// 2.5e-15) and the last product added to 1.5 * 2^52, whose low word is then
-// the rounded weight.  14 vector instructions; the polynomial over all of
+// rint(MQ_ATTN_ONE 2^(-tau d)) + 128 for 0 <= tau d < 1000: tau d to the next
+// 1/64 by the 1.5 * 2^46 shift, 2^(j/64) from the table that the wave's lanes
+// hold (lane j), a polynomial of degree 4 on the rest (|f| <= 1/128, within
+// 2.5e-15) and the last product added to 1.5 * 2^52 + 128, whose low word is
+// then the rounded weight and 128.  The high words of the table lack j << 14,
+// which k << 14 (k = 64 n + j) adds again with the exponent n.  11 vector
+// instructions and two reads across lanes; the polynomial over all of
 // [-1/2, 1/2] (degree 10) took 18.
+constexpr int32_t kBias = 128;
 struct WeightTable {
     int lo, hi;  // MQ_ATTN_ONE * 2^(lane/64)
     __device__ void init()
     {
-        const double e = (double)MQ_ATTN_ONE * exp2_poly((double)(threadIdx.x & 63) / 64.0);
+        const int lane = threadIdx.x & 63;
+        const double e = (double)MQ_ATTN_ONE * exp2_poly((double)lane / 64.0);
         lo = (int)(uint32_t)__double_as_longlong(e);
-        hi = (int)(__double_as_longlong(e) >> 32);
+        hi = (int)(__double_as_longlong(e) >> 32) - (lane << 14);
     }
     __device__ int32_t weight(double tau, uint32_t d) const
     {
@@ -92,28 +96,25 @@ struct WeightTable {
         const double f = __builtin_fma(-tau, x, -(t - kShift));
         const int32_t k = rint_low(t);
         const int tl = __builtin_amdgcn_ds_bpermute(k << 2, lo);
-        const int th = __builtin_amdgcn_ds_bpermute(k << 2, hi) + ((k & ~63) << 14);
+        const int th = __builtin_amdgcn_ds_bpermute(k << 2, hi) + (k << 14);
         const double e = __longlong_as_double(((int64_t)th << 32) | (uint32_t)tl);
         double q = 0x1.3b2ad0385b409p-7;
         q = __builtin_fma(q, f, 0x1.c6b0c40d8c4e9p-5);
         q = __builtin_fma(q, f, 0x1.ebfbdff82ac52p-3);
         q = __builtin_fma(q, f, 0x1.62e42fefa0352p-1);
         q = __builtin_fma(q, f, 1.0);
-        return rint_low(__builtin_fma(q, e, kRintShift));
+        return rint_low(__builtin_fma(q, e, kRintShift + kBias));
     }
 };
 
-// The weights of four scores as the two byte planes of 32-bit words: w =
-// 256 hi + lo with both bytes signed (w <= 127 * 256).
+// Four weights (each with kBias) as two planes of signed bytes, w = 256 hi +
+// lo: the bias makes byte 1 the one, byte 0 less 128 the other.
 __device__ inline void pack_weights4(const int32_t* w, int& hi, int& lo)
 {
-    lo = (int)__builtin_amdgcn_perm(__builtin_amdgcn_perm((uint32_t)w[3], (uint32_t)w[2], 0x0c0c0400u),
-                                    __builtin_amdgcn_perm((uint32_t)w[1], (uint32_t)w[0], 0x0c0c0400u),
-                                    0x05040100u);
-    const uint32_t h0 = (uint32_t)w[0] + 128, h1 = (uint32_t)w[1] + 128, h2 = (uint32_t)w[2] + 128,
-                   h3 = (uint32_t)w[3] + 128;
-    hi = (int)__builtin_amdgcn_perm(__builtin_amdgcn_perm(h3, h2, 0x0c0c0501u),
-                                    __builtin_amdgcn_perm(h1, h0, 0x0c0c0501u), 0x05040100u);
+    const uint32_t p = __builtin_amdgcn_perm((uint32_t)w[1], (uint32_t)w[0], 0x05010400u);
+    const uint32_t q = __builtin_amdgcn_perm((uint32_t)w[3], (uint32_t)w[2], 0x05010400u);
+    lo = (int)(__builtin_amdgcn_perm(q, p, 0x05040100u) ^ 0x80808080u);
+    hi = (int)__builtin_amdgcn_perm(q, p, 0x07060302u);
 }
 
 // The state of a wave's 16 rows.
@@ -357,19 +358,32 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
     // scores of keys 64 h + 16 g + 4 j + i
     v4i c[2][4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 2; ++h) {
+        constexpr int J = KS <= 2 ? 4 : 2;  // tiles at once: products in flight, registers
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v4i a = zero;
+        for (int j0 = 0; j0 < 4; j0 += J) {
+            v4i kf[J][KS];
 #pragma unroll
-            for (int s = 0; s < KS; ++s) a = mfma(src.key(h, j, s), st.qh[s], a);
+            for (int j = 0; j < J; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) a[i] = (int)((uint32_t)a[i] << 8);
+                for (int s = 0; s < KS; ++s) kf[j][s] = src.key(h, j0 + j, s);
 #pragma unroll
-            for (int s = 0; s < KS; ++s) a = mfma(src.key(h, j, s), st.ql[s], a);
-            c[h][j] = a;
-            if (j & 1) __builtin_amdgcn_sched_barrier(0);  // bounds the registers
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+                    c[h][j0 + j] = mfma(kf[j][s], st.qh[s], s ? c[h][j0 + j] : zero);
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    c[h][j0 + j][i] = (int)((uint32_t)c[h][j0 + j][i] << 8);
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int j = 0; j < J; ++j) c[h][j0 + j] = mfma(kf[j][s], st.ql[s], c[h][j0 + j]);
+            __builtin_amdgcn_sched_barrier(0);  // bounds the registers
         }
+    }
     if (st.cz != 0) {
         const Source again = src.again();
 #pragma unroll
@@ -389,20 +403,26 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
     const bool mask = !full || placed != 0xff;
     uint32_t seen = 0xffffffffu;  // bit 16 h + 4 j + i
     if (mask) {
-        const int64_t first = blk * kBlk + 16 * g;
-        const int32_t hi = (int32_t)max(min(sees.hi - first, (int64_t)1000), (int64_t)-1);
-        const int32_t lo = (int32_t)max(min(sees.lo - first, (int64_t)1000), (int64_t)-1);
-        const int32_t sink = (int32_t)max(min(p.sinks - first, (int64_t)1000), (int64_t)0);
+        // of the 16 keys of a half from `first` on those below n, as bits
+        auto below = [](int64_t n, int64_t first) {
+            const int32_t k = (int32_t)max(min(n - first, (int64_t)16), (int64_t)0);
+            return (1u << k) - 1;
+        };
+        seen = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t first = blk * kBlk + 64 * h + 16 * g;
+            uint32_t bits = below(sees.hi + 1, first);
+            bits &= ~below(sees.lo + 1, first) | below(p.sinks, first);
+            if (!((placed >> (4 * h + g)) & 1)) bits = 0;
+            seen |= bits << (16 * h);
+        }
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            const int at = 64 * (i >> 4) + (i & 15);
-            if (!(at <= hi && (at > lo || at < sink))) seen &= ~(1u << i);
+            const int keep = __builtin_amdgcn_sbfe((int)seen, i, 1);  // all ones or 0
+            const int x = c[i >> 4][(i >> 2) & 3][i & 3];
+            c[i >> 4][(i >> 2) & 3][i & 3] = (x & keep) | (kNone & ~keep);
         }
-        if (!((placed >> g) & 1)) seen &= 0xffff0000u;
-        if (!((placed >> (4 + g)) & 1)) seen &= 0x0000ffffu;
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (!((seen >> i) & 1)) c[i >> 4][(i >> 2) & 3][i & 3] = kNone;
     }
     int32_t m = kNone;
 #pragma unroll
@@ -461,17 +481,33 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
         s = mfma(ones, wl[1], mfma(ones, wl[0], s));
         st.z = __builtin_fma(f, (double)s[0], st.z);
     }
+    constexpr int E = ND % 4 == 0 ? 4 : 2;  // tiles at once
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt) {
-        const v4i v0 = src.value(0, dt), v1 = src.value(1, dt);
-        v4i s = mfma(v1, wh[1], mfma(v0, wh[0], zero));
+    for (int d0 = 0; d0 < ND; d0 += E) {
+        v4i v[E][2], s[E];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = (int)((uint32_t)s[i] << 8);
-        s = mfma(v1, wl[1], mfma(v0, wl[0], s));
+        for (int e = 0; e < E; ++e) {
+            v[e][0] = src.value(0, d0 + e);
+            v[e][1] = src.value(1, d0 + e);
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            st.acc[dt][i] = __builtin_fma(f, (double)s[i], st.acc[dt][i]);
-        if (dt & 1) __builtin_amdgcn_sched_barrier(0);
+        for (int e = 0; e < E; ++e) s[e] = mfma(v[e][0], wh[0], zero);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[e] = mfma(v[e][1], wh[1], s[e]);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[e][i] = (int)((uint32_t)s[e][i] << 8);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[e] = mfma(v[e][0], wl[0], s[e]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[e] = mfma(v[e][1], wl[1], s[e]);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                st.acc[d0 + e][i] = __builtin_fma(f, (double)s[e][i], st.acc[d0 + e][i]);
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
@@ -741,9 +777,7 @@ __global__ __launch_bounds__(NW < 4 ? 256 : 64 * NW) void paged_attn_join_kernel
     if (row >= p.T * p.H) return;
     const int w = wave % NW;
     const int64_t t = row / p.H;
-    const int32_t* starts = p.kv.starts;
-    const int32_t b = find_seq(p.kv.B, t, [=](int32_t i) { return (int64_t)starts[i]; });
-    if (t < starts[b] || t >= starts[b + 1]) return;
+    if (t >= p.kv.starts[p.kv.B]) return;  // rows of no sequence
     const double* mz = p.mz + row * p.splits * 2;
     double m = (double)kNone, f[kMaxSplits / 64], z = 0.0;
 #pragma unroll
