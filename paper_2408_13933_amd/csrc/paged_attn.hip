@@ -355,33 +355,38 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
     const v4i zero = {0, 0, 0, 0};
     const v4i ones = {0x01010101, 0x01010101, 0x01010101, 0x01010101};
 
-    // scores of keys 64 h + 16 g + 4 j + i
+    // scores of keys 64 h + 16 g + 4 j + i; J of the eight tiles at once, the
+    // next ones' fragments read before these are multiplied
     v4i c[2][4];
+    {
+        constexpr int J = KS <= 2 ? 4 : 2, N = 8 / J;
+        v4i kf[2][J][KS];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        constexpr int J = KS <= 2 ? 4 : 2;  // tiles at once: products in flight, registers
+        for (int n = 0; n <= N; ++n) {
+            if (n < N) {
 #pragma unroll
-        for (int j0 = 0; j0 < 4; j0 += J) {
-            v4i kf[J][KS];
+                for (int j = 0; j < J; ++j)
 #pragma unroll
-            for (int j = 0; j < J; ++j)
-#pragma unroll
-                for (int s = 0; s < KS; ++s) kf[j][s] = src.key(h, j0 + j, s);
+                    for (int s = 0; s < KS; ++s)
+                        kf[n & 1][j][s] = src.key((n * J + j) >> 2, (n * J + j) & 3, s);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (n == 0) continue;
+            v4i hi[J], lo[J];
+            const auto& k = kf[(n - 1) & 1];
 #pragma unroll
             for (int s = 0; s < KS; ++s)
 #pragma unroll
-                for (int j = 0; j < J; ++j)
-                    c[h][j0 + j] = mfma(kf[j][s], st.qh[s], s ? c[h][j0 + j] : zero);
+                for (int j = 0; j < J; ++j) {
+                    hi[j] = mfma(k[j][s], st.qh[s], s ? hi[j] : zero);
+                    lo[j] = mfma(k[j][s], st.ql[s], s ? lo[j] : zero);
+                }
 #pragma unroll
             for (int j = 0; j < J; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    c[h][j0 + j][i] = (int)((uint32_t)c[h][j0 + j][i] << 8);
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-#pragma unroll
-                for (int j = 0; j < J; ++j) c[h][j0 + j] = mfma(kf[j][s], st.ql[s], c[h][j0 + j]);
-            __builtin_amdgcn_sched_barrier(0);  // bounds the registers
+                    c[((n - 1) * J + j) >> 2][((n - 1) * J + j) & 3][i] = (hi[j][i] << 8) + lo[j][i];
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     if (st.cz != 0) {
@@ -429,12 +434,22 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
     for (int i = 0; i < 32; ++i) m = max(m, c[i >> 4][(i >> 2) & 3][i & 3]);
     m = row_max(m);
 
-    // weights
+    // weights; the first values' fragments are read before the last of them
+    constexpr int E = ND % 4 == 0 ? 4 : 2;  // output tiles at once
+    v4i v[2][E][2];
+    auto read_values = [&](int n) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            v[n & 1][e][0] = src.value(0, n * E + e);
+            v[n & 1][e][1] = src.value(1, n * E + e);
+        }
+    };
     v4i wh[2], wl[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
+            if (h == 1 && j == 2) read_values(0);
             int32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -475,38 +490,31 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
         st.m = m_new;
     }
     {
-        v4i s = mfma(ones, wh[1], mfma(ones, wh[0], zero));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = (int)((uint32_t)s[i] << 8);
-        s = mfma(ones, wl[1], mfma(ones, wl[0], s));
-        st.z = __builtin_fma(f, (double)s[0], st.z);
+        const v4i hi = mfma(ones, wh[1], mfma(ones, wh[0], zero));
+        const v4i lo = mfma(ones, wl[1], mfma(ones, wl[0], zero));
+        st.z = __builtin_fma(f, (double)((hi[0] << 8) + lo[0]), st.z);
     }
-    constexpr int E = ND % 4 == 0 ? 4 : 2;  // tiles at once
 #pragma unroll
-    for (int d0 = 0; d0 < ND; d0 += E) {
-        v4i v[E][2], s[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            v[e][0] = src.value(0, d0 + e);
-            v[e][1] = src.value(1, d0 + e);
+    for (int n = 0; n < ND / E; ++n) {
+        if (n + 1 < ND / E) {
+            read_values(n + 1);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        const auto& x = v[n & 1];
+        v4i hi[E], lo[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) s[e] = mfma(v[e][0], wh[0], zero);
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int e = 0; e < E; ++e) s[e] = mfma(v[e][1], wh[1], s[e]);
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[e][i] = (int)((uint32_t)s[e][i] << 8);
-#pragma unroll
-        for (int e = 0; e < E; ++e) s[e] = mfma(v[e][0], wl[0], s[e]);
-#pragma unroll
-        for (int e = 0; e < E; ++e) s[e] = mfma(v[e][1], wl[1], s[e]);
+            for (int e = 0; e < E; ++e) {
+                hi[e] = mfma(x[e][h], wh[h], h ? hi[e] : zero);
+                lo[e] = mfma(x[e][h], wl[h], h ? lo[e] : zero);
+            }
 #pragma unroll
         for (int e = 0; e < E; ++e)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                st.acc[d0 + e][i] = __builtin_fma(f, (double)s[e][i], st.acc[d0 + e][i]);
+                st.acc[n * E + e][i] = __builtin_fma(f, (double)((hi[e][i] << 8) + lo[e][i]),
+                                                     st.acc[n * E + e][i]);
         __builtin_amdgcn_sched_barrier(0);
     }
 }
@@ -749,21 +757,59 @@ __global__ __launch_bounds__(256, KS <= 2 ? 2 : 1) void paged_attn_split_kernel(
     split_rows<KS, ND>(p, tile, blockIdx.y, i0, i1, blockIdx.z, lds);
 }
 
-// grid (tiles of 64 rows, G, splits); a sequence's last 16 rows or fewer are
-// split among the waves.
+// Work-groups go to the eight XCDs in turn, each with an L2 of its own: those
+// that read the same keys (a cache head's part) are given to one XCD, or to
+// 8 / n of them in turn where there are n < 8 such parts.  The tiles of an
+// XCD come heaviest first up to the middle (the last tokens of a prompt see
+// the most keys), then lightest first, so that a CU's two work-groups add up
+// to the same.
+struct Place {
+    int64_t tile;
+    int32_t part;  // g + G * split
+};
+__device__ inline Place place_of(const AttnArgs& p, int64_t id, int64_t tiles)
+{
+    const int64_t parts = (int64_t)p.kv.G * p.splits;
+    Place w;
+    int64_t n = tiles, at;
+    if (parts % 8 == 0) {
+        const int64_t slot = id >> 3;
+        w.part = (int32_t)((slot / tiles) * 8 + (id & 7));
+        at = slot % tiles;
+    } else if (8 % parts == 0) {
+        const int64_t r = 8 / parts;
+        w.part = (int32_t)((id & 7) % parts);
+        n = (tiles + r - 1) / r;
+        at = id >> 3;
+        w.tile = ((id & 7) / parts);  // of every r tiles
+        at = at < n - n / 2 ? n - 1 - at : at - (n - n / 2);
+        w.tile += at * r;
+        return w;
+    } else {
+        w.part = (int32_t)(id / tiles);
+        at = id % tiles;
+    }
+    w.tile = at < n - n / 2 ? n - 1 - at : at - (n - n / 2);
+    return w;
+}
+
+// One work-group per tile of 64 rows, cache head and split; a sequence's last
+// 16 rows or fewer are split among the waves.
 template <int KS, int ND>
-__global__ __launch_bounds__(256, KS <= 2 ? 2 : 1) void paged_attn_tile_kernel(AttnArgs p)
+__global__ __launch_bounds__(256, KS <= 2 ? 2 : 1) void paged_attn_tile_kernel(AttnArgs p,
+                                                                               int64_t tiles)
 {
     __shared__ __attribute__((aligned(1024))) int8_t lds[2 * kStage<KS, ND>];
+    const Place w = place_of(p, blockIdx.x, tiles);
+    const int32_t g0 = w.part % p.kv.G, split = w.part / p.kv.G;
     Tile tile;
-    // the last tiles of a prompt see the most keys: they go first
-    if (!find_tile<kTile>(p, gridDim.x - 1 - blockIdx.x, tile)) return;
+    if (w.tile >= tiles || !find_tile<kTile>(p, w.tile, tile)) return;
     int64_t i0, i1;
-    split_range(p, tile, blockIdx.z, i0, i1);
+    split_range(p, tile, split, i0, i1);
     if (tile.rows - tile.row0 <= kRows)
-        split_rows<KS, ND>(p, tile, blockIdx.y, i0, i1, blockIdx.z, reinterpret_cast<double*>(lds));
+        split_rows<KS, ND>(p, tile, g0, i0, i1, split, reinterpret_cast<double*>(lds));
     else
-        share_keys<KS, ND>(p, tile, blockIdx.y, i0, i1, blockIdx.z, (MQ_LDS int8_t*)lds);
+        share_keys<KS, ND>(p, tile, g0, i0, i1, split, (MQ_LDS int8_t*)lds);
 }
 
 // Joins the splits: NW waves per row and 64 channels, each every NW-th split.
@@ -850,11 +896,19 @@ template <int ND>
 void launch_main(const AttnArgs& p, int64_t B, hipStream_t s)
 {
     constexpr int KS = (ND + 3) / 4;
-    const bool t = tiled(p.T, B, p.grp);
-    const dim3 grid((unsigned)row_tiles(p.T, B, p.grp, t ? kTile : kRows), (unsigned)p.kv.G,
+    const int64_t parts = (int64_t)p.kv.G * p.splits;
+    if (tiled(p.T, B, p.grp)) {
+        const int64_t tiles = row_tiles(p.T, B, p.grp, kTile);
+        // (see place_of)
+        const int64_t n = parts % 8 != 0 && 8 % parts == 0
+                              ? 8 * ((tiles + 8 / parts - 1) / (8 / parts))
+                              : tiles * parts;
+        paged_attn_tile_kernel<KS, ND><<<(unsigned)n, 256, 0, s>>>(p, tiles);
+        return;
+    }
+    const dim3 grid((unsigned)row_tiles(p.T, B, p.grp, kRows), (unsigned)p.kv.G,
                     (unsigned)p.splits);
-    if (t) paged_attn_tile_kernel<KS, ND><<<grid, 256, 0, s>>>(p);
-    else paged_attn_split_kernel<KS, ND><<<grid, 256, 0, s>>>(p);
+    paged_attn_split_kernel<KS, ND><<<grid, 256, 0, s>>>(p);
 }
 
 }  // namespace
