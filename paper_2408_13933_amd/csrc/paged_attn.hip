@@ -43,7 +43,8 @@ struct AttnArgs {
     double tau;           // log2(e) * q_scale * k_scale * logit_scale
     double v_scale, out_scale;
     uint32_t d_cut;       // logit distances from here on weigh nothing
-    int64_t window, sinks;
+    int32_t window, sinks; // window 0: none
+    int32_t page_bytes;    // of a page's keys, and of its values (at most 2^28)
     int32_t vec_q, vec_y; // query rows in 16-byte chunks, output rows in fours of codes
     int32_t splits;
     double* mz;           // [T * H][splits][2]: maximum and weight sum of a part
@@ -88,21 +89,34 @@ struct WeightTable {
         lo = (int)(uint32_t)__double_as_longlong(e);
         hi = (int)(__double_as_longlong(e) >> 32) - (lane << 14);
     }
-    __device__ int32_t weight(double tau, uint32_t d) const
+    // A weight on its way: the table's reads take a while.
+    struct Part {
+        double f;
+        int k, lo, hi;
+    };
+    __device__ Part begin(double tau, uint32_t d) const
     {
         constexpr double kShift = 105553116266496.0;  // 1.5 * 2^46
+        Part w;
         const double x = (double)d;
         const double t = __builtin_fma(-tau, x, kShift);
-        const double f = __builtin_fma(-tau, x, -(t - kShift));
-        const int32_t k = rint_low(t);
-        const int tl = __builtin_amdgcn_ds_bpermute(k << 2, lo);
-        const int th = __builtin_amdgcn_ds_bpermute(k << 2, hi) + (k << 14);
-        const double e = __longlong_as_double(((int64_t)th << 32) | (uint32_t)tl);
+        w.f = __builtin_fma(-tau, x, -(t - kShift));
+        w.k = rint_low(t);
+        w.lo = __builtin_amdgcn_ds_bpermute(w.k << 2, lo);
+        w.hi = __builtin_amdgcn_ds_bpermute(w.k << 2, hi);
+        // computed here, not where it is used
+        asm volatile("" : "+v"(w.f), "+v"(w.k));
+        return w;
+    }
+    __device__ static int32_t end(const Part& w)
+    {
+        const double e =
+            __longlong_as_double(((int64_t)(w.hi + (w.k << 14)) << 32) | (uint32_t)w.lo);
         double q = 0x1.3b2ad0385b409p-7;
-        q = __builtin_fma(q, f, 0x1.c6b0c40d8c4e9p-5);
-        q = __builtin_fma(q, f, 0x1.ebfbdff82ac52p-3);
-        q = __builtin_fma(q, f, 0x1.62e42fefa0352p-1);
-        q = __builtin_fma(q, f, 1.0);
+        q = __builtin_fma(q, w.f, 0x1.c6b0c40d8c4e9p-5);
+        q = __builtin_fma(q, w.f, 0x1.ebfbdff82ac52p-3);
+        q = __builtin_fma(q, w.f, 0x1.62e42fefa0352p-1);
+        q = __builtin_fma(q, w.f, 1.0);
         return rint_low(__builtin_fma(q, e, kRintShift + kBias));
     }
 };
@@ -196,45 +210,59 @@ __device__ inline void load_queries(const AttnArgs& p, int64_t t, int32_t head, 
 
 // What one row sees: positions (lo, hi], and below the sinks.
 struct Sees {
-    int64_t lo, hi;
+    int32_t lo, hi;
 };
 
 // The page list's entries for a block's eight 16-key groups, in the lanes' low
 // three bits, as they are (looked at when the block's turn comes, so that the
 // load can be under way until then).  Blocks past the list are never asked for.
-__device__ inline int32_t load_pages(const AttnArgs& p, int32_t b, int64_t blk)
+__device__ inline int32_t load_pages(const AttnArgs& p, int32_t b, int32_t blk)
 {
-    const int64_t e = (blk * kBlk + 16 * (threadIdx.x & 7)) >> p.kv.shift;
+    const int64_t e = ((int64_t)blk * kBlk + 16 * (threadIdx.x & 7)) >> p.kv.shift;
     return p.kv.table[(int64_t)b * p.kv.ld + min(e, p.kv.ld - 1)];
 }
 // Those that are a place in the cache, else -1.
-__device__ inline int32_t valid_pages(const AttnArgs& p, int64_t blk, int32_t pages)
+__device__ inline int32_t valid_pages(const AttnArgs& p, int32_t blk, int32_t pages)
 {
-    const int64_t e = (blk * kBlk + 16 * (threadIdx.x & 7)) >> p.kv.shift;
-    return e < p.kv.ld && pages >= 0 && (int64_t)pages < p.kv.pages ? pages : -1;
+    const int64_t e = ((int64_t)blk * kBlk + 16 * (threadIdx.x & 7)) >> p.kv.shift;
+    return e < p.kv.ld && pages >= 0 && pages < (int32_t)p.kv.pages ? pages : -1;
 }
 
-// Offsets of a block's keys and values for this lane: of half h, the key row
+// Where a lane reads a block's keys and values of half h: the key row
 // 16 (r >> 2) + (r & 3) of tile 0 (tile j: 4 j rows on) from channel 16 g on,
-// and 16 values of channel r from key 16 g on.  Groups without a place get
-// page 0's (they are masked).
-__device__ inline int64_t key_offset(const AttnArgs& p, int32_t g0, int64_t blk, int32_t pages,
-                                     int h)
+// and 16 values of channel r from key 16 g on.  `base` is the address in page
+// 0 and slot 0 of the block, `group` the lane whose page it is.  Groups
+// without a place get page 0's (they are masked).
+struct Spot {
+    const MQ_GLOBAL int8_t* base;
+    int32_t group;
+    __device__ static Spot key(const AttnArgs& p, int32_t g0, int h)
+    {
+        const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+        const int32_t slot = (64 * h + 16 * (r >> 2)) & ((1 << p.kv.shift) - 1);
+        return Spot{(const MQ_GLOBAL int8_t*)p.kv.k +
+                        ((((int64_t)g0 << p.kv.shift) + slot + (r & 3)) * p.kv.D + 16 * g),
+                    4 * h + (r >> 2)};
+    }
+    __device__ static Spot value(const AttnArgs& p, int32_t g0, int h)
+    {
+        const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+        const int32_t slot = (64 * h + 16 * g) & ((1 << p.kv.shift) - 1);
+        return Spot{(const MQ_GLOBAL int8_t*)p.kv.v +
+                        ((((int64_t)g0 * p.kv.D + r) << p.kv.shift) + slot),
+                    4 * h + g};
+    }
+    // in the block's page; slot: bytes from the page's start to the block (a
+    // page of more than 128 slots)
+    __device__ const MQ_GLOBAL int8_t* at(const AttnArgs& p, int32_t pages, int32_t slot) const
+    {
+        const uint32_t pg = (uint32_t)max(__shfl(pages, group), 0);
+        return base + ((uint64_t)pg * (uint32_t)p.page_bytes + (uint32_t)slot);
+    }
+};
+__device__ inline int32_t block_slot(const AttnArgs& p, int32_t blk)
 {
-    const int lane = threadIdx.x & 63, r = lane & 15;
-    const int64_t at = blk * kBlk + 64 * h + 16 * (r >> 2);
-    const int64_t pg = max(__shfl(pages, 4 * h + (r >> 2)), 0);
-    return ((((pg * p.kv.G + g0) << p.kv.shift) + (at & (((int64_t)1 << p.kv.shift) - 1))) +
-            (r & 3)) * p.kv.D;
-}
-__device__ inline int64_t value_offset(const AttnArgs& p, int32_t g0, int64_t blk, int32_t pages,
-                                       int h)
-{
-    const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-    const int64_t at = blk * kBlk + 64 * h + 16 * g;
-    const int64_t pg = max(__shfl(pages, 4 * h + g), 0);
-    return ((((pg * p.kv.G + g0) * p.kv.D) + r) << p.kv.shift) +
-           (at & (((int64_t)1 << p.kv.shift) - 1));
+    return (blk * kBlk) & ((1 << p.kv.shift) - 1);
 }
 
 // Channels are taken in steps of 64 (KS of them) by the scores and in tiles of
@@ -242,16 +270,17 @@ __device__ inline int64_t value_offset(const AttnArgs& p, int32_t g0, int64_t bl
 // there reads the head's first channels.  For the scores the query planes are
 // neutral there, the outputs of such a tile are dropped.
 
-// Channel offset of the lane's chunk of a key row in 64-channel step s.
+// Offset of the lane's chunk of a key row in 64-channel step s from that in
+// step 0.
 __device__ inline int32_t key_chunk(const AttnArgs& p, int s)
 {
-    const int32_t d = 64 * s + 16 * ((threadIdx.x & 63) >> 4);
-    return d < p.kv.D ? d : 0;
+    const int32_t c = 16 * ((threadIdx.x & 63) >> 4);
+    return 64 * s + c < p.kv.D ? 64 * s : -c;
 }
 // Offset of output tile dt's values from tile 0's.
-__device__ inline int64_t value_tile(const AttnArgs& p, int dt)
+__device__ inline int32_t value_tile(const AttnArgs& p, int dt)
 {
-    return 16 * dt < p.kv.D ? (int64_t)(16 * dt) << p.kv.shift : 0;
+    return 16 * dt < p.kv.D ? (16 * dt) << p.kv.shift : 0;
 }
 
 // Fragments of a block straight from the cache.
@@ -259,17 +288,15 @@ template <int KS>
 struct FromCache {
     const MQ_GLOBAL int8_t* k[2];
     const MQ_GLOBAL int8_t* v[2];
-    int32_t chunk[KS];
     const AttnArgs& p;
-    __device__ FromCache(const AttnArgs& a, int32_t g0, int64_t blk, int32_t pages) : p(a)
+    __device__ FromCache(const AttnArgs& a, int32_t g0, int32_t blk, int32_t pages) : p(a)
     {
+        const int32_t slot = block_slot(p, blk);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            k[h] = (const MQ_GLOBAL int8_t*)p.kv.k + key_offset(p, g0, blk, pages, h);
-            v[h] = (const MQ_GLOBAL int8_t*)p.kv.v + value_offset(p, g0, blk, pages, h);
+            k[h] = Spot::key(p, g0, h).at(p, pages, slot * p.kv.D);
+            v[h] = Spot::value(p, g0, h).at(p, pages, slot);
         }
-#pragma unroll
-        for (int s = 0; s < KS; ++s) chunk[s] = key_chunk(p, s);
     }
     // The same fragments, to be read anew (their registers are not kept).
     __device__ FromCache again() const
@@ -280,7 +307,7 @@ struct FromCache {
     }
     __device__ v4i key(int h, int j, int s) const
     {
-        return *reinterpret_cast<const MQ_GLOBAL v4i*>(k[h] + 4 * j * p.kv.D + chunk[s]);
+        return *reinterpret_cast<const MQ_GLOBAL v4i*>(k[h] + (4 * j * p.kv.D + key_chunk(p, s)));
     }
     __device__ v4i value(int h, int dt) const
     {
@@ -317,38 +344,47 @@ __device__ inline void wait_staged()
     __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // vmcnt(0), the others left alone
 }
 
-// The wave's share of a block into a stage: two of the eight key tiles and
-// half of one half's values.
+// A wave's share of a block into a stage: two of the eight key tiles and half
+// of one half's values.
 template <int KS, int ND>
-__device__ inline void stage_block(const AttnArgs& p, int32_t g0, int64_t blk, int32_t pages,
-                                   int wave, MQ_LDS int8_t* stage)
-{
-    const int kh = wave >> 1, vh = wave & 1;
-    const int8_t* k = p.kv.k + key_offset(p, g0, blk, pages, kh);
-    const int8_t* v = p.kv.v + value_offset(p, g0, blk, pages, vh);
+struct Stager {
+    Spot key, value;
+    int32_t last;  // key_chunk of the last step (the others are 64 s)
+    __device__ Stager(const AttnArgs& p, int32_t g0, int wave)
+    {
+        key = Spot::key(p, g0, wave >> 1);
+        key.base += (8 * (wave & 1)) * p.kv.D;
+        value = Spot::value(p, g0, wave & 1);
+        last = key_chunk(p, KS - 1);
+    }
+    __device__ void operator()(const AttnArgs& p, int32_t blk, int32_t pages, int wave,
+                               MQ_LDS int8_t* stage) const
+    {
+        const int32_t slot = block_slot(p, blk);
+        const MQ_GLOBAL int8_t* k = key.at(p, pages, slot * p.kv.D);
+        const MQ_GLOBAL int8_t* v = value.at(p, pages, slot);
+        MQ_LDS int8_t* ks = stage + (2 * wave * KS) * 1024;
 #pragma unroll
-    for (int jj = 0; jj < 2; ++jj) {
-        const int j = 2 * (wave & 1) + jj;
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
+            for (int s = 0; s < KS; ++s)
+                __builtin_amdgcn_global_load_lds(
+                    (const MQ_GLOBAL void*)(k + (4 * j * p.kv.D + (s < KS - 1 ? 64 * s : last))),
+                    (MQ_LDS void*)(ks + (j * KS + s) * 1024), 16, 0, 0);
+        MQ_LDS int8_t* vs = stage + (8 * KS + ND * (wave & 1) + (wave >> 1)) * 1024;
+#pragma unroll
+        for (int i = 0; i < ND / 2; ++i)
             __builtin_amdgcn_global_load_lds(
-                (const MQ_GLOBAL void*)(k + 4 * j * p.kv.D + key_chunk(p, s)),
-                (MQ_LDS void*)(stage + ((4 * kh + j) * KS + s) * 1024), 16, 0, 0);
+                (const MQ_GLOBAL void*)(v + value_tile(p, 2 * i + (wave >> 1))),
+                (MQ_LDS void*)(vs + 2 * i * 1024), 16, 0, 0);
     }
-#pragma unroll
-    for (int i = 0; i < ND / 2; ++i) {
-        const int dt = 2 * i + (wave >> 1);
-        __builtin_amdgcn_global_load_lds(
-            (const MQ_GLOBAL void*)(v + value_tile(p, dt)),
-            (MQ_LDS void*)(stage + (8 * KS + ND * vh + dt) * 1024), 16, 0, 0);
-    }
-}
+};
 
 // One block of 128 positions for the wave's rows.  pages: of its groups;
 // full: every row sees all of its positions that have a place.
 template <int KS, int ND, class Source>
 __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table, Rows<KS, ND>& st,
-                                    const Source& src, int32_t pages, int64_t blk,
+                                    const Source& src, int32_t pages, int32_t blk,
                                     const Sees& sees, bool full)
 {
     const int lane = threadIdx.x & 63, g = lane >> 4;
@@ -359,7 +395,7 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
     // next ones' fragments read before these are multiplied
     v4i c[2][4];
     {
-        constexpr int J = KS <= 2 ? 4 : 2, N = 8 / J;
+        constexpr int J = 2, N = 8 / J;
         v4i kf[2][J][KS];
 #pragma unroll
         for (int n = 0; n <= N; ++n) {
@@ -409,14 +445,13 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
     uint32_t seen = 0xffffffffu;  // bit 16 h + 4 j + i
     if (mask) {
         // of the 16 keys of a half from `first` on those below n, as bits
-        auto below = [](int64_t n, int64_t first) {
-            const int32_t k = (int32_t)max(min(n - first, (int64_t)16), (int64_t)0);
-            return (1u << k) - 1;
+        auto below = [](int32_t n, int32_t first) {
+            return (1u << max(min(n - first, 16), 0)) - 1;  // n >= 0
         };
         seen = 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int64_t first = blk * kBlk + 64 * h + 16 * g;
+            const int32_t first = blk * kBlk + 64 * h + 16 * g;
             uint32_t bits = below(sees.hi + 1, first);
             bits &= ~below(sees.lo + 1, first) | below(p.sinks, first);
             if (!((placed >> (4 * h + g)) & 1)) bits = 0;
@@ -434,8 +469,11 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
     for (int i = 0; i < 32; ++i) m = max(m, c[i >> 4][(i >> 2) & 3][i & 3]);
     m = row_max(m);
 
+    const int32_t m_new = max(st.m, m);
+    const double f = factor(p, m_new, m);
+
     // weights; the first values' fragments are read before the last of them
-    constexpr int E = ND % 4 == 0 ? 4 : 2;  // output tiles at once
+    constexpr int E = 2;  // output tiles at once
     v4i v[2][E][2];
     auto read_values = [&](int n) {
 #pragma unroll
@@ -445,24 +483,39 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
         }
     };
     v4i wh[2], wl[2];
+    // so many weights begin before the last so many end (registers for three
+    // waves per SIMD where the state is small)
+    constexpr int A = KS == 1 ? 2 : 4, N = 32 / A;
+    WeightTable::Part part[2][A];
+    int32_t w[4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int n = 0; n <= N; ++n) {
+        if (n < N) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (h == 1 && j == 2) read_values(0);
-            int32_t w[4];
+            for (int i = 0; i < A; ++i) {
+                const int x = A * n + i;
+                part[n & 1][i] = table.begin(
+                    p.tau, min((uint32_t)m - (uint32_t)c[x >> 4][(x >> 2) & 3][x & 3], p.d_cut));
+            }
+        }
+        if (n == N) read_values(0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (n == 0) continue;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                w[i] = table.weight(p.tau, min((uint32_t)m - (uint32_t)c[h][j][i], p.d_cut));
+        for (int i = 0; i < A; ++i)
+            w[(A * (n - 1) + i) & 3] = WeightTable::end(part[(n - 1) & 1][i]);
+        if (A * n % 4 == 0) {
+            const int x = A * n / 4 - 1;
             int hi4, lo4;
             pack_weights4(w, hi4, lo4);
-            // here and not after all of the table's reads, whose results
-            // would be kept until then
             asm volatile("" : "+v"(hi4), "+v"(lo4));
-            wh[h][j] = hi4;
-            wl[h][j] = lo4;
-            if (j & 1) __builtin_amdgcn_sched_barrier(0);
+            wh[x >> 2][x & 3] = hi4;
+            wl[x >> 2][x & 3] = lo4;
+        } else {
+            asm volatile("" : "+v"(w[0]), "+v"(w[1]));
         }
+        __builtin_amdgcn_sched_barrier(0);
+    }
 
     if (mask) {
 #pragma unroll
@@ -478,8 +531,6 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
     }
 
     // the block joins the rows' state
-    const int32_t m_new = max(st.m, m);
-    const double f = factor(p, m_new, m);
     if (__ballot(m > st.m) != 0) {
         const double rs = factor(p, m_new, st.m);
         st.z *= rs;
@@ -535,18 +586,20 @@ __device__ inline void store_out(const AttnArgs& p, int64_t t, int32_t head, int
     else static_cast<int16_t*>(p.y)[at] = (int16_t)q;
 }
 
-// A tile of rows of one sequence and the blocks that its rows see.
+// A tile of rows of one sequence and the blocks that its rows see.  Positions
+// are below 2^31 and above -2^26 (lengths are int32).
 struct Tile {
     int32_t b;
-    int64_t s0, pos0;        // the sequence's first token row and its position
-    int64_t row0, rows;      // first row (token, head of the group) and the sequence's rows
-    int64_t n, skip0, skip1; // blocks to walk: n, without those in [skip0, skip1)
-    int64_t hi_min, hi_max;  // positions of the first and last token
-    __device__ int64_t block(int64_t i) const { return i < skip0 ? i : i + (skip1 - skip0); }
+    int32_t s0, pos0;         // the sequence's first token row and its position
+    uint32_t row0, rows;      // first row (token, head of the group), the sequence's rows
+    int32_t n, skip0, skip1;  // blocks to walk: n, without those in [skip0, skip1)
+    int32_t hi_min, hi_max;   // positions of the first and last token
+    __device__ int32_t block(int32_t i) const { return i < skip0 ? i : i + (skip1 - skip0); }
     // Every row sees all positions of the block.
-    __device__ bool full(const AttnArgs& p, int64_t blk) const
+    __device__ bool full(const AttnArgs& p, int32_t blk) const
     {
-        return (blk + 1) * kBlk - 1 <= hi_min && (p.window == 0 || blk * kBlk > hi_max - p.window);
+        return blk * kBlk + (kBlk - 1) <= hi_min &&
+               (p.window == 0 || blk * kBlk > hi_max - p.window);
     }
 };
 
@@ -558,21 +611,23 @@ __device__ inline bool find_tile(const AttnArgs& p, int64_t index, Tile& t)
     const int32_t* starts = p.kv.starts;
     const int32_t grp = p.grp;
     t.b = find_seq(p.kv.B, index, [=](int32_t i) { return (int64_t)starts[i] * grp / R + i; });
-    t.s0 = starts[t.b];
-    const int64_t s1 = starts[t.b + 1], len = p.kv.lens[t.b];
-    if (t.s0 < 0 || s1 > p.T || t.s0 >= s1) return false;
-    t.row0 = (index - (t.s0 * grp / R + t.b)) * R;
-    t.rows = (s1 - t.s0) * grp;
-    if (t.row0 < 0 || t.row0 >= t.rows) return false;
-    t.pos0 = len - (s1 - t.s0);
-    t.hi_max = t.pos0 + (min(t.row0 + R, t.rows) - 1) / grp;
-    t.hi_min = t.pos0 + t.row0 / grp;
-    const int64_t list = ((p.kv.ld << p.kv.shift) + kBlk - 1) / kBlk;  // blocks with places
-    const int64_t end = t.hi_max < 0 ? 0 : min(t.hi_max / kBlk + 1, list);
+    const int32_t s0 = starts[t.b], s1 = starts[t.b + 1], len = max(p.kv.lens[t.b], 0);
+    if (s0 < 0 || s1 > (int32_t)p.T || s0 >= s1) return false;
+    const int64_t row0 = (index - ((int64_t)s0 * grp / R + t.b)) * R;
+    t.s0 = s0;
+    t.rows = (uint32_t)(s1 - s0) * (uint32_t)grp;  // below 2^32 (T H D is below 2^36)
+    if (row0 < 0 || row0 >= (int64_t)t.rows) return false;
+    t.row0 = (uint32_t)row0;
+    t.pos0 = len - (s1 - s0);
+    t.hi_max = t.pos0 + (int32_t)((min(t.row0 + (R - 1), t.rows - 1)) / (uint32_t)grp);
+    t.hi_min = t.pos0 + (int32_t)(t.row0 / (uint32_t)grp);
+    // blocks with places, up to the last row's
+    const int64_t list = ((p.kv.ld << p.kv.shift) + kBlk - 1) / kBlk;
+    const int32_t end = t.hi_max < 0 ? 0 : (int32_t)min((int64_t)(t.hi_max / kBlk + 1), list);
     t.skip0 = t.skip1 = 0;
     if (p.window > 0) {
-        t.skip1 = t.hi_min - p.window + 1 > 0 ? min((t.hi_min - p.window + 1) / kBlk, end) : 0;
-        t.skip0 = min((p.sinks + kBlk - 1) / kBlk, t.skip1);
+        t.skip1 = t.hi_min >= p.window ? min((t.hi_min - p.window + 1) / kBlk, end) : 0;
+        t.skip0 = min((int32_t)(((int64_t)p.sinks + kBlk - 1) / kBlk), t.skip1);
     }
     t.n = end - (t.skip1 - t.skip0);
     return true;
@@ -584,38 +639,37 @@ struct RowAt {
     int64_t t;
     int32_t head;
     Sees sees;
-    __device__ RowAt(const AttnArgs& p, const Tile& tile, int64_t first, int32_t g0)
+    __device__ RowAt(const AttnArgs& p, const Tile& tile, uint32_t first, int32_t g0)
     {
-        const int64_t x = first + (threadIdx.x & 15);
+        const uint32_t x = first + (threadIdx.x & 15);  // no overflow: rows below 2^32 - 64
         have = x < tile.rows;
-        const uint32_t row = (uint32_t)(have ? x : tile.rows - 1);  // rows < 2^26 * 2^10 / G
-        const uint32_t tok = row / (uint32_t)p.grp;
-        t = tile.s0 + tok;
+        const uint32_t row = have ? x : tile.rows - 1, tok = row / (uint32_t)p.grp;
+        t = (int64_t)tile.s0 + tok;
         head = g0 * p.grp + (int32_t)(row - tok * (uint32_t)p.grp);
-        sees.hi = tile.pos0 + tok;
-        sees.lo = p.window > 0 ? sees.hi - p.window : -1;
+        sees.hi = max(tile.pos0 + (int32_t)tok, -1);
+        sees.lo = p.window > 0 && sees.hi >= p.window ? sees.hi - p.window : -1;
     }
 };
 
 // Four waves share 16 rows and take every fourth block of [i0, i1); their
 // states are joined through LDS.
 template <int KS, int ND>
-__device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g0, int64_t i0,
-                                  int64_t i1, int split, double* lds)
+__device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g0, int32_t i0,
+                                  int32_t i1, int split, double* lds)
 {
     const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const RowAt row(p, tile, tile.row0, g0);
     Rows<KS, ND> st;
     st.clear();
-    int64_t i = i0 + wave;
+    int32_t i = i0 + wave;
     if (i < i1) {
         WeightTable table;
         table.init();
         int32_t pages = load_pages(p, tile.b, tile.block(i));
         load_queries<KS>(p, row.t, row.head, row.have, st.qh, st.ql, st.cz);
         for (; i < i1; i += kWaves) {
-            const int64_t blk = tile.block(i);
+            const int32_t blk = tile.block(i);
             pages = valid_pages(p, blk, pages);
             const FromCache<KS> src(p, g0, blk, pages);
             const int32_t next = load_pages(p, tile.b, tile.block(min(i + kWaves, i1 - 1)));
@@ -664,8 +718,8 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
 // Every wave has 16 rows of its own; all walk over blocks [i0, i1), staged in
 // LDS by the four together, the next block on its way during this one.
 template <int KS, int ND>
-__device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g0, int64_t i0,
-                                  int64_t i1, int split, MQ_LDS int8_t* lds)
+__device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g0, int32_t i0,
+                                  int32_t i1, int split, MQ_LDS int8_t* lds)
 {
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -676,18 +730,18 @@ __device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g
         WeightTable table;
         table.init();
         int32_t pages = valid_pages(p, tile.block(i0), load_pages(p, tile.b, tile.block(i0)));
-        stage_block<KS, ND>(p, g0, tile.block(i0), pages, wave, lds);
+        const Stager<KS, ND> stage(p, g0, wave);
+        stage(p, tile.block(i0), pages, wave, lds);
         int32_t next = load_pages(p, tile.b, tile.block(min(i0 + 1, i1 - 1)));
         load_queries<KS>(p, row.t, row.head, row.have, st.qh, st.ql, st.cz);
         wait_staged();
         __syncthreads();
-        for (int64_t i = i0; i < i1; ++i) {
-            const int64_t blk = tile.block(i);
-            const int buf = (int)(i - i0) & 1;
-            const int64_t blk1 = tile.block(min(i + 1, i1 - 1));
+        for (int32_t i = i0; i < i1; ++i) {
+            const int32_t blk = tile.block(i);
+            const int buf = (i - i0) & 1;
+            const int32_t blk1 = tile.block(min(i + 1, i1 - 1));
             next = valid_pages(p, blk1, next);
-            if (i + 1 < i1)
-                stage_block<KS, ND>(p, g0, blk1, next, wave, lds + (buf ^ 1) * kStage<KS, ND>);
+            if (i + 1 < i1) stage(p, blk1, next, wave, lds + (buf ^ 1) * kStage<KS, ND>);
             const int32_t after = load_pages(p, tile.b, tile.block(min(i + 2, i1 - 1)));
             const FromLds<KS, ND> src{lds + buf * kStage<KS, ND> + lane * 16};
             attend_block<KS, ND>(p, table, st, src, pages, blk, row.sees, tile.full(p, blk));
@@ -737,22 +791,22 @@ __device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g
 }
 
 // The split's blocks [i0, i1) of the tile.
-__device__ inline void split_range(const AttnArgs& p, const Tile& t, int split, int64_t& i0,
-                                   int64_t& i1)
+__device__ inline void split_range(const AttnArgs& p, const Tile& t, int split, int32_t& i0,
+                                   int32_t& i1)
 {
-    const int64_t per = (t.n + p.splits - 1) / p.splits;
+    const int32_t per = (t.n + p.splits - 1) / p.splits;
     i0 = per * split;
     i1 = min(i0 + per, t.n);
 }
 
 // grid (tiles of 16 rows, G, splits)
 template <int KS, int ND>
-__global__ __launch_bounds__(256, KS <= 2 ? 2 : 1) void paged_attn_split_kernel(AttnArgs p)
+__global__ __launch_bounds__(256, KS == 1 ? 3 : KS == 2 ? 2 : 1) void paged_attn_split_kernel(AttnArgs p)
 {
     __shared__ double lds[kWaves * 4 * 64 + kWaves * kRows * 3 / 2];
     Tile tile;
     if (!find_tile<kRows>(p, blockIdx.x, tile)) return;
-    int64_t i0, i1;
+    int32_t i0, i1;
     split_range(p, tile, blockIdx.z, i0, i1);
     split_rows<KS, ND>(p, tile, blockIdx.y, i0, i1, blockIdx.z, lds);
 }
@@ -796,7 +850,7 @@ __device__ inline Place place_of(const AttnArgs& p, int64_t id, int64_t tiles)
 // One work-group per tile of 64 rows, cache head and split; a sequence's last
 // 16 rows or fewer are split among the waves.
 template <int KS, int ND>
-__global__ __launch_bounds__(256, KS <= 2 ? 2 : 1) void paged_attn_tile_kernel(AttnArgs p,
+__global__ __launch_bounds__(256, KS == 1 ? 3 : KS == 2 ? 2 : 1) void paged_attn_tile_kernel(AttnArgs p,
                                                                                int64_t tiles)
 {
     __shared__ __attribute__((aligned(1024))) int8_t lds[2 * kStage<KS, ND>];
@@ -804,7 +858,7 @@ __global__ __launch_bounds__(256, KS <= 2 ? 2 : 1) void paged_attn_tile_kernel(A
     const int32_t g0 = w.part % p.kv.G, split = w.part / p.kv.G;
     Tile tile;
     if (w.tile >= tiles || !find_tile<kTile>(p, w.tile, tile)) return;
-    int64_t i0, i1;
+    int32_t i0, i1;
     split_range(p, tile, split, i0, i1);
     if (tile.rows - tile.row0 <= kRows)
         split_rows<KS, ND>(p, tile, g0, i0, i1, split, reinterpret_cast<double*>(lds));
@@ -950,13 +1004,15 @@ hipError_t launch_paged_attn(const KvArgs& kv, const int16_t* q, int64_t ldq, in
     // distance (tau d_cut <= 40 + tau)
     const double cut = 40.0 / p.tau;
     p.d_cut = cut < 4294967295.0 ? (uint32_t)std::ceil(cut) : 0xFFFFFFFFu;
-    p.window = window;
-    p.sinks = window > 0 ? sinks : 0;
+    // positions are below 2^31: a window of as many hides nothing
+    p.window = window < 0x7FFFFFFF ? (int32_t)window : 0;
+    p.sinks = p.window > 0 ? (int32_t)std::min<int64_t>(sinks, 0x7FFFFFFF) : 0;
+    p.page_bytes = (kv.G * kv.D) << kv.shift;
     p.vec_q = ((uintptr_t)q % 16) == 0 && ldq % 8 == 0;
     p.vec_y = ((uintptr_t)y % (out_bits / 2)) == 0 && ldy % 4 == 0;
     // the blocks that a row of a windowed call walks over
     if (window > 0 && window < max_len)
-        max_len = std::min(max_len, window + std::min(p.sinks, max_len) + 2 * kBlk);
+        max_len = std::min(max_len, window + std::min<int64_t>(p.sinks, max_len) + 2 * kBlk);
     int64_t splits = split_count(T, kv.B, H, kv.G, kv.D, max_len);
     const int64_t one = T * H * (kv.D + 2) * 8;
     splits = ws ? std::min(splits, std::max<int64_t>(ws_bytes / one, 1)) : 1;
