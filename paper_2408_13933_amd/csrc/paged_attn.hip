@@ -932,14 +932,18 @@ int64_t row_tiles(int64_t T, int64_t B, int32_t grp, int R) { return T * grp / R
 // Whether the sequences have more rows than a wave takes, on average.
 bool tiled(int64_t T, int64_t B, int32_t grp) { return T * grp > B * kRows; }
 
-// Parts the keys of every tile are split into: two work-groups per CU, at
-// least a block per wave in each.
+// Parts the keys of every tile are split into: as many work-groups as the chip
+// holds at once, at least a block per wave in each.  With fewer or more (us,
+// main kernel): 64 sequences up to 4096 keys, 4 heads of 64, 256 work-groups
+// 35, 512 23, 768 27, 1024 28; 2 up to 120000, one head of 256: 64 work-groups
+// 41, 256 28, 470 36.
 int64_t split_count(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D, int64_t max_len)
 {
     const int32_t grp = H / G;
     const int R = tiled(T, B, grp) ? kTile : kRows;
     const int64_t groups = std::max(T * grp / R, std::min(B, T)) * G;
-    int64_t s = 512 / std::max<int64_t>(groups, 1);
+    // two work-groups per CU fit, one where the state is large (D > 128)
+    int64_t s = (D > 128 ? 256 : 512) / std::max<int64_t>(groups, 1);
     const int64_t blocks = (max_len + kBlk - 1) / kBlk;
     s = std::min(s, (blocks + kWaves - 1) / kWaves);
     s = std::min<int64_t>(s, MQ_ATTN_MAX_WORKSPACE / (T * H * (D + 2) * 8));
