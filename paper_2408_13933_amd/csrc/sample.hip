@@ -586,6 +586,7 @@ struct DrawLds {
     unsigned long long mass[kBins];
     uint64_t word[kEntries];  // listed or gathered words, as order() has them
     uint64_t near[2 * kNear];
+    uint32_t cursor[kBins];
     int64_t wave64[kDrawWaves];
     int32_t wave32[kDrawWaves];
     CutLds cuts;
@@ -914,49 +915,51 @@ template <class F, class Sum>
 __device__ __forceinline__ int32_t draw_by_segments(const SampleArgs& a, const Row& r, const typename F::T* x,
                                     DrawLds& lds, const Cut& cut, double u, Sum sum)
 {
-    const int tid = threadIdx.x, lane = tid & 63;
-    int64_t s = 0, all = 0, base = 0, total = 0;
-    for (int i = tid; i < a.segs; i += kDrawThreads) s += sum(i);
-    block_scan<kDrawWaves>(s, &total, lds.wave64);
+    const int tid = threadIdx.x;
+    // neighbouring segments per thread
+    const int each = (a.segs + kDrawThreads - 1) / kDrawThreads, first = tid * each;
+    int64_t s = 0, total = 0;
+    for (int i = first; i < min(first + each, a.segs); ++i) s += sum(i);
+    int64_t run = block_scan<kDrawWaves>(s, &total, lds.wave64);
     const int64_t target = min((int64_t)(u * (double)total), total - 1);
-    if (tid == 0) lds.sel[0] = 0;
-    __syncthreads();
-    for (int s0 = 0; s0 < a.segs; s0 += kDrawThreads) {
-        const int i = s0 + tid;
-        const int64_t v = i < a.segs ? sum(i) : 0;
-        const int64_t before = base + block_scan<kDrawWaves>(v, &all, lds.wave64);
-        if (target >= before && target < before + v) {
-            lds.sel[0] = (uint32_t)i;
-            lds.sel64[0] = before;
-        }
-        base += all;
+    if (tid == 0) {
+        lds.sel[0] = 0;
+        lds.sel64[0] = 0;
     }
     __syncthreads();
-    const int32_t i0 = (int32_t)lds.sel[0] * kSeg;
-    int64_t run = lds.sel64[0];
+    if (target >= run && target < run + s) {
+        int i = first;
+        for (int64_t v; target >= run + (v = sum(i)); ++i) run += v;
+        lds.sel[0] = (uint32_t)i;
+        lds.sel64[0] = run;
+    }
     __syncthreads();
-    if (tid < 64) {
-        bool done = false;
-#pragma unroll 1
-        for (int j0 = 0; j0 < kSeg / 64 && !done; j0 += 8) {
-            typename F::V v8[8];
-            load_words<F>(a, x, i0 + 64 * j0, i0 + 64 * j0 + lane, v8);
+    // neighbouring words of that segment per thread
+    constexpr int per = kSeg / kDrawThreads;
+    const int32_t i0 = (int32_t)lds.sel[0] * kSeg + tid * per;
+    run = lds.sel64[0];
+    typename F::T v[per];
+    int64_t w[per];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (done) continue;
-                const int32_t i = i0 + 64 * (j0 + j) + lane;
-                const uint32_t k = F::key(v8[j]);
-                int64_t c = cut.keeps(k, (uint32_t)i) ? weight<F>(r, lds.table, k) : 0;
-                if (c < r.floor) c = 0;
-                c = wave_scan(c);
-                const uint64_t hit = __ballot(run + c > target);
-                if (hit) {
-                    if (lane == __builtin_ctzll(hit)) lds.sel[0] = (uint32_t)i;
-                    done = true;
-                }
-                run += wave_read(c, 63);
-            }
+    for (int j = 0; j < per; ++j) v[j] = x[min(i0 + j, a.V - 1)];
+    s = 0;
+#pragma unroll
+    for (int j = 0; j < per; ++j) {
+        const uint32_t k = i0 + j < a.V ? F::key(F::load(v[j])) : 0;
+        w[j] = cut.keeps(k, (uint32_t)(i0 + j)) ? weight<F>(r, lds.table, k) : 0;
+        if (w[j] < r.floor) w[j] = 0;
+        s += w[j];
+    }
+    int64_t all;
+    run += block_scan<kDrawWaves>(s, &all, lds.wave64);
+    if (target >= run && target < run + s) {
+        int32_t at = i0;
+#pragma unroll
+        for (int j = 0; j < per; ++j) {
+            at += target >= run + w[j];  // (not once it is reached: the rest adds to run)
+            run += w[j];
         }
+        lds.sel[0] = (uint32_t)at;
     }
     __syncthreads();
     return (int32_t)lds.sel[0];
@@ -1019,39 +1022,83 @@ __device__ __forceinline__ int64_t store_lists(const SampleArgs& a, int64_t m, u
     return n;
 }
 
-// The draw from the n <= kDrawThreads first words of the order, unordered in
-// lds.near, which hold the kept ones: a thread per word.  mass: top_p's, or
-// negative: p of the sum of the first k.
+// The draw from the `few` <= kDrawThreads listed words (n in LDS, in index
+// order, counted by bin) of the bins up to `bin`, which hold the kept ones: a
+// thread per word.  mass: top_p's, or negative: p of the sum of the first k.
+//
+// A word's place in the order is what the bins before its own hold and what
+// comes before it in its own.
 template <class F>
 __device__ __forceinline__ int32_t draw_few(const SampleArgs& a, const Row& r, DrawLds& lds, int n,
-                                            double mass, double u)
+                                            int32_t bin, int few, double mass, double u)
 {
-    const int e = threadIdx.x;
-    order_words(lds.near, n, lds.near + kNear);
-    __syncthreads();
-    const uint64_t word = e < n ? lds.near[kNear + e] : 0;
-    const int64_t w = e < n && (r.k == 0 || e < r.k) ? weight<F>(r, lds.table, key_of(word)) : 0;
-    int64_t total;
-    const int64_t before = block_scan<kDrawWaves>(w, &total, lds.wave64);
-    if (mass < 0.0) mass = r.p * (double)total;
-    const bool kept = (r.p >= 1.0 || e == 0 || (double)before < mass) && w >= r.floor;
-    const int64_t kw = kept ? w : 0;
-    lds.mass[e] = (unsigned long long)kw;
-    block_scan<kDrawWaves>(kw, &total, lds.wave64);
-    const int64_t target = min((int64_t)(u * (double)total), total - 1);
-    // the kept weight of the words before this one in index order
-    int64_t run = 0;
-    for (int o = 0; o < n; o += 8) {  // (past n the weights are 0)
-        uint32_t idx[8];
-        int64_t kw8[8];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    // the words of these bins, in index order
+    constexpr int turns = kEntries / kDrawThreads;
+    const int32_t part = ((n + kDrawWaves - 1) / kDrawWaves + 63) & ~63;
+    const int32_t i0 = min(wave * part, n), i1 = min(i0 + part, n);
+    uint32_t mine = 0;  // bit j: the lane's word of turn j is one of them
+    int cnt = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            idx[i] = (uint32_t)lds.near[kNear + o + i];
-            kw8[i] = (int64_t)lds.mass[o + i];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) run += idx[i] < (uint32_t)word ? kw8[i] : 0;
+    for (int j = 0; j < turns; ++j) {
+        const int32_t i = i0 + 64 * j + lane;
+        const bool here = i < i1 && bin_of<F>(r, key_of(lds.word[i])) <= bin;
+        mine |= (uint32_t)here << j;
+        cnt += __popcll(__ballot(here));
     }
+    // and the places of the bins
+    const uint32_t c0 = lds.count[place_of(2 * tid)], c1 = lds.count[place_of(2 * tid + 1)];
+    if (lane == 0) lds.wave32[wave] = cnt;
+    int64_t total;
+    const int64_t start = block_scan<kDrawWaves>((int64_t)(c0 + c1), &total, lds.wave64);
+    lds.cursor[2 * tid] = (uint32_t)start;
+    lds.cursor[2 * tid + 1] = (uint32_t)start + c0;
+    int at = 0;
+#pragma unroll
+    for (int w = 0; w < kDrawWaves; ++w) at += w < wave ? lds.wave32[w] : 0;
+#pragma unroll
+    for (int j = 0; j < turns; ++j) {
+        const uint64_t hit = __ballot((mine >> j) & 1);
+        if ((mine >> j) & 1) lds.near[at + __popcll(hit & below)] = lds.word[i0 + 64 * j + lane];
+        at += __popcll(hit);
+    }
+    __syncthreads();
+    const bool have = tid < few;
+    const uint64_t word = have ? lds.near[tid] : 0;
+    const uint32_t key = key_of(word);
+    const int32_t own = have ? bin_of<F>(r, key) : 0;
+    if (have) lds.near[kNear + atomicAdd(&lds.cursor[own], 1u)] = word;
+    __syncthreads();
+    int rank = 0;
+    if (have) {
+        const int end = (int)lds.cursor[own];
+        int o = end - (int)lds.count[place_of(own)];
+        rank = o;
+        for (; o + 8 <= end; o += 8) {
+            uint64_t t[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = lds.near[kNear + o + i];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rank += t[i] < word;
+        }
+        for (; o < end; ++o) rank += lds.near[kNear + o] < word;
+    }
+    const int64_t w = have && (r.k == 0 || rank < r.k) ? weight<F>(r, lds.table, key) : 0;
+    // the weights before it in the order
+    if (have) lds.mass[rank] = (unsigned long long)w;
+    __syncthreads();
+    const int64_t sorted = have ? (int64_t)lds.mass[tid] : 0;
+    const int64_t ahead = block_scan<kDrawWaves>(sorted, &total, lds.wave64);
+    if (have) lds.mass[tid] = (unsigned long long)ahead;
+    __syncthreads();
+    const int64_t before = have ? (int64_t)lds.mass[rank] : 0;
+    if (mass < 0.0) mass = r.p * (double)total;
+    const bool kept = (r.p >= 1.0 || rank == 0 || (double)before < mass) && w >= r.floor;
+    const int64_t kw = have && kept ? w : 0;
+    // the kept weights before it in index order
+    const int64_t run = block_scan<kDrawWaves>(kw, &total, lds.wave64);
+    const int64_t target = min((int64_t)(u * (double)total), total - 1);
     if (kw > 0 && target >= run && target < run + kw) lds.sel[0] = (uint32_t)word;
     __syncthreads();
     return (int32_t)lds.sel[0];
@@ -1169,11 +1216,8 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs
         const int32_t bin = (int32_t)lds.sel[0];
         const int64_t count = lds.sel64[0] + lds.count[place_of(bin)];
         if (count <= kNear) {
-            for (int i = tid; i < n; i += kDrawThreads)
-                if (bin_of<F>(r, key_of(lds.word[i])) <= bin)
-                    lds.near[atomicAdd(&lds.sel[1], 1u)] = lds.word[i];
-            __syncthreads();
-            const int32_t tok = draw_few<F>(a, r, lds, (int)count, r.k > 0 ? -1.0 : target, u);
+            const int32_t tok = draw_few<F>(a, r, lds, (int)n, bin, (int)count,
+                                            r.k > 0 ? -1.0 : target, u);
             if (tid == 0) a.tokens[row] = tok;
             return;
         }
