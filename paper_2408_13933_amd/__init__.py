@@ -884,6 +884,15 @@ def _device_and_stream(t, name, stream):
     return dev, _stream_ptr(stream)
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory for a call on ``stream``: from that stream's own, since a block
+    of the current stream's may still be in use there."""
+    if stream is None:
+        return _torch_mod.empty(shape, dtype=dtype, device=device)
+    with _torch_mod.cuda.stream(stream):
+        return _torch_mod.empty(shape, dtype=dtype, device=device)
+
+
 def _flat(t, dtype, dev, name, shape):
     """Pointer of a contiguous tensor of a shape on the call's device."""
     if not isinstance(t, _torch_mod.Tensor) or t.get_device() != dev:
@@ -952,11 +961,11 @@ def mq_rope_append(q, k, v, aq: float, zq: int, aqo: float, zqo: int, ak: float,
     torch = _torch_mod
     c, b, (G, D, _, _) = _kv_args(dev, k_cache, v_cache, starts, lens, pages)
     shape = T, HD = q.shape
-    H = HD // D
-    if H * D != HD:
+    if D == 0 or HD % D:
         raise ValueError("q's row length must be heads * D")
+    H = HD // D
     i16 = torch.int16
-    out = torch.empty((T, HD), dtype=i16, device=q.device) if out is None else out
+    out = _empty((T, HD), i16, q.device, stream) if out is None else out
     ptab, positions = None, 0
     if table is not None:
         positions = table.numel() // D
@@ -992,14 +1001,14 @@ def mq_paged_attn(q, q_scale: float, q_zp: int, k_cache, k_scale: float, v_cache
     torch = _torch_mod
     c, b, (G, D, B, keys) = _kv_args(dev, k_cache, v_cache, starts, lens, pages)
     shape = T, HD = q.shape
-    H = HD // D
-    if H * D != HD:
+    if D == 0 or HD % D:
         raise ValueError("q's row length must be heads * D")
+    H = HD // D
     odt = _act_dtype(out_bits)
-    out = torch.empty((T, HD), dtype=odt, device=q.device) if out is None else out
+    out = _empty((T, HD), odt, q.device, stream) if out is None else out
     if workspace is None:
         n = lib().mq_paged_attn_workspace_bytes(T, B, H, G, D, max_len or keys)
-        workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n > 0 else None
+        workspace = _empty(n, torch.uint8, q.device, stream) if n > 0 else None
     ws, ws_bytes = (None, 0) if workspace is None else \
         (_flat(workspace, torch.uint8, dev, "workspace", workspace.shape), workspace.numel())
     _check(lib().mq_paged_attn(*_rows(q, torch.int16, dev, "q", shape), T, H, q_scale, q_zp, c,
@@ -1031,10 +1040,9 @@ def mq_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, a
         raise ValueError("logits must be a float32 or int16 tensor [M][V]")
     M, V = shape = logits.shape
     per_row = (M,)
-    out = torch.empty(M, dtype=i32, device=logits.device) if out is None else out
+    out = _empty(M, i32, logits.device, stream) if out is None else out
     if workspace is None:
-        workspace = torch.empty(mq_sample_workspace_bytes(M, V), dtype=torch.uint8,
-                                device=logits.device)
+        workspace = _empty(mq_sample_workspace_bytes(M, V), torch.uint8, logits.device, stream)
     ptr, ld = _rows(logits, dt, dev, "logits", shape)
     _check(lib().mq_sample(
         ptr, 32 if dt is f32 else 16, M, V, ld, alpha, zp,

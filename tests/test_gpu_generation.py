@@ -113,6 +113,29 @@ def test_append_many_sequences():
     _append_case(rng, 2, 1, 16, 16, list(new), list(rng.integers(1, 20, B)))
 
 
+@pytest.mark.parametrize("D", [112, 176, 208, 240])
+def test_append_heads_that_leave_lanes_idle(D):
+    rng = np.random.default_rng(D)
+    _append_case(rng, 7, 7, D, 16, [1, 20, 3], [5, 20, 30])
+    _append_case(rng, 7, 7, D, 16, [900, 3500], [950, 3500])  # a wave per token
+
+
+@pytest.mark.parametrize("fq,fqo,fk,fko", [
+    # codes that saturate: a scale ratio whose terms are too large for the
+    # short way, just below and far above
+    ((1.3e-3, 32767), (3.3e-4, -32768), (2.0, -32768), (0.51, 127)),
+    ((3.0e-2, -32768), (3.0e-4, 32767), (1.0e3, 5), (1.0e-3, -128)),
+    # powers of two without rotation: every second quotient is a tie
+    ((0.5, 0), (1.0, 3), (0.5, 1), (1.0, -7)),
+])
+@pytest.mark.parametrize("positions", [None, 0])
+def test_append_formats(monkeypatch, fq, fqo, fk, fko, positions):
+    for name, f in dict(QF=fq, QO=fqo, KF=fk, KO=fko).items():
+        monkeypatch.setitem(globals(), name, f)
+    rng = np.random.default_rng(11)
+    _append_case(rng, 4, 2, 64, 16, [20, 1, 3], [20, 40, 30], positions=positions)
+
+
 def test_append_equals_rope_apply():
     """A prompt's rotation is mq_rope_apply's, bit for bit."""
     mq = _mq()
