@@ -7,6 +7,9 @@
 
 namespace mq {
 
+// Work-groups of a launch are fewer (of 256 threads, whose number is below 2^32).
+constexpr int64_t kMaxBlocks = (int64_t)1 << 24;
+
 struct KvArgs {
     int8_t* k;             // [pages][G][page][D]
     int8_t* v;             // [pages][G][D][page]

@@ -321,7 +321,7 @@ hipError_t launch_rope_append(const KvArgs& kv, const int16_t* q, int64_t ldq, c
     p.v_chunks = (kv.G * kv.D + 255) / 256;
     const int64_t tiles = T / 16 + 2 * (int64_t)kv.B;
     const int64_t blocks = p.rot + tiles * p.v_chunks;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+    if (blocks >= kMaxBlocks) return hipErrorInvalidConfiguration;
     if (vec) rope_append_kernel<true><<<(unsigned)blocks, 256, 0, s>>>(p);
     else rope_append_kernel<false><<<(unsigned)blocks, 256, 0, s>>>(p);
     return hipGetLastError();

@@ -63,6 +63,12 @@ mq_status kv_validate(const mq_kv_cache* c, const mq_kv_batch* b, int64_t T, int
     return MQ_OK;
 }
 
+// (a launch over more work-groups than there may be is refused before it)
+mq_status kv_launched(hipError_t e)
+{
+    return e == hipErrorInvalidConfiguration ? MQ_ERR_UNSUPPORTED : from_hip(e);
+}
+
 bool row_stride_ok(int64_t ld, int64_t row) { return ld >= row && ld < ((int64_t)1 << 40); }
 
 }  // namespace
@@ -775,9 +781,9 @@ mq_status mq_rope_append(const int16_t* q, int64_t ldq, const int16_t* k, int64_
     if (angles && (positions < 0 || positions > ((int64_t)1 << 40))) return MQ_ERR_INVALID_ARG;
     if (T == 0 || batch->B == 0) return MQ_OK;
     if (!q || !k || !v || !q_out) return MQ_ERR_INVALID_ARG;
-    return from_hip(mq::launch_rope_append(kv, q, ldq, k, ldk, v, ldv, T, H, aq, zq, aqo, zqo, ak,
-                                           zk, ako, zko, angles, positions, q_out, ldo,
-                                           as_stream(stream)));
+    return kv_launched(mq::launch_rope_append(kv, q, ldq, k, ldk, v, ldv, T, H, aq, zq, aqo, zqo,
+                                              ak, zk, ako, zko, angles, positions, q_out, ldo,
+                                              as_stream(stream)));
 }
 
 int64_t mq_paged_attn_workspace_bytes(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D,
@@ -812,10 +818,10 @@ mq_status mq_paged_attn(const int16_t* q, int64_t ldq, int64_t T, int32_t H, flo
     if (T == 0 || batch->B == 0) return MQ_OK;
     if (!q || !y) return MQ_ERR_INVALID_ARG;
     if (max_len == 0) max_len = batch->ld << kv.shift;
-    return from_hip(mq::launch_paged_attn(kv, q, ldq, T, H, q_scale, q_zp, k_scale, v_scale, v_zp,
-                                          logit_scale, window, sinks, out_scale, out_zp, out_bits,
-                                          y, ldy, max_len, workspace, workspace_bytes,
-                                          as_stream(stream)));
+    return kv_launched(mq::launch_paged_attn(kv, q, ldq, T, H, q_scale, q_zp, k_scale, v_scale,
+                                             v_zp, logit_scale, window, sinks, out_scale, out_zp,
+                                             out_bits, y, ldy, max_len, workspace, workspace_bytes,
+                                             as_stream(stream)));
 }
 
 int64_t mq_sample_workspace_bytes(int64_t M, int64_t V)

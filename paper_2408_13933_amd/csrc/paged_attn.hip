@@ -877,7 +877,7 @@ __global__ __launch_bounds__(NW < 4 ? 256 : 64 * NW) void paged_attn_join_kernel
     if (row >= p.T * p.H) return;
     const int w = wave % NW;
     const int64_t t = row / p.H;
-    if (t >= p.kv.starts[p.kv.B]) return;  // rows of no sequence
+    if (t < p.kv.starts[0] || t >= p.kv.starts[p.kv.B]) return;  // rows of no sequence
     const double* mz = p.mz + row * p.splits * 2;
     double m = (double)kNone, f[kMaxSplits / 64], z = 0.0;
 #pragma unroll
@@ -951,7 +951,7 @@ int64_t split_count(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D, int64
 }
 
 template <int ND>
-void launch_main(const AttnArgs& p, int64_t B, hipStream_t s)
+hipError_t launch_main(const AttnArgs& p, int64_t B, hipStream_t s)
 {
     constexpr int KS = (ND + 3) / 4;
     const int64_t parts = (int64_t)p.kv.G * p.splits;
@@ -961,12 +961,15 @@ void launch_main(const AttnArgs& p, int64_t B, hipStream_t s)
         const int64_t n = parts % 8 != 0 && 8 % parts == 0
                               ? 8 * ((tiles + 8 / parts - 1) / (8 / parts))
                               : tiles * parts;
+        if (n >= kMaxBlocks) return hipErrorInvalidConfiguration;
         paged_attn_tile_kernel<KS, ND><<<(unsigned)n, 256, 0, s>>>(p, tiles);
-        return;
+        return hipGetLastError();
     }
-    const dim3 grid((unsigned)row_tiles(p.T, B, p.grp, kRows), (unsigned)p.kv.G,
-                    (unsigned)p.splits);
+    const int64_t n = row_tiles(p.T, B, p.grp, kRows);
+    if (n >= kMaxBlocks) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)n, (unsigned)p.kv.G, (unsigned)p.splits);
     paged_attn_split_kernel<KS, ND><<<grid, 256, 0, s>>>(p);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -987,6 +990,7 @@ hipError_t launch_paged_attn(const KvArgs& kv, const int16_t* q, int64_t ldq, in
 {
     AttnArgs p;
     p.kv = kv;
+    if (kv.pages == 0) p.kv.ld = 0;  // no place: no block is looked at
     p.q = q;
     p.y = y;
     p.ldq = ldq;
@@ -1023,17 +1027,17 @@ hipError_t launch_paged_attn(const KvArgs& kv, const int16_t* q, int64_t ldq, in
     p.splits = (int32_t)splits;
     p.mz = static_cast<double*>(ws);
     p.sums = p.mz + T * H * splits * 2;
+    hipError_t e;
     switch ((kv.D + 31) / 32) {
-    case 1: launch_main<2>(p, kv.B, s); break;
-    case 2: launch_main<4>(p, kv.B, s); break;
-    case 3: launch_main<6>(p, kv.B, s); break;
-    case 4: launch_main<8>(p, kv.B, s); break;
-    case 5: launch_main<10>(p, kv.B, s); break;
-    case 6: launch_main<12>(p, kv.B, s); break;
-    case 7: launch_main<14>(p, kv.B, s); break;
-    default: launch_main<16>(p, kv.B, s); break;
+    case 1: e = launch_main<2>(p, kv.B, s); break;
+    case 2: e = launch_main<4>(p, kv.B, s); break;
+    case 3: e = launch_main<6>(p, kv.B, s); break;
+    case 4: e = launch_main<8>(p, kv.B, s); break;
+    case 5: e = launch_main<10>(p, kv.B, s); break;
+    case 6: e = launch_main<12>(p, kv.B, s); break;
+    case 7: e = launch_main<14>(p, kv.B, s); break;
+    default: e = launch_main<16>(p, kv.B, s); break;
     }
-    hipError_t e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
     const unsigned chunks = (unsigned)((kv.D + 63) / 64);
     const int64_t rows = T * H;

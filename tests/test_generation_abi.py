@@ -8,7 +8,7 @@ import pytest
 import paper_2408_13933_amd as mq
 
 NZ = 256  # aligned, never dereferenced
-INVALID = 1
+INVALID, UNSUPPORTED = 1, 2
 
 
 def _cache(**kw):
@@ -84,6 +84,15 @@ def test_append_refuses(kw):
 ])
 def test_attend_refuses(kw):
     assert attend(**kw) == INVALID
+
+
+def test_more_work_groups_than_a_launch_has():
+    many = (1 << 26) - 1
+    assert append(T=many) == UNSUPPORTED
+    assert append(batch=_batch(B=many)) == UNSUPPORTED
+    assert attend(batch=_batch(B=many)) == UNSUPPORTED
+    wide = dict(H=1024, ldq=1 << 14, ldy=1 << 14)
+    assert attend(T=1 << 20, cache=_cache(G=1024, D=16), **wide) == UNSUPPORTED
 
 
 def test_nothing_to_do():

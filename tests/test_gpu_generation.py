@@ -263,6 +263,50 @@ def test_attend_rows_that_see_nothing():
     assert (got[0:3] == -11).all() and (got[5:8] == -11).all() and (got[-1] == -11).all()
 
 
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("out_bits", [8, 16])
+def test_attend_cache_without_pages(new, out_bits):
+    """No page, or a page list without entries: every row gets the code of 0."""
+    import torch
+    mq = _mq()
+    H, G, D, B = 8, 2, 64, 3
+    i32 = dict(dtype=torch.int32, device="cuda")
+    q = torch.randint(-9000, 9000, (B * new, H * D), dtype=torch.int16, device="cuda")
+    starts, lens = torch.arange(B + 1, **i32) * new, torch.tensor([500, 40, 300], **i32)
+    for pages, entries in ((0, 32), (0, 0), (4, 0)):
+        kc = torch.ones((pages, G, 16, D), dtype=torch.int8, device="cuda")
+        vc = torch.ones((pages, G, D, 16), dtype=torch.int8, device="cuda")
+        table = torch.zeros((B, entries), **i32)
+        y = mq.mq_paged_attn(q, 1e-4, 0, kc, 0.05, vc, *VF, starts, lens, table, 0.125, 0.01, -11,
+                             out_bits)
+        assert (y == -11).all()
+        qo = mq.mq_rope_append(q, q[:, :G * D], kc.new_ones((B * new, G * D)), *QF, *QO, *KF, *KO,
+                               kc, vc, starts, lens, table)
+        assert (kc == 1).all() and (vc == 1).all() and qo.shape == q.shape
+
+
+def test_attend_rows_outside_the_sequences_are_left():
+    """Rows before the first sequence and behind the last keep what they hold,
+    also where the keys are split."""
+    import torch
+    mq = _mq()
+    H, G, D, B = 8, 2, 64, 2
+    i32 = dict(dtype=torch.int32, device="cuda")
+    q = torch.randint(-9000, 9000, (7, H * D), dtype=torch.int16, device="cuda")
+    kc = torch.randint(-100, 101, (64, G, 16, D), dtype=torch.int8, device="cuda")
+    vc = torch.randint(-100, 101, (64, G, D, 16), dtype=torch.int8, device="cuda")
+    table = torch.arange(128, **i32).reshape(2, 64) % 64
+    assert mq.mq_paged_attn_workspace_bytes(7, B, H, G, D, 1024) > 0
+    y = torch.full((7, H * D), 77, dtype=torch.int8, device="cuda")
+    mq.mq_paged_attn(q, 1e-4, 0, kc, 0.05, vc, *VF, torch.tensor([2, 3, 5], **i32),
+                     torch.tensor([1000, 900], **i32), table, 0.125, 0.01, -11, 8, out=y)
+    assert (y[:2] == 77).all() and (y[5:] == 77).all()
+    z = torch.empty((3, H * D), dtype=torch.int8, device="cuda")
+    mq.mq_paged_attn(q[2:5], 1e-4, 0, kc, 0.05, vc, *VF, torch.tensor([0, 1, 3], **i32),
+                     torch.tensor([1000, 900], **i32), table, 0.125, 0.01, -11, 8, out=z)
+    assert torch.equal(y[2:5], z)
+
+
 def test_attend_extreme_codes_and_scales():
     """The largest logits that the formats allow (sums at the ends of 32
     bits), one dominant key, equal keys, tiny and large logit scales."""
