@@ -866,53 +866,62 @@ __global__ __launch_bounds__(256, KS == 1 ? 3 : KS == 2 ? 2 : 1) void paged_attn
         share_keys<KS, ND>(p, tile, g0, i0, i1, split, (MQ_LDS int8_t*)lds);
 }
 
-// Joins the splits: NW waves per row and 64 channels, each every NW-th split.
+// Joins the splits: NW waves per row and 64 channels, each every NW-th split
+// (up to 8, 64 or all of them).  Latency bounds it: the first eight sums are
+// read before the maxima they are weighed by are looked at.
 template <int NW>
 __global__ __launch_bounds__(NW < 4 ? 256 : 64 * NW) void paged_attn_join_kernel(AttnArgs p)
 {
     __shared__ double lds[NW][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     constexpr int units = NW < 4 ? 4 / NW : 1;
+    constexpr int slots = NW < 16 ? 1 : kMaxSplits / 64;  // of 64 splits
     const int64_t row = (int64_t)blockIdx.x * units + wave / NW;
     if (row >= p.T * p.H) return;
     const int w = wave % NW;
-    const int64_t t = row / p.H;
-    if (t < p.kv.starts[0] || t >= p.kv.starts[p.kv.B]) return;  // rows of no sequence
-    const double* mz = p.mz + row * p.splits * 2;
-    double m = (double)kNone, f[kMaxSplits / 64], z = 0.0;
-#pragma unroll
-    for (int i = 0; i < kMaxSplits / 64; ++i) {
-        f[i] = lane + 64 * i < p.splits ? mz[2 * (lane + 64 * i)] : (double)kNone;
-        m = fmax(m, f[i]);
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmax(m, __shfl_xor(m, o));
-#pragma unroll
-    for (int i = 0; i < kMaxSplits / 64; ++i) {
-        f[i] = exp2_poly(fmax(-p.tau * (m - f[i]), -1000.0));
-        if (lane + 64 * i < p.splits) z = __builtin_fma(f[i], mz[2 * (lane + 64 * i) + 1], z);
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o);
     const int32_t d = blockIdx.y * 64 + lane;
     const bool have = d < p.kv.D;
     const double* x = p.sums + row * p.splits * p.kv.D + (have ? d : 0);
+    const double* mz = p.mz + row * p.splits * 2;
+    double v[8], m[slots], f[slots], zs[slots];
+    auto load = [&](int i, int s0) {
+        const int end = min(64, p.splits - 64 * i);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (s0 + u * NW < end) v[u] = x[(int64_t)(64 * i + s0 + u * NW) * p.kv.D];
+    };
+#pragma unroll
+    for (int i = 0; i < slots; ++i) {
+        const int s = min(lane + 64 * i, p.splits - 1);
+        m[i] = mz[2 * s];
+        zs[i] = mz[2 * s + 1];
+    }
+    load(0, w);
+    const int64_t t = row / p.H;
+    if (t < p.kv.starts[0] || t >= p.kv.starts[p.kv.B]) return;  // rows of no sequence
+    double top = m[0], z = 0.0;
+#pragma unroll
+    for (int i = 1; i < slots; ++i) top = fmax(top, m[i]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmax(top, __shfl_xor(top, o));
+#pragma unroll
+    for (int i = 0; i < slots; ++i) {
+        f[i] = exp2_poly(fmax(-p.tau * (top - m[i]), -1000.0));
+        if (lane + 64 * i < p.splits) z = __builtin_fma(f[i], zs[i], z);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o);
     double acc = 0.0;
 #pragma unroll
-    for (int i = 0; i < kMaxSplits / 64; ++i) {
+    for (int i = 0; i < slots; ++i) {
         const int end = min(64, p.splits - 64 * i);
-        for (int s0 = w; s0 < end; s0 += 8 * NW) {  // eight loads in flight
-            double v[8];
+        for (int s0 = w; s0 < end; s0 += 8 * NW) {
+            if (i > 0 || s0 > w) load(i, s0);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int s = min(s0 + u * NW, end - 1);
-                v[u] = x[(int64_t)(64 * i + s) * p.kv.D];
-            }
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const double fs = __shfl(f[i], (s0 + u * NW) & 63);
-                if (s0 + u * NW < end) acc = __builtin_fma(fs, v[u], acc);
-            }
+            for (int u = 0; u < 8; ++u)
+                if (s0 + u * NW < end)
+                    acc = __builtin_fma(__shfl(f[i], s0 + u * NW), v[u], acc);
         }
     }
     if (NW > 1) {
