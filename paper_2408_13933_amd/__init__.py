@@ -862,19 +862,32 @@ def mq_probe_read(buf, blocks: int, waves: int, unroll: int = 8, sink=None, stre
 
 
 # The calls of a generated token are as small as the kernels behind them, so
-# these helpers look at each tensor once and build no ctypes objects (append
-# for one token: 11.8 us on the host with them, 7 without; the launch alone
-# takes 4).
+# these helpers look at each tensor once, in one condition that is taken apart
+# only where it fails, and build no ctypes objects.  Append for one token, 10
+# tensors: 9.8 us on the host, 4.4 of them the call and its launch; 10.6 with
+# a condition for each property, 12 with ctypes structures.
 _KV_CACHE, _KV_BATCH = struct.Struct("qqqiiixxxx"), struct.Struct("qqqqq")
+
+
+def _refuse(t, dtype, dev, name, shape=None, rows=False):
+    """Says what is wrong with a tensor."""
+    if not isinstance(t, _torch().Tensor) or t.get_device() != dev:
+        raise ValueError(f"{name} must be a GPU tensor on the current device, as the others")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    raise ValueError(f"{name} must be a view of contiguous rows that do not overlap" if rows else
+                     f"{name} must be contiguous")
 
 
 def _device_and_stream(t, name, stream):
     """The device of the call's tensors, which has to be the current one, and
     the handle of the stream to use."""
     torch = _torch_mod or _torch()
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    dev = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if dev < 0:
         raise ValueError(f"{name} must be a GPU tensor")
-    dev = t.get_device()
     if dev != torch.cuda.current_device() if _get_device is None else dev != _get_device():
         raise ValueError(f"{name} must be on the current device")
     if stream is None and _get_raw_stream is not None:
@@ -895,53 +908,60 @@ def _empty(shape, dtype, device, stream):
 
 def _flat(t, dtype, dev, name, shape):
     """Pointer of a contiguous tensor of a shape on the call's device."""
-    if not isinstance(t, _torch_mod.Tensor) or t.get_device() != dev:
-        raise ValueError(f"{name} must be a GPU tensor on the same device")
-    if t.dtype is not dtype:
-        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    if t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    return t.data_ptr()
+    try:
+        if (t.dtype is dtype and t.shape == shape and t.is_contiguous() and
+                t.get_device() == dev):
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _refuse(t, dtype, dev, name, shape)
+
+
+def _any_shape(t, dtype, dev, name):
+    """Pointer and elements of a contiguous tensor on the call's device."""
+    try:
+        if t.dtype is dtype and t.is_contiguous() and t.get_device() == dev:
+            return t.data_ptr(), t.numel()
+    except AttributeError:
+        pass
+    _refuse(t, dtype, dev, name)
 
 
 def _rows(t, dtype, dev, name, shape):
     """Pointer and row stride (elements) of a [rows][cols] view whose rows are
     contiguous."""
-    if not isinstance(t, _torch_mod.Tensor) or t.get_device() != dev:
-        raise ValueError(f"{name} must be a GPU tensor on the same device")
-    if t.dtype is not dtype:
-        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
-    rows, cols = shape
-    ld, step = t.stride()
-    if rows <= 1:
-        ld = cols
-    if (cols > 1 and step != 1) or ld < cols:
-        raise ValueError(f"{name} must be a view of contiguous rows that do not overlap")
-    return t.data_ptr(), ld
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == dev:
+            ld, step = t.stride()
+            rows, cols = shape
+            if step == 1 and ld >= cols:
+                return t.data_ptr(), ld
+            if (step == 1 or cols <= 1) and (ld >= cols or rows <= 1):
+                return t.data_ptr(), max(ld, cols)
+    except AttributeError:
+        pass
+    _refuse(t, dtype, dev, name, shape, rows=True)
 
 
-def _kv_args(dev, k_cache, v_cache, starts, lens, pages):
+def _kv_args(dev, q, k_cache, v_cache, starts, lens, pages):
     """The bytes of mq_kv_cache and mq_kv_batch for the cache tensors k
     [pages][G][page][D], v [pages][G][D][page] and the batch's int32 tensors,
-    and (G, D, B, keys that a page list holds)."""
+    and (G, D, heads of q, B, keys that a page list holds)."""
     i8, i32 = _torch_mod.int8, _torch_mod.int32
-    n, G, page, D = k_cache.shape
-    B, ld = pages.shape
-    c = _KV_CACHE.pack(_flat(k_cache, i8, dev, "k_cache", (n, G, page, D)),
+    try:
+        n, G, page, D = k_cache.shape
+        B, ld = pages.shape
+        _, row = q.shape
+    except (AttributeError, ValueError):
+        raise ValueError("k_cache must be [pages][G][page][D], pages [B][entries], q [T][H * D]")
+    if D == 0 or row % D:
+        raise ValueError("q's row length must be heads * D")
+    c = _KV_CACHE.pack(_any_shape(k_cache, i8, dev, "k_cache")[0],
                        _flat(v_cache, i8, dev, "v_cache", (n, G, D, page)), n, page, G, D)
     b = _KV_BATCH.pack(_flat(starts, i32, dev, "starts", (B + 1,)),
                        _flat(lens, i32, dev, "lens", (B,)),
-                       _flat(pages, i32, dev, "pages", (B, ld)), B, ld)
-    return c, b, (G, D, B, ld * page)
-
-
-def _kv_shapes(q, k_cache, pages):
-    if k_cache.dim() != 4 or pages.dim() != 2 or q.dim() != 2:
-        raise ValueError("k_cache must be [pages][G][page][D], pages [B][entries], q [T][H * D]")
+                       _any_shape(pages, i32, dev, "pages")[0], B, ld)
+    return c, b, G, D, row // D, B, ld * page
 
 
 def mq_rope_append(q, k, v, aq: float, zq: int, aqo: float, zqo: int, ak: float, zk: int,
@@ -955,25 +975,24 @@ def mq_rope_append(q, k, v, aq: float, zq: int, aqo: float, zqo: int, ak: float,
     place; rows [starts[b], starts[b+1]) belong to sequence b of length lens[b]
     (these tokens included) with page list pages[b].  table: fp64 angles of
     mq_rope_table from position 0 on (positions * D values), or None for no
-    rotation."""
-    _kv_shapes(q, k_cache, pages)
+    rotation.  Rows of out without a token are left as they were (those of a
+    new out hold anything)."""
     dev, st = _device_and_stream(q, "q", stream)
     torch = _torch_mod
-    c, b, (G, D, _, _) = _kv_args(dev, k_cache, v_cache, starts, lens, pages)
-    shape = T, HD = q.shape
-    if D == 0 or HD % D:
-        raise ValueError("q's row length must be heads * D")
-    H = HD // D
-    i16 = torch.int16
-    out = _empty((T, HD), i16, q.device, stream) if out is None else out
-    ptab, positions = None, 0
-    if table is not None:
-        positions = table.numel() // D
-        ptab = _flat(table, torch.float64, dev, "table", table.shape)
-    _check(lib().mq_rope_append(*_rows(q, i16, dev, "q", shape), *_rows(k, i16, dev, "k", (T, G * D)),
-                                *_rows(v, torch.int8, dev, "v", (T, G * D)), T, H, aq, zq, aqo, zqo,
-                                ak, zk, ako, zko, ptab, positions, c, b,
-                                *_rows(out, i16, dev, "out", shape), st), "mq_rope_append")
+    c, b, G, D, H, _, _ = _kv_args(dev, q, k_cache, v_cache, starts, lens, pages)
+    shape, i16 = q.shape, torch.int16
+    T, kv = shape[0], (shape[0], G * D)
+    pq, ldq = _rows(q, i16, dev, "q", shape)
+    pk, ldk = _rows(k, i16, dev, "k", kv)
+    pv, ldv = _rows(v, torch.int8, dev, "v", kv)
+    if out is None:
+        out = _empty(shape, i16, q.device, stream)
+    po, ldo = _rows(out, i16, dev, "out", shape)
+    pt, n = (None, 0) if table is None else _any_shape(table, torch.float64, dev, "table")
+    status = lib().mq_rope_append(pq, ldq, pk, ldk, pv, ldv, T, H, aq, zq, aqo, zqo, ak, zk, ako,
+                                  zko, pt, n // D, c, b, po, ldo, st)
+    if status:
+        raise MQError(status, "mq_rope_append")
     return out
 
 
@@ -990,31 +1009,33 @@ def mq_paged_attn(q, q_scale: float, q_zp: int, k_cache, k_scale: float, v_cache
                   out_zp: int, out_bits: int = 8, window: int = 0, sinks: int = 0,
                   max_len: int = 0, out=None, workspace=None, stream=None):
     """Attention of the new tokens' query codes q [T][H * D] over their
-    sequences' cached keys and values: the context codes [T][H * D].
+    sequences' cached keys and values: the context codes [T][H * D].  Rows of
+    out that belong to no sequence are left as they were (those of a new out
+    hold anything).
 
     Each row sees the keys at or before its position, with ``window`` > 0 only
     the last ``window`` of them and the first ``sinks``.  max_len: the longest
     sequence as far as the caller knows (0: what the page list holds).
     workspace: a uint8 tensor kept by the caller (allocated here if None)."""
-    _kv_shapes(q, k_cache, pages)
     dev, st = _device_and_stream(q, "q", stream)
     torch = _torch_mod
-    c, b, (G, D, B, keys) = _kv_args(dev, k_cache, v_cache, starts, lens, pages)
-    shape = T, HD = q.shape
-    if D == 0 or HD % D:
-        raise ValueError("q's row length must be heads * D")
-    H = HD // D
-    odt = _act_dtype(out_bits)
-    out = _empty((T, HD), odt, q.device, stream) if out is None else out
+    c, b, G, D, H, B, keys = _kv_args(dev, q, k_cache, v_cache, starts, lens, pages)
+    shape, odt = q.shape, _act_dtype(out_bits)
+    T = shape[0]
+    pq, ldq = _rows(q, torch.int16, dev, "q", shape)
+    if out is None:
+        out = _empty(shape, odt, q.device, stream)
+    po, ldo = _rows(out, odt, dev, "out", shape)
     if workspace is None:
         n = lib().mq_paged_attn_workspace_bytes(T, B, H, G, D, max_len or keys)
         workspace = _empty(n, torch.uint8, q.device, stream) if n > 0 else None
-    ws, ws_bytes = (None, 0) if workspace is None else \
-        (_flat(workspace, torch.uint8, dev, "workspace", workspace.shape), workspace.numel())
-    _check(lib().mq_paged_attn(*_rows(q, torch.int16, dev, "q", shape), T, H, q_scale, q_zp, c,
-                               k_scale, v_scale, v_zp, b, logit_scale, window, sinks, out_scale,
-                               out_zp, out_bits, *_rows(out, odt, dev, "out", shape), max_len, ws,
-                               ws_bytes, st), "mq_paged_attn")
+    ws, n = (None, 0) if workspace is None else \
+        _any_shape(workspace, torch.uint8, dev, "workspace")
+    status = lib().mq_paged_attn(pq, ldq, T, H, q_scale, q_zp, c, k_scale, v_scale, v_zp, b,
+                                 logit_scale, window, sinks, out_scale, out_zp, out_bits, po, ldo,
+                                 max_len, ws, n, st)
+    if status:
+        raise MQError(status, "mq_paged_attn")
     return out
 
 
@@ -1044,15 +1065,16 @@ def mq_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, a
     if workspace is None:
         workspace = _empty(mq_sample_workspace_bytes(M, V), torch.uint8, logits.device, stream)
     ptr, ld = _rows(logits, dt, dev, "logits", shape)
-    _check(lib().mq_sample(
+    ws, n = _any_shape(workspace, torch.uint8, dev, "workspace")
+    status = lib().mq_sample(
         ptr, 32 if dt is f32 else 16, M, V, ld, alpha, zp,
         None if temperature is None else _flat(temperature, f32, dev, "temperature", per_row),
         None if top_k is None else _flat(top_k, i32, dev, "top_k", per_row),
         None if top_p is None else _flat(top_p, f32, dev, "top_p", per_row),
         None if min_p is None else _flat(min_p, f32, dev, "min_p", per_row),
-        _flat(u, f32, dev, "u", per_row), _flat(out, i32, dev, "out", per_row),
-        _flat(workspace, torch.uint8, dev, "workspace", workspace.shape), workspace.numel(), st),
-        "mq_sample")
+        _flat(u, f32, dev, "u", per_row), _flat(out, i32, dev, "out", per_row), ws, n, st)
+    if status:
+        raise MQError(status, "mq_sample")
     return out
 
 
