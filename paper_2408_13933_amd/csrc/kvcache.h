@@ -51,4 +51,18 @@ __device__ inline int32_t find_seq(int32_t B, int64_t x, Key key)
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
+hipError_t launch_rope_append(const KvArgs& kv, const int16_t* q, int64_t ldq, const int16_t* k,
+                              int64_t ldk, const int8_t* v, int64_t ldv, int64_t T, int32_t H,
+                              float aq, int32_t zq, float aqo, int32_t zqo, float ak, int32_t zk,
+                              float ako, int32_t zko, const double* angles, int64_t positions,
+                              int16_t* q_out, int64_t ldo, hipStream_t s);
+hipError_t launch_paged_attn(const KvArgs& kv, const int16_t* q, int64_t ldq, int64_t T, int32_t H,
+                             float q_scale, int32_t q_zp, float k_scale, float v_scale,
+                             int32_t v_zp, float logit_scale, int64_t window, int64_t sinks,
+                             float out_scale, int32_t out_zp, int32_t out_bits, void* y,
+                             int64_t ldy, int64_t max_len, void* ws, int64_t ws_bytes,
+                             hipStream_t s);
+int64_t paged_attn_workspace(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D,
+                             int64_t max_len);
+
 }  // namespace mq

@@ -7,6 +7,7 @@
 #include "kvcache.h"
 #include "mq.h"
 #include "mq_internal.h"
+#include "sample.h"
 
 namespace {
 

@@ -193,29 +193,6 @@ constexpr int kA16TileM = 128, kA16TileK = 64;
 hipError_t launch_transpose_i8(const int8_t* x, int64_t rows, int64_t cols, int64_t ldx,
                                int8_t* y, hipStream_t s);
 
-// The paged key/value cache (see kvcache.h).
-struct KvArgs;
-hipError_t launch_rope_append(const KvArgs& kv, const int16_t* q, int64_t ldq, const int16_t* k,
-                              int64_t ldk, const int8_t* v, int64_t ldv, int64_t T, int32_t H,
-                              float aq, int32_t zq, float aqo, int32_t zqo, float ak, int32_t zk,
-                              float ako, int32_t zko, const double* angles, int64_t positions,
-                              int16_t* q_out, int64_t ldo, hipStream_t s);
-hipError_t launch_paged_attn(const KvArgs& kv, const int16_t* q, int64_t ldq, int64_t T, int32_t H,
-                             float q_scale, int32_t q_zp, float k_scale, float v_scale,
-                             int32_t v_zp, float logit_scale, int64_t window, int64_t sinks,
-                             float out_scale, int32_t out_zp, int32_t out_bits, void* y,
-                             int64_t ldy, int64_t max_len, void* ws, int64_t ws_bytes,
-                             hipStream_t s);
-int64_t paged_attn_workspace(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D,
-                             int64_t max_len);
-
-// Workspace of launch_sample: for all rows (within its bound), or the least.
-int64_t sample_workspace(int64_t M, int64_t V, bool least);
-hipError_t launch_sample(const void* x, int32_t bits, int64_t M, int64_t V, int64_t ld, float alpha,
-                         int32_t zp, const float* temperature, const int32_t* top_k,
-                         const float* top_p, const float* min_p, const float* u, int32_t* tokens,
-                         void* ws, int64_t ws_bytes, hipStream_t s);
-
 hipError_t launch_qlinear_generic(const QLinearArgs& p, hipStream_t s);
 hipError_t launch_qlinear_decode(const QLinearArgs& p, hipStream_t s);
 // one token (M = 1, 8-bit codes): the vector-ALU GEMV the decode path takes

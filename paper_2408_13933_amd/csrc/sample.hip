@@ -17,10 +17,18 @@
 // 4. draw: a block per row finds the cut among the listed or gathered words,
 //    then the word; rows that neither serves (a top_k larger than the lists
 //    hold, thousands of equal logits at the cut) walk over the whole row.
+//
+// One reading of the logits bounds many rows, and the vector arithmetic of
+// the weights (25 instructions each, fp64) those that need them all; one row
+// is four launches, each its own latency.  us: 512 rows of 256000 fp32, settings
+// mixed, 104 + 40 + 38 + 25 (the scan 5.0 TB/s, all 2.6); 48 rows of 32000
+// codes, top_p, 5.2 + 8.0 + 7.5 + 11.7; one row of 256000, top_k, 5.3 + 1.7 + 1.7
+// + 10.7.  Rows of top_p over flat logits, 512 of 256000: 160 + 190 for the
+// second and third.
 #include <algorithm>
 
 #include "codes.h"
-#include "mq_internal.h"
+#include "sample.h"
 #include "wave.h"
 
 namespace mq {
