@@ -348,3 +348,41 @@ def test_attend_long_rows():
     """A long sequence of nearly equal logits: the weights keep their bits."""
     rng = np.random.default_rng(10)
     _attn_case(rng, 2, 1, 64, 64, [2], [70001], q_std=300, out_scale=1e-5)
+
+
+def test_offsets_past_32_bits():
+    """A cache and rows whose offsets need more than 32 bits: the same codes as
+    with a small cache and dense rows."""
+    mq = _mq()
+    import torch
+    H, G, D, page, B, new, before = 4, 2, 256, 128, 2, 20, 300
+    per, T = -(-(before + new) // page), B * new
+    g = torch.Generator(device="cuda").manual_seed(3)
+    i8, i16 = dict(dtype=torch.int8, device="cuda"), dict(dtype=torch.int16, device="cuda")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    small = [torch.randint(-100, 101, s, generator=g, **i8)
+             for s in ((B * per, G, page, D), (B * per, G, D, page))]
+    pages = torch.randperm(B * per, generator=g, device="cuda").to(torch.int32).reshape(B, per)
+    n = (1 << 32) // (G * page * D) + B * per  # 2^32 bytes and some pages
+    large = [torch.empty((n, *t.shape[1:]), **i8) for t in small]
+    for a, b in zip(large, small):
+        a[n - B * per:] = b
+    wide = (1 << 31) // T + H * D  # codes per row: the last rows' offsets in bytes need 33 bits
+    q, k = (torch.randint(-9000, 9001, (T, h * D), generator=g, **i16) for h in (H, G))
+    v = torch.randint(-100, 101, (T, G * D), generator=g, **i8)
+    qw = torch.empty((T, wide), **i16)[:, :H * D]
+    qw.copy_(q)
+    ow = torch.empty((T, wide), **i16)[:, :H * D]
+    yw = torch.empty((T, wide), **i16)[:, :H * D]
+    starts, lens = torch.arange(B + 1, **i32) * new, torch.tensor([before + new, 130], **i32)
+    table = mq.mq_rope_table(before + new, D)
+    got = []
+    for (kc, vc), pg, x, o, y in ((small, pages, q, None, None),
+                                  (large, pages + (n - B * per), qw, ow, yw)):
+        r = mq.mq_rope_append(x, k, v, *QF, *QO, *KF, *KO, kc, vc, starts, lens, pg, table=table,
+                              out=o)
+        c = mq.mq_paged_attn(r, *QO, kc, KO[0], vc, *VF, starts, lens, pg, 1e-3, 1e-3, 5, 16, out=y)
+        got.append((r.clone(), c.clone(), kc[-B * per:].clone(), vc[-B * per:].clone()))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    assert len(torch.unique(got[0][1])) > 100

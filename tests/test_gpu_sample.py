@@ -194,3 +194,22 @@ def test_frequencies():
     count = np.bincount(y, minlength=V)
     # a grid of M points puts M * prob, give or take one, into an interval
     assert (np.abs(count - M * prob) <= 1 + 1e-3).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "int16"])
+def test_rows_past_32_bits(dtype):
+    """Rows whose offsets in words need more than 32 bits."""
+    mq = _mq()
+    import torch
+    M, V, ld = 4, 5000, 1_500_000_000
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randint(-3000, 3001, (M, V), generator=g, device="cuda").to(getattr(torch, dtype))
+    w = torch.empty((M, ld), dtype=x.dtype, device="cuda")[:, :V]
+    w.copy_(x)
+    u = torch.rand(M, generator=g, device="cuda")
+    t = torch.full((M,), 900.0, device="cuda")
+    kw = dict(temperature=t, top_p=torch.tensor([1.0, 0.9, 0.5, 1.0], device="cuda"),
+              top_k=torch.tensor([0, 0, 700, 20], dtype=torch.int32, device="cuda"))
+    want = mq.mq_sample(x, u, **kw)
+    assert torch.equal(mq.mq_sample(w, u, **kw), want)
+    assert len(set(want.tolist())) == M
