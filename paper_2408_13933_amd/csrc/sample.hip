@@ -22,7 +22,7 @@
 // the weights (25 instructions each, fp64) those that need them all; one row
 // is four launches, each its own latency.  us: 512 rows of 256000 fp32, settings
 // mixed, 104 + 40 + 38 + 25 (the scan 5.0 TB/s, all 2.6); 48 rows of 32000
-// codes, top_p, 5.2 + 8.0 + 7.5 + 11.7; one row of 256000, top_k, 5.3 + 1.7 + 1.7
+// codes, top_p, 5.2 + 8.0 + 7.5 + 10.3; one row of 256000, top_k, 5.3 + 1.7 + 1.7
 // + 10.7.  Rows of top_p over flat logits, 512 of 256000: 160 + 190 for the
 // second and third.
 #include <algorithm>
@@ -975,24 +975,32 @@ __device__ __forceinline__ int32_t draw_by_segments(const SampleArgs& a, const R
 
 // A wave's lists of one turn, all loads under way at once.
 constexpr int kTurn = 16;
+__device__ __forceinline__ int draw_wave()
+{
+    return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+}
+// Lanes below this one in a mask.
+__device__ __forceinline__ int lanes_below(uint64_t mask)
+{
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32),
+                                          __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
 struct Lists {
     uint2 e[kTurn];
-    uint32_t n;  // lane i: of list i
+    uint32_t n;  // lane i: of list i (0 past the wave's)
+    int lists;   // of this wave in the turn
     __device__ __forceinline__ void load(const SampleArgs& a, int64_t m, int s0)
     {
-        const int lane = threadIdx.x & 63, first = s0 + (threadIdx.x >> 6) * kTurn;
-        n = a.info[m * a.segs + min(first + (lane & (kTurn - 1)), a.segs - 1)].z;
+        // neighbouring lists, as many for each wave
+        const int lane = threadIdx.x & 63, left = min(a.segs - s0, kTurn * kDrawWaves);
+        const int each = (left + kDrawWaves - 1) / kDrawWaves, first = s0 + draw_wave() * each;
+        lists = min(max(s0 + left - first, 0), each);
+        const int64_t at = m * a.segs + min(first, a.segs - 1);
+        n = lane < lists ? a.info[at + lane].z : 0;
+        // (places past the list's words: anything)
 #pragma unroll
-        for (int i = 0; i < kTurn; ++i) {
-            const int64_t s = m * a.segs + min(first + i, a.segs - 1);
-            e[i] = a.list[s * kList + lane];  // places past the list's words: anything
-        }
-        if (first + (lane & (kTurn - 1)) >= a.segs) n = 0;
-    }
-    __device__ __forceinline__ bool has(int i, uint32_t bound) const
-    {
-        return (threadIdx.x & 63) < (uint32_t)__builtin_amdgcn_readlane((int)n, i) &&
-               e[i].x >= bound;
+        for (int i = 0; i < kTurn; ++i)
+            if ((i & ~3) < lists) e[i] = a.list[(at + min(i, max(lists - 1, 0))) * kList + lane];
     }
 };
 
@@ -1001,30 +1009,39 @@ struct Lists {
 __device__ __forceinline__ int64_t store_lists(const SampleArgs& a, int64_t m, uint32_t bound,
                                                Lists& t, DrawLds& lds)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    const int lane = threadIdx.x & 63, wave = draw_wave();
     int64_t n = 0;
     for (int s0 = 0; s0 < a.segs; s0 += kTurn * kDrawWaves) {
         if (s0) t.load(a, m, s0);
+        uint64_t hit[kTurn];
         int mine = 0;
 #pragma unroll
-        for (int i = 0; i < kTurn; ++i) mine += __popcll(__ballot(t.has(i, bound)));
+        for (int i = 0; i < kTurn; ++i)
+            if ((i & ~3) < t.lists) {  // (four at a time)
+                hit[i] = __ballot(lane < __builtin_amdgcn_readlane((int)t.n, i) &&
+                                  t.e[i].x >= bound);
+                mine += __popcll(hit[i]);
+            }
         __syncthreads();
         if (lane == 0) lds.wave32[wave] = mine;
         __syncthreads();
-        int64_t at = n;
+        int before = 0, all = 0;
 #pragma unroll
         for (int w = 0; w < kDrawWaves; ++w) {
-            if (w < wave) at += lds.wave32[w];
-            n += lds.wave32[w];
+            before += w < wave ? lds.wave32[w] : 0;
+            all += lds.wave32[w];
         }
+        // (places past the last: not stored; n stays below 2^22)
+        int at = __builtin_amdgcn_readfirstlane((int)n + before);
 #pragma unroll
-        for (int i = 0; i < kTurn; ++i) {
-            const uint64_t hit = __ballot(t.has(i, bound));
-            const int64_t to = at + __popcll(hit & below);
-            if (t.has(i, bound) && to < kEntries) lds.word[to] = order(t.e[i].x, t.e[i].y);
-            at += __popcll(hit);
-        }
+        for (int i = 0; i < kTurn; ++i)
+            if ((i & ~3) < t.lists) {
+                const int to = at + lanes_below(hit[i]);
+                if (((hit[i] >> lane) & 1) && to < kEntries)
+                    lds.word[to] = order(t.e[i].x, t.e[i].y);
+                at += __popcll(hit[i]);
+            }
+        n += all;
     }
     __syncthreads();
     return n;
@@ -1040,18 +1057,17 @@ template <class F>
 __device__ __forceinline__ int32_t draw_few(const SampleArgs& a, const Row& r, DrawLds& lds, int n,
                                             int32_t bin, int few, double mass, double u)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    const int tid = threadIdx.x, lane = tid & 63, wave = draw_wave();
     // the words of these bins, in index order
-    constexpr int turns = kEntries / kDrawThreads;
+    static_assert(kEntries / kDrawThreads <= 32, "a bit per turn");
     const int32_t part = ((n + kDrawWaves - 1) / kDrawWaves + 63) & ~63;
     const int32_t i0 = min(wave * part, n), i1 = min(i0 + part, n);
     uint32_t mine = 0;  // bit j: the lane's word of turn j is one of them
     int cnt = 0;
-#pragma unroll
-    for (int j = 0; j < turns; ++j) {
+#pragma unroll 1
+    for (int j = 0; i0 + 64 * j < i1; ++j) {
         const int32_t i = i0 + 64 * j + lane;
-        const bool here = i < i1 && bin_of<F>(r, key_of(lds.word[i])) <= bin;
+        const bool here = i < i1 && bin_of<F>(r, key_of(lds.word[min(i, n - 1)])) <= bin;
         mine |= (uint32_t)here << j;
         cnt += __popcll(__ballot(here));
     }
@@ -1065,10 +1081,11 @@ __device__ __forceinline__ int32_t draw_few(const SampleArgs& a, const Row& r, D
     int at = 0;
 #pragma unroll
     for (int w = 0; w < kDrawWaves; ++w) at += w < wave ? lds.wave32[w] : 0;
-#pragma unroll
-    for (int j = 0; j < turns; ++j) {
-        const uint64_t hit = __ballot((mine >> j) & 1);
-        if ((mine >> j) & 1) lds.near[at + __popcll(hit & below)] = lds.word[i0 + 64 * j + lane];
+#pragma unroll 1
+    for (int j = 0; i0 + 64 * j < i1; ++j) {
+        const bool here = (mine >> j) & 1;
+        const uint64_t hit = __ballot(here);
+        if (here) lds.near[at + lanes_below(hit)] = lds.word[i0 + 64 * j + lane];
         at += __popcll(hit);
     }
     __syncthreads();
