@@ -282,3 +282,65 @@ def test_stream_other_than_the_current_one():
         side.synchronize()
         assert torch.equal(got, want)
         torch.cuda.synchronize()
+
+
+def test_binding_refuses():
+    """Tensors of another type, shape, layout or device, and streams of another
+    device, are refused before anything is launched."""
+    import types
+
+    import torch
+    model = Model(2, 64)
+    mq = model.mq
+    i32 = dict(dtype=torch.int32, device="cuda")
+    base = dict(q=torch.zeros((3, H * D), dtype=torch.int16, device="cuda"),
+                k=torch.zeros((3, G * D), dtype=torch.int16, device="cuda"),
+                v=torch.zeros((3, G * D), dtype=torch.int8, device="cuda"), kc=model.kc,
+                vc=model.vc, starts=torch.tensor([0, 1, 3], **i32),
+                lens=torch.tensor([5, 9], **i32), pages=model.pages, table=model.table, out=None,
+                stream=None, ws=None, logits=torch.zeros((2, 50), device="cuda"),
+                u=torch.zeros(2, device="cuda"), t=None, k0=None, tok=None)
+
+    def append(a):
+        return mq.mq_rope_append(a.q, a.k, a.v, *QF, *QO, *KF, *KO, a.kc, a.vc, a.starts, a.lens,
+                                 a.pages, table=a.table, out=a.out, stream=a.stream)
+
+    def attend(a):
+        return mq.mq_paged_attn(a.q, *QO, a.kc, KO[0], a.vc, *VF, a.starts, a.lens, a.pages, 0.125,
+                                *OF, 16, out=a.out, workspace=a.ws, stream=a.stream)
+
+    def sample(a):
+        return mq.mq_sample(a.logits, a.u, temperature=a.t, top_k=a.k0, out=a.tok,
+                            workspace=a.ws, stream=a.stream)
+
+    cuda = dict(device="cuda")
+    other = types.SimpleNamespace(device_index=torch.cuda.current_device() + 1, cuda_stream=0)
+    both = [dict(q=base["q"].cpu()), dict(q=None), dict(q=base["q"].float()), dict(q=base["q"][0]),
+            dict(q=base["q"][:, :-1]), dict(q=base["q"].t().contiguous().t()),
+            dict(kc=base["kc"].cpu()), dict(kc=base["kc"].to(torch.int16)),
+            dict(kc=base["kc"].transpose(2, 3)), dict(vc=model.kc), dict(vc=None),
+            dict(starts=base["starts"][:2]), dict(starts=base["starts"].long()),
+            dict(lens=base["starts"]), dict(lens=[5, 9]), dict(pages=base["pages"][:1]),
+            dict(pages=base["pages"].t()), dict(out=base["q"][:2]), dict(out=base["v"]),
+            dict(stream=other)]
+    cases = {append: both + [dict(k=base["q"]), dict(v=base["k"]), dict(v=base["v"].cpu()),
+                             dict(table=base["table"].float()), dict(table=base["table"].cpu())],
+             attend: both + [dict(ws=torch.zeros(512, **cuda)),
+                             dict(ws=torch.zeros(512, dtype=torch.uint8))],
+             sample: [dict(logits=base["logits"].cpu()), dict(logits=base["logits"].half()),
+                      dict(logits=base["logits"][0]), dict(logits=base["logits"].t()),
+                      dict(u=base["u"][:1]), dict(u=base["u"].double()), dict(u=None),
+                      dict(t=torch.zeros(3, **cuda)), dict(k0=torch.zeros(2, **cuda)),
+                      dict(k0=torch.zeros(2, dtype=torch.int64, **cuda)),
+                      dict(tok=torch.zeros(2, dtype=torch.int64, **cuda)),
+                      dict(tok=torch.zeros(2, dtype=torch.int32)),
+                      dict(ws=torch.zeros(512, **cuda)), dict(stream=other)]}
+    for call, wrong in cases.items():
+        call(types.SimpleNamespace(**base))
+        for kw in wrong:
+            with pytest.raises(ValueError):
+                call(types.SimpleNamespace(**{**base, **kw}))
+    small = torch.zeros(512, dtype=torch.uint8, **cuda)
+    with pytest.raises(mq.MQError):  # less than a row's
+        sample(types.SimpleNamespace(**{**base, "ws": small}))
+    torch.cuda.synchronize()
