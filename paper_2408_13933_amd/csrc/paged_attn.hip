@@ -587,13 +587,20 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
     }
 }
 
-// The code of a row's channel from its sums.
-__device__ inline int32_t out_code(const AttnArgs& p, double s, double z)
+// The code of a row's channel, y / out_scale = (sum f S - v_zp z) unit with
+// unit = v_scale / (z out_scale): one division per row, three roundings to
+// 2^-53.  With a division by z and one by out_scale per channel a prompt of
+// 1024 took 26.7 us instead of 25.0, one token of 8 heads of 256 over 30 keys
+// 14.7 instead of 13.2.
+__device__ inline double out_unit(const AttnArgs& p, double z)
 {
-#pragma clang fp contract(off)
-    const double v = z > 0.0 ? p.v_scale * (s - (double)p.v_zp * z) / z : 0.0;
-    return p.out_bits == 8 ? requant_f64<8>(v, p.out_scale, p.out_zp)
-                           : requant_f64<16>(v, p.out_scale, p.out_zp);
+    return z > 0.0 ? p.v_scale / (z * p.out_scale) : 0.0;
+}
+__device__ inline int32_t out_code(const AttnArgs& p, double s, double z, double unit)
+{
+    const double t = limit_quotient(__builtin_fma(-(double)p.v_zp, z, s) * unit);
+    const int32_t q = rint_low(t + kRintShift) + p.out_zp;
+    return p.out_bits == 8 ? clamp_code<8>(q) : clamp_code<16>(q);
 }
 
 __device__ inline void store_out(const AttnArgs& p, int64_t t, int32_t head, int32_t d, int32_t q)
@@ -669,8 +676,10 @@ struct RowAt {
 };
 
 // Four waves share 16 rows and take every fourth block of [i0, i1); their
-// states are joined through LDS.
-template <int KS, int ND>
+// states are joined through LDS, J output tiles at a time.
+template <int J>
+constexpr int kJoinDoubles = J * kWaves * 4 * 64 + kWaves * kRows * 3 / 2;
+template <int KS, int ND, int J>
 __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g0, int32_t i0,
                                   int32_t i1, int split, double* lds)
 {
@@ -695,7 +704,7 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
         }
     }
 
-    double* lz = lds + kWaves * 4 * 64;                                  // [wave][row]
+    double* lz = lds + J * kWaves * 4 * 64;                              // [wave][row]
     int32_t* lm = reinterpret_cast<int32_t*>(lz + kWaves * kRows);       // [wave][row]
     if (g == 0) {
         lm[wave * kRows + r] = st.m;
@@ -715,20 +724,28 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
         p.mz[2 * at] = (double)m;
         p.mz[2 * at + 1] = z;
     }
+    const double unit = out_unit(p, z);
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt) {
-        if (16 * dt >= p.kv.D) break;
+    for (int d0 = 0; d0 < ND; d0 += J) {
+        if (16 * d0 >= p.kv.D) break;
+        if (d0) __syncthreads();
+#pragma unroll
+        for (int e = 0; e < J && d0 + e < ND; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                lds[((e * kWaves + wave) * 4 + i) * 64 + lane] = f * st.acc[d0 + e][i];
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) lds[(wave * 4 + i) * 64 + lane] = f * st.acc[dt][i];
-        __syncthreads();
-        double s = 0.0;
+        for (int e = 0; e < J && d0 + e < ND; ++e) {
+            double s = 0.0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) s += lds[(w * 4 + wave) * 64 + lane];
-        if (!row.have) continue;
-        const int32_t d = 16 * dt + 4 * g + wave;
-        if (p.splits > 1) p.sums[at * p.kv.D + d] = s;
-        else store_out(p, row.t, row.head, d, out_code(p, s, z));
+            for (int w = 0; w < kWaves; ++w) s += lds[((e * kWaves + w) * 4 + wave) * 64 + lane];
+            const int32_t d = 16 * (d0 + e) + 4 * g + wave;
+            if (row.have && d < p.kv.D) {
+                if (p.splits > 1) p.sums[at * p.kv.D + d] = s;
+                else store_out(p, row.t, row.head, d, out_code(p, s, z, unit));
+            }
+        }
     }
 }
 
@@ -784,12 +801,13 @@ __device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g
         }
         return;
     }
+    const double unit = out_unit(p, st.z);
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) {
         if (16 * dt >= p.kv.D) break;
         int32_t q[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = out_code(p, st.acc[dt][i], st.z);
+        for (int i = 0; i < 4; ++i) q[i] = out_code(p, st.acc[dt][i], st.z, unit);
         const int32_t d = 16 * dt + 4 * g;
         const int64_t at = row.t * p.ldy + (int64_t)row.head * p.kv.D + d;
         if (!p.vec_y) {
@@ -820,12 +838,13 @@ __device__ inline void split_range(const AttnArgs& p, const Tile& t, int split, 
 template <int KS, int ND>
 __global__ __launch_bounds__(256, KS == 1 ? 3 : KS == 2 ? 2 : 1) void paged_attn_split_kernel(AttnArgs p)
 {
-    __shared__ double lds[kWaves * 4 * 64 + kWaves * kRows * 3 / 2];
+    constexpr int J = ND < 4 ? ND : 4;
+    __shared__ double lds[kJoinDoubles<J>];
     Tile tile;
     if (!find_tile<kRows>(p, blockIdx.x, tile)) return;
     int32_t i0, i1;
     split_range(p, tile, blockIdx.z, i0, i1);
-    split_rows<KS, ND>(p, tile, blockIdx.y, i0, i1, blockIdx.z, lds);
+    split_rows<KS, ND, J>(p, tile, blockIdx.y, i0, i1, blockIdx.z, lds);
 }
 
 // Work-groups go to the eight XCDs in turn, each with an L2 of its own: those
@@ -878,7 +897,7 @@ __global__ __launch_bounds__(256, KS == 1 ? 3 : KS == 2 ? 2 : 1) void paged_attn
     int32_t i0, i1;
     split_range(p, tile, split, i0, i1);
     if (tile.rows - tile.row0 <= kRows)
-        split_rows<KS, ND>(p, tile, g0, i0, i1, split, reinterpret_cast<double*>(lds));
+        split_rows<KS, ND, 1>(p, tile, g0, i0, i1, split, reinterpret_cast<double*>(lds));
     else
         share_keys<KS, ND>(p, tile, g0, i0, i1, split, (MQ_LDS int8_t*)lds);
 }
@@ -949,7 +968,7 @@ __global__ __launch_bounds__(NW < 4 ? 256 : 64 * NW) void paged_attn_join_kernel
 #pragma unroll
         for (int i = 0; i < NW; ++i) acc += lds[i][lane];
     }
-    if (have) store_out(p, t, (int32_t)(row % p.H), d, out_code(p, acc, z));
+    if (have) store_out(p, t, (int32_t)(row % p.H), d, out_code(p, acc, z, out_unit(p, z)));
 }
 
 // Row tiles of all sequences, at most.
