@@ -303,6 +303,8 @@ __device__ inline int32_t value_tile(const AttnArgs& p, int dt)
 // Fragments of a block straight from the cache.
 template <int KS>
 struct FromCache {
+    // one wave per SIMD: registers for reads well ahead
+    static constexpr bool kAhead = KS >= 3;
     const MQ_GLOBAL int8_t* k[2];
     const MQ_GLOBAL int8_t* v[2];
     const AttnArgs& p;
@@ -336,6 +338,7 @@ struct FromCache {
 // then values (h, dt).
 template <int KS, int ND>
 struct FromLds {
+    static constexpr bool kAhead = false;
     const MQ_LDS int8_t* at;  // of this lane
     __device__ FromLds again() const
     {
@@ -412,7 +415,7 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
     // next ones' fragments read before these are multiplied
     v4i c[2][4];
     {
-        constexpr int J = 2, N = 8 / J;
+        constexpr int J = Source::kAhead ? 4 : 2, N = 8 / J;
         v4i kf[2][J][KS];
 #pragma unroll
         for (int n = 0; n <= N; ++n) {
@@ -456,6 +459,24 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
             }
     }
 
+    // the values' fragments: some from here on, or the first of them before the
+    // last of the weights
+    constexpr int E = 2, NV = ND / E;  // output tiles at once
+    constexpr int kGroups = Source::kAhead ? 4 : 2;
+    v4i v[kGroups][E][2];
+    auto read_values = [&](int n) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            v[n % kGroups][e][0] = src.value(0, n * E + e);
+            v[n % kGroups][e][1] = src.value(1, n * E + e);
+        }
+    };
+    if constexpr (Source::kAhead) {
+#pragma unroll
+        for (int n = 0; n < kGroups; ++n) read_values(n);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+
     // the largest that the row sees, without what has no place
     const uint32_t placed = (uint32_t)__ballot(pages >= 0) & 0xff;
     const bool mask = !full || placed != 0xff;
@@ -489,16 +510,7 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
     const int32_t m_new = max(st.m, m);
     const double f = factor(p, m_new, m);
 
-    // weights; the first values' fragments are read before the last of them
-    constexpr int E = 2;  // output tiles at once
-    v4i v[2][E][2];
-    auto read_values = [&](int n) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            v[n & 1][e][0] = src.value(0, n * E + e);
-            v[n & 1][e][1] = src.value(1, n * E + e);
-        }
-    };
+    // weights
     v4i wh[2], wl[2];
     // so many weights begin before the last so many end (registers for three
     // waves per SIMD where the state is small)
@@ -515,7 +527,7 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
                     p.tau, min((uint32_t)m - (uint32_t)c[x >> 4][(x >> 2) & 3][x & 3], p.d_cut));
             }
         }
-        if (n == N) read_values(0);
+        if (!Source::kAhead && n == N) read_values(0);
         __builtin_amdgcn_sched_barrier(0);
         if (n == 0) continue;
 #pragma unroll
@@ -563,12 +575,12 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
         st.z = __builtin_fma(f, (double)((hi[0] << 8) + lo[0]), st.z);
     }
 #pragma unroll
-    for (int n = 0; n < ND / E; ++n) {
-        if (n + 1 < ND / E) {
+    for (int n = 0; n < NV; ++n) {
+        if (!Source::kAhead && n + 1 < NV) {
             read_values(n + 1);
             __builtin_amdgcn_sched_barrier(0);
         }
-        const auto& x = v[n & 1];
+        const auto& x = v[n % kGroups];
         v4i hi[E], lo[E];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -577,6 +589,7 @@ __device__ inline void attend_block(const AttnArgs& p, const WeightTable& table,
                 hi[e] = mfma(x[e][h], wh[h], h ? hi[e] : zero);
                 lo[e] = mfma(x[e][h], wl[h], h ? lo[e] : zero);
             }
+        if (Source::kAhead && n + kGroups < NV) read_values(n + kGroups);
 #pragma unroll
         for (int e = 0; e < E; ++e)
 #pragma unroll
