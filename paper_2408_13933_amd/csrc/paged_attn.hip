@@ -25,9 +25,9 @@
 // that need no registers, and a CU's two work-groups overlap.  Few rows are one
 // wave's, so the keys are split instead, among four waves and among work-groups.
 // us, kernel (and join): one token over 1531 keys, 32 heads of 64 on 4, 7.6
-// (3.2); 64 tokens over up to 4096, 67 MB, 23 (4.8); 2 over up to 120000, 8
-// heads of 256 on 1, 61 MB, 28.9 (5.4); 24 windows of 1000, 46 MB, 23; a prompt
-// of 1024, 26; 500 tokens over 16000, 32 heads of 128 on 8, 280 (15): 0.9 POP/s
+// (3.2); 64 tokens over up to 4096, 67 MB, 21 (4.8); 2 over up to 120000, 8
+// heads of 256 on 1, 61 MB, 26 (5.4); 24 windows of 1000, 46 MB, 21; a prompt
+// of 1024, 25; 500 tokens over 16000, 32 heads of 128 on 8, 272 (14): 0.95 POP/s
 // of int8 products.
 #include <algorithm>
 #include <cmath>
@@ -303,7 +303,10 @@ __device__ inline int32_t value_tile(const AttnArgs& p, int dt)
 // Fragments of a block straight from the cache.
 template <int KS>
 struct FromCache {
-    // one wave per SIMD: registers for reads well ahead
+    // One wave per SIMD: registers for reads well ahead.  Four key tiles at once
+    // and eight value tiles from the weights on took 2 sequences of 120000 keys
+    // from 34.1 us to 31.6 (all sixteen: 33.6); with three waves per SIMD there
+    // are no registers for it (spills).
     static constexpr bool kAhead = KS >= 3;
     const MQ_GLOBAL int8_t* k[2];
     const MQ_GLOBAL int8_t* v[2];
