@@ -820,8 +820,9 @@ __device__ __forceinline__ Cut cut_row(const SampleArgs& a, const Row& r, const 
         const uint32_t bin = lds.sel[0];
         n0 = lds.sel64[0];
         m0 = lds.sel64[1];
-        hi = hi - (bin << shift);
-        lo = max(lo, hi - ((1u << shift) - 1));
+        hi = hi - (bin << shift);  // still >= lo: the bin holds a word
+        const uint32_t span = (1u << shift) - 1;
+        if (hi - lo > span) lo = hi - span;  // (keys of codes start at 1: hi - span may wrap)
         if (shift == 0) {
             ties = lds.count[place_of((int32_t)bin)];
             break;
