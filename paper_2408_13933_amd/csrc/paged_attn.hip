@@ -230,21 +230,6 @@ struct Sees {
     int32_t lo, hi;
 };
 
-// The page list's entries for a block's eight 16-key groups, in the lanes' low
-// three bits, as they are (looked at when the block's turn comes, so that the
-// load can be under way until then).  Blocks past the list are never asked for.
-__device__ inline int32_t load_pages(const AttnArgs& p, int32_t b, int32_t blk)
-{
-    const int64_t e = ((int64_t)blk * kBlk + 16 * (threadIdx.x & 7)) >> p.kv.shift;
-    return p.kv.table[(int64_t)b * p.kv.ld + min(e, p.kv.ld - 1)];
-}
-// Those that are a place in the cache, else -1.
-__device__ inline int32_t valid_pages(const AttnArgs& p, int32_t blk, int32_t pages)
-{
-    const int64_t e = ((int64_t)blk * kBlk + 16 * (threadIdx.x & 7)) >> p.kv.shift;
-    return e < p.kv.ld && pages >= 0 && pages < (int32_t)p.kv.pages ? pages : -1;
-}
-
 // Where a lane reads a block's keys and values of half h: the key row
 // 16 (r >> 2) + (r & 3) of tile 0 (tile j: 4 j rows on) from channel 16 g on,
 // and 16 values of channel r from key 16 g on.  `base` is the address in page
@@ -634,6 +619,7 @@ struct Tile {
     uint32_t row0, rows;      // first row (token, head of the group), the sequence's rows
     int32_t n, skip0, skip1;  // blocks to walk: n, without those in [skip0, skip1)
     int32_t hi_min, hi_max;   // positions of the first and last token
+    int32_t last;             // of the page list's entries, the last one that a row sees
     __device__ int32_t block(int32_t i) const { return i < skip0 ? i : i + (skip1 - skip0); }
     // Every row sees all positions of the block.
     __device__ bool full(const AttnArgs& p, int32_t blk) const
@@ -642,6 +628,23 @@ struct Tile {
                (p.window == 0 || blk * kBlk > hi_max - p.window);
     }
 };
+
+// The page list's entries for a block's eight 16-key groups, in the lanes' low
+// three bits, as they are (looked at when the block's turn comes, so that the
+// load can be under way until then).  Entries past the tile's last are not read.
+__device__ inline int32_t page_entry(const AttnArgs& p, int32_t blk)
+{
+    return (blk * kBlk + 16 * (int32_t)(threadIdx.x & 7)) >> p.kv.shift;
+}
+__device__ inline int32_t load_pages(const AttnArgs& p, const Tile& t, int32_t blk)
+{
+    return p.kv.table[(int64_t)t.b * p.kv.ld + min(page_entry(p, blk), t.last)];
+}
+// Those that are a place in the cache, else -1.
+__device__ inline int32_t valid_pages(const AttnArgs& p, const Tile& t, int32_t blk, int32_t pages)
+{
+    return page_entry(p, blk) <= t.last && pages >= 0 && pages < (int32_t)p.kv.pages ? pages : -1;
+}
 
 // The tile's index counts from floor(starts[b] grp / R) + b for sequence b: an
 // upper bound of the tiles before it that needs no scan.
@@ -664,6 +667,7 @@ __device__ inline bool find_tile(const AttnArgs& p, int64_t index, Tile& t)
     // blocks with places, up to the last row's
     const int64_t list = ((p.kv.ld << p.kv.shift) + kBlk - 1) / kBlk;
     const int32_t end = t.hi_max < 0 ? 0 : (int32_t)min((int64_t)(t.hi_max / kBlk + 1), list);
+    t.last = (int32_t)min((int64_t)(t.hi_max >> p.kv.shift), p.kv.ld - 1);
     t.skip0 = t.skip1 = 0;
     if (p.window > 0) {
         t.skip1 = t.hi_min >= p.window ? min((t.hi_min - p.window + 1) / kBlk, end) : 0;
@@ -708,13 +712,13 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
     if (i < i1) {
         WeightTable table;
         table.init();
-        int32_t pages = load_pages(p, tile.b, tile.block(i));
+        int32_t pages = load_pages(p, tile, tile.block(i));
         load_queries<KS>(p, row.t, row.head, row.have, st.qh, st.ql, st.cz);
         for (; i < i1; i += kWaves) {
             const int32_t blk = tile.block(i);
-            pages = valid_pages(p, blk, pages);
+            pages = valid_pages(p, tile, blk, pages);
             const FromCache<KS> src(p, g0, blk, pages);
-            const int32_t next = load_pages(p, tile.b, tile.block(min(i + kWaves, i1 - 1)));
+            const int32_t next = load_pages(p, tile, tile.block(min(i + kWaves, i1 - 1)));
             attend_block<KS, ND>(p, table, st, src, pages, blk, row.sees, tile.full(p, blk));
             pages = next;
         }
@@ -779,10 +783,10 @@ __device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g
     if (i0 < i1) {
         WeightTable table;
         table.init();
-        int32_t pages = valid_pages(p, tile.block(i0), load_pages(p, tile.b, tile.block(i0)));
+        int32_t pages = valid_pages(p, tile, tile.block(i0), load_pages(p, tile, tile.block(i0)));
         const Stager<KS, ND> stage(p, g0, wave);
         stage(p, tile.block(i0), pages, wave, lds);
-        int32_t next = load_pages(p, tile.b, tile.block(min(i0 + 1, i1 - 1)));
+        int32_t next = load_pages(p, tile, tile.block(min(i0 + 1, i1 - 1)));
         load_queries<KS>(p, row.t, row.head, row.have, st.qh, st.ql, st.cz);
         wait_staged();
         __syncthreads();
@@ -790,9 +794,9 @@ __device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g
             const int32_t blk = tile.block(i);
             const int buf = (i - i0) & 1;
             const int32_t blk1 = tile.block(min(i + 1, i1 - 1));
-            next = valid_pages(p, blk1, next);
+            next = valid_pages(p, tile, blk1, next);
             if (i + 1 < i1) stage(p, blk1, next, wave, lds + (buf ^ 1) * kStage<KS, ND>);
-            const int32_t after = load_pages(p, tile.b, tile.block(min(i + 2, i1 - 1)));
+            const int32_t after = load_pages(p, tile, tile.block(min(i + 2, i1 - 1)));
             const FromLds<KS, ND> src{lds + buf * kStage<KS, ND> + lane * 16};
             attend_block<KS, ND>(p, table, st, src, pages, blk, row.sees, tile.full(p, blk));
             pages = next;
