@@ -14,9 +14,11 @@
 //    or, for top_p, per bin of logit distance from the largest.
 // 3. gather (top_p rows whose cut is below what the lists hold): the words of
 //    the cut's bin, and the weights above it per 2048 words.
-// 4. draw: a block per row finds the cut among the listed or gathered words,
-//    then the word; rows that neither serves (a top_k larger than the lists
-//    hold, thousands of equal logits at the cut) walk over the whole row.
+// 4. draw: a block per row finds the cut among the listed or gathered words, by
+//    bins of logit distance or, where too many of the listed share one, by the
+//    bits of their keys, then the word; rows that neither serves (a top_k
+//    larger than the lists hold, thousands of equal logits at the cut) walk
+//    over the whole row by key bits.
 //
 // One reading of the logits bounds many rows, and the vector arithmetic of
 // the weights (25 instructions each, fp64) those that need them all; one row
@@ -24,7 +26,8 @@
 // mixed, 104 + 40 + 38 + 25 (the scan 5.0 TB/s, all 2.6); 48 rows of 32000
 // codes, top_p, 5.2 + 8.0 + 7.5 + 10.3; one row of 256000, top_k, 5.3 + 1.7 + 1.7
 // + 10.7.  Rows of top_p over flat logits, 512 of 256000: 160 + 190 for the
-// second and third.
+// second and third.  top_k = 300 of flat rows, per call: 1 row of 100000 28, 256
+// rows of 256000 82 (over the whole row instead of the lists 330 and 1510).
 #include <algorithm>
 
 #include "codes.h"
@@ -770,11 +773,11 @@ __device__ __forceinline__ bool cut_gathered(const SampleArgs& a, const Row& r, 
     return true;
 }
 
-// The cut over the whole row, bit by bit of the keys from the top: the words
-// that have the leading bits found so far are counted by the next ten.
+// The cut over all the words, bit by bit of the keys from the top: those that
+// have the leading bits found so far are counted by the next ten.
 template <class F, bool MASS>
-__device__ __forceinline__ Cut cut_row(const SampleArgs& a, const Row& r, const Words<F>& ws, DrawLds& lds,
-                       int64_t count, double target)
+__device__ __forceinline__ Cut cut_search(const SampleArgs& a, const Row& r, const Words<F>& ws,
+                                          DrawLds& lds, int64_t count, double target)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     uint32_t lo = 1, hi = r.kmax;
@@ -1225,6 +1228,7 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs
         block_scan<kDrawWaves>(s, &all, lds.wave64);
         listed = r.k > 0 || (double)all >= target;
     }
+    bool found = false;
     if (listed) {
         // the bin of top_k's cut, without top_k of top_p's
         if (tid < 64) {
@@ -1249,20 +1253,21 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs
         }
         __syncthreads();
         if (r.k > 0) {
-            listed = cut_listed<F, false>(a, r, lds, (int)n, r.k, 0.0, cut);
-            if (listed && r.p < 1.0)
-                listed = cut_listed<F, true>(a, r, lds, (int)n, 0, r.p * (double)cut.mass, cut);
+            found = cut_listed<F, false>(a, r, lds, (int)n, r.k, 0.0, cut);
+            if (found && r.p < 1.0)
+                found = cut_listed<F, true>(a, r, lds, (int)n, 0, r.p * (double)cut.mass, cut);
         } else {
-            listed = cut_listed<F, true>(a, r, lds, (int)n, 0, target, cut);
+            found = cut_listed<F, true>(a, r, lds, (int)n, 0, target, cut);
         }
     }
+    // the listed words hold the cut, in whichever way it is found
     const Words<F> ws{&lds, x, listed ? (int32_t)n : a.V, listed};
-    if (!listed) {
+    if (!found) {
         if (r.k > 0) {
-            cut = cut_row<F, false>(a, r, ws, lds, r.k, 0.0);
+            cut = cut_search<F, false>(a, r, ws, lds, r.k, 0.0);
             target = r.p * (double)cut.mass;
         }
-        if (r.p < 1.0) cut = cut_row<F, true>(a, r, ws, lds, 0, target);
+        if (r.p < 1.0) cut = cut_search<F, true>(a, r, ws, lds, 0, target);
     }
     const int32_t tok = draw_word<F>(a, r, ws, lds, cut, u);
     if (tid == 0) a.tokens[row] = tok;

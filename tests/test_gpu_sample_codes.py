@@ -1,7 +1,8 @@
 """mq_sample on rows of 16-bit codes whose cut lies among the lowest codes:
 masked words (codes have no -infinity, so a mask writes -32768) and flat rows
-at the bottom of the range, found over the whole row.  Tokens equal the plain
-form's (tests/generation.py, Python integers)."""
+at the bottom of the range, found over the whole row; flat rows of either type
+whose cut is among the listed words.  Tokens equal the plain form's
+(tests/generation.py, Python integers)."""
 import numpy as np
 import pytest
 
@@ -69,3 +70,17 @@ def test_widths_of_the_range(bits):
     for kw in (dict(p=[0.97] * M), dict(p=[0.9] * M), dict(k=[7000] * M),
                dict(k=[8999] * M, p=[0.99] * M), dict(k=[200] * M)):
         _run(x, u, alpha=alpha, **kw)
+
+
+@pytest.mark.parametrize("dtype", [np.float32, np.int16])
+def test_flat_rows_whose_lists_hold_the_cut(dtype):
+    """top_k within the listed words of a row so flat that more of them share
+    one distance bin than there is room for."""
+    rng = np.random.default_rng(2)
+    M, V = len(U), 100000
+    x = rng.standard_normal((M, V)) * (2 if dtype == np.float32 else 4000)
+    x = x.astype(dtype)
+    x[1, rng.permutation(V)[:900]] = x[1].max()  # more equal words than there is room for
+    for kw in (dict(k=[300] * M), dict(k=[500] * M, p=[0.4] * M),
+               dict(k=[550] * M, p=[0.9] * M, floor=[0.5] * M), dict(p=[0.002] * M)):
+        _run(x, U, t=[3e4] * M, alpha=1e-3, **kw)
