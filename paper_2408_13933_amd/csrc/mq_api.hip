@@ -844,7 +844,7 @@ mq_status mq_sample(const void* logits, int32_t bits, int64_t M, int64_t V, int6
     if (!logits || !u || !tokens || !workspace) return MQ_ERR_INVALID_ARG;
     if ((uintptr_t)workspace % 256 != 0 || workspace_bytes < mq::sample_workspace(M, V, true))
         return MQ_ERR_INVALID_ARG;
-    return from_hip(mq::launch_sample(logits, bits, M, V, ld, alpha, zp, temperature, top_k, top_p,
+    return from_hip(mq::launch_sample(logits, bits, M, V, ld, alpha, temperature, top_k, top_p,
                                       min_p, u, tokens, workspace, workspace_bytes,
                                       as_stream(stream)));
 }

@@ -9,8 +9,8 @@ namespace mq {
 // Workspace of launch_sample: for all rows (within its bound), or the least.
 int64_t sample_workspace(int64_t M, int64_t V, bool least);
 hipError_t launch_sample(const void* x, int32_t bits, int64_t M, int64_t V, int64_t ld, float alpha,
-                         int32_t zp, const float* temperature, const int32_t* top_k,
-                         const float* top_p, const float* min_p, const float* u, int32_t* tokens,
-                         void* ws, int64_t ws_bytes, hipStream_t s);
+                         const float* temperature, const int32_t* top_k, const float* top_p,
+                         const float* min_p, const float* u, int32_t* tokens, void* ws,
+                         int64_t ws_bytes, hipStream_t s);
 
 }  // namespace mq

@@ -62,8 +62,7 @@ struct SampleArgs {
     const void* x;
     int64_t ld;
     int32_t V, segs;
-    double alpha;           // logit = alpha * (code - zp) for 16-bit codes
-    int32_t zp;
+    double alpha;           // of 16-bit codes, whose zero-point drops out of all distances
     const float* temperature;
     const int32_t* top_k;
     const float* top_p;
@@ -401,7 +400,6 @@ __global__ __launch_bounds__(256) void sample_sums_kernel(SampleArgs a, int64_t 
 struct Found {
     int32_t bin;
     int64_t count, mass;
-    int64_t total;  // mass of all bins
 };
 
 // Bins in LDS are kept so that the lanes that hold 16 neighbouring ones each
@@ -424,7 +422,6 @@ __device__ inline Found find_bin(const uint32_t* count, const unsigned long long
     }
     const int64_t ns = wave_scan(n), ws = wave_scan(w);
     Found f;
-    f.total = wave_read(ws, 63);
     // the first lane that reaches the target, or the last with anything; then
     // the same among its bins
     const uint64_t hit = __ballot(reaches(ns, ws)), some = __ballot(n > 0);
@@ -642,9 +639,8 @@ __device__ __forceinline__ void order_words(const uint64_t* src, int n, uint64_t
 // The cut among n ordered words of one bin, by count (words of the bin kept)
 // or by mass; before: the mass of the bins before.  Wave 0 looks, all get it.
 template <class F, bool MASS>
-__device__ __forceinline__ Cut cut_in_order(const SampleArgs& a, const Row& r, DrawLds& lds,
-                                            const uint64_t* word, int n, int64_t before,
-                                            int64_t keep, double target)
+__device__ __forceinline__ Cut cut_in_order(const Row& r, DrawLds& lds, const uint64_t* word,
+                                            int n, int64_t before, int64_t keep, double target)
 {
     __syncthreads();
     if (threadIdx.x < 64) {
@@ -691,8 +687,8 @@ struct Words {
 // The cut over the listed words in LDS by their bins (count and mass there
 // already); false if its bin holds more words than there is room for.
 template <class F, bool MASS>
-__device__ __forceinline__ bool cut_listed(const SampleArgs& a, const Row& r, DrawLds& lds, int n,
-                                  int64_t keep, double target, Cut& cut)
+__device__ __forceinline__ bool cut_listed(const Row& r, DrawLds& lds, int n, int64_t keep,
+                                           double target, Cut& cut)
 {
     if (threadIdx.x < 64) {
         const Found f = find_bin(lds.count, lds.mass, [=](int64_t c, int64_t w) {
@@ -715,7 +711,7 @@ __device__ __forceinline__ bool cut_listed(const SampleArgs& a, const Row& r, Dr
             lds.near[atomicAdd(&lds.sel[1], 1u)] = lds.word[i];
     __syncthreads();
     order_words(lds.near, near, lds.near + kNear);
-    cut = cut_in_order<F, MASS>(a, r, lds, lds.near + kNear, near, mass, keep - count, target);
+    cut = cut_in_order<F, MASS>(r, lds, lds.near + kNear, near, mass, keep - count, target);
     return true;
 }
 
@@ -723,9 +719,9 @@ __device__ __forceinline__ bool cut_listed(const SampleArgs& a, const Row& r, Dr
 // many words and so much mass come before them.  False if too many share the
 // finer bin.
 template <class F, bool MASS>
-__device__ __forceinline__ bool cut_gathered(const SampleArgs& a, const Row& r, DrawLds& lds, int n,
-                                             int b0, int b1, int64_t count, int64_t mass,
-                                             int64_t keep, double target, Cut& cut)
+__device__ __forceinline__ bool cut_gathered(const Row& r, DrawLds& lds, int n, int b0, int b1,
+                                             int64_t count, int64_t mass, int64_t keep,
+                                             double target, Cut& cut)
 {
     const double fine = (double)kBins / (double)(b1 - b0 + 1);
     // -1: not one of them
@@ -769,15 +765,15 @@ __device__ __forceinline__ bool cut_gathered(const SampleArgs& a, const Row& r, 
         if (sub_bin(key_of(lds.word[i])) == bin) lds.near[atomicAdd(&lds.sel[1], 1u)] = lds.word[i];
     __syncthreads();
     order_words(lds.near, near, lds.near + kNear);
-    cut = cut_in_order<F, MASS>(a, r, lds, lds.near + kNear, near, m0, keep - c0, target);
+    cut = cut_in_order<F, MASS>(r, lds, lds.near + kNear, near, m0, keep - c0, target);
     return true;
 }
 
 // The cut over all the words, bit by bit of the keys from the top: those that
 // have the leading bits found so far are counted by the next ten.
 template <class F, bool MASS>
-__device__ __forceinline__ Cut cut_search(const SampleArgs& a, const Row& r, const Words<F>& ws,
-                                          DrawLds& lds, int64_t count, double target)
+__device__ __forceinline__ Cut cut_search(const Row& r, const Words<F>& ws, DrawLds& lds,
+                                          int64_t count, double target)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     uint32_t lo = 1, hi = r.kmax;
@@ -876,8 +872,8 @@ __device__ __forceinline__ Cut cut_search(const SampleArgs& a, const Row& r, con
 // The word at which the running weight of the kept ones, in index order,
 // passes u times their total; every wave walks a contiguous part.
 template <class F>
-__device__ __forceinline__ int32_t draw_word(const SampleArgs& a, const Row& r, const Words<F>& ws, DrawLds& lds,
-                             const Cut& cut, double u)
+__device__ __forceinline__ int32_t draw_word(const Row& r, const Words<F>& ws, DrawLds& lds,
+                                             const Cut& cut, double u)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int32_t part = ((ws.n + kDrawWaves - 1) / kDrawWaves + 63) & ~63;
@@ -1058,8 +1054,8 @@ __device__ __forceinline__ int64_t store_lists(const SampleArgs& a, int64_t m, u
 // A word's place in the order is what the bins before its own hold and what
 // comes before it in its own.
 template <class F>
-__device__ __forceinline__ int32_t draw_few(const SampleArgs& a, const Row& r, DrawLds& lds, int n,
-                                            int32_t bin, int few, double mass, double u)
+__device__ __forceinline__ int32_t draw_few(const Row& r, DrawLds& lds, int n, int32_t bin,
+                                            int few, double mass, double u)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = draw_wave();
     // the words of these bins, in index order
@@ -1179,12 +1175,12 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs
             if (r.k > 0 && f.k == kBins) {  // fewer than k have a weight
                 mass = r.p * (double)f.k_mass;
             } else if (r.k > 0) {
-                found = cut_gathered<F, false>(a, r, lds, n, f.k, f.k, f.k_count, f.k_mass, r.k, 0.0,
+                found = cut_gathered<F, false>(r, lds, n, f.k, f.k, f.k_count, f.k_mass, r.k, 0.0,
                                                cut);
                 mass = r.p * (double)cut.mass;
             }
             if (found && r.p < 1.0)
-                found = cut_gathered<F, true>(a, r, lds, n, f.p0, f.p1, 0, f.p_mass, 0, mass, cut);
+                found = cut_gathered<F, true>(r, lds, n, f.p0, f.p1, 0, f.p_mass, 0, mass, cut);
         }
         if (found) {
             // the segments' sums, which the kept ones of these words join
@@ -1246,30 +1242,30 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(SampleArgs
         const int32_t bin = (int32_t)lds.sel[0];
         const int64_t count = lds.sel64[0] + lds.count[place_of(bin)];
         if (count <= kNear) {
-            const int32_t tok = draw_few<F>(a, r, lds, (int)n, bin, (int)count,
+            const int32_t tok = draw_few<F>(r, lds, (int)n, bin, (int)count,
                                             r.k > 0 ? -1.0 : target, u);
             if (tid == 0) a.tokens[row] = tok;
             return;
         }
         __syncthreads();
         if (r.k > 0) {
-            found = cut_listed<F, false>(a, r, lds, (int)n, r.k, 0.0, cut);
+            found = cut_listed<F, false>(r, lds, (int)n, r.k, 0.0, cut);
             if (found && r.p < 1.0)
-                found = cut_listed<F, true>(a, r, lds, (int)n, 0, r.p * (double)cut.mass, cut);
+                found = cut_listed<F, true>(r, lds, (int)n, 0, r.p * (double)cut.mass, cut);
         } else {
-            found = cut_listed<F, true>(a, r, lds, (int)n, 0, target, cut);
+            found = cut_listed<F, true>(r, lds, (int)n, 0, target, cut);
         }
     }
     // the listed words hold the cut, in whichever way it is found
     const Words<F> ws{&lds, x, listed ? (int32_t)n : a.V, listed};
     if (!found) {
         if (r.k > 0) {
-            cut = cut_search<F, false>(a, r, ws, lds, r.k, 0.0);
+            cut = cut_search<F, false>(r, ws, lds, r.k, 0.0);
             target = r.p * (double)cut.mass;
         }
-        if (r.p < 1.0) cut = cut_search<F, true>(a, r, ws, lds, 0, target);
+        if (r.p < 1.0) cut = cut_search<F, true>(r, ws, lds, 0, target);
     }
-    const int32_t tok = draw_word<F>(a, r, ws, lds, cut, u);
+    const int32_t tok = draw_word<F>(r, ws, lds, cut, u);
     if (tid == 0) a.tokens[row] = tok;
 }
 
@@ -1316,9 +1312,9 @@ int64_t sample_workspace(int64_t M, int64_t V, bool least)
 }
 
 hipError_t launch_sample(const void* x, int32_t bits, int64_t M, int64_t V, int64_t ld, float alpha,
-                         int32_t zp, const float* temperature, const int32_t* top_k,
-                         const float* top_p, const float* min_p, const float* u, int32_t* tokens,
-                         void* ws, int64_t ws_bytes, hipStream_t s)
+                         const float* temperature, const int32_t* top_k, const float* top_p,
+                         const float* min_p, const float* u, int32_t* tokens, void* ws,
+                         int64_t ws_bytes, hipStream_t s)
 {
     SampleArgs a;
     a.x = x;
@@ -1326,7 +1322,6 @@ hipError_t launch_sample(const void* x, int32_t bits, int64_t M, int64_t V, int6
     a.V = (int32_t)V;
     a.segs = segments(V);
     a.alpha = alpha;
-    a.zp = zp;
     a.temperature = temperature;
     a.top_k = top_k;
     a.top_p = top_p;
