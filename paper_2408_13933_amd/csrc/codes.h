@@ -43,6 +43,19 @@ __device__ inline double exp2_poly(double x)
     return __builtin_amdgcn_ldexp(p, rint_low(t));
 }
 
+// The same by a table of 2^(j/64): adding kTableShift leaves 64 x, rounded, in
+// the low word, and the rest, |f| <= 1/128, takes a polynomial of degree 4
+// (within 2.5e-15 of 2^f).
+constexpr double kTableShift = 105553116266496.0;  // 1.5 * 2^46
+__device__ inline double exp2_rest(double f)
+{
+    double p = 0x1.3b2ad0385b409p-7;
+    p = __builtin_fma(p, f, 0x1.c6b0c40d8c4e9p-5);
+    p = __builtin_fma(p, f, 0x1.ebfbdff82ac52p-3);
+    p = __builtin_fma(p, f, 0x1.62e42fefa0352p-1);
+    return __builtin_fma(p, f, 1.0);
+}
+
 template <int BITS>
 __device__ inline int32_t clamp_code(int32_t q)
 {

@@ -89,13 +89,12 @@ __device__ inline int32_t row_max(int32_t m)
 }
 
 // rint(MQ_ATTN_ONE 2^(-tau d)) + 128 for 0 <= tau d < 1000: tau d to the next
-// 1/64 by the 1.5 * 2^46 shift, 2^(j/64) from the table that the wave's lanes
-// hold (lane j), a polynomial of degree 4 on the rest (|f| <= 1/128, within
-// 2.5e-15) and the last product added to 1.5 * 2^52 + 128, whose low word is
-// then the rounded weight and 128.  The high words of the table lack j << 14,
-// which k << 14 (k = 64 n + j) adds again with the exponent n.  11 vector
-// instructions and two reads across lanes; the polynomial over all of
-// [-1/2, 1/2] (degree 10) took 18.
+// 1/64, 2^(j/64) from the table that the wave's lanes hold (lane j), exp2_rest
+// and the last product added to 1.5 * 2^52 + 128, whose low word is then the
+// rounded weight and 128.  The high words of the table lack j << 14, which
+// k << 14 (k = 64 n + j) adds again with the exponent n.  11 vector instructions
+// and two reads across lanes; the polynomial over all of [-1/2, 1/2] (degree
+// 10) took 18.
 constexpr int32_t kBias = 128;
 struct WeightTable {
     int lo, hi;  // MQ_ATTN_ONE * 2^(lane/64)
@@ -113,11 +112,10 @@ struct WeightTable {
     };
     __device__ Part begin(double tau, uint32_t d) const
     {
-        constexpr double kShift = 105553116266496.0;  // 1.5 * 2^46
         Part w;
         const double x = (double)d;
-        const double t = __builtin_fma(-tau, x, kShift);
-        w.f = __builtin_fma(-tau, x, -(t - kShift));
+        const double t = __builtin_fma(-tau, x, kTableShift);
+        w.f = __builtin_fma(-tau, x, -(t - kTableShift));
         w.k = rint_low(t);
         w.lo = __builtin_amdgcn_ds_bpermute(w.k << 2, lo);
         w.hi = __builtin_amdgcn_ds_bpermute(w.k << 2, hi);
@@ -129,12 +127,7 @@ struct WeightTable {
     {
         const double e =
             __longlong_as_double(((int64_t)(w.hi + (w.k << 14)) << 32) | (uint32_t)w.lo);
-        double q = 0x1.3b2ad0385b409p-7;
-        q = __builtin_fma(q, w.f, 0x1.c6b0c40d8c4e9p-5);
-        q = __builtin_fma(q, w.f, 0x1.ebfbdff82ac52p-3);
-        q = __builtin_fma(q, w.f, 0x1.62e42fefa0352p-1);
-        q = __builtin_fma(q, w.f, 1.0);
-        return rint_low(__builtin_fma(q, e, kRintShift + kBias));
+        return rint_low(__builtin_fma(exp2_rest(w.f), e, kRintShift + kBias));
     }
 };
 

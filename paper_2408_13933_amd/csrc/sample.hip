@@ -158,28 +158,21 @@ __device__ inline double distance(const Row& r, int32_t v)
 }
 
 // rint(2^40 2^-z): z to the next 1/64, 2^(j/64) from a table in LDS (2^40 of
-// it in entry j), a polynomial of degree 4 on the rest (within 2.5e-15); the
-// last product is added to 1.5 * 2^52, whose low bits are then the rounded
-// weight.
+// it in entry j), exp2_rest; the last product is added to 1.5 * 2^52, whose low
+// bits are then the rounded weight.
 __device__ inline void init_table(double* table)  // by the block, which waits afterwards
 {
     if (threadIdx.x < 64) table[threadIdx.x] = kOne * exp2_poly((double)threadIdx.x / 64.0);
 }
 __device__ inline int64_t weight_at(const double* table, double z)
 {
-    constexpr double kShift = 105553116266496.0;  // 1.5 * 2^46
-    const double t = kShift - z;
-    const double f = (kShift - t) - z;
+    const double t = kTableShift - z;
+    const double f = (kTableShift - t) - z;
     const int32_t k = rint_low(t);
     const int64_t e = __double_as_longlong(table[k & 63]);
     const int32_t hi = (int32_t)(e >> 32) + ((k & ~63) << 14);  // the exponent, k / 64 lower
-    double q = 0x1.3b2ad0385b409p-7;
-    q = __builtin_fma(q, f, 0x1.c6b0c40d8c4e9p-5);
-    q = __builtin_fma(q, f, 0x1.ebfbdff82ac52p-3);
-    q = __builtin_fma(q, f, 0x1.62e42fefa0352p-1);
-    q = __builtin_fma(q, f, 1.0);
     const double w = __builtin_fma(
-        q, __longlong_as_double(((int64_t)hi << 32) | (uint32_t)e), kRintShift);
+        exp2_rest(f), __longlong_as_double(((int64_t)hi << 32) | (uint32_t)e), kRintShift);
     return __double_as_longlong(w) - __double_as_longlong(kRintShift);
 }
 template <class F>
