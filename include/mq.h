@@ -732,8 +732,9 @@ typedef struct mq_kv_batch {
  *   ak, zk / ako, zko  format of k (int16) and of the cached keys (int8)
  *   0 <= T < 2^26; H a multiple of G, H <= 1024, (T + B) (H + G) D < 2^36;
  *   ldq, ldo >= H * D; ldk, ldv >= G * D, all < 2^40; two tokens must not
- *   share a place in the cache.  A call that takes 2^24 work-groups or more
- *   (tens of millions of tokens or sequences) is MQ_ERR_UNSUPPORTED.
+ *   share a place in the cache.  A call that takes 2^24 work-groups or more is
+ *   MQ_ERR_UNSUPPORTED; from 4096 tokens on it takes
+ *   T / 4 + (T / 16 + 2 B) * ceil(G * D / 256).
  * Any alignment of q, k and q_out is taken; with 8-byte aligned rows of all
  * three the codes move in wide accesses.
  */
@@ -785,8 +786,9 @@ mq_status mq_rope_append(const int16_t* q, int64_t ldq, const int16_t* k, int64_
  *   ldq, ldy >= H * D, < 2^40;
  *   scales finite and > 0, sigma <= 1024; q_zp int16, v_zp int8, out_zp in
  *   out_bits' range; window, sinks, max_len, workspace_bytes >= 0.  A call
- *   that takes 2^24 work-groups or more (tens of millions of tokens or
- *   sequences) is MQ_ERR_UNSUPPORTED.
+ *   that takes 2^24 work-groups or more is MQ_ERR_UNSUPPORTED: T * (H / G) / 64
+ *   + B of them per cache head, or, with T * (H / G) <= 16 B, T * (H / G) / 16 +
+ *   B for all.
  */
 mq_status mq_paged_attn(const int16_t* q, int64_t ldq, int64_t T, int32_t H, float q_scale,
                         int32_t q_zp, const mq_kv_cache* cache, float k_scale, float v_scale,
