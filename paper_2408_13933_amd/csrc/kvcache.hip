@@ -7,8 +7,8 @@
 // few.  A wave rotates all heads of a token, so that the angles are read and
 // scaled once and each lane keeps its pairs' in registers; of few tokens
 // several waves share the heads, up to 4096 waves in all.  32 heads of 64, 4 of
-// the cache, us: 1 token 3.4 (one wave per token: 5.1), 250 sequences' one token
-// each 5.9 (7.5), 4740 tokens 16.4 for 45 MB (five waves per token 27, a
+// the cache, us: 1 token 3.3 (one wave per token: 5.1), 250 sequences' one token
+// each 5.8 (7.5), 4740 tokens 15.9 for 45 MB (five waves per token 27, a
 // block per token 22).
 #include <algorithm>
 

@@ -24,11 +24,12 @@
 // Rows of several waves share the keys: these come once into LDS, by copies
 // that need no registers, and a CU's two work-groups overlap.  Few rows are one
 // wave's, so the keys are split instead, among four waves and among work-groups.
-// us, kernel (and join): one token over 1531 keys, 32 heads of 64 on 4, 7.6
-// (3.2); 64 tokens over up to 4096, 67 MB, 21 (4.8); 2 over up to 120000, 8
-// heads of 256 on 1, 61 MB, 26 (5.4); 24 windows of 1000, 46 MB, 21; a prompt
-// of 1024, 25; 500 tokens over 16000, 32 heads of 128 on 8, 272 (14): 0.95 POP/s
-// of int8 products.
+// us, kernel (and join) traced in a row: one token over 1531 keys, 32 heads of
+// 64 on 4, 7.5 (3.3); 64 tokens over up to 4096, 67 MB, 23.7 (4.0); 2 over up
+// to 120000, 8 heads of 256 on 1, 61 MB, 26.2 (4.7); 24 windows of 1000, 46 MB,
+// 20.9; a prompt of 1024, 29.0; 500 tokens over 16000, 32 heads of 128 on 8, 282
+// (12.8): 0.92 POP/s of int8 products.  A call in a row without the tracer:
+// 12.3, 25.6, 31.5, 21.5, 25.0, 287.
 #include <algorithm>
 #include <cmath>
 

@@ -23,11 +23,13 @@
 // One reading of the logits bounds many rows, and the vector arithmetic of
 // the weights (25 instructions each, fp64) those that need them all; one row
 // is four launches, each its own latency.  us: 512 rows of 256000 fp32, settings
-// mixed, 104 + 40 + 38 + 25 (the scan 5.0 TB/s, all 2.6); 48 rows of 32000
-// codes, top_p, 5.2 + 8.0 + 7.5 + 10.3; one row of 256000, top_k, 5.3 + 1.7 + 1.7
+// mixed, 98 + 36 + 34 + 24 (the scan 5.4 TB/s, all 2.7); 48 rows of 32000
+// codes, top_p, 5.2 + 8.0 + 7.4 + 10.0; one row of 256000, top_k, 5.2 + 1.8 + 1.8
 // + 10.7.  Rows of top_p over flat logits, 512 of 256000: 160 + 190 for the
 // second and third.  top_k = 300 of flat rows, per call: 1 row of 100000 28, 256
-// rows of 256000 82 (over the whole row instead of the lists 330 and 1510).
+// rows of 256000 82 (over the whole row instead of the lists 330 and 1510).  A
+// walk over the whole row, 1000 codes over words masked with the lowest: 1 row
+// of 32000 170 to 180, 64 of 256000 1400 to 1540.
 #include <algorithm>
 
 #include "codes.h"
