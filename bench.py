@@ -62,6 +62,7 @@ TRAFFIC_FILES = {
         ROOT, "profiles", "qlinear_prefill_gate_up_tinyllama_m2048_hbm_traffic.txt"),
 }
 KERNEL_SOURCES = ("paper_2408_13933_amd/csrc/qlinear_prefill.hip",
+                  "paper_2408_13933_amd/csrc/qlinear_tiles.h",
                   "paper_2408_13933_amd/csrc/qlinear_decode.hip",
                   "paper_2408_13933_amd/csrc/qlinear_gemv.hip",
                   "paper_2408_13933_amd/csrc/requant.h",

@@ -849,6 +849,78 @@ mq_status mq_sample(const void* logits, int32_t bits, int64_t M, int64_t V, int6
 int64_t mq_sample_workspace_bytes(int64_t M, int64_t V);
 
 /*
+ * Scales that are found at run time.  The calls above run on static formats,
+ * measured before (Section 4.2); those below serve models without calibrated
+ * ranges, or inputs that leave them: activations quantized token by token
+ * (the dynamic quantization that Section 3.1 weighs the static one against),
+ * a cache with a scale for each block of tokens and head.  What lies between
+ * the integer products is floating point of one of these types.
+ */
+typedef enum { MQ_F32 = 0, MQ_BF16 = 1, MQ_F16 = 2 } mq_type;
+
+/*
+ * mq_quantize_tokens -- symmetric 8-bit codes of every row by its own largest
+ * magnitude:
+ *   s[m]   = max(max_k |x[m][k]|, 2^-60) / 127       (one fp32 division)
+ *   x_q    = rint(x * (1 / s[m]))   (fp32: the inverse, then the product)
+ * so |x_q| <= 127.  A row that holds an infinity or NaN gets s = NaN and codes
+ * 0, which makes it NaN in what is computed from it and leaves other rows alone.
+ *   x       device, of `type`, row m at x + m * ldx
+ *   x_q     device int8 [M][K]     scale  device fp32 [M]
+ *   rowsum  device int32 [M], sum_k x_q[m][k] (for asymmetric weights), or NULL
+ *   0 <= M < 2^24, 1 <= K <= MQ_MAX_K, K <= ldx < 2^40.  Any alignment of the
+ *   type; rows of x on 16 bytes with K % 8 == 0 move in wide accesses.
+ */
+mq_status mq_quantize_tokens(const void* x, int32_t type, int64_t M, int64_t K, int64_t ldx,
+                             int8_t* x_q, float* scale, int32_t* rowsum, void* stream);
+
+/*
+ * mq_qlinear_tokens -- the linear layer on the codes of mq_quantize_tokens:
+ *   c       = sum_k a_q[m][k] * (W_q[n][k] - w_zp[n])           exact, int32
+ *   y[m][n] = ((float)c * w_scale[n]) * a_scale[m] + bias[n]
+ * each step rounded once in fp32, the result once to y's type; without bias
+ * the last sum is left out.  Every path gives the same bits.
+ *   a_q       device int8 [M][K], codes in [-127, 127]
+ *   a_scale   device fp32 [M]
+ *   a_rowsum  device int32 [M] (of mq_quantize_tokens) and w_zp device int32
+ *             [N] for asymmetric weights, both NULL for symmetric ones
+ *   w_q, w_bits, w_scale  as for mq_qlinear (mq_pack_weights) or
+ *             mq_qlinear_asym (mq_pack_weights_asym, w_zp in w_bits' range)
+ *   bias      device fp32 [N] or NULL
+ *   y         device [M][N] of y_type; must not overlap the inputs
+ *   workspace, workspace_bytes, path  as for mq_qlinear_ws, with the bytes of
+ *             mq_qlinear_workspace_bytes (any out_bits)
+ *   M, N >= 0 (0: nothing to do), 1 <= K <= MQ_MAX_K, even for w_bits 4; the
+ *   shapes and alignments of the tuned kernels are those of mq_qlinear.
+ */
+mq_status mq_qlinear_tokens(const int8_t* a_q, const float* a_scale, const int32_t* a_rowsum,
+                            int64_t M, int64_t K, int64_t N, const void* w_q, int32_t w_bits,
+                            const float* w_scale, const int32_t* w_zp, const float* bias, void* y,
+                            int32_t y_type, void* workspace, int64_t workspace_bytes,
+                            int32_t path, void* stream);
+
+/*
+ * mq_linear_tokens -- mq_quantize_tokens and mq_qlinear_tokens of its result
+ * in one call, bit for bit: a linear layer from floating activations to
+ * floating outputs.  One token over few channels takes one launch.
+ *   x          device, of x_type, row m at x + m * ldx; 0 <= M < 2^24
+ *   workspace  device, 256-byte aligned, any contents, overwritten (codes,
+ *              scales, row sums, the K split's parts); at least the bytes of
+ *              mq_linear_tokens_workspace_bytes with splits = 0, with those of
+ *              splits = 1 the product may split K.  Calls that may run at the
+ *              same time must not share it.
+ * Everything else as in the two calls.
+ */
+mq_status mq_linear_tokens(const void* x, int32_t x_type, int64_t ldx, int64_t M, int64_t K,
+                           int64_t N, const void* w_q, int32_t w_bits, const float* w_scale,
+                           const int32_t* w_zp, const float* bias, void* y, int32_t y_type,
+                           void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Workspace bytes of mq_linear_tokens (-1: invalid sizes). */
+int64_t mq_linear_tokens_workspace_bytes(int64_t M, int64_t K, int64_t N, int32_t w_bits,
+                                         int32_t splits);
+
+/*
  * mq_dequant -- inverse of Eq.(4): y = alpha * (float)(q - zp), one exact
  * integer subtraction and one fp32 multiply.
  *   q      device int8 (bits 8) or int16 (bits 16) [numel]

@@ -25,6 +25,8 @@ __all__ = [
     "mq_qlinear_group", "MAX_GROUP", "QLinearOut", "mq_qlinear_dequant",
     "mq_rope_append", "mq_paged_attn", "mq_paged_attn_workspace_bytes",
     "ATTN_BLOCK", "ATTN_ONE", "mq_sample", "mq_sample_workspace_bytes",
+    "F32", "BF16", "F16", "mq_quantize_tokens", "mq_qlinear_tokens", "mq_linear_tokens",
+    "mq_linear_tokens_workspace_bytes",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -75,6 +77,7 @@ class QLinearOut(ctypes.Structure):
 
 
 ATTN_BLOCK, ATTN_ONE = 128, 32512  # MQ_ATTN_BLOCK, MQ_ATTN_ONE
+F32, BF16, F16 = 0, 1, 2  # mq_type
 
 
 def lib():
@@ -163,7 +166,15 @@ def lib():
     L.mq_sample_workspace_bytes.restype = c_i64
     L.mq_sample.argtypes = [c_p, c_i32, c_i64, c_i64, c_i64, c_f, c_i32, c_p, c_p, c_p, c_p, c_p,
                             c_p, c_p, c_i64, c_p]
-    for name in ("mq_sample", "mq_rope_append", "mq_paged_attn", "mq_qlinear_dequant", "mq_qlinear_group", "mq_probe_read", "mq_attn_matmul", "mq_transpose_i8", "mq_act_params", "mq_fold_weights", "mq_fold_acts", "mq_quantize_act",
+    L.mq_quantize_tokens.argtypes = [c_p, c_i32, c_i64, c_i64, c_i64, c_p, c_p, c_p, c_p]
+    L.mq_qlinear_tokens.argtypes = [c_p, c_p, c_p, c_i64, c_i64, c_i64, c_p, c_i32, c_p, c_p, c_p,
+                                    c_p, c_i32, c_p, c_i64, c_i32, c_p]
+    L.mq_linear_tokens.argtypes = [c_p, c_i32, c_i64, c_i64, c_i64, c_i64, c_p, c_i32, c_p, c_p,
+                                   c_p, c_p, c_i32, c_p, c_i64, c_p]
+    L.mq_linear_tokens_workspace_bytes.argtypes = [c_i64, c_i64, c_i64, c_i32, c_i32]
+    L.mq_linear_tokens_workspace_bytes.restype = c_i64
+    for name in ("mq_quantize_tokens", "mq_qlinear_tokens", "mq_linear_tokens",
+                 "mq_sample", "mq_rope_append", "mq_paged_attn", "mq_qlinear_dequant", "mq_qlinear_group", "mq_probe_read", "mq_attn_matmul", "mq_transpose_i8", "mq_act_params", "mq_fold_weights", "mq_fold_acts", "mq_quantize_act",
                  "mq_pack_weights", "mq_qlinear", "mq_qlinear_ex", "mq_qlinear_ws", "mq_dequant",
                  "mq_qlinear_noalloc",
                  "mq_pack_weights_asym", "mq_act_rowsum", "mq_quantize_act_rowsum",
@@ -1075,6 +1086,126 @@ def mq_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, a
         _flat(u, f32, dev, "u", per_row), _flat(out, i32, dev, "out", per_row), ws, n, st)
     if status:
         raise MQError(status, "mq_sample")
+    return out
+
+
+# --------------------------------------------------------------------------
+# Scales found at run time: floating activations, codes by each token's own
+# magnitude.
+_TYPES = {}
+
+
+def _type_of(t, name):
+    """mq_type of a floating tensor."""
+    if not _TYPES:
+        torch = _torch()
+        _TYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    try:
+        return _TYPES[t.dtype]
+    except (AttributeError, KeyError):
+        raise ValueError(f"{name} must be a float32, bfloat16 or float16 tensor")
+
+
+def mq_quantize_tokens(x, out=None, scale=None, rowsum=None, stream=None):
+    """8-bit codes of x [M][K] by each row's largest magnitude: (codes int8
+    [M][K], scales fp32 [M]).  rowsum: an int32 tensor [M] that gets the codes'
+    sums (asymmetric weights need them), or None."""
+    dev, st = _device_and_stream(x, "x", stream)
+    torch = _torch_mod
+    t = _type_of(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x must be [M][K]")
+    M, K = shape = x.shape
+    if out is None:
+        out = _empty(shape, torch.int8, x.device, stream)
+    if scale is None:
+        scale = _empty((M,), torch.float32, x.device, stream)
+    px, ldx = _rows(x, x.dtype, dev, "x", shape)
+    status = lib().mq_quantize_tokens(
+        px, t, M, K, ldx, _flat(out, torch.int8, dev, "out", shape),
+        _flat(scale, torch.float32, dev, "scale", (M,)),
+        None if rowsum is None else _flat(rowsum, torch.int32, dev, "rowsum", (M,)), st)
+    if status:
+        raise MQError(status, "mq_quantize_tokens")
+    return out, scale
+
+
+def _token_weights(dev, K, w_q, w_bits, w_scale, w_zp, bias):
+    """Output channels and pointers of a token product's weights."""
+    torch = _torch_mod
+    try:
+        N = w_q.shape[0]
+    except (AttributeError, IndexError):
+        raise ValueError("w_q must be a tensor [N][K] (int8) or [N][K/2] (uint8)")
+    f32 = torch.float32
+    return N, (_flat(w_q, torch.int8, dev, "w_q", (N, K)) if w_bits == 8 else
+               _flat(w_q, torch.uint8, dev, "w_q", (N, K // 2))), \
+        _flat(w_scale, f32, dev, "w_scale", (N,)), \
+        None if w_zp is None else _flat(w_zp, torch.int32, dev, "w_zp", (N,)), \
+        None if bias is None else _flat(bias, f32, dev, "bias", (N,))
+
+
+def mq_qlinear_tokens(a_q, a_scale, w_q, w_bits: int, w_scale, w_zp=None, a_rowsum=None,
+                      bias=None, out=None, out_dtype=None, path: int = PATH_AUTO,
+                      workspace=None, stream=None):
+    """The linear layer on the codes and scales of mq_quantize_tokens: floating
+    outputs [M][N] of out's type (out_dtype where it is made here, float32 by
+    default).  w_zp and a_rowsum: asymmetric weights.  workspace as for
+    mq_qlinear (a K split; zero-filled once)."""
+    dev, st = _device_and_stream(a_q, "a_q", stream)
+    torch = _torch_mod
+    if a_q.dim() != 2:
+        raise ValueError("a_q must be [M][K]")
+    M, K = a_q.shape
+    N, pw, ps, pz, pb = _token_weights(dev, K, w_q, w_bits, w_scale, w_zp, bias)
+    if out is None:
+        out = _empty((M, N), out_dtype or torch.float32, a_q.device, stream)
+    t = _type_of(out, "out")
+    ws, n = (None, 0) if workspace is None else \
+        _any_shape(workspace, torch.uint8, dev, "workspace")
+    status = lib().mq_qlinear_tokens(
+        _flat(a_q, torch.int8, dev, "a_q", (M, K)),
+        _flat(a_scale, torch.float32, dev, "a_scale", (M,)),
+        None if a_rowsum is None else _flat(a_rowsum, torch.int32, dev, "a_rowsum", (M,)), M, K, N,
+        pw, w_bits, ps, pz, pb, _flat(out, out.dtype, dev, "out", (M, N)), t, ws, n, path, st)
+    if status:
+        raise MQError(status, "mq_qlinear_tokens")
+    return out
+
+
+def mq_linear_tokens_workspace_bytes(M: int, K: int, N: int, w_bits: int = 8,
+                                     splits: bool = True) -> int:
+    """Workspace bytes of mq_linear_tokens, with or without a K split."""
+    n = lib().mq_linear_tokens_workspace_bytes(M, K, N, w_bits, int(splits))
+    if n < 0:
+        raise ValueError(f"mq_linear_tokens_workspace_bytes: invalid sizes {(M, K, N, w_bits)}")
+    return n
+
+
+def mq_linear_tokens(x, w_q, w_bits: int, w_scale, w_zp=None, bias=None, out=None,
+                     out_dtype=None, workspace=None, stream=None):
+    """Linear layer from floating activations x [M][K], quantized token by token,
+    to floating outputs [M][N] (of out's type, or out_dtype, or x's).
+    workspace: a uint8 tensor kept by the caller (allocated here if None)."""
+    dev, st = _device_and_stream(x, "x", stream)
+    torch = _torch_mod
+    tx = _type_of(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x must be [M][K]")
+    M, K = shape = x.shape
+    N, pw, ps, pz, pb = _token_weights(dev, K, w_q, w_bits, w_scale, w_zp, bias)
+    if out is None:
+        out = _empty((M, N), out_dtype or x.dtype, x.device, stream)
+    ty = _type_of(out, "out")
+    if workspace is None:
+        workspace = _empty(mq_linear_tokens_workspace_bytes(M, K, N, w_bits), torch.uint8,
+                           x.device, stream)
+    px, ldx = _rows(x, x.dtype, dev, "x", shape)
+    ws, n = _any_shape(workspace, torch.uint8, dev, "workspace")
+    status = lib().mq_linear_tokens(px, tx, ldx, M, K, N, pw, w_bits, ps, pz, pb,
+                                    _flat(out, out.dtype, dev, "out", (M, N)), ty, ws, n, st)
+    if status:
+        raise MQError(status, "mq_linear_tokens")
     return out
 
 

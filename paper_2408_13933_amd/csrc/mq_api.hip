@@ -5,6 +5,7 @@
 #include <cstdint>
 
 #include "kvcache.h"
+#include "linear_tokens.h"
 #include "mq.h"
 #include "mq_internal.h"
 #include "sample.h"
@@ -69,6 +70,10 @@ mq_status kv_launched(hipError_t e)
 {
     return e == hipErrorInvalidConfiguration ? MQ_ERR_UNSUPPORTED : from_hip(e);
 }
+
+// rows that a call quantizes, a work-group each (a launch has fewer than 2^32
+// threads)
+constexpr int64_t kMaxTokens = 1 << 24;
 
 bool row_stride_ok(int64_t ld, int64_t row) { return ld >= row && ld < ((int64_t)1 << 40); }
 
@@ -847,6 +852,116 @@ mq_status mq_sample(const void* logits, int32_t bits, int64_t M, int64_t V, int6
     return from_hip(mq::launch_sample(logits, bits, M, V, ld, alpha, temperature, top_k, top_p,
                                       min_p, u, tokens, workspace, workspace_bytes,
                                       as_stream(stream)));
+}
+
+mq_status mq_quantize_tokens(const void* x, int32_t type, int64_t M, int64_t K, int64_t ldx,
+                             int8_t* x_q, float* scale, int32_t* rowsum, void* stream)
+{
+    if (!mq::type_ok(type) || M < 0 || M >= kMaxTokens || K < 1 || K > MQ_MAX_K ||
+        !row_stride_ok(ldx, K))
+        return MQ_ERR_INVALID_ARG;
+    if (M == 0) return MQ_OK;
+    if (!x || !x_q || !scale) return MQ_ERR_INVALID_ARG;
+    return from_hip(mq::launch_quantize_tokens(x, type, M, K, ldx, x_q, scale, rowsum, nullptr, 0,
+                                               as_stream(stream)));
+}
+
+// Validation shared by the token products (the activations apart).
+static mq_status tokens_validate(int64_t M, int64_t K, int64_t N, const void* w_q, int32_t w_bits,
+                                 const float* w_scale, const int32_t* w_zp, const float* bias,
+                                 void* y, int32_t y_type, void* workspace, int64_t workspace_bytes,
+                                 int32_t path, mq::QLinearArgs* p, int32_t* path_out)
+{
+    // (the requantizing layers' checks of what both have)
+    static const int32_t unused = 0;
+    mq_status st = mq::qlinear_validate(w_q, 8, w_zp, M, K, N, w_q, w_bits, w_scale, w_zp, &unused,
+                                        1.0f, 0, 1.0f, 0, 16, bias, y, workspace, workspace_bytes,
+                                        path, p, path_out);
+    if (st == MQ_OK && !mq::type_ok(y_type)) st = MQ_ERR_INVALID_ARG;
+    p->a = nullptr;
+    p->a_rowsum = nullptr;
+    p->colsum = nullptr;
+    p->y = nullptr;
+    return st;
+}
+
+mq_status mq_qlinear_tokens(const int8_t* a_q, const float* a_scale, const int32_t* a_rowsum,
+                            int64_t M, int64_t K, int64_t N, const void* w_q, int32_t w_bits,
+                            const float* w_scale, const int32_t* w_zp, const float* bias, void* y,
+                            int32_t y_type, void* workspace, int64_t workspace_bytes,
+                            int32_t path, void* stream)
+{
+    mq::QLinearArgs p;
+    int32_t resolved = MQ_PATH_AUTO;
+    const mq_status st = tokens_validate(M, K, N, w_q, w_bits, w_scale, w_zp, bias, y, y_type,
+                                         workspace, workspace_bytes, path, &p, &resolved);
+    if (st != MQ_OK) return st;
+    if (M == 0 || N == 0) return MQ_OK;
+    if (!a_q || !a_scale || (w_zp == nullptr) != (a_rowsum == nullptr)) return MQ_ERR_INVALID_ARG;
+    p.a = a_q;
+    p.a_rowsum = a_rowsum;
+    return from_hip(mq::launch_qlinear_tokens(p, mq::TokenArgs{a_scale, y, y_type}, resolved,
+                                              as_stream(stream)));
+}
+
+// Workspace of mq_linear_tokens: the K split's counters (4 KiB at most) and
+// parts, then scales, row sums and codes.
+struct TokenSpace {
+    int64_t split, scale, rowsum, codes, bytes;
+};
+static TokenSpace token_space(int64_t M, int64_t K, int64_t split)
+{
+    auto up = [](int64_t v) { return (v + 255) / 256 * 256; };
+    TokenSpace w;
+    w.split = split;
+    w.scale = up(split);
+    w.rowsum = w.scale + up(M * 4);
+    w.codes = w.rowsum + up(M * 4);
+    w.bytes = w.codes + up(M * K);
+    return w;
+}
+
+int64_t mq_linear_tokens_workspace_bytes(int64_t M, int64_t K, int64_t N, int32_t w_bits,
+                                         int32_t splits)
+{
+    const int64_t split = mq_qlinear_workspace_bytes(M, K, N, w_bits, 16);
+    if (split < 0 || M >= kMaxTokens || (splits != 0 && splits != 1)) return -1;
+    return token_space(M, K, splits ? split : 0).bytes;
+}
+
+mq_status mq_linear_tokens(const void* x, int32_t x_type, int64_t ldx, int64_t M, int64_t K,
+                           int64_t N, const void* w_q, int32_t w_bits, const float* w_scale,
+                           const int32_t* w_zp, const float* bias, void* y, int32_t y_type,
+                           void* workspace, int64_t workspace_bytes, void* stream)
+{
+    mq::QLinearArgs p;
+    int32_t path = MQ_PATH_AUTO;
+    const mq_status st = tokens_validate(M, K, N, w_q, w_bits, w_scale, w_zp, bias, y, y_type,
+                                         workspace, workspace_bytes, MQ_PATH_AUTO, &p, &path);
+    if (st != MQ_OK) return st;
+    if (!mq::type_ok(x_type) || !row_stride_ok(ldx, K) || M >= kMaxTokens)
+        return MQ_ERR_INVALID_ARG;
+    if (M == 0 || N == 0) return MQ_OK;
+    if (!x || !workspace) return MQ_ERR_INVALID_ARG;
+    int64_t split = M <= 16 ? 0 : mq::prefill_workspace_bytes(p);
+    if (token_space(M, K, split).bytes > workspace_bytes) split = 0;
+    const TokenSpace w = token_space(M, K, split);
+    if (w.bytes > workspace_bytes) return MQ_ERR_INVALID_ARG;
+    const hipStream_t s = as_stream(stream);
+    int8_t* ws = static_cast<int8_t*>(workspace);
+    p.ws = split ? ws : nullptr;
+    p.ws_bytes = split;
+    mq::TokenArgs t{reinterpret_cast<float*>(ws + w.scale), y, y_type};
+    p.a = ws + w.codes;
+    if (mq::one_token_fused(p, x, x_type))
+        return from_hip(mq::launch_linear_one_token(p, t, x, x_type, s));
+    int32_t* rowsum = w_zp ? reinterpret_cast<int32_t*>(ws + w.rowsum) : nullptr;
+    p.a_rowsum = rowsum;
+    const int64_t counters = split ? mq::prefill_counter_bytes(p) / 4 : 0;
+    const hipError_t e = mq::launch_quantize_tokens(
+        x, x_type, M, K, ldx, ws + w.codes, reinterpret_cast<float*>(ws + w.scale), rowsum,
+        reinterpret_cast<int32_t*>(ws), counters, s);
+    return from_hip(e != hipSuccess ? e : mq::launch_qlinear_tokens(p, t, path, s));
 }
 
 }  // extern "C"
