@@ -921,6 +921,60 @@ int64_t mq_linear_tokens_workspace_bytes(int64_t M, int64_t K, int64_t N, int32_
                                          int32_t splits);
 
 /*
+ * mq_block_cache -- a paged key/value cache in 8 bits with a scale for each
+ * aligned block of tokens and head: a code c stands for c * scale.
+ *   k        device int8 [pages][G][page][D]
+ *   v        device int8 [pages][G][page / 16][D][16]: the 16 codes of one
+ *            channel over 16 tokens are contiguous, 16 tokens' channels follow
+ *            each other
+ *   k_scale, v_scale  device fp32 [pages][G][page / block], positive
+ *   block    tokens per scale, a power of two in [16, page]
+ *   everything else as in mq_kv_cache.  A position's place goes by mq_kv_batch.
+ */
+typedef struct mq_block_cache {
+    int8_t* k;
+    int8_t* v;
+    float* k_scale;
+    float* v_scale;
+    int64_t pages;
+    int32_t page;
+    int32_t block;
+    int32_t G;
+    int32_t D;
+} mq_block_cache;
+
+/*
+ * mq_rope_append_blocks -- mq_rope_append for floating projections and a cache
+ * with block scales.  Queries and keys are rotated in fp64,
+ *   u' = u cos - w sin,  w' = w cos + u sin   (pairs i, i + D/2)
+ * and rounded once to fp32; queries then to their type.  For every block and
+ * head that gets tokens, with A the largest finite magnitude of its new
+ * elements and s_old its scale if it holds tokens before the call's first one
+ * in it (else, or where that scale is not positive and finite, 0):
+ *   s  = max(s_old, max(A, 2^-60) / 127)              the block's scale
+ *   codes it holds   c = rint(c * (s_old / s))        where s is not s_old
+ *   new codes        c = rint(x * (1 / s))
+ * in fp32 (a code is off by half a step for every time its block's scale
+ * grew).  Infinities become codes +-127, NaN 0.
+ *   q, k, v   device, of `type`, row t at + t * ldq (ldk, ldv): H heads of D
+ *             queries, G heads of keys and of values
+ *   angles    as in mq_rope_append (table of mq_rope_table), 16-byte aligned, or
+ *             NULL: none
+ *   q_out     device, of `type`, row t at q_out + t * ldo; may be q itself
+ *             with ldo == ldq
+ *   sizes, strides, positions as in mq_rope_append; two sequences must not
+ *   append to the same block.  What lies past a sequence's last token in its
+ *   block is left as it was.  A call that takes 2^24 work-groups or more is
+ *   MQ_ERR_UNSUPPORTED: it takes at most
+ *   max(1024, T / 4) + 2 G (T / block + 2 B).
+ */
+mq_status mq_rope_append_blocks(const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                const void* v, int64_t ldv, int32_t type, int64_t T, int32_t H,
+                                const double* angles, int64_t positions,
+                                const mq_block_cache* cache, const mq_kv_batch* batch, void* q_out,
+                                int64_t ldo, void* stream);
+
+/*
  * mq_dequant -- inverse of Eq.(4): y = alpha * (float)(q - zp), one exact
  * integer subtraction and one fp32 multiply.
  *   q      device int8 (bits 8) or int16 (bits 16) [numel]

@@ -26,7 +26,7 @@ __all__ = [
     "mq_rope_append", "mq_paged_attn", "mq_paged_attn_workspace_bytes",
     "ATTN_BLOCK", "ATTN_ONE", "mq_sample", "mq_sample_workspace_bytes",
     "F32", "BF16", "F16", "mq_quantize_tokens", "mq_qlinear_tokens", "mq_linear_tokens",
-    "mq_linear_tokens_workspace_bytes",
+    "mq_linear_tokens_workspace_bytes", "mq_rope_append_blocks",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -173,7 +173,9 @@ def lib():
                                    c_p, c_p, c_i32, c_p, c_i64, c_p]
     L.mq_linear_tokens_workspace_bytes.argtypes = [c_i64, c_i64, c_i64, c_i32, c_i32]
     L.mq_linear_tokens_workspace_bytes.restype = c_i64
-    for name in ("mq_quantize_tokens", "mq_qlinear_tokens", "mq_linear_tokens",
+    L.mq_rope_append_blocks.argtypes = [c_p, c_i64, c_p, c_i64, c_p, c_i64, c_i32, c_i64, c_i32,
+                                        c_p, c_i64, c_s, c_s, c_p, c_i64, c_p]
+    for name in ("mq_rope_append_blocks", "mq_quantize_tokens", "mq_qlinear_tokens", "mq_linear_tokens",
                  "mq_sample", "mq_rope_append", "mq_paged_attn", "mq_qlinear_dequant", "mq_qlinear_group", "mq_probe_read", "mq_attn_matmul", "mq_transpose_i8", "mq_act_params", "mq_fold_weights", "mq_fold_acts", "mq_quantize_act",
                  "mq_pack_weights", "mq_qlinear", "mq_qlinear_ex", "mq_qlinear_ws", "mq_dequant",
                  "mq_qlinear_noalloc",
@@ -1206,6 +1208,67 @@ def mq_linear_tokens(x, w_q, w_bits: int, w_scale, w_zp=None, bias=None, out=Non
                                     _flat(out, out.dtype, dev, "out", (M, N)), ty, ws, n, st)
     if status:
         raise MQError(status, "mq_linear_tokens")
+    return out
+
+
+_BLOCK_CACHE = struct.Struct("qqqqqiiii")
+
+
+def _block_args(dev, q, k_cache, k_scale, v_cache, v_scale, starts, lens, pages):
+    """The bytes of mq_block_cache and mq_kv_batch for the cache tensors k
+    [pages][G][page][D], v [pages][G][page / 16][D][16] and their scales
+    [pages][G][page / block], and (G, D, heads of q, B, keys that a page list
+    holds)."""
+    torch = _torch_mod
+    i8, i32, f32 = torch.int8, torch.int32, torch.float32
+    try:
+        n, G, page, D = k_cache.shape
+        nb = k_scale.shape[2]
+        B, ld = pages.shape
+        _, row = q.shape
+    except (AttributeError, IndexError, ValueError):
+        raise ValueError("k_cache must be [pages][G][page][D], its scales [pages][G][page / block], "
+                         "pages [B][entries], q [T][H * D]")
+    if D == 0 or row % D or nb == 0 or page % nb:
+        raise ValueError("q's row length must be heads * D, a page whole blocks")
+    scales = (n, G, nb)
+    c = _BLOCK_CACHE.pack(_any_shape(k_cache, i8, dev, "k_cache")[0],
+                          _flat(v_cache, i8, dev, "v_cache", (n, G, page // 16, D, 16)),
+                          _flat(k_scale, f32, dev, "k_scale", scales),
+                          _flat(v_scale, f32, dev, "v_scale", scales), n, page, page // nb, G, D)
+    b = _KV_BATCH.pack(_flat(starts, i32, dev, "starts", (B + 1,)),
+                       _flat(lens, i32, dev, "lens", (B,)),
+                       _any_shape(pages, i32, dev, "pages")[0], B, ld)
+    return c, b, G, D, row // D, B, ld * page
+
+
+def mq_rope_append_blocks(q, k, v, k_cache, k_scale, v_cache, v_scale, starts, lens, pages,
+                          table=None, out=None, stream=None):
+    """Rotates the new tokens' queries q [T][H * D] (returned, of q's type) and
+    keys k [T][G * D] by their positions and writes keys and values v [T][G * D]
+    to the cache's pages as 8-bit codes of their blocks' scales.
+
+    k_cache int8 [pages][G][page][D], v_cache int8 [pages][G][page / 16][D][16] and
+    their scales fp32 [pages][G][page / block] are updated in place; sequences,
+    page lists, table and out as in mq_rope_append."""
+    dev, st = _device_and_stream(q, "q", stream)
+    torch = _torch_mod
+    t = _type_of(q, "q")
+    c, b, G, D, H, _, _ = _block_args(dev, q, k_cache, k_scale, v_cache, v_scale, starts, lens,
+                                      pages)
+    shape, dt = q.shape, q.dtype
+    T, kv = shape[0], (shape[0], G * D)
+    pq, ldq = _rows(q, dt, dev, "q", shape)
+    pk, ldk = _rows(k, dt, dev, "k", kv)
+    pv, ldv = _rows(v, dt, dev, "v", kv)
+    if out is None:
+        out = _empty(shape, dt, q.device, stream)
+    po, ldo = _rows(out, dt, dev, "out", shape)
+    pt, n = (None, 0) if table is None else _any_shape(table, torch.float64, dev, "table")
+    status = lib().mq_rope_append_blocks(pq, ldq, pk, ldk, pv, ldv, t, T, H, pt, n // D, c, b, po,
+                                         ldo, st)
+    if status:
+        raise MQError(status, "mq_rope_append_blocks")
     return out
 
 

@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstdint>
 
+#include "kvblocks.h"
 #include "kvcache.h"
 #include "linear_tokens.h"
 #include "mq.h"
@@ -62,6 +63,23 @@ mq_status kv_validate(const mq_kv_cache* c, const mq_kv_batch* b, int64_t T, int
     out->G = c->G;
     out->D = c->D;
     out->shift = __builtin_ctz((unsigned)c->page);
+    return MQ_OK;
+}
+
+mq_status block_cache_validate(const mq_block_cache* c, const mq_kv_batch* b, int64_t T, int32_t H,
+                               mq::BlockCache* out)
+{
+    if (!c) return MQ_ERR_INVALID_ARG;
+    const mq_kv_cache kv{c->k, c->v, c->pages, c->page, c->G, c->D};
+    const mq_status st = kv_validate(&kv, b, T, H, &out->kv);
+    if (st != MQ_OK) return st;
+    if (c->block < 16 || c->block > c->page || (c->block & (c->block - 1)) != 0)
+        return MQ_ERR_INVALID_ARG;
+    if (T > 0 && b->B > 0 && c->pages > 0 && (!c->k_scale || !c->v_scale))
+        return MQ_ERR_INVALID_ARG;
+    out->k_scale = c->k_scale;
+    out->v_scale = c->v_scale;
+    out->bshift = __builtin_ctz((unsigned)c->block);
     return MQ_OK;
 }
 
@@ -962,6 +980,27 @@ mq_status mq_linear_tokens(const void* x, int32_t x_type, int64_t ldx, int64_t M
         x, x_type, M, K, ldx, ws + w.codes, reinterpret_cast<float*>(ws + w.scale), rowsum,
         reinterpret_cast<int32_t*>(ws), counters, s);
     return from_hip(e != hipSuccess ? e : mq::launch_qlinear_tokens(p, t, path, s));
+}
+
+mq_status mq_rope_append_blocks(const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                const void* v, int64_t ldv, int32_t type, int64_t T, int32_t H,
+                                const double* angles, int64_t positions,
+                                const mq_block_cache* cache, const mq_kv_batch* batch, void* q_out,
+                                int64_t ldo, void* stream)
+{
+    mq::BlockCache c;
+    const mq_status st = block_cache_validate(cache, batch, T, H, &c);
+    if (st != MQ_OK) return st;
+    const int64_t hd = (int64_t)H * c.kv.D, gd = (int64_t)c.kv.G * c.kv.D;
+    if (!row_stride_ok(ldq, hd) || !row_stride_ok(ldo, hd) || !row_stride_ok(ldk, gd) ||
+        !row_stride_ok(ldv, gd) || !mq::type_ok(type))
+        return MQ_ERR_INVALID_ARG;
+    if (angles && (positions < 0 || positions > ((int64_t)1 << 40) || (uintptr_t)angles % 16 != 0))
+        return MQ_ERR_INVALID_ARG;
+    if (T == 0 || batch->B == 0) return MQ_OK;
+    if (!q || !k || !v || !q_out) return MQ_ERR_INVALID_ARG;
+    return kv_launched(mq::launch_append_blocks(c, q, ldq, k, ldk, v, ldv, type, T, H, angles,
+                                                positions, q_out, ldo, as_stream(stream)));
 }
 
 }  // extern "C"

@@ -45,3 +45,115 @@ def unpack4(w):
 def pack4(w):
     u = w.view(np.uint8) & 15
     return np.ascontiguousarray(u[:, 0::2] | (u[:, 1::2] << 4))
+
+
+# ---------------------------------------------------------------------------
+# The cache with block scales.  Token-major arrays: keys and values as
+# [pages][G][page][D] codes; the values' own layout by v_layout/v_rows.
+
+def v_layout(v):
+    """[pages][G][page][D] to the cache's [pages][G][page / 16][D][16]."""
+    n, G, page, D = v.shape
+    return np.ascontiguousarray(v.reshape(n, G, page // 16, 16, D).swapaxes(3, 4))
+
+
+def v_rows(v):
+    n, G, g, D, _ = v.shape
+    return np.ascontiguousarray(v.swapaxes(3, 4).reshape(n, G, g * 16, D))
+
+
+def place(pages, n_pages, page, b, pos):
+    if pos < 0 or pos // page >= pages.shape[1]:
+        return None
+    at = int(pages[b, pos // page])
+    return (at, pos % page) if 0 <= at < n_pages else None
+
+
+def rotate(x, heads, angle):
+    """One token's fp32 values by cos/sin pairs [D/2][2] (None: not) in fp64,
+    rounded to fp32."""
+    u = x.astype(np.float64).reshape(heads, 2, -1)
+    if angle is None:
+        return x.reshape(heads, -1)
+    c, s = angle[:, 0], angle[:, 1]
+    with np.errstate(invalid="ignore", over="ignore"):
+        return np.concatenate((u[:, 0] * c - u[:, 1] * s, u[:, 1] * c + u[:, 0] * s),
+                              axis=1).astype(f4)
+
+
+def _finite_max(x):
+    a = np.abs(x[np.isfinite(x)])
+    return a.max() if a.size else f4(0)
+
+
+def _block_codes(x, s):
+    with np.errstate(invalid="ignore", over="ignore"):
+        c = np.rint(np.clip(x * (f4(1.0) / s), f4(-127), f4(127)))
+    return np.where(np.isnan(x), 0, c).astype(np.int8)
+
+
+def append_blocks(q, k, v, kc, ks, vc, vs, starts, lens, pages, angles, out):
+    """fp32 rows q, k, v; updates the codes [pages][G][page][D], the scales
+    [pages][G][page / block] and the queries' rows of out in place."""
+    n_pages, G, page, D = kc.shape
+    block = page // ks.shape[2]
+    for b in range(len(lens)):
+        s0, s1, n = int(starts[b]), int(starts[b + 1]), int(lens[b])
+        toks = [(t, n - s1 + t) for t in range(s0, s1)]
+        toks = [(t, p) for t, p in toks if p >= 0 and (angles is None or p < len(angles))]
+        new = {}
+        for t, p in toks:
+            ang = None if angles is None else angles[p]
+            out[t] = rotate(q[t], q.shape[1] // D, ang).reshape(-1)
+            new[p] = rotate(k[t], G, ang), v[t].reshape(G, D)
+        for i in sorted({p // block for p in new}):
+            at = place(pages, n_pages, page, b, i * block)
+            if at is None:
+                continue
+            pg, slot = at
+            ps = [p for p in new if p // block == i]
+            lo = min(ps) - i * block
+            for which, codes, scales in ((0, kc, ks), (1, vc, vs)):
+                x = np.stack([new[p][which] for p in ps])  # [tokens][G][D]
+                for g in range(G):
+                    old = scales[pg, g, slot // block] if lo else f4(0)
+                    if not (old > 0 and np.isfinite(old)):
+                        old = f4(0)
+                    s = np.maximum(old, scale_of(_finite_max(x[:, g])))
+                    before = scales[pg, g, slot // block]
+                    if lo and not before == s:
+                        c = codes[pg, g, slot:slot + lo]
+                        c[...] = np.rint(c.astype(f4) * (old / s)).astype(np.int8)
+                    scales[pg, g, slot // block] = s
+                    codes[pg, g, slot + lo:slot + lo + len(ps)] = _block_codes(x[:, g], s)
+
+
+def attn_blocks(q, kc, ks, vc, vs, starts, lens, pages, logit_scale, window=0, sinks=0):
+    """The rows' contexts [T][H * D] in fp64, and per row and head the sum of
+    weights times |value| (a bound of rounding errors goes by it)."""
+    n_pages, G, page, D = kc.shape
+    block = page // ks.shape[2]
+    T, H = q.shape[0], q.shape[1] // D
+    y, size = np.zeros((T, H, D)), np.zeros((T, H))
+    for b in range(len(lens)):
+        n = min(int(lens[b]), pages.shape[1] * page)
+        pos = [p for p in range(n) if place(pages, n_pages, page, b, p) is not None]
+        pos = np.array(pos, dtype=np.int64)
+        pg, slot = pages[b, pos // page], pos % page
+        for h in range(H):
+            g = h // (H // G)
+            keys = kc[pg, g, slot] * ks[pg, g, slot // block].astype(np.float64)[:, None]
+            vals = vc[pg, g, slot] * vs[pg, g, slot // block].astype(np.float64)[:, None]
+            for t in range(starts[b], starts[b + 1]):
+                at = int(lens[b]) - int(starts[b + 1]) + t
+                see = pos <= at
+                if window > 0:
+                    see &= (pos > at - window) | (pos < sinks)
+                if not see.any():
+                    continue
+                x = keys[see] @ q[t, h * D:(h + 1) * D].astype(np.float64) * logit_scale
+                w = np.exp(x - x.max())
+                w /= w.sum()
+                y[t, h] = w @ vals[see]
+                size[t, h] = (w[:, None] * np.abs(vals[see])).sum(0).max()
+    return y.reshape(T, H * D), size

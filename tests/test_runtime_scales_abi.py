@@ -1,6 +1,8 @@
 """Refusals of the entry points whose scales are found at run time: every
 invalid argument is turned away on the host before anything is enqueued.  No
 GPU is touched: the pointers are never read."""
+import struct
+
 import pytest
 
 import paper_2408_13933_amd as mq
@@ -80,3 +82,67 @@ def test_layer_workspace():
     # codes, scales and row sums; with a K split the parts too
     assert f(40, 4096, 256, 8, False) >= 40 * (4096 + 8)
     assert f(40, 16384, 256, 8) > f(40, 16384, 256, 8, False)
+
+
+def _cache(**kw):
+    a = dict(k=NZ, v=NZ, ks=NZ, vs=NZ, pages=8, page=32, block=16, G=2, D=64)
+    a.update(kw)
+    return struct.pack("qqqqqiiii", *((a[n] or 0) for n in ("k", "v", "ks", "vs", "pages", "page",
+                                                            "block", "G", "D")))
+
+
+def _batch(**kw):
+    a = dict(starts=NZ, lens=NZ, table=NZ, B=3, ld=4)
+    a.update(kw)
+    return struct.pack("qqqqq", a["starts"] or 0, a["lens"] or 0, a["table"] or 0, a["B"], a["ld"])
+
+
+def append(cache=None, batch=None, no_cache=False, no_batch=False, **kw):
+    a = dict(q=NZ, ldq=512, k=NZ, ldk=128, v=NZ, ldv=128, type=1, T=5, H=8, angles=NZ,
+             positions=100, q_out=NZ, ldo=512)
+    a.update(kw)
+    c = None if no_cache else cache or _cache()
+    b = None if no_batch else batch or _batch()
+    return mq.lib().mq_rope_append_blocks(a["q"], a["ldq"], a["k"], a["ldk"], a["v"], a["ldv"],
+                                          a["type"], a["T"], a["H"], a["angles"], a["positions"],
+                                          c, b, a["q_out"], a["ldo"], None)
+
+
+CACHES = [dict(k=None), dict(v=None), dict(ks=None), dict(vs=None), dict(k=NZ + 8), dict(v=NZ + 4),
+          dict(pages=-1), dict(pages=1 << 31), dict(page=8, block=8), dict(page=24), dict(page=0),
+          dict(page=2048), dict(block=8), dict(block=24), dict(block=64), dict(block=0),
+          dict(block=-16), dict(G=0), dict(G=3), dict(G=1025), dict(D=8), dict(D=24), dict(D=0),
+          dict(D=272)]
+BATCHES = [dict(starts=None), dict(lens=None), dict(table=None), dict(B=-1), dict(B=1 << 26),
+           dict(ld=-1), dict(ld=(1 << 31) + 1), dict(B=1 << 20, ld=1 << 20)]
+CALLS = [append]
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_cache_and_batch_are_checked(call):
+    assert call(no_cache=True) == INVALID and call(no_batch=True) == INVALID
+    for kw in CACHES:
+        assert call(cache=_cache(**kw)) == INVALID, kw
+    for kw in BATCHES:
+        assert call(batch=_batch(**kw)) == INVALID, kw
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_no_rows_or_sequences(call):
+    assert call(T=0, q=None) == 0
+    assert call(batch=_batch(B=0, starts=None, lens=None, table=None)) == 0
+
+
+@pytest.mark.parametrize("kw", [
+    dict(q=None), dict(k=None), dict(v=None), dict(q_out=None), dict(T=-1), dict(T=1 << 26),
+    dict(H=0), dict(H=7), dict(H=1026), dict(ldq=511), dict(ldk=127), dict(ldv=127), dict(ldo=511),
+    dict(ldq=1 << 40), dict(type=3), dict(type=-1), dict(positions=-1), dict(angles=NZ + 8),
+    dict(T=(1 << 26) - 1, H=1024, ldq=1 << 16, ldo=1 << 16)])
+def test_append_refuses(kw):
+    assert append(**kw) == INVALID
+
+
+def test_more_work_groups_than_a_launch_has():
+    many = (1 << 26) - 1
+    assert append(T=many) == UNSUPPORTED
+    assert append(batch=_batch(B=many)) == UNSUPPORTED
