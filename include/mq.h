@@ -975,6 +975,43 @@ mq_status mq_rope_append_blocks(const void* q, int64_t ldq, const void* k, int64
                                 int64_t ldo, void* stream);
 
 /*
+ * mq_paged_attn_blocks -- attention of the new tokens of each sequence over its
+ * keys and values in a cache with block scales (the new tokens' own among them:
+ * append first), in one pass.  Query head h reads head h / (H / G) of the cache.
+ * The row at position pos sees the keys j <= pos and, with a sliding window,
+ * (j > pos - window or j < sinks) that have a place in the cache, and its output is
+ *   y_d = sum_j w_j v_jd v_scale[j] / sum_j w_j,
+ *   w_j = exp(logit_scale * k_scale[j] * sum_d q_d k_jd)
+ * with sums, maxima and weights in fp32.  Products take fp16 operands: codes and
+ * bf16 and fp16 queries exactly, fp32 queries to 22 bits; weights to 11 bits (22
+ * for fp32) of their own.  A row that sees nothing gets 0; a row of q that holds
+ * an infinity or NaN gets NaN.  What lies in places that no row sees, scales
+ * included, changes nothing.
+ *   q      device, of `type`, row t at q + t * ldq: H heads of D
+ *   y      device, of `type`, row t at y + t * ldy; must not overlap q or the
+ *          cache
+ *   logit_scale  finite, >= 0
+ *   cache  scales of what is seen positive and finite; value scales below 2^-67
+ *          count as that
+ *   window 0: none, else >= 1; sinks, max_len as in mq_paged_attn
+ *   workspace  as in mq_paged_attn, with mq_paged_attn_blocks_workspace_bytes;
+ *          how many parts the keys are split into changes the order of sums
+ *   sizes as in mq_paged_attn.  A call that takes 2^24 work-groups or more is
+ *   MQ_ERR_UNSUPPORTED: at most T * (H / G) / 64 + B of them per cache head, or,
+ *   with T * (H / G) <= 16 B, T * (H / G) / 16 + B for all.
+ */
+mq_status mq_paged_attn_blocks(const void* q, int64_t ldq, int32_t type, int64_t T, int32_t H,
+                               const mq_block_cache* cache, const mq_kv_batch* batch,
+                               float logit_scale, int64_t window, int64_t sinks, void* y,
+                               int64_t ldy, int64_t max_len, void* workspace,
+                               int64_t workspace_bytes, void* stream);
+
+/* Workspace bytes mq_paged_attn_blocks can use for these sizes (0: the keys are
+ * not split; -1: invalid arguments), at most MQ_ATTN_MAX_WORKSPACE. */
+int64_t mq_paged_attn_blocks_workspace_bytes(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D,
+                                             int64_t max_len);
+
+/*
  * mq_dequant -- inverse of Eq.(4): y = alpha * (float)(q - zp), one exact
  * integer subtraction and one fp32 multiply.
  *   q      device int8 (bits 8) or int16 (bits 16) [numel]

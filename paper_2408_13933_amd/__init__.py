@@ -27,6 +27,7 @@ __all__ = [
     "ATTN_BLOCK", "ATTN_ONE", "mq_sample", "mq_sample_workspace_bytes",
     "F32", "BF16", "F16", "mq_quantize_tokens", "mq_qlinear_tokens", "mq_linear_tokens",
     "mq_linear_tokens_workspace_bytes", "mq_rope_append_blocks",
+    "mq_paged_attn_blocks", "mq_paged_attn_blocks_workspace_bytes",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -175,7 +176,11 @@ def lib():
     L.mq_linear_tokens_workspace_bytes.restype = c_i64
     L.mq_rope_append_blocks.argtypes = [c_p, c_i64, c_p, c_i64, c_p, c_i64, c_i32, c_i64, c_i32,
                                         c_p, c_i64, c_s, c_s, c_p, c_i64, c_p]
-    for name in ("mq_rope_append_blocks", "mq_quantize_tokens", "mq_qlinear_tokens", "mq_linear_tokens",
+    L.mq_paged_attn_blocks_workspace_bytes.argtypes = [c_i64, c_i64, c_i32, c_i32, c_i32, c_i64]
+    L.mq_paged_attn_blocks_workspace_bytes.restype = c_i64
+    L.mq_paged_attn_blocks.argtypes = [c_p, c_i64, c_i32, c_i64, c_i32, c_s, c_s, c_f, c_i64, c_i64,
+                                       c_p, c_i64, c_i64, c_p, c_i64, c_p]
+    for name in ("mq_paged_attn_blocks", "mq_rope_append_blocks", "mq_quantize_tokens", "mq_qlinear_tokens", "mq_linear_tokens",
                  "mq_sample", "mq_rope_append", "mq_paged_attn", "mq_qlinear_dequant", "mq_qlinear_group", "mq_probe_read", "mq_attn_matmul", "mq_transpose_i8", "mq_act_params", "mq_fold_weights", "mq_fold_acts", "mq_quantize_act",
                  "mq_pack_weights", "mq_qlinear", "mq_qlinear_ex", "mq_qlinear_ws", "mq_dequant",
                  "mq_qlinear_noalloc",
@@ -1269,6 +1274,45 @@ def mq_rope_append_blocks(q, k, v, k_cache, k_scale, v_cache, v_scale, starts, l
                                          ldo, st)
     if status:
         raise MQError(status, "mq_rope_append_blocks")
+    return out
+
+
+def mq_paged_attn_blocks_workspace_bytes(T: int, B: int, H: int, G: int, D: int,
+                                         max_len: int) -> int:
+    """Workspace bytes mq_paged_attn_blocks can use for these sizes (0: none)."""
+    n = lib().mq_paged_attn_blocks_workspace_bytes(T, B, H, G, D, max_len)
+    if n < 0:
+        raise ValueError("mq_paged_attn_blocks_workspace_bytes: invalid sizes "
+                         f"{(T, B, H, G, D, max_len)}")
+    return n
+
+
+def mq_paged_attn_blocks(q, k_cache, k_scale, v_cache, v_scale, starts, lens, pages,
+                         logit_scale: float, window: int = 0, sinks: int = 0, max_len: int = 0,
+                         out=None, workspace=None, stream=None):
+    """Attention of the new tokens' queries q [T][H * D] over their sequences'
+    keys and values in a cache with block scales (mq_rope_append_blocks): the
+    contexts [T][H * D] of q's type.  Everything else as in mq_paged_attn."""
+    dev, st = _device_and_stream(q, "q", stream)
+    torch = _torch_mod
+    t = _type_of(q, "q")
+    c, b, G, D, H, B, keys = _block_args(dev, q, k_cache, k_scale, v_cache, v_scale, starts, lens,
+                                         pages)
+    shape, dt = q.shape, q.dtype
+    T = shape[0]
+    pq, ldq = _rows(q, dt, dev, "q", shape)
+    if out is None:
+        out = _empty(shape, dt, q.device, stream)
+    po, ldo = _rows(out, dt, dev, "out", shape)
+    if workspace is None:
+        n = lib().mq_paged_attn_blocks_workspace_bytes(T, B, H, G, D, max_len or keys)
+        workspace = _empty(n, torch.uint8, q.device, stream) if n > 0 else None
+    ws, n = (None, 0) if workspace is None else \
+        _any_shape(workspace, torch.uint8, dev, "workspace")
+    status = lib().mq_paged_attn_blocks(pq, ldq, t, T, H, c, b, logit_scale, window, sinks, po, ldo,
+                                        max_len, ws, n, st)
+    if status:
+        raise MQError(status, "mq_paged_attn_blocks")
     return out
 
 

@@ -1003,4 +1003,34 @@ mq_status mq_rope_append_blocks(const void* q, int64_t ldq, const void* k, int64
                                                 positions, q_out, ldo, as_stream(stream)));
 }
 
+int64_t mq_paged_attn_blocks_workspace_bytes(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D,
+                                             int64_t max_len)
+{
+    if (mq_paged_attn_workspace_bytes(T, B, H, G, D, max_len) < 0) return -1;  // the same checks
+    return mq::attn_blocks_workspace(T, B, H, G, D, max_len);
+}
+
+mq_status mq_paged_attn_blocks(const void* q, int64_t ldq, int32_t type, int64_t T, int32_t H,
+                               const mq_block_cache* cache, const mq_kv_batch* batch,
+                               float logit_scale, int64_t window, int64_t sinks, void* y,
+                               int64_t ldy, int64_t max_len, void* workspace,
+                               int64_t workspace_bytes, void* stream)
+{
+    mq::BlockCache c;
+    const mq_status st = block_cache_validate(cache, batch, T, H, &c);
+    if (st != MQ_OK) return st;
+    const int64_t hd = (int64_t)H * c.kv.D;
+    if (!row_stride_ok(ldq, hd) || !row_stride_ok(ldy, hd) || !mq::type_ok(type))
+        return MQ_ERR_INVALID_ARG;
+    if (!std::isfinite(logit_scale) || logit_scale < 0.0f) return MQ_ERR_INVALID_ARG;
+    if (window < 0 || sinks < 0 || max_len < 0 || workspace_bytes < 0) return MQ_ERR_INVALID_ARG;
+    if (workspace && (uintptr_t)workspace % 256 != 0) return MQ_ERR_INVALID_ARG;
+    if (T == 0 || batch->B == 0) return MQ_OK;
+    if (!q || !y) return MQ_ERR_INVALID_ARG;
+    if (max_len == 0) max_len = batch->ld << c.kv.shift;
+    return kv_launched(mq::launch_attn_blocks(c, q, ldq, type, T, H, logit_scale, window, sinks, y,
+                                              ldy, max_len, workspace, workspace_bytes,
+                                              as_stream(stream)));
+}
+
 }  // extern "C"

@@ -35,6 +35,7 @@
 
 #include "codes.h"
 #include "kvcache.h"
+#include "kvwalk.h"
 #include "mq_internal.h"
 #include "requant.h"
 
@@ -49,6 +50,7 @@ constexpr int kRows = 16;             // rows per wave
 constexpr int kWaves = 4;             // waves per work-group
 constexpr int kTile = kRows * kWaves; // rows per work-group where the waves share keys
 constexpr int kMaxSplits = 256;
+using Tile = RowTile<kBlk>;
 constexpr int32_t kNone = INT32_MIN;  // no key seen (|c| <= 65535 * 128 * 256 < 2^31)
 
 struct AttnArgs {
@@ -218,11 +220,6 @@ __device__ inline void load_queries(const AttnArgs& p, int64_t t, int32_t head, 
         for (int s = 0; s < KS; ++s) split_a16(raw[s][0], raw[s][1], qh[s], ql[s]);
     }
 }
-
-// What one row sees: positions (lo, hi], and below the sinks.
-struct Sees {
-    int32_t lo, hi;
-};
 
 // Where a lane reads a block's keys and values of half h: the key row
 // 16 (r >> 2) + (r & 3) of tile 0 (tile j: 4 j rows on) from channel 16 g on,
@@ -605,24 +602,6 @@ __device__ inline void store_out(const AttnArgs& p, int64_t t, int32_t head, int
     else static_cast<int16_t*>(p.y)[at] = (int16_t)q;
 }
 
-// A tile of rows of one sequence and the blocks that its rows see.  Positions
-// are below 2^31 and above -2^26 (lengths are int32).
-struct Tile {
-    int32_t b;
-    int32_t s0, pos0;         // the sequence's first token row and its position
-    uint32_t row0, rows;      // first row (token, head of the group), the sequence's rows
-    int32_t n, skip0, skip1;  // blocks to walk: n, without those in [skip0, skip1)
-    int32_t hi_min, hi_max;   // positions of the first and last token
-    int32_t last;             // of the page list's entries, the last one that a row sees
-    __device__ int32_t block(int32_t i) const { return i < skip0 ? i : i + (skip1 - skip0); }
-    // Every row sees all positions of the block.
-    __device__ bool full(const AttnArgs& p, int32_t blk) const
-    {
-        return blk * kBlk + (kBlk - 1) <= hi_min &&
-               (p.window == 0 || blk * kBlk > hi_max - p.window);
-    }
-};
-
 // The page list's entries for a block's eight 16-key groups, in the lanes' low
 // three bits, as they are (looked at when the block's turn comes, so that the
 // load can be under way until then).  Entries past the tile's last are not read.
@@ -639,55 +618,6 @@ __device__ inline int32_t valid_pages(const AttnArgs& p, const Tile& t, int32_t 
 {
     return page_entry(p, blk) <= t.last && pages >= 0 && pages < (int32_t)p.kv.pages ? pages : -1;
 }
-
-// The tile's index counts from floor(starts[b] grp / R) + b for sequence b: an
-// upper bound of the tiles before it that needs no scan.
-template <int R>
-__device__ inline bool find_tile(const AttnArgs& p, int64_t index, Tile& t)
-{
-    const int32_t* starts = p.kv.starts;
-    const int32_t grp = p.grp;
-    t.b = find_seq(p.kv.B, index, [=](int32_t i) { return (int64_t)starts[i] * grp / R + i; });
-    const int32_t s0 = starts[t.b], s1 = starts[t.b + 1], len = max(p.kv.lens[t.b], 0);
-    if (s0 < 0 || s1 > (int32_t)p.T || s0 >= s1) return false;
-    const int64_t row0 = (index - ((int64_t)s0 * grp / R + t.b)) * R;
-    t.s0 = s0;
-    t.rows = (uint32_t)(s1 - s0) * (uint32_t)grp;  // below 2^32 (T H D is below 2^36)
-    if (row0 < 0 || row0 >= (int64_t)t.rows) return false;
-    t.row0 = (uint32_t)row0;
-    t.pos0 = len - (s1 - s0);
-    t.hi_max = t.pos0 + (int32_t)((min(t.row0 + (R - 1), t.rows - 1)) / (uint32_t)grp);
-    t.hi_min = t.pos0 + (int32_t)(t.row0 / (uint32_t)grp);
-    // blocks with places, up to the last row's
-    const int64_t list = ((p.kv.ld << p.kv.shift) + kBlk - 1) / kBlk;
-    const int32_t end = t.hi_max < 0 ? 0 : (int32_t)min((int64_t)(t.hi_max / kBlk + 1), list);
-    t.last = (int32_t)min((int64_t)(t.hi_max >> p.kv.shift), p.kv.ld - 1);
-    t.skip0 = t.skip1 = 0;
-    if (p.window > 0) {
-        t.skip1 = t.hi_min >= p.window ? min((t.hi_min - p.window + 1) / kBlk, end) : 0;
-        t.skip0 = min((int32_t)(((int64_t)p.sinks + kBlk - 1) / kBlk), t.skip1);
-    }
-    t.n = end - (t.skip1 - t.skip0);
-    return true;
-}
-
-// Row lane & 15 of the 16 from `first` on: token row, query head, what it sees.
-struct RowAt {
-    bool have;
-    int64_t t;
-    int32_t head;
-    Sees sees;
-    __device__ RowAt(const AttnArgs& p, const Tile& tile, uint32_t first, int32_t g0)
-    {
-        const uint32_t x = first + (threadIdx.x & 15);  // no overflow: rows below 2^32 - 64
-        have = x < tile.rows;
-        const uint32_t row = have ? x : tile.rows - 1, tok = row / (uint32_t)p.grp;
-        t = (int64_t)tile.s0 + tok;
-        head = g0 * p.grp + (int32_t)(row - tok * (uint32_t)p.grp);
-        sees.hi = max(tile.pos0 + (int32_t)tok, -1);
-        sees.lo = p.window > 0 && sees.hi >= p.window ? sees.hi - p.window : -1;
-    }
-};
 
 // Four waves share 16 rows and take every fourth block of [i0, i1); their
 // states are joined through LDS, J output tiles at a time.
@@ -839,15 +769,6 @@ __device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g
     }
 }
 
-// The split's blocks [i0, i1) of the tile.
-__device__ inline void split_range(const AttnArgs& p, const Tile& t, int split, int32_t& i0,
-                                   int32_t& i1)
-{
-    const int32_t per = (t.n + p.splits - 1) / p.splits;
-    i0 = per * split;
-    i1 = min(i0 + per, t.n);
-}
-
 // grid (tiles of 16 rows, G, splits)
 template <int KS, int ND>
 __global__ __launch_bounds__(256, KS == 1 ? 3 : KS == 2 ? 2 : 1) void paged_attn_split_kernel(AttnArgs p)
@@ -855,46 +776,10 @@ __global__ __launch_bounds__(256, KS == 1 ? 3 : KS == 2 ? 2 : 1) void paged_attn
     constexpr int J = ND < 4 ? ND : 4;
     __shared__ double lds[kJoinDoubles<J>];
     Tile tile;
-    if (!find_tile<kRows>(p, blockIdx.x, tile)) return;
+    if (!find_tile<kRows, kBlk>(p, blockIdx.x, tile)) return;
     int32_t i0, i1;
     split_range(p, tile, blockIdx.z, i0, i1);
     split_rows<KS, ND, J>(p, tile, blockIdx.y, i0, i1, blockIdx.z, lds);
-}
-
-// Work-groups go to the eight XCDs in turn, each with an L2 of its own: those
-// that read the same keys (a cache head's part) are given to one XCD, or to
-// 8 / n of them in turn where there are n < 8 such parts.  The tiles of an
-// XCD come heaviest first up to the middle (the last tokens of a prompt see
-// the most keys), then lightest first, so that a CU's two work-groups add up
-// to the same.
-struct Place {
-    int64_t tile;
-    int32_t part;  // g + G * split
-};
-__device__ inline Place place_of(const AttnArgs& p, int64_t id, int64_t tiles)
-{
-    const int64_t parts = (int64_t)p.kv.G * p.splits;
-    Place w;
-    int64_t n = tiles, at;
-    if (parts % 8 == 0) {
-        const int64_t slot = id >> 3;
-        w.part = (int32_t)((slot / tiles) * 8 + (id & 7));
-        at = slot % tiles;
-    } else if (8 % parts == 0) {
-        const int64_t r = 8 / parts;
-        w.part = (int32_t)((id & 7) % parts);
-        n = (tiles + r - 1) / r;
-        at = id >> 3;
-        w.tile = ((id & 7) / parts);  // of every r tiles
-        at = at < n - n / 2 ? n - 1 - at : at - (n - n / 2);
-        w.tile += at * r;
-        return w;
-    } else {
-        w.part = (int32_t)(id / tiles);
-        at = id % tiles;
-    }
-    w.tile = at < n - n / 2 ? n - 1 - at : at - (n - n / 2);
-    return w;
 }
 
 // One work-group per tile of 64 rows, cache head and split; a sequence's last
@@ -907,7 +792,7 @@ __global__ __launch_bounds__(256, KS == 1 ? 3 : KS == 2 ? 2 : 1) void paged_attn
     const Place w = place_of(p, blockIdx.x, tiles);
     const int32_t g0 = w.part % p.kv.G, split = w.part / p.kv.G;
     Tile tile;
-    if (w.tile >= tiles || !find_tile<kTile>(p, w.tile, tile)) return;
+    if (w.tile >= tiles || !find_tile<kTile, kBlk>(p, w.tile, tile)) return;
     int32_t i0, i1;
     split_range(p, tile, split, i0, i1);
     if (tile.rows - tile.row0 <= kRows)
@@ -984,9 +869,6 @@ __global__ __launch_bounds__(NW < 4 ? 256 : 64 * NW) void paged_attn_join_kernel
     }
     if (have) store_out(p, t, (int32_t)(row % p.H), d, out_code(p, acc, z, out_unit(p, z)));
 }
-
-// Row tiles of all sequences, at most.
-int64_t row_tiles(int64_t T, int64_t B, int32_t grp, int R) { return T * grp / R + B; }
 
 // Whether the sequences have more rows than a wave takes, on average.
 bool tiled(int64_t T, int64_t B, int32_t grp) { return T * grp > B * kRows; }

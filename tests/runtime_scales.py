@@ -129,31 +129,57 @@ def append_blocks(q, k, v, kc, ks, vc, vs, starts, lens, pages, angles, out):
 
 
 def attn_blocks(q, kc, ks, vc, vs, starts, lens, pages, logit_scale, window=0, sinks=0):
-    """The rows' contexts [T][H * D] in fp64, and per row and head the sum of
-    weights times |value| (a bound of rounding errors goes by it)."""
+    """The rows' contexts [T][H * D] in fp64 and what bounds their rounding
+    errors, per row and head: the largest over channels of sum w |v|, over keys of
+    sum |q k| logit_scale, the keys seen (0: none)."""
     n_pages, G, page, D = kc.shape
     block = page // ks.shape[2]
     T, H = q.shape[0], q.shape[1] // D
-    y, size = np.zeros((T, H, D)), np.zeros((T, H))
+    y, size, most, count = np.zeros((T, H, D)), np.zeros((T, H)), np.zeros((T, H)), np.zeros((T, H))
     for b in range(len(lens)):
         n = min(int(lens[b]), pages.shape[1] * page)
         pos = [p for p in range(n) if place(pages, n_pages, page, b, p) is not None]
         pos = np.array(pos, dtype=np.int64)
         pg, slot = pages[b, pos // page], pos % page
+        at = np.arange(starts[b], starts[b + 1]) + int(lens[b]) - int(starts[b + 1])
         for h in range(H):
             g = h // (H // G)
-            keys = kc[pg, g, slot] * ks[pg, g, slot // block].astype(np.float64)[:, None]
-            vals = vc[pg, g, slot] * vs[pg, g, slot // block].astype(np.float64)[:, None]
+            # (scales of what no row sees may be anything)
+            with np.errstate(invalid="ignore", over="ignore"):
+                k = kc[pg, g, slot] * ks[pg, g, slot // block].astype(np.float64)[:, None]
+                v = vc[pg, g, slot] * vs[pg, g, slot // block].astype(np.float64)[:, None]
             for t in range(starts[b], starts[b + 1]):
-                at = int(lens[b]) - int(starts[b + 1]) + t
-                see = pos <= at
+                p = at[t - starts[b]]
+                see = pos <= p
                 if window > 0:
-                    see &= (pos > at - window) | (pos < sinks)
+                    see &= (pos > p - window) | (pos < sinks)
                 if not see.any():
                     continue
-                x = keys[see] @ q[t, h * D:(h + 1) * D].astype(np.float64) * logit_scale
+                r = q[t, h * D:(h + 1) * D].astype(np.float64)
+                x = k[see] @ r * logit_scale
                 w = np.exp(x - x.max())
                 w /= w.sum()
-                y[t, h] = w @ vals[see]
-                size[t, h] = (w[:, None] * np.abs(vals[see])).sum(0).max()
-    return y.reshape(T, H * D), size
+                y[t, h] = w @ v[see]
+                size[t, h] = (w @ np.abs(v[see])).max()
+                most[t, h] = (np.abs(k[see]) @ np.abs(r)).max() * logit_scale
+                count[t, h] = see.sum()
+    return y.reshape(T, H * D), size, most, count
+
+
+def attn_bound(size, most, count, D, bits, vs_log2):
+    """How far a context of attn_blocks may be off before its last rounding, per
+    row and head.  With u = 2^-24 and logits in log2 units, X = most * log2(e):
+    a logit is the sum of at most D products in fp32 (D u X, as much again for
+    the order inside an instruction's sums; fp32 queries are short of 2^-22 X), its
+    factor has three roundings (4 u X), the exponent adds log2 of the value scale
+    and the maximum (numbers up to X + |log2 vs| + 8: four roundings); a weight
+    takes its exp2 (2^-22) and its rounding (2^-11 for 16-bit types, else 2^-22);
+    numerator and denominator each sum `count` terms over steps of 64 ((count /
+    16 + 64) u); every relative error of a weight counts in both.  Weights too
+    small for fp16 are short of 2^-25 of 2^1 at least (the largest is >= 2): count
+    * 2^-26 of the values."""
+    u, X = 2.0 ** -24, most * 1.4426950408889634
+    logit = (2 * D * u + 2.0 ** -22 + 4 * u) * X + 4 * u * (X + vs_log2 + 8)
+    weight = 2.0 ** -22 + (2.0 ** -11 if bits == 16 else 2.0 ** -22)
+    rel = 2 * (0.6931471805599453 * logit + weight + (count / 16 + 64) * u)
+    return size * rel * 1.01, count * 2.0 ** -26

@@ -115,7 +115,20 @@ CACHES = [dict(k=None), dict(v=None), dict(ks=None), dict(vs=None), dict(k=NZ + 
           dict(D=272)]
 BATCHES = [dict(starts=None), dict(lens=None), dict(table=None), dict(B=-1), dict(B=1 << 26),
            dict(ld=-1), dict(ld=(1 << 31) + 1), dict(B=1 << 20, ld=1 << 20)]
-CALLS = [append]
+
+
+def attend(cache=None, batch=None, no_cache=False, no_batch=False, **kw):
+    a = dict(q=NZ, ldq=512, type=1, T=5, H=8, ls=0.125, window=0, sinks=0, y=NZ, ldy=512,
+             max_len=0, ws=NZ, wsb=0)
+    a.update(kw)
+    c = None if no_cache else cache or _cache()
+    b = None if no_batch else batch or _batch()
+    return mq.lib().mq_paged_attn_blocks(a["q"], a["ldq"], a["type"], a["T"], a["H"], c, b, a["ls"],
+                                         a["window"], a["sinks"], a["y"], a["ldy"], a["max_len"],
+                                         a["ws"], a["wsb"], None)
+
+
+CALLS = [append, attend]
 
 
 @pytest.mark.parametrize("call", CALLS)
@@ -146,3 +159,26 @@ def test_more_work_groups_than_a_launch_has():
     many = (1 << 26) - 1
     assert append(T=many) == UNSUPPORTED
     assert append(batch=_batch(B=many)) == UNSUPPORTED
+    assert attend(batch=_batch(B=many)) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("kw", [
+    dict(q=None), dict(y=None), dict(T=-1), dict(T=1 << 26), dict(H=0), dict(H=9), dict(ldq=511),
+    dict(ldy=511), dict(ldy=1 << 40), dict(type=3), dict(type=-1), dict(ls=-0.1), dict(ls=NAN),
+    dict(ls=float("inf")), dict(window=-1), dict(sinks=-1), dict(max_len=-1), dict(wsb=-1),
+    dict(ws=NZ + 16, wsb=4096)])
+def test_attend_refuses(kw):
+    assert attend(**kw) == INVALID
+
+
+def test_attention_workspace():
+    f = mq.mq_paged_attn_blocks_workspace_bytes
+    for args in [(-1, 1, 8, 2, 64, 1), (1, -1, 8, 2, 64, 1), (1, 1, 0, 2, 64, 1),
+                 (1, 1, 8, 3, 64, 1), (1, 1, 8, 2, 60, 1), (1, 1, 8, 2, 272, 1),
+                 (1, 1, 8, 2, 64, -1), (1 << 26, 1, 8, 2, 64, 1)]:
+        assert mq.lib().mq_paged_attn_blocks_workspace_bytes(*args) == -1
+        with pytest.raises(ValueError):
+            f(*args)
+    for args in [(1, 1, 32, 4, 64, 1 << 20), (512, 512, 64, 8, 128, 1 << 17),
+                 (4096, 1, 32, 4, 64, 4096), (1, 1, 8, 1, 256, 100), (0, 0, 8, 1, 64, 9)]:
+        assert 0 <= f(*args) <= 64 << 20
