@@ -1012,6 +1012,58 @@ int64_t mq_paged_attn_blocks_workspace_bytes(int64_t T, int64_t B, int32_t H, in
                                              int64_t max_len);
 
 /*
+ * mq_logit_rules -- what mq_adjust_logits applies.  Every part may be left out
+ * (its first pointer NULL).
+ *   history      device int32 [M][ldh]: the words that row m's sequence holds, its
+ *                prompt first, hist_lens[m] of them (limited to `cols`, the words a
+ *                row has room for; cols <= ldh); words outside [0, V) count nothing
+ *   hist_lens    device int32 [M]
+ *   prompt_lens  device int32 [M]: the first so many are the prompt (NULL: 0)
+ *   repetition, presence, frequency  device fp32 [M], NULL: 1, 0, 0
+ *   bias_starts  device int32 [M + 1], ascending: row m's entries of bias_tokens
+ *                (int32) and bias_values (fp32), bias_n in all, are
+ *                [bias_starts[m], bias_starts[m + 1]); of entries for one word the
+ *                last counts
+ *   mask         device uint32 [M][ldm]: word i is allowed where bit i % 32 of entry
+ *                i / 32 is set
+ */
+typedef struct mq_logit_rules {
+    const int32_t* history;
+    const int32_t* hist_lens;
+    const int32_t* prompt_lens;
+    int64_t ldh;
+    int64_t cols;
+    const float* repetition;
+    const float* presence;
+    const float* frequency;
+    const int32_t* bias_starts;
+    const int32_t* bias_tokens;
+    const float* bias_values;
+    int64_t bias_n;
+    const uint32_t* mask;
+    int64_t ldm;
+} mq_logit_rules;
+
+/*
+ * mq_adjust_logits -- changes every row of logits x [M][V] in place, before
+ * mq_sample draws from them.  For a word that row m's sequence holds, n times
+ * past its prompt:
+ *   x = x > 0 ? x / repetition[m] : x * repetition[m]
+ *   x = (x - frequency[m] * n) - presence[m]            where n > 0
+ * then, for a word with a bias, x = x + bias; a word that the mask forbids
+ * becomes -infinity.  Each step is rounded once in fp32, the result once to x's
+ * type.  Other words are not touched, nor read.
+ *   x      device, of `type` (fp32 for mq_sample), row m at x + m * ld
+ *   rules  host struct
+ *   0 <= M < 2^31; 1 <= V <= MQ_SAMPLE_MAX_V; V <= ld < 2^40; cols >= 0,
+ *   cols <= ldh < 2^40; ceil(V / 32) <= ldm < 2^40; 0 <= bias_n < 2^31.  A call
+ *   that takes 2^23 work-groups or more, M * ceil(V / 4096), is
+ *   MQ_ERR_UNSUPPORTED.
+ */
+mq_status mq_adjust_logits(void* x, int32_t type, int64_t M, int64_t V, int64_t ld,
+                           const mq_logit_rules* rules, void* stream);
+
+/*
  * mq_dequant -- inverse of Eq.(4): y = alpha * (float)(q - zp), one exact
  * integer subtraction and one fp32 multiply.
  *   q      device int8 (bits 8) or int16 (bits 16) [numel]

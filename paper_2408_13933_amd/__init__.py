@@ -28,6 +28,7 @@ __all__ = [
     "F32", "BF16", "F16", "mq_quantize_tokens", "mq_qlinear_tokens", "mq_linear_tokens",
     "mq_linear_tokens_workspace_bytes", "mq_rope_append_blocks",
     "mq_paged_attn_blocks", "mq_paged_attn_blocks_workspace_bytes",
+    "mq_adjust_logits",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -180,7 +181,8 @@ def lib():
     L.mq_paged_attn_blocks_workspace_bytes.restype = c_i64
     L.mq_paged_attn_blocks.argtypes = [c_p, c_i64, c_i32, c_i64, c_i32, c_s, c_s, c_f, c_i64, c_i64,
                                        c_p, c_i64, c_i64, c_p, c_i64, c_p]
-    for name in ("mq_paged_attn_blocks", "mq_rope_append_blocks", "mq_quantize_tokens", "mq_qlinear_tokens", "mq_linear_tokens",
+    L.mq_adjust_logits.argtypes = [c_p, c_i32, c_i64, c_i64, c_i64, c_s, c_p]
+    for name in ("mq_adjust_logits", "mq_paged_attn_blocks", "mq_rope_append_blocks", "mq_quantize_tokens", "mq_qlinear_tokens", "mq_linear_tokens",
                  "mq_sample", "mq_rope_append", "mq_paged_attn", "mq_qlinear_dequant", "mq_qlinear_group", "mq_probe_read", "mq_attn_matmul", "mq_transpose_i8", "mq_act_params", "mq_fold_weights", "mq_fold_acts", "mq_quantize_act",
                  "mq_pack_weights", "mq_qlinear", "mq_qlinear_ex", "mq_qlinear_ws", "mq_dequant",
                  "mq_qlinear_noalloc",
@@ -1314,6 +1316,61 @@ def mq_paged_attn_blocks(q, k_cache, k_scale, v_cache, v_scale, starts, lens, pa
     if status:
         raise MQError(status, "mq_paged_attn_blocks")
     return out
+
+
+_LOGIT_RULES = struct.Struct("qqqqqqqqqqqqqq")
+
+
+def mq_adjust_logits(logits, history=None, hist_lens=None, prompt_lens=None, repetition=None,
+                     presence=None, frequency=None, bias=None, mask=None, stream=None):
+    """Changes logits [M][V] (float32, bfloat16 or float16) in place and returns
+    them: penalties for the words of history int32 [M][words] (hist_lens[m] of
+    them, the first prompt_lens[m] the prompt) by repetition, presence and
+    frequency fp32 [M]; bias: (starts int32 [M + 1], words int32, values fp32);
+    mask: int32 (or uint32) [M][>= V / 32], bit i % 32 of entry i / 32 allows word i."""
+    dev, st = _device_and_stream(logits, "logits", stream)
+    torch = _torch_mod
+    t = _type_of(logits, "logits")
+    f32, i32 = torch.float32, torch.int32
+    if logits.dim() != 2:
+        raise ValueError("logits must be [M][V]")
+    M, V = shape = logits.shape
+    px, ld = _rows(logits, logits.dtype, dev, "logits", shape)
+    row = (M,)
+    ph = pl = pp = ldh = cols = 0
+    if history is not None:
+        try:
+            cols = history.shape[1]
+        except (AttributeError, IndexError):
+            raise ValueError("history must be an int32 tensor [M][words]")
+        ph, ldh = _rows(history, i32, dev, "history", (M, cols))
+        pl = _flat(hist_lens, i32, dev, "hist_lens", row)
+        pp = 0 if prompt_lens is None else _flat(prompt_lens, i32, dev, "prompt_lens", row)
+    ps = pt = pv = n = 0
+    if bias is not None:
+        starts, words, values = bias
+        pt, n = _any_shape(words, i32, dev, "bias words")
+        ps = _flat(starts, i32, dev, "bias starts", (M + 1,))
+        pv = _flat(values, f32, dev, "bias values", words.shape)
+    pm = ldm = 0
+    if mask is not None:
+        try:
+            dt, entries = mask.dtype, mask.shape[1]
+        except (AttributeError, IndexError):
+            raise ValueError("mask must be an int32 or uint32 tensor [M][entries]")
+        if (dt is not i32 and dt is not torch.uint32) or entries * 32 < V:
+            raise ValueError("mask must be int32 or uint32 with a bit for every word")
+        pm, ldm = _rows(mask, dt, dev, "mask", (M, entries))
+    rules = _LOGIT_RULES.pack(
+        ph, pl, pp, ldh, cols,
+        0 if repetition is None else _flat(repetition, f32, dev, "repetition", row),
+        0 if presence is None else _flat(presence, f32, dev, "presence", row),
+        0 if frequency is None else _flat(frequency, f32, dev, "frequency", row),
+        ps, pt, pv, n, pm, ldm)
+    status = lib().mq_adjust_logits(px, t, M, V, ld, rules, st)
+    if status:
+        raise MQError(status, "mq_adjust_logits")
+    return logits
 
 
 def mq_dequant(q, alpha: float, zp: int, out=None, stream=None):

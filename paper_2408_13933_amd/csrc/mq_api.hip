@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstdint>
 
+#include "adjust.h"
 #include "kvblocks.h"
 #include "kvcache.h"
 #include "linear_tokens.h"
@@ -1031,6 +1032,27 @@ mq_status mq_paged_attn_blocks(const void* q, int64_t ldq, int32_t type, int64_t
     return kv_launched(mq::launch_attn_blocks(c, q, ldq, type, T, H, logit_scale, window, sinks, y,
                                               ldy, max_len, workspace, workspace_bytes,
                                               as_stream(stream)));
+}
+
+mq_status mq_adjust_logits(void* x, int32_t type, int64_t M, int64_t V, int64_t ld,
+                           const mq_logit_rules* rules, void* stream)
+{
+    if (!mq::type_ok(type) || M < 0 || M > 0x7FFFFFFF || V < 1 || V > MQ_SAMPLE_MAX_V ||
+        !row_stride_ok(ld, V) || !rules)
+        return MQ_ERR_INVALID_ARG;
+    const mq_logit_rules& r = *rules;
+    if (r.history && (r.cols < 0 || !row_stride_ok(r.ldh, r.cols))) return MQ_ERR_INVALID_ARG;
+    if (r.mask && !row_stride_ok(r.ldm, (V + 31) / 32)) return MQ_ERR_INVALID_ARG;
+    if (r.bias_starts && (r.bias_n < 0 || r.bias_n > 0x7FFFFFFE)) return MQ_ERR_INVALID_ARG;
+    if (M == 0) return MQ_OK;
+    if (!x || (r.history && !r.hist_lens)) return MQ_ERR_INVALID_ARG;
+    if (r.bias_starts && r.bias_n > 0 && (!r.bias_tokens || !r.bias_values))
+        return MQ_ERR_INVALID_ARG;
+    if (!r.history && !r.bias_starts && !r.mask) return MQ_OK;
+    const mq::AdjustArgs p{x, M, V, ld, r.history, r.ldh, r.cols, r.hist_lens, r.prompt_lens,
+                           r.repetition, r.presence, r.frequency, r.bias_starts, r.bias_tokens,
+                           r.bias_values, r.bias_n, r.mask, r.ldm};
+    return kv_launched(mq::launch_adjust(p, type, as_stream(stream)));
 }
 
 }  // extern "C"

@@ -183,3 +183,35 @@ def attn_bound(size, most, count, D, bits, vs_log2):
     weight = 2.0 ** -22 + (2.0 ** -11 if bits == 16 else 2.0 ** -22)
     rel = 2 * (0.6931471805599453 * logit + weight + (count / 16 + 64) * u)
     return size * rel * 1.01, count * 2.0 ** -26
+
+
+def adjust_logits(x, history=None, lens=None, prompts=None, repetition=None, presence=None,
+                  frequency=None, bias=None, mask=None):
+    """fp32 logits [M][V] changed step by step, each rounded to fp32."""
+    x = x.astype(f4).copy()
+    M, V = x.shape
+    for m in range(M):
+        if history is not None:
+            words = history[m, :max(0, min(int(lens[m]), history.shape[1]))]
+            p = max(0, int(prompts[m])) if prompts is not None else 0
+            drawn = words[p:]
+            r = f4(1) if repetition is None else repetition[m]
+            for w in np.unique(words[(words >= 0) & (words < V)]):
+                x[m, w] = x[m, w] / r if x[m, w] > 0 else x[m, w] * r
+                n = int((drawn == w).sum())
+                if n:
+                    f = f4(0) if frequency is None else frequency[m]
+                    x[m, w] = x[m, w] - f * f4(n)
+                    x[m, w] = x[m, w] - (f4(0) if presence is None else presence[m])
+        if bias is not None:
+            starts, words, values = bias
+            last = {}
+            for i in range(max(0, starts[m]), min(starts[m + 1], len(words))):
+                if 0 <= words[i] < V:
+                    last[words[i]] = values[i]
+            for w, v in last.items():
+                x[m, w] = x[m, w] + v
+        if mask is not None:
+            bits = np.unpackbits(np.ascontiguousarray(mask[m]).view(np.uint8), bitorder="little")
+            x[m, bits[:V] == 0] = -np.inf
+    return x

@@ -182,3 +182,29 @@ def test_attention_workspace():
     for args in [(1, 1, 32, 4, 64, 1 << 20), (512, 512, 64, 8, 128, 1 << 17),
                  (4096, 1, 32, 4, 64, 4096), (1, 1, 8, 1, 256, 100), (0, 0, 8, 1, 64, 9)]:
         assert 0 <= f(*args) <= 64 << 20
+
+
+def adjust(no_rules=False, **kw):
+    a = dict(x=NZ, type=0, M=3, V=100, ld=100, h=NZ, hl=NZ, pl=NZ, ldh=8, cols=8, r=NZ, p=NZ, f=NZ,
+             bs=NZ, bt=NZ, bv=NZ, bn=4, m=NZ, ldm=4)
+    a.update(kw)
+    rules = struct.pack("14q", *((a[n] or 0) for n in ("h", "hl", "pl", "ldh", "cols", "r", "p",
+                                                       "f", "bs", "bt", "bv", "bn", "m", "ldm")))
+    return mq.lib().mq_adjust_logits(a["x"], a["type"], a["M"], a["V"], a["ld"],
+                                     None if no_rules else rules, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(no_rules=True), dict(x=None), dict(type=3), dict(type=-1), dict(M=-1), dict(M=1 << 31),
+    dict(V=0), dict(V=(1 << 22) + 1, ld=1 << 23, ldm=1 << 20), dict(ld=99), dict(ld=1 << 40),
+    dict(hl=None), dict(cols=-1), dict(ldh=7), dict(ldh=1 << 40), dict(bt=None), dict(bv=None),
+    dict(bn=-1), dict(bn=1 << 31), dict(ldm=3), dict(ldm=1 << 40)])
+def test_adjust_refuses(kw):
+    assert adjust(**kw) == INVALID
+
+
+def test_adjust_nothing_to_do_and_too_much():
+    assert adjust(M=0, x=None) == 0
+    assert adjust(h=None, bs=None, m=None) == 0
+    assert adjust(M=1 << 23) == UNSUPPORTED
+    assert adjust(M=1 << 13, V=1 << 22, ld=1 << 22, ldm=1 << 17) == UNSUPPORTED
