@@ -26,6 +26,7 @@
 #include "kvwalk.h"
 #include "mq_internal.h"
 #include "tokens.h"
+#include "wave.h"
 
 #define MQ_LDS __attribute__((address_space(3)))
 #define MQ_GLOBAL __attribute__((address_space(1)))
@@ -36,17 +37,20 @@ namespace {
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
 constexpr int kBlk = 64;                  // key positions per step
 constexpr int kRows = 16;                 // rows per set
-constexpr int kWaves = 4;                 // waves per work-group
+constexpr int kWaves = 4;                 // waves per work-group that share keys
 // sets per wave where the waves share keys (fp32 rows of more than 192 channels
 // leave registers for one)
 template <int KS, int N>
 constexpr int kSets = KS == 4 && N == 2 ? 1 : 2;
 template <int KS, int N>
 constexpr int kTile = kRows * kSets<KS, N> * kWaves;
-constexpr int kMaxSplits = 256;
+constexpr int kMaxParts = 512;
+// sequences of a call whose parts are planned on the device, 64 per lane register
+constexpr int kPlanRegs = 4, kPlanned = 64 * kPlanRegs;
 constexpr float kNone = -1e30f;           // running maximum of a row that has seen nothing
 constexpr float kTop = 8.0f, kLag = 7.0f; // weights up to 2^(kTop + kLag)
 using Tile = RowTile<kBlk>;
@@ -65,9 +69,13 @@ struct AttnArgs {
     int32_t window, sinks; // window 0: none
     int32_t page_bytes;    // of a page's keys, and of its values (at most 2^28)
     int32_t vec_q, vec_y;  // query rows in 16-byte chunks, output rows in fours of elements
-    int32_t splits;
-    float* ml;             // [T * H][splits][2]: maximum and weight sum of a part
-    float* sums;           // [T * H][splits][D]
+    int32_t splits;        // of every tile of rows that share keys
+    int32_t target;        // work-groups to plan the rows' parts for; 0: one part each
+    int32_t slots;         // work-groups of such rows per head
+    // sums of weights times codes, maximum and weight sum of a part: [row][split] of
+    // tiles, [head][work-group][16 rows] of planned parts
+    float* sums;           // [][D]
+    float* ml;             // [][2]
 };
 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -80,7 +88,6 @@ __device__ inline v4f mfma(v8h a, v8h b, v4f c)
 // 16 codes as fp16, exact: the byte c + 128 in the low bits of 1024 is 1152 + c.
 __device__ inline void to_half(const v4i& x, v8h (&h)[2])
 {
-    typedef _Float16 v2h __attribute__((ext_vector_type(2)));
     const v2h off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -164,7 +171,7 @@ __device__ inline void load_queries(const AttnArgs& p, const RowAt& row, Rows<KS
     const int g = (threadIdx.x & 63) >> 4;
     const int64_t at = row.t * p.ldq + (int64_t)row.head * p.kv.D;
     float x[KS][16];
-    float most = 0.0f;
+    uint32_t most = 0;  // as bits: NaN and infinities are the largest
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
         const int d = 64 * s + 16 * g;
@@ -176,12 +183,18 @@ __device__ inline void load_queries(const AttnArgs& p, const RowAt& row, Rows<KS
             else load16<MQ_F16>(p, at + d, x[s]);
         }
 #pragma unroll
-        for (int j = 0; j < 16; ++j) most = fmaxf(most, fabsf(x[s][j]));
+        for (int j = 0; j < 16; ++j) most = max(most, abs_bits(x[s][j]));
     }
-    most = row_max(most);
-    // 2^e <= most < 2^(e + 1); the row times 2^(14 - e), the products by its inverse
-    const uint32_t e = min(max(abs_bits(most) >> 23, 27u), 254u);
-    const float up = __builtin_bit_cast(float, (268u - e) << 23);
+    uint32_t o;
+    most = swap16(most, o);
+    most = max(most, o);
+    most = swap32(most, o);
+    most = max(most, o);
+    // 2^e <= most < 2^(e + 1); the row times 2^(14 - e), the products by its inverse;
+    // a row that is not finite becomes NaN throughout
+    const uint32_t e = min(max(most >> 23, 27u), 254u);
+    const float up = most < kInfBits ? __builtin_bit_cast(float, (268u - e) << 23)
+                                     : __builtin_nanf("");
     st.a = p.tau * __builtin_bit_cast(float, (e - 14u) << 23);
 #pragma unroll
     for (int s = 0; s < KS; ++s)
@@ -230,25 +243,25 @@ __device__ inline bool is_page(const AttnArgs& p, const Tile& t, int32_t blk, in
 struct Addr {
     const MQ_GLOBAL int8_t* k;
     const MQ_GLOBAL int8_t* v;
-    int64_t scale;
+    uint64_t scale;
     bool placed;  // the value group
     __device__ Addr(const AttnArgs& p, const Tile& t, int32_t g0, int32_t blk, const Pages& pg)
     {
         const Spot s;
-        const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-        const int32_t mask = (1 << p.kv.shift) - 1;
-        const int32_t kp = is_page(p, t, blk, s.key, pg.key) ? pg.key : 0;
+        const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+        const uint32_t mask = (1u << p.kv.shift) - 1, D = (uint32_t)p.kv.D;
+        const uint32_t kp = is_page(p, t, blk, s.key, pg.key) ? (uint32_t)pg.key : 0;
         placed = is_page(p, t, blk, s.value, pg.value);
-        const int32_t vp = placed ? pg.value : 0;
-        const int32_t ks = (blk * kBlk + 16 * s.key) & mask, vs = (blk * kBlk + 16 * s.value) & mask;
-        const int64_t head = (int64_t)g0 << p.kv.shift;
+        const uint32_t vp = placed ? (uint32_t)pg.value : 0;
+        // in a page, whose bytes are at most 2^28 (the head's part uniform)
+        const uint32_t head = (uint32_t)g0 << p.kv.shift;
+        const uint32_t ks = (blk * kBlk + 16 * s.key) & mask, vs = (blk * kBlk + 16 * s.value) & mask;
         k = (const MQ_GLOBAL int8_t*)p.kv.k +
-            ((uint64_t)(uint32_t)kp * (uint32_t)p.page_bytes +
-             (uint64_t)((head + ks + (r & 3)) * p.kv.D + 16 * g));
+            ((uint64_t)kp * (uint32_t)p.page_bytes + (head * D + (ks + (r & 3)) * D + 16 * g));
         v = (const MQ_GLOBAL int8_t*)p.kv.v +
-            ((uint64_t)(uint32_t)vp * (uint32_t)p.page_bytes +
-             (uint64_t)((head + vs) * p.kv.D + 16 * r));
-        scale = (((int64_t)vp * p.kv.G + g0) << (p.kv.shift - p.bshift)) + (vs >> p.bshift);
+            ((uint64_t)vp * (uint32_t)p.page_bytes + (head * D + vs * D + 16 * r));
+        scale = (uint64_t)vp * ((uint32_t)p.kv.G << (p.kv.shift - p.bshift)) +
+                ((head + vs) >> p.bshift);
     }
 };
 
@@ -264,7 +277,7 @@ __device__ inline int32_t value_tile(const AttnArgs& p, int dt)
     return 16 * dt < p.kv.D ? 256 * dt : 0;
 }
 
-// One block for the wave's sets.  key(j, s), value(dt): fragments; read():
+// One block for the wave's sets.  key(j, s, h), value(dt, h): fragments; read():
 // called once the keys have been used; ks, vs: the lane's scales, placed: whether
 // its group has a place; full: every row sees every position.
 template <int KS, int ND, int N, int NR, class Key, class Value, class Read>
@@ -275,12 +288,13 @@ __device__ inline void attend_block(const AttnArgs& p, Rows<KS, ND, N> (&st)[NR]
     const int g = (threadIdx.x & 63) >> 4;
     // scores of keys 16 g + 4 j + i
     v4f c[NR][4];
+    if (NR > 1) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             v8h k[2];
-            to_half(key(j, s), k);
+            key(j, s, k);
 #pragma unroll
             for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -290,37 +304,34 @@ __device__ inline void attend_block(const AttnArgs& p, Rows<KS, ND, N> (&st)[NR]
                         c[n][j] = mfma(k[h], st[n].q[e][s][h],
                                        s + h + e ? c[n][j] : v4f{0.0f, 0.0f, 0.0f, 0.0f});
         }
+    if (NR > 1) __builtin_amdgcn_s_setprio(0);
     read();
     const bool mask = !full || __ballot(!placed) != 0;
     v8h w[NR][N][2];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-        uint32_t seen = 0xffff;
         float kn = ks, vn = fmaxf(vs, 0x1p-67f);
         if (mask) {
             const int32_t first = blk * kBlk + 16 * g;
             // of the 16 keys from `first` on those below x, as bits
             auto below = [&](int32_t x) { return (1u << max(min(x - first, 16), 0)) - 1; };
-            seen = below(sees[n].hi + 1) & (~below(sees[n].lo + 1) | below(p.sinks));
+            uint32_t seen = below(sees[n].hi + 1) & (~below(sees[n].lo + 1) | below(p.sinks));
             if (!placed) seen = 0;
             if (seen == 0) kn = vn = 1.0f;  // (the scales there may be anything)
-        }
-        const float a = st[n].a * kn, lv = __builtin_amdgcn_logf(vn);
-        float x[16], m;
-        if (mask) {
-            m = -__builtin_inff();
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                x[i] = __builtin_fmaf(c[n][i >> 2][i & 3], a, lv);
-                x[i] = (seen >> i) & 1 ? x[i] : -__builtin_inff();
-                m = fmaxf(m, x[i]);
+                const int keep = __builtin_amdgcn_sbfe((int)seen, i, 1);  // all ones or 0
+                const float y = c[n][i >> 2][i & 3];  // (a bit cast of an element casts the first)
+                const int x = __builtin_bit_cast(int, y);
+                c[n][i >> 2][i & 3] = __builtin_bit_cast(float, (x & keep) | ((int)0xff800000u & ~keep));
             }
-        } else {
-            m = c[n][0][0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) m = fmaxf(m, c[n][i >> 2][i & 3]);
-            m = __builtin_fmaf(m, a, lv);
         }
+        // (not 0: a product with -infinity stays that)
+        const float a = fmaxf(st[n].a * kn, 0x1p-126f), lv = __builtin_amdgcn_logf(vn);
+        float m = c[n][0][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) m = fmaxf(m, c[n][i >> 2][i & 3]);
+        m = __builtin_fmaf(m, a, lv);
         m = row_max(m);
         if (__ballot(m > st[n].m + kLag) != 0) {
             m = fmaxf(m, st[n].m);
@@ -330,25 +341,27 @@ __device__ inline void attend_block(const AttnArgs& p, Rows<KS, ND, N> (&st)[NR]
             for (int dt = 0; dt < ND; ++dt) st[n].acc[dt] *= f;
             st[n].m = m;
         }
-        const float b = kTop - st[n].m;
-        float sum = 0.0f;
+        const float b = lv + (kTop - st[n].m);
+        float x[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            x[i] = exp2_fast(mask ? x[i] + b : __builtin_fmaf(c[n][i >> 2][i & 3], a, lv + b));
-            sum += x[i];
-        }
-        st[n].l = __builtin_fmaf(sum, exp2_fast(-lv), st[n].l);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
+            x[i] = exp2_fast(__builtin_fmaf(c[n][i >> 2][i & 3], a, b));
             const _Float16 h = (_Float16)x[i];
             w[n][0][i >> 3][i & 7] = h;
             if constexpr (N == 2) w[n][1][i >> 3][i & 7] = (_Float16)(x[i] - (float)h);
         }
+        // (not of the rounded ones: a weight by a small value scale may be below
+        // fp16 and still count here)
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += x[i];
+        st[n].l = __builtin_fmaf(sum, exp2_fast(-lv), st[n].l);
     }
+    if (NR > 1) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) {
         v8h v[2];
-        to_half(value(dt), v);
+        value(dt, v);
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -356,6 +369,7 @@ __device__ inline void attend_block(const AttnArgs& p, Rows<KS, ND, N> (&st)[NR]
 #pragma unroll
                 for (int e = 0; e < N; ++e) st[n].acc[dt] = mfma(v[h], w[n][e][h], st[n].acc[dt]);
     }
+    if (NR > 1) __builtin_amdgcn_s_setprio(0);
 }
 
 // 1 / l; 0 for a row that sees nothing.
@@ -384,17 +398,23 @@ __device__ inline void store_four(const AttnArgs& p, int64_t t, int32_t head, in
     }
 }
 
-// Four waves share 16 rows and take every fourth block of [i0, i1), straight from
+// Where a part's state goes: sums + at D and ml + 2 at, row r's 16 rows on; or,
+// of a row's only part, to the outputs.
+struct PartAt {
+    bool only;
+    int64_t at;
+};
+
+// W waves share 16 rows and take every W-th block of [i0, i1), straight from
 // the cache; their states are joined through LDS.
-template <int ND>
-constexpr int kJoinFloats = kWaves * (4 * ND * 64 + 2 * kRows);
-template <int KS, int ND, int N>
+template <int ND, int W>
+constexpr int kJoinFloats = W * (4 * ND * 64 + 2 * kRows);
+template <int KS, int ND, int N, int W>
 __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g0, int32_t i0,
-                                  int32_t i1, int split, float* lds)
+                                  int32_t i1, const RowAt& row, PartAt part, float* lds)
 {
     const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const RowAt row(p, tile, tile.row0, g0);
     const Sees sees[1] = {row.sees};
     Rows<KS, ND, N> st[1];
     st[0].clear();
@@ -402,94 +422,116 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
     if (i < i1) {
         Pages pg = load_pages(p, tile, tile.block(i));
         load_queries(p, row, st[0]);
-        v4i kf[4][KS];
-        float ks, vs;
+        // values are read a block ahead; keys too where there are registers for them,
+        // else once the block before has its scores
+        constexpr bool kAhead = KS <= 2;
+        struct Block {
+            v4i k[4][KS], v[ND];
+            float ks, vs;
+            bool placed;
+        };
+        Block buf[2];
         Addr at(p, tile, g0, tile.block(i), pg);
-        auto read_keys = [&]() {
-            ks = p.k_scale[at.scale];
-            vs = p.v_scale[at.scale];
+        auto read_keys = [&](Block& x) {
+            x.ks = p.k_scale[at.scale];
+            x.vs = p.v_scale[at.scale];
+            x.placed = at.placed;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int s = 0; s < KS; ++s)
-                    kf[j][s] = *reinterpret_cast<const MQ_GLOBAL v4i*>(
+                    x.k[j][s] = *reinterpret_cast<const MQ_GLOBAL v4i*>(
                         at.k + (4 * j * p.kv.D + key_chunk(p, s)));
         };
-        read_keys();
-        pg = load_pages(p, tile, tile.block(min(i + kWaves, i1 - 1)));
-        for (; i < i1; i += kWaves) {
-            const int32_t blk = tile.block(i);
-            v4i vf[ND];
+        auto read_values = [&](Block& x) {
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt)
-                vf[dt] = *reinterpret_cast<const MQ_GLOBAL v4i*>(at.v + value_tile(p, dt));
-            const float ks0 = ks, vs0 = vs;
-            const bool placed = at.placed;
+                x.v[dt] = *reinterpret_cast<const MQ_GLOBAL v4i*>(at.v + value_tile(p, dt));
+        };
+        auto ahead = [&](int32_t x) { return tile.block(min(x, i1 - 1)); };
+        read_keys(buf[0]);
+        read_values(buf[0]);
+        pg = load_pages(p, tile, ahead(i + W));
+        auto block = [&](Block& now, Block& next) {
+            const int32_t blk = tile.block(i);
+            at = Addr(p, tile, g0, ahead(i + W), pg);
+            pg = load_pages(p, tile, ahead(i + 2 * W));
+            if constexpr (kAhead) read_keys(next);
+            read_values(next);
+            __builtin_amdgcn_sched_barrier(0);
+            // (what is read without registers to spare goes into the keys just used)
+            const float ks = now.ks, vs = now.vs;
+            const bool placed = now.placed;
             attend_block<KS, ND, N, 1>(
-                p, st, sees, blk, tile.full(p, blk), placed, ks0, vs0,
-                [&](int j, int s) { return kf[j][s]; }, [&](int dt) { return vf[dt]; },
+                p, st, sees, blk, tile.full(p, blk), placed, ks, vs,
+                [&](int j, int s, v8h (&k)[2]) { to_half((kAhead ? now : buf[0]).k[j][s], k); },
+                [&](int dt, v8h (&v)[2]) { to_half(now.v[dt], v); },
                 [&]() {
-                    const int32_t next = tile.block(min(i + kWaves, i1 - 1));
-                    at = Addr(p, tile, g0, next, pg);
-                    read_keys();
-                    pg = load_pages(p, tile, tile.block(min(i + 2 * kWaves, i1 - 1)));
+                    if constexpr (!kAhead) {
+                        read_keys(buf[0]);
+                        next.ks = buf[0].ks;
+                        next.vs = buf[0].vs;
+                        next.placed = buf[0].placed;
+                    }
                 });
+        };
+        for (; i < i1; i += W) {
+            block(buf[0], buf[1]);
+            i += W;
+            if (i >= i1) break;
+            block(buf[1], buf[0]);
         }
     }
-    float* lm = lds + kWaves * 4 * ND * 64;  // [wave][row]
-    float* ll = lm + kWaves * kRows;
+    float* lm = lds + W * 4 * ND * 64;  // [wave][row]
+    float* ll = lm + W * kRows;
     const float l = row_sum(st[0].l);
     if (g == 0) {
         lm[wave * kRows + r] = st[0].m;
         ll[wave * kRows + r] = l;
     }
+    v4f* acc = reinterpret_cast<v4f*>(lds);  // [wave][tile][lane]
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) lds[((wave * ND + dt) * 4 + e) * 64 + lane] = st[0].acc[dt][e];
+    for (int dt = 0; dt < ND; ++dt) acc[(wave * ND + dt) * 64 + lane] = st[0].acc[dt];
     __syncthreads();
     float m = kNone;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, lm[w * kRows + r]);
-    float f[kWaves], sum = 0.0f;
+    for (int w = 0; w < W; ++w) m = fmaxf(m, lm[w * kRows + r]);
+    float f[W], sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
         f[w] = exp2_fast(lm[w * kRows + r] - m);
         sum = __builtin_fmaf(f[w], ll[w * kRows + r], sum);
     }
     if (!row.have) return;
-    const int64_t part = (row.t * p.H + row.head) * p.splits + split;
-    if (p.splits > 1 && wave == 0 && g == 0) {
-        p.ml[2 * part] = m;
-        p.ml[2 * part + 1] = sum;
+    if (!part.only && wave == 0 && g == 0) {
+        p.ml[2 * part.at] = m;
+        p.ml[2 * part.at + 1] = sum;
     }
     const float unit = out_unit(sum);
 #pragma unroll
-    for (int dt = wave; dt < ND; dt += kWaves) {
+    for (int i = 0; i < (ND + W - 1) / W; ++i) {
+        const int dt = W * i + wave;
         const int32_t d = 16 * dt + 4 * g;
         if (16 * dt >= p.kv.D) break;
         v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w)
+        for (int w = 0; w < W; ++w) {
+            const v4f x = acc[(w * ND + dt) * 64 + lane];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = __builtin_fmaf(f[w], lds[((w * ND + dt) * 4 + e) * 64 + lane], v[e]);
-        if (p.splits > 1) *reinterpret_cast<v4f*>(p.sums + part * p.kv.D + d) = v;
+            for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(f[w], x[e], v[e]);
+        }
+        if (!part.only) *reinterpret_cast<v4f*>(p.sums + part.at * p.kv.D + d) = v;
         else store_four(p, row.t, row.head, d, v * unit);
     }
 }
 
-// The wave's own copies into LDS have landed (they count as vector memory).
-__device__ inline void wait_staged()
-{
-    __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // vmcnt(0), the others left alone
-}
-
-// Every wave has sets of its own; all walk over blocks [i0, i1), staged in LDS by
-// the four together in the order of the lanes (keys (j, s), then values: 1 KB
-// each), the next block on its way during this one.
+// Every wave has sets of its own; all walk over blocks [i0, i1), whose codes the
+// four together put into LDS as fp16, in the order of the lanes: keys (j, s), then
+// values, two halves of 1 KB each.  The next block's codes are read during this one
+// and converted once for all waves (by every wave for itself: 228 us instead of
+// WAVEFIG for 500 tokens over 16000, 32 heads of 128 on 8).
 template <int KS, int ND>
-constexpr int kStage = (4 * KS + ND) * 1024;
+constexpr int kStage = (4 * KS + ND) * 2048;
 template <int KS, int ND, int N>
 __device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g0, int32_t i0,
                                   int32_t i1, int split, MQ_LDS int8_t* lds)
@@ -511,51 +553,65 @@ __device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g
         float ks = 0.0f, vs = 0.0f;
         bool placed = false;
         // the wave's share: key tile j = wave, every fourth value tile
-        auto stage = [&](int32_t blk, MQ_LDS int8_t* to) {
+        constexpr int NV = (ND + 3) / 4;
+        v4i kf[KS], vf[NV];
+        auto read = [&](int32_t blk) {
             const Addr at(p, tile, g0, blk, pg);
             ks = p.k_scale[at.scale];
             vs = p.v_scale[at.scale];
             placed = at.placed;
 #pragma unroll
             for (int s = 0; s < KS; ++s)
-                __builtin_amdgcn_global_load_lds(
-                    (const MQ_GLOBAL void*)(at.k + (4 * wave * p.kv.D + key_chunk(p, s))),
-                    (MQ_LDS void*)(to + (wave * KS + s) * 1024), 16, 0, 0);
+                kf[s] = *reinterpret_cast<const MQ_GLOBAL v4i*>(
+                    at.k + (4 * wave * p.kv.D + key_chunk(p, s)));
 #pragma unroll
-            for (int i = 0; i < (ND + 3) / 4; ++i) {
+            for (int i = 0; i < NV; ++i)
+                vf[i] = *reinterpret_cast<const MQ_GLOBAL v4i*>(at.v + value_tile(p, 4 * i + wave));
+        };
+        auto put = [&](MQ_LDS int8_t* to) {
+            to += lane * 16;
+            v8h h[2];
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                to_half(kf[s], h);
+                *reinterpret_cast<MQ_LDS v8h*>(to + (wave * KS + s) * 2048) = h[0];
+                *reinterpret_cast<MQ_LDS v8h*>(to + (wave * KS + s) * 2048 + 1024) = h[1];
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
                 const int dt = 4 * i + wave;
-                if (dt < ND)
-                    __builtin_amdgcn_global_load_lds(
-                        (const MQ_GLOBAL void*)(at.v + value_tile(p, dt)),
-                        (MQ_LDS void*)(to + (4 * KS + dt) * 1024), 16, 0, 0);
+                if (ND % 4 != 0 && dt >= ND) break;
+                to_half(vf[i], h);
+                *reinterpret_cast<MQ_LDS v8h*>(to + (4 * KS + dt) * 2048) = h[0];
+                *reinterpret_cast<MQ_LDS v8h*>(to + (4 * KS + dt) * 2048 + 1024) = h[1];
             }
         };
-        stage(tile.block(i0), lds);
+        read(tile.block(i0));
         pg = load_pages(p, tile, tile.block(min(i0 + 1, i1 - 1)));
 #pragma unroll
         for (int n = 0; n < NR; ++n) load_queries(p, row[n], st[n]);
-        wait_staged();
+        put(lds);
         __syncthreads();
         for (int32_t i = i0; i < i1; ++i) {
             const int32_t blk = tile.block(i);
             const int buf = (i - i0) & 1;
             const float ks0 = ks, vs0 = vs;
             const bool placed0 = placed;
-            if (i + 1 < i1) {
-                stage(tile.block(i + 1), lds + (buf ^ 1) * kStage<KS, ND>);
-                pg = load_pages(p, tile, tile.block(min(i + 2, i1 - 1)));
-            }
+            read(tile.block(min(i + 1, i1 - 1)));
+            pg = load_pages(p, tile, tile.block(min(i + 2, i1 - 1)));
             const MQ_LDS int8_t* at = lds + buf * kStage<KS, ND> + lane * 16;
             attend_block<KS, ND, N, NR>(
                 p, st, sees, blk, tile.full(p, blk), placed0, ks0, vs0,
-                [&](int j, int s) {
-                    return *reinterpret_cast<const MQ_LDS v4i*>(at + (j * KS + s) * 1024);
+                [&](int j, int s, v8h (&k)[2]) {
+                    k[0] = *reinterpret_cast<const MQ_LDS v8h*>(at + (j * KS + s) * 2048);
+                    k[1] = *reinterpret_cast<const MQ_LDS v8h*>(at + (j * KS + s) * 2048 + 1024);
                 },
-                [&](int dt) {
-                    return *reinterpret_cast<const MQ_LDS v4i*>(at + (4 * KS + dt) * 1024);
+                [&](int dt, v8h (&v)[2]) {
+                    v[0] = *reinterpret_cast<const MQ_LDS v8h*>(at + (4 * KS + dt) * 2048);
+                    v[1] = *reinterpret_cast<const MQ_LDS v8h*>(at + (4 * KS + dt) * 2048 + 1024);
                 },
                 []() {});
-            wait_staged();
+            put(lds + (buf ^ 1) * kStage<KS, ND>);
             __syncthreads();
         }
     }
@@ -579,16 +635,132 @@ __device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g
     }
 }
 
-// grid (tiles of 16 rows, G, splits)
-template <int KS, int ND, int N>
-__global__ __launch_bounds__(256, KS <= 2 ? 2 : 1) void attn_blocks_split_kernel(AttnArgs p)
+// The parts of a call's rows: every sequence's tiles of 16 rows, its blocks split
+// into parts of about the same size over all sequences.  Every work-group (and the
+// join) works it out from the lengths for itself.
+struct Plan {
+    int32_t b;             // the work-group's sequence, or -1
+    int32_t tile, part;    // its tile and part of it
+    int32_t parts;         // of each of the sequence's tiles
+    int32_t first;         // work-group of the tile's first part
+    int32_t s0, s1, len;
+};
+// x: work-group, or (row >= 0) the work-group of that token row's first head of
+// the group plus `head`.
+__device__ inline Plan make_plan(const AttnArgs& p, int waves, int32_t x, int64_t token,
+                                 int32_t head)
 {
-    __shared__ __attribute__((aligned(16))) float lds[kJoinFloats<ND>];
+    const int lane = threadIdx.x & 63;
+    int32_t s0[kPlanRegs], s1[kPlanRegs], len[kPlanRegs], tiles[kPlanRegs], n[kPlanRegs];
+#pragma unroll
+    for (int i = 0; i < kPlanRegs; ++i) {
+        const int32_t b = min(lane + 64 * i, p.kv.B - 1);
+        if (64 * i >= p.kv.B) {  // uniform
+            s0[i] = s1[i] = len[i] = 0;
+            continue;
+        }
+        s0[i] = p.kv.starts[b];
+        s1[i] = p.kv.starts[b + 1];
+        len[i] = p.kv.lens[b];
+    }
+    const int32_t list = (int32_t)min((p.kv.ld << p.kv.shift) / kBlk + 1, (int64_t)1 << 25);
+    int64_t total = 0;
+#pragma unroll
+    for (int i = 0; i < kPlanRegs; ++i) {
+        if (64 * i >= p.kv.B) break;
+        const bool ok = lane + 64 * i < p.kv.B && s0[i] >= 0 && s1[i] <= (int32_t)p.T &&
+                        s0[i] < s1[i];
+        if (!ok) s1[i] = s0[i];
+        const int32_t rows = ok ? s1[i] - s0[i] : 0;
+        tiles[i] = (rows * p.grp + kRows - 1) / kRows;  // (T * grp <= 16 B on this path)
+        // blocks up to the last token's, without those that a window hides from all
+        const int32_t last = max(len[i], 0) - 1;
+        int32_t end = last < 0 ? 0 : min(last / kBlk + 1, list);
+        if (p.window > 0) {
+            const int64_t seen = (int64_t)last - rows - p.window;  // hidden up to here
+            const int32_t hide = (int32_t)(seen >> 6) - (int32_t)(((int64_t)p.sinks + kBlk - 1) >> 6);
+            if (seen > 0) end -= max(min(hide, end), 0);
+        }
+        n[i] = max(end, 1);
+        total += (int64_t)tiles[i] * n[i];
+    }
+    static_assert(kBlk == 64, "shifts");
+    // blocks of a part: at least one per wave, whole rounds of the waves (waves: a
+    // power of two)
+    uint32_t per = waves;
+    if (p.target > 0) {
+        total = wave_sum(total);
+        const double each = (double)total * (double)p.kv.G / (double)p.target;
+        per = max(per, (uint32_t)min(each, 1073741824.0) + 1);
+    }
+    per = (per + waves - 1) & ~(uint32_t)(waves - 1);
+    Plan w;
+    w.b = -1;
+    int32_t base = 0;
+#pragma unroll
+    for (int i = 0; i < kPlanRegs; ++i) {
+        if (64 * i >= p.kv.B) break;
+        int32_t parts = 1;
+        if (p.target > 0)
+            parts = (int32_t)min(max(((uint32_t)n[i] + per / 2) / per, 1u), (uint32_t)kMaxParts);
+        const int32_t mine = tiles[i] * parts, after = wave_scan(mine);
+        bool hit;
+        if (token >= 0) hit = tiles[i] > 0 && token >= s0[i] && token < s1[i];
+        else hit = x >= base + after - mine && x < base + after;
+        const uint64_t at = __ballot(hit);
+        if (at != 0 && w.b < 0) {
+            const int l = 63 - __builtin_clzll(at);
+            w.b = 64 * i + l;
+            w.parts = __builtin_amdgcn_readlane(parts, l);
+            w.s0 = __builtin_amdgcn_readlane(s0[i], l);
+            w.s1 = __builtin_amdgcn_readlane(s1[i], l);
+            w.len = __builtin_amdgcn_readlane(len[i], l);
+            const int32_t before = base + __builtin_amdgcn_readlane(after - mine, l);
+            if (token >= 0) {
+                w.tile = (((int32_t)token - w.s0) * p.grp + head) / kRows;
+                w.part = 0;
+                // (starts that do not ascend: more work-groups than there are)
+                if (before < 0 || (int64_t)before + (int64_t)(w.tile + 1) * w.parts > p.slots)
+                    w.parts = 0;
+            } else {
+                w.tile = (int32_t)((uint32_t)(x - before) / (uint32_t)w.parts);
+                w.part = x - before - w.tile * w.parts;
+            }
+            w.first = before + w.tile * w.parts;
+        }
+        base += __builtin_amdgcn_readlane(after, 63);
+    }
+    return w;
+}
+
+// grid (work-groups per head, G).  PLAN: parts by make_plan; else (more sequences)
+// a work-group per tile of 16 rows.
+template <int KS, int ND, int N, int W, bool PLAN>
+__global__ __launch_bounds__(64 * W, KS <= 2 ? 2 : 1) void attn_blocks_rows_kernel(AttnArgs p)
+{
+    __shared__ __attribute__((aligned(16))) float lds[kJoinFloats<ND, W>];
+    const int32_t g0 = blockIdx.y;
     Tile tile;
-    if (!find_tile<kRows, kBlk>(p, blockIdx.x, tile)) return;
-    int32_t i0, i1;
-    split_range(p, tile, blockIdx.z, i0, i1);
-    split_rows<KS, ND, N>(p, tile, blockIdx.y, i0, i1, blockIdx.z, lds);
+    int32_t i0 = 0, i1;
+    PartAt part{true, 0};
+    if constexpr (PLAN) {
+        const Plan w = make_plan(p, W, (int32_t)blockIdx.x, -1, 0);
+        if (w.b < 0) return;
+        set_tile<kRows>(p, w.b, w.s0, w.s1, max(w.len, 0), (uint32_t)w.tile * kRows, tile);
+        i1 = tile.n;
+        if (w.parts > 1) {
+            const int32_t per = (tile.n + w.parts - 1) / w.parts;
+            i0 = per * w.part;
+            i1 = min(i0 + per, tile.n);
+            part.only = false;
+            part.at = ((int64_t)g0 * p.slots + blockIdx.x) * kRows + (threadIdx.x & 15);
+        }
+    } else {
+        if (!find_tile<kRows, kBlk>(p, blockIdx.x, tile)) return;
+        i1 = tile.n;
+    }
+    const RowAt row(p, tile, tile.row0, g0);
+    split_rows<KS, ND, N, W>(p, tile, g0, i0, i1, row, part, lds);
 }
 
 // One work-group per tile of rows, cache head and split; a sequence's last 16 rows
@@ -597,8 +769,8 @@ template <int KS, int ND, int N>
 __global__ __launch_bounds__(256, KS <= 2 ? 2 : 1) void attn_blocks_tile_kernel(AttnArgs p,
                                                                                 int64_t tiles)
 {
-    constexpr int kBytes = 2 * kStage<KS, ND> > kJoinFloats<ND> * 4 ? 2 * kStage<KS, ND>
-                                                                    : kJoinFloats<ND> * 4;
+    constexpr int kJoin = kJoinFloats<ND, kWaves> * 4;
+    constexpr int kBytes = 2 * kStage<KS, ND> > kJoin ? 2 * kStage<KS, ND> : kJoin;
     __shared__ __attribute__((aligned(1024))) int8_t lds[kBytes];
     const Place w = place_of(p, blockIdx.x, tiles);
     const int32_t g0 = w.part % p.kv.G, split = w.part / p.kv.G;
@@ -606,80 +778,191 @@ __global__ __launch_bounds__(256, KS <= 2 ? 2 : 1) void attn_blocks_tile_kernel(
     if (w.tile >= tiles || !find_tile<kTile<KS, N>, kBlk>(p, w.tile, tile)) return;
     int32_t i0, i1;
     split_range(p, tile, split, i0, i1);
-    if (tile.rows - tile.row0 <= kRows)
-        split_rows<KS, ND, N>(p, tile, g0, i0, i1, split, reinterpret_cast<float*>(lds));
-    else
+    if (tile.rows - tile.row0 <= kRows) {
+        const RowAt row(p, tile, tile.row0, g0);
+        const PartAt part{p.splits == 1, (row.t * p.H + row.head) * p.splits + split};
+        split_rows<KS, ND, N, kWaves>(p, tile, g0, i0, i1, row, part, reinterpret_cast<float*>(lds));
+    } else {
         share_keys<KS, ND, N>(p, tile, g0, i0, i1, split, (MQ_LDS int8_t*)lds);
+    }
 }
 
-// Joins the splits: a wave per row and 64 channels.
-__global__ __launch_bounds__(256) void attn_blocks_join_kernel(AttnArgs p)
+// Joins the planned parts of a row and head, a work-group per 64 channels: 16 lanes
+// have four channels each of four parts at once, the four waves take turns; up to
+// 128 parts' reads are under way together.
+__global__ __launch_bounds__(256) void attn_blocks_join_kernel(AttnArgs p, int plan_waves)
 {
+    __shared__ float f[kMaxParts];
+    __shared__ __attribute__((aligned(16))) v4f sums[4][64];
     const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (row >= p.T * p.H) return;
-    const int64_t t = row / p.H;
-    if (t < p.kv.starts[0] || t >= p.kv.starts[p.kv.B]) return;  // rows of no sequence
-    const int32_t d = blockIdx.y * 64 + lane;
-    const bool have = d < p.kv.D;
-    const float* ml = p.ml + row * p.splits * 2;
-    const float* x = p.sums + row * p.splits * p.kv.D + (have ? d : 0);
-    float m = kNone;
-    for (int s = lane; s < p.splits; s += 64) m = fmaxf(m, ml[2 * s]);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t t = blockIdx.x / p.H;
+    const int32_t head = (int32_t)(blockIdx.x - t * p.H), D = p.kv.D;
+    const int32_t g0 = head / p.grp, h = head - g0 * p.grp;
+    const Plan w = make_plan(p, plan_waves, 0, t, h);
+    if (w.b < 0 || w.parts <= 1) return;  // rows of no sequence, or done
+    const int32_t parts = w.parts, r = (int32_t)(((t - w.s0) * p.grp + h) & (kRows - 1));
+    const int64_t at = ((int64_t)g0 * p.slots + w.first) * kRows + r;
+    const float* ml = p.ml + 2 * at;
+    constexpr int kRegs = kMaxParts / 64;
+    float m[kRegs], l[kRegs], most = kNone;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    float l = 0.0f, acc = 0.0f;
+    for (int i = 0; i < kRegs; ++i) {
+        const int s = lane + 64 * i;
+        m[i] = s < parts ? ml[2 * kRows * s] : kNone;
+        l[i] = s < parts ? ml[2 * kRows * s + 1] : 0.0f;
+    }
+    const int32_t which = 4 * wave + (lane >> 4), d = 64 * (int32_t)blockIdx.y + 4 * (lane & 15);
+    const float* x = p.sums + at * D + min(d, D - 4);
+    constexpr int U = 8;
+    v4f v[U];
+    auto load = [&](int32_t s0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t s = min(s0 + 16 * u + which, parts - 1);
+            v[u] = *reinterpret_cast<const v4f*>(x + (int64_t)s * kRows * D);
+        }
+    };
+    load(0);
+#pragma unroll
+    for (int i = 0; i < kRegs; ++i) most = fmaxf(most, m[i]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kRegs; ++i) {
+        const float e = exp2_fast(m[i] - most);
+        if (wave == 0 && lane + 64 * i < parts) f[lane + 64 * i] = e;
+        sum = __builtin_fmaf(e, l[i], sum);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    __syncthreads();
+    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int32_t s0 = 0; s0 < parts; s0 += 16 * U) {
+        if (s0 > 0) load(s0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t s = s0 + 16 * u + which;
+            const float e = s < parts ? f[s] : 0.0f;
+            if (s < parts)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(e, v[u][c], acc[c]);
+        }
+    }
+    sums[wave][lane] = acc;
+    __syncthreads();
+    if (threadIdx.x >= 16 || d >= D) return;
+    acc = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc += sums[i >> 2][16 * (i & 3) + lane];
+    store_four(p, t, head, d, acc * out_unit(sum));
+}
+
+// Joins the splits of tiles, a lane per four channels of a row and head.
+__global__ __launch_bounds__(256) void attn_blocks_join_tiles_kernel(AttnArgs p)
+{
+    const uint32_t each = (uint32_t)p.kv.D / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = i / each, t = row / p.H;
+    const int32_t d = 4 * (int32_t)(i - row * each);
+    if (row >= p.T * p.H || t < p.kv.starts[0] || t >= p.kv.starts[p.kv.B]) return;
+    const float* ml = p.ml + row * p.splits * 2;
+    const float* x = p.sums + row * p.splits * p.kv.D + d;
+    float m = kNone, l = 0.0f;
+    for (int s = 0; s < p.splits; ++s) m = fmaxf(m, ml[2 * s]);
+    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int s = 0; s < p.splits; ++s) {
         const float f = exp2_fast(ml[2 * s] - m);
         l = __builtin_fmaf(f, ml[2 * s + 1], l);
-        acc = __builtin_fmaf(f, x[(int64_t)s * p.kv.D], acc);
+        const v4f v = *reinterpret_cast<const v4f*>(x + (int64_t)s * p.kv.D);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(f, v[c], acc[c]);
     }
-    if (have) store_one(p, t, (int32_t)(row % p.H), d, acc * out_unit(l));
+    store_four(p, t, (int32_t)(row - t * p.H), d, acc * out_unit(l));
 }
 
 // Whether the sequences have more rows than a set, on average.
 bool tiled(int64_t T, int64_t B, int32_t grp) { return T * grp > B * kRows; }
 
-// Parts the keys of every tile are split into: as many work-groups as the chip
-// holds at once, at least a block per wave in each.
-int64_t split_count(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D, int64_t max_len)
+// Work-groups that the chip holds at once (of rows: one of eight waves per CU, or
+// of four with the registers of a wave per SIMD; of tiles: two per CU, or one).
+constexpr int64_t kCUs = 256;
+
+// How the keys are split: `splits` of every tile, or planned parts.
+struct Split {
+    int64_t splits = 1, target = 0, slots = 0, bytes = 0;
+    int waves = 0;  // of a work-group of rows
+};
+Split choose_split(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D, int64_t max_len,
+                   int64_t ws_bytes)
 {
+    Split c;
     const int32_t grp = H / G;
-    const int R = tiled(T, B, grp) ? kTile<1, 1> : kRows;
-    const int64_t groups = std::max(T * grp / R, std::min(B, T)) * G;
-    int64_t s = (D > 128 ? 256 : 512) / std::max<int64_t>(groups, 1);
-    const int64_t blocks = (max_len + kBlk - 1) / kBlk;
-    s = std::min(s, (blocks + kWaves - 1) / kWaves);
-    s = std::min<int64_t>(s, MQ_ATTN_MAX_WORKSPACE / (T * H * (D + 2) * 4));
-    return std::max<int64_t>(1, std::min<int64_t>(s, kMaxSplits));
+    const int64_t blocks = (max_len + kBlk - 1) / kBlk, row = (D + 2) * 4;
+    ws_bytes = std::min<int64_t>(ws_bytes, MQ_ATTN_MAX_WORKSPACE);
+    if (tiled(T, B, grp)) {
+        // at least a block per wave in each
+        const int64_t groups = std::max(T * grp / kTile<1, 1>, std::min(B, T)) * G;
+        int64_t s = (D > 128 ? kCUs : 2 * kCUs) / std::max<int64_t>(groups, 1);
+        s = std::min(s, (blocks + kWaves - 1) / kWaves);
+        s = std::min<int64_t>(s, ws_bytes / (T * H * row));
+        c.splits = std::max<int64_t>(1, std::min<int64_t>(s, kMaxParts));
+        c.bytes = c.splits > 1 ? c.splits * T * H * row : 0;
+        return c;
+    }
+    const int64_t tiles = row_tiles(T, B, grp, kRows);
+    c.slots = tiles;
+    // eight waves on a CU: one work-group of a few tiles', two of many's; above 128
+    // channels their registers leave one wave per SIMD
+    c.waves = D > 128 || std::min(tiles, std::max<int64_t>(B, T * grp / kRows)) * G > kCUs ? 4 : 8;
+    // (up to four blocks per wave are one part's, whose launch needs no join; eight
+    // where the sequences alone fill the chip)
+    if (B > kPlanned || blocks <= (std::min(B, T) * G >= kCUs ? 8 : 4) * c.waves) return c;
+    const int64_t target = D > 128 || c.waves == 8 ? kCUs : 2 * kCUs;
+    const int64_t slots = tiles + (target + G - 1) / G;
+    if (slots * G * kRows * row > ws_bytes) return c;
+    c.target = target;
+    c.slots = slots;
+    c.bytes = slots * G * kRows * row;
+    return c;
+}
+
+template <int ND, int N, int W>
+hipError_t launch_rows(const AttnArgs& p, hipStream_t s)
+{
+    constexpr int KS = (ND + 3) / 4;
+    const dim3 grid((unsigned)p.slots, (unsigned)p.kv.G);
+    if (p.kv.B <= kPlanned) attn_blocks_rows_kernel<KS, ND, N, W, true><<<grid, 64 * W, 0, s>>>(p);
+    else attn_blocks_rows_kernel<KS, ND, N, W, false><<<grid, 64 * W, 0, s>>>(p);
+    return hipGetLastError();
 }
 
 template <int ND, int N>
-hipError_t launch_main(const AttnArgs& p, int64_t B, hipStream_t s)
+hipError_t launch_main(const AttnArgs& p, const Split& c, hipStream_t s)
 {
     constexpr int KS = (ND + 3) / 4;
-    const int64_t parts = (int64_t)p.kv.G * p.splits;
-    if (tiled(p.T, B, p.grp)) {
-        const int64_t tiles = row_tiles(p.T, B, p.grp, kTile<KS, N>);
-        // (see place_of)
-        const int64_t n = parts % 8 != 0 && 8 % parts == 0
-                              ? 8 * ((tiles + 8 / parts - 1) / (8 / parts))
-                              : tiles * parts;
-        if (n >= kMaxBlocks) return hipErrorInvalidConfiguration;
-        attn_blocks_tile_kernel<KS, ND, N><<<(unsigned)n, 256, 0, s>>>(p, tiles);
-        return hipGetLastError();
+    if (c.waves > 0) {
+        if (c.slots * p.kv.G >= kMaxBlocks / 2) return hipErrorInvalidConfiguration;
+        if constexpr (KS <= 2)
+            if (c.waves == 8) return launch_rows<ND, N, 8>(p, s);
+        return launch_rows<ND, N, 4>(p, s);
     }
-    const int64_t n = row_tiles(p.T, B, p.grp, kRows);
+    const int64_t parts = (int64_t)p.kv.G * p.splits;
+    const int64_t tiles = row_tiles(p.T, p.kv.B, p.grp, kTile<KS, N>);
+    // (see place_of)
+    const int64_t n = parts % 8 != 0 && 8 % parts == 0
+                          ? 8 * ((tiles + 8 / parts - 1) / (8 / parts))
+                          : tiles * parts;
     if (n >= kMaxBlocks) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)n, (unsigned)p.kv.G, (unsigned)p.splits);
-    attn_blocks_split_kernel<KS, ND, N><<<grid, 256, 0, s>>>(p);
+    attn_blocks_tile_kernel<KS, ND, N><<<(unsigned)n, 256, 0, s>>>(p, tiles);
     return hipGetLastError();
 }
 
 template <int ND>
-hipError_t launch_terms(const AttnArgs& p, int64_t B, hipStream_t s)
+hipError_t launch_terms(const AttnArgs& p, const Split& c, hipStream_t s)
 {
-    return p.type == MQ_F32 ? launch_main<ND, 2>(p, B, s) : launch_main<ND, 1>(p, B, s);
+    return p.type == MQ_F32 ? launch_main<ND, 2>(p, c, s) : launch_main<ND, 1>(p, c, s);
 }
 
 }  // namespace
@@ -688,8 +971,7 @@ int64_t attn_blocks_workspace(int64_t T, int64_t B, int32_t H, int32_t G, int32_
                               int64_t max_len)
 {
     if (T == 0 || B == 0) return 0;
-    const int64_t s = split_count(T, B, H, G, D, max_len);
-    return s > 1 ? s * T * H * (D + 2) * 4 : 0;
+    return choose_split(T, B, H, G, D, max_len, MQ_ATTN_MAX_WORKSPACE).bytes;
 }
 
 hipError_t launch_attn_blocks(const BlockCache& c, const void* q, int64_t ldq, int32_t type,
@@ -722,26 +1004,34 @@ hipError_t launch_attn_blocks(const BlockCache& c, const void* q, int64_t ldq, i
     // the blocks that a row of a windowed call walks over
     if (p.window > 0 && window < max_len)
         max_len = std::min(max_len, window + std::min<int64_t>(p.sinks, max_len) + 2 * kBlk);
-    int64_t splits = split_count(T, c.kv.B, H, c.kv.G, c.kv.D, max_len);
-    const int64_t one = T * H * (c.kv.D + 2) * 4;
-    splits = ws ? std::min(splits, std::max<int64_t>(ws_bytes / one, 1)) : 1;
-    p.splits = (int32_t)splits;
+    const Split split = choose_split(T, c.kv.B, H, c.kv.G, c.kv.D, max_len, ws ? ws_bytes : 0);
+    if (split.slots > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+    p.splits = (int32_t)split.splits;
+    p.target = (int32_t)split.target;
+    p.slots = (int32_t)split.slots;
     p.sums = static_cast<float*>(ws);
-    p.ml = p.sums + T * H * splits * c.kv.D;
+    p.ml = p.sums + split.bytes / ((c.kv.D + 2) * 4) * c.kv.D;
     hipError_t err;
     switch ((c.kv.D + 31) / 32) {
-    case 1: err = launch_terms<2>(p, c.kv.B, s); break;
-    case 2: err = launch_terms<4>(p, c.kv.B, s); break;
-    case 3: err = launch_terms<6>(p, c.kv.B, s); break;
-    case 4: err = launch_terms<8>(p, c.kv.B, s); break;
-    case 5: err = launch_terms<10>(p, c.kv.B, s); break;
-    case 6: err = launch_terms<12>(p, c.kv.B, s); break;
-    case 7: err = launch_terms<14>(p, c.kv.B, s); break;
-    default: err = launch_terms<16>(p, c.kv.B, s); break;
+    case 1: err = launch_terms<2>(p, split, s); break;
+    case 2: err = launch_terms<4>(p, split, s); break;
+    case 3: err = launch_terms<6>(p, split, s); break;
+    case 4: err = launch_terms<8>(p, split, s); break;
+    case 5: err = launch_terms<10>(p, split, s); break;
+    case 6: err = launch_terms<12>(p, split, s); break;
+    case 7: err = launch_terms<14>(p, split, s); break;
+    default: err = launch_terms<16>(p, split, s); break;
     }
-    if (err != hipSuccess || splits == 1) return err;
-    attn_blocks_join_kernel<<<dim3((unsigned)((T * H + 3) / 4), (unsigned)((c.kv.D + 63) / 64)),
-                              256, 0, s>>>(p);
+    if (err != hipSuccess || split.bytes == 0) return err;
+    // (T * H is far below the number of work-groups of a launch: two parts of every row
+    // fit the workspace)
+    if (split.target > 0) {
+        const dim3 grid((unsigned)(T * H), (unsigned)((c.kv.D + 63) / 64));
+        attn_blocks_join_kernel<<<grid, 256, 0, s>>>(p, split.waves);
+    } else {
+        const int64_t n = (T * H * (c.kv.D / 4) + 255) / 256;
+        attn_blocks_join_tiles_kernel<<<(unsigned)n, 256, 0, s>>>(p);
+    }
     return hipGetLastError();
 }
 

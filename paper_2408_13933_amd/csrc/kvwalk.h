@@ -33,6 +33,39 @@ struct RowTile {
     }
 };
 
+// What a tile of R rows from t.row0 on sees; len: the sequence's length, s1: the end
+// of its token rows.
+template <int R, int BLK, class Args>
+__device__ inline void set_seen(const Args& p, int32_t s1, int32_t len, RowTile<BLK>& t)
+{
+    const int32_t grp = p.grp;
+    t.pos0 = len - (s1 - t.s0);
+    t.hi_max = t.pos0 + (int32_t)((min(t.row0 + (R - 1), t.rows - 1)) / (uint32_t)grp);
+    t.hi_min = t.pos0 + (int32_t)(t.row0 / (uint32_t)grp);
+    // blocks with places, up to the last row's
+    const int64_t list = ((p.kv.ld << p.kv.shift) + BLK - 1) / BLK;
+    const int32_t end = t.hi_max < 0 ? 0 : (int32_t)min((int64_t)(t.hi_max / BLK + 1), list);
+    t.last = (int32_t)min((int64_t)(t.hi_max >> p.kv.shift), p.kv.ld - 1);
+    t.skip0 = t.skip1 = 0;
+    if (p.window > 0) {
+        t.skip1 = t.hi_min >= p.window ? min((t.hi_min - p.window + 1) / BLK, end) : 0;
+        t.skip0 = min((int32_t)(((int64_t)p.sinks + BLK - 1) / BLK), t.skip1);
+    }
+    t.n = end - (t.skip1 - t.skip0);
+}
+
+// Tile of R rows from row0 on of sequence b with token rows [s0, s1).
+template <int R, int BLK, class Args>
+__device__ inline void set_tile(const Args& p, int32_t b, int32_t s0, int32_t s1, int32_t len,
+                                uint32_t row0, RowTile<BLK>& t)
+{
+    t.b = b;
+    t.s0 = s0;
+    t.rows = (uint32_t)(s1 - s0) * (uint32_t)p.grp;
+    t.row0 = row0;
+    set_seen<R>(p, s1, len, t);
+}
+
 // The tile's index counts from floor(starts[b] grp / R) + b for sequence b: an
 // upper bound of the tiles before it that needs no scan.
 template <int R, int BLK, class Args>
@@ -48,19 +81,7 @@ __device__ inline bool find_tile(const Args& p, int64_t index, RowTile<BLK>& t)
     t.rows = (uint32_t)(s1 - s0) * (uint32_t)grp;  // below 2^32 (T H D is below 2^36)
     if (row0 < 0 || row0 >= (int64_t)t.rows) return false;
     t.row0 = (uint32_t)row0;
-    t.pos0 = len - (s1 - s0);
-    t.hi_max = t.pos0 + (int32_t)((min(t.row0 + (R - 1), t.rows - 1)) / (uint32_t)grp);
-    t.hi_min = t.pos0 + (int32_t)(t.row0 / (uint32_t)grp);
-    // blocks with places, up to the last row's
-    const int64_t list = ((p.kv.ld << p.kv.shift) + BLK - 1) / BLK;
-    const int32_t end = t.hi_max < 0 ? 0 : (int32_t)min((int64_t)(t.hi_max / BLK + 1), list);
-    t.last = (int32_t)min((int64_t)(t.hi_max >> p.kv.shift), p.kv.ld - 1);
-    t.skip0 = t.skip1 = 0;
-    if (p.window > 0) {
-        t.skip1 = t.hi_min >= p.window ? min((t.hi_min - p.window + 1) / BLK, end) : 0;
-        t.skip0 = min((int32_t)(((int64_t)p.sinks + BLK - 1) / BLK), t.skip1);
-    }
-    t.n = end - (t.skip1 - t.skip0);
+    set_seen<R>(p, s1, len, t);
     return true;
 }
 

@@ -35,6 +35,17 @@ __device__ inline int64_t wave_scan(int64_t v)
     return v;
 }
 
+__device__ inline int32_t wave_scan(int32_t v)
+{
+    v += (int32_t)dpp0<0x111, 0xf>((uint32_t)v);
+    v += (int32_t)dpp0<0x112, 0xf>((uint32_t)v);
+    v += (int32_t)dpp0<0x114, 0xf>((uint32_t)v);
+    v += (int32_t)dpp0<0x118, 0xf>((uint32_t)v);
+    v += (int32_t)dpp0<0x142, 0xa>((uint32_t)v);
+    v += (int32_t)dpp0<0x143, 0xc>((uint32_t)v);
+    return v;
+}
+
 // A lane's value in all lanes.
 __device__ inline int64_t wave_read(int64_t v, int lane)
 {

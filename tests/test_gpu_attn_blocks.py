@@ -205,6 +205,7 @@ def test_bad_queries_do_not_spread(type):
         starts, lens, pg, pool = gen.batch(rng, [new] * 3, [200, 70, 90], 16)
         q, _ = _queries(rng, 3 * new, H * D, type, 0)
         g, i = _put(_pool(rng, pool, G, 16, D, 16), (starts, lens, pg))
+        g[0][:, 0, :, 100 - 64] = -5  # every product with the infinity is -infinity
         good = mq.mq_paged_attn_blocks(q, *g, *i, 0.125)
         q2 = q.clone()
         q2[new, 3], q2[0, 100] = float("nan"), float("inf")
