@@ -42,12 +42,7 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 constexpr int kBlk = 64;                  // key positions per step
 constexpr int kRows = 16;                 // rows per set
 constexpr int kWaves = 4;                 // waves per work-group that share keys
-// sets per wave where the waves share keys (fp32 rows of more than 192 channels
-// leave registers for one)
-template <int KS, int N>
-constexpr int kSets = KS == 4 && N == 2 ? 1 : 2;
-template <int KS, int N>
-constexpr int kTile = kRows * kSets<KS, N> * kWaves;
+constexpr int kTile = 32 * kWaves;        // rows per work-group where the waves share keys
 constexpr int kMaxParts = 512;
 // sequences of a call whose parts are planned on the device, 64 per lane register
 constexpr int kPlanRegs = 4, kPlanned = 64 * kPlanRegs;
@@ -164,6 +159,27 @@ __device__ inline void load16(const AttnArgs& p, int64_t i, float (&x)[16])
     }
 }
 
+// A row's queries from bits of its largest magnitude: times a power of two, as N
+// fp16 terms; returns the factor of its products, in units of log2.  2^e <= most <
+// 2^(e + 1): the row times 2^(14 - e).  A row that is not finite becomes NaN
+// throughout.
+struct Scaled {
+    float up, a;
+    __device__ Scaled(const AttnArgs& p, uint32_t most)
+    {
+        const uint32_t e = min(max(most >> 23, 27u), 254u);
+        up = most < kInfBits ? __builtin_bit_cast(float, (268u - e) << 23) : __builtin_nanf("");
+        a = p.tau * __builtin_bit_cast(float, (e - 14u) << 23);
+    }
+};
+template <int N>
+__device__ inline void load16_any(const AttnArgs& p, int64_t i, float (&x)[16])
+{
+    if constexpr (N == 2) load16<MQ_F32>(p, i, x);
+    else if (p.type == MQ_BF16) load16<MQ_BF16>(p, i, x);
+    else load16<MQ_F16>(p, i, x);
+}
+
 // N == 2: fp32 queries.  Channels past the head and rows past the tile are 0.
 template <int KS, int ND, int N>
 __device__ inline void load_queries(const AttnArgs& p, const RowAt& row, Rows<KS, ND, N>& st)
@@ -177,11 +193,7 @@ __device__ inline void load_queries(const AttnArgs& p, const RowAt& row, Rows<KS
         const int d = 64 * s + 16 * g;
 #pragma unroll
         for (int j = 0; j < 16; ++j) x[s][j] = 0.0f;
-        if (row.have && d < p.kv.D) {
-            if constexpr (N == 2) load16<MQ_F32>(p, at + d, x[s]);
-            else if (p.type == MQ_BF16) load16<MQ_BF16>(p, at + d, x[s]);
-            else load16<MQ_F16>(p, at + d, x[s]);
-        }
+        if (row.have && d < p.kv.D) load16_any<N>(p, at + d, x[s]);
 #pragma unroll
         for (int j = 0; j < 16; ++j) most = max(most, abs_bits(x[s][j]));
     }
@@ -190,21 +202,56 @@ __device__ inline void load_queries(const AttnArgs& p, const RowAt& row, Rows<KS
     most = max(most, o);
     most = swap32(most, o);
     most = max(most, o);
-    // 2^e <= most < 2^(e + 1); the row times 2^(14 - e), the products by its inverse;
-    // a row that is not finite becomes NaN throughout
-    const uint32_t e = min(max(most >> 23, 27u), 254u);
-    const float up = most < kInfBits ? __builtin_bit_cast(float, (268u - e) << 23)
-                                     : __builtin_nanf("");
-    st.a = p.tau * __builtin_bit_cast(float, (e - 14u) << 23);
+    const Scaled sc(p, most);
+    st.a = sc.a;
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            const float v = x[s][j] * up;
+            const float v = x[s][j] * sc.up;
             const _Float16 h = (_Float16)v;
             st.q[0][s][j >> 3][j & 7] = h;
             if constexpr (N == 2) st.q[1][s][j >> 3][j & 7] = (_Float16)(v - (float)h);
         }
+}
+// The same for 32 rows: channels 32 u + 16 (lane >> 5) on; in two passes over the row,
+// whose channels do not all fit beside the rest.
+template <int DT, int N>
+__device__ inline float load_queries32(const AttnArgs& p, const RowAt& row, v8h (&q)[N][DT][2])
+{
+    const int hh = (threadIdx.x & 63) >> 5;
+    const int64_t at = row.t * p.ldq + (int64_t)row.head * p.kv.D;
+    uint32_t most = 0;
+    auto chunk = [&](int u, float (&x)[16]) {
+        const int d = 32 * u + 16 * hh;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[j] = 0.0f;
+        if (row.have && d < p.kv.D) load16_any<N>(p, at + d, x);
+    };
+#pragma unroll
+    for (int u = 0; u < DT; ++u) {
+        float x[16];
+        chunk(u, x);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) most = max(most, abs_bits(x[j]));
+    }
+    uint32_t o;
+    most = swap32(most, o);
+    most = max(most, o);
+    const Scaled sc(p, most);
+#pragma unroll
+    for (int u = 0; u < DT; ++u) {
+        float x[16];
+        chunk(u, x);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const float v = x[j] * sc.up;
+            const _Float16 h = (_Float16)v;
+            q[0][u][j >> 3][j & 7] = h;
+            if constexpr (N == 2) q[1][u][j >> 3][j & 7] = (_Float16)(v - (float)h);
+        }
+    }
+    return sc.a;
 }
 
 // Where a lane reads a block: keys 16 (r >> 2) + (r & 3) of tile 0 (tile j: 4 j rows
@@ -277,100 +324,57 @@ __device__ inline int32_t value_tile(const AttnArgs& p, int dt)
     return 16 * dt < p.kv.D ? 256 * dt : 0;
 }
 
-// One block for the wave's sets.  key(j, s, h), value(dt, h): fragments; read():
-// called once the keys have been used; ks, vs: the lane's scales, placed: whether
-// its group has a place; full: every row sees every position.
-template <int KS, int ND, int N, int NR, class Key, class Value, class Read>
-__device__ inline void attend_block(const AttnArgs& p, Rows<KS, ND, N> (&st)[NR],
-                                    const Sees (&sees)[NR], int32_t blk, bool full, bool placed,
-                                    float ks, float vs, Key key, Value value, Read read)
-{
-    const int g = (threadIdx.x & 63) >> 4;
-    // scores of keys 16 g + 4 j + i
-    v4f c[NR][4];
-    if (NR > 1) __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            v8h k[2];
-            key(j, s, k);
-#pragma unroll
-            for (int n = 0; n < NR; ++n)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        c[n][j] = mfma(k[h], st[n].q[e][s][h],
-                                       s + h + e ? c[n][j] : v4f{0.0f, 0.0f, 0.0f, 0.0f});
-        }
-    if (NR > 1) __builtin_amdgcn_s_setprio(0);
-    read();
-    const bool mask = !full || __ballot(!placed) != 0;
-    v8h w[NR][N][2];
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-        float kn = ks, vn = fmaxf(vs, 0x1p-67f);
-        if (mask) {
-            const int32_t first = blk * kBlk + 16 * g;
-            // of the 16 keys from `first` on those below x, as bits
-            auto below = [&](int32_t x) { return (1u << max(min(x - first, 16), 0)) - 1; };
-            uint32_t seen = below(sees[n].hi + 1) & (~below(sees[n].lo + 1) | below(p.sinks));
-            if (!placed) seen = 0;
-            if (seen == 0) kn = vn = 1.0f;  // (the scales there may be anything)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int keep = __builtin_amdgcn_sbfe((int)seen, i, 1);  // all ones or 0
-                const float y = c[n][i >> 2][i & 3];  // (a bit cast of an element casts the first)
-                const int x = __builtin_bit_cast(int, y);
-                c[n][i >> 2][i & 3] = __builtin_bit_cast(float, (x & keep) | ((int)0xff800000u & ~keep));
-            }
-        }
+// How 16 scores of a lane become weights, 2^(a c + b); lv, iv: log2 and inverse of
+// the value scale.
+struct Weigh {
+    float a, b, lv, iv;
+    // what the row's running maximum has to be compared with
+    __device__ float top(float row_a, float ks, float vs, float most)
+    {
         // (not 0: a product with -infinity stays that)
-        const float a = fmaxf(st[n].a * kn, 0x1p-126f), lv = __builtin_amdgcn_logf(vn);
-        float m = c[n][0][0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) m = fmaxf(m, c[n][i >> 2][i & 3]);
-        m = __builtin_fmaf(m, a, lv);
-        m = row_max(m);
-        if (__ballot(m > st[n].m + kLag) != 0) {
-            m = fmaxf(m, st[n].m);
-            const float f = exp2_fast(st[n].m - m);
-            st[n].l *= f;
-#pragma unroll
-            for (int dt = 0; dt < ND; ++dt) st[n].acc[dt] *= f;
-            st[n].m = m;
-        }
-        const float b = lv + (kTop - st[n].m);
-        float x[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            x[i] = exp2_fast(__builtin_fmaf(c[n][i >> 2][i & 3], a, b));
-            const _Float16 h = (_Float16)x[i];
-            w[n][0][i >> 3][i & 7] = h;
-            if constexpr (N == 2) w[n][1][i >> 3][i & 7] = (_Float16)(x[i] - (float)h);
-        }
-        // (not of the rounded ones: a weight by a small value scale may be below
-        // fp16 and still count here)
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sum += x[i];
-        st[n].l = __builtin_fmaf(sum, exp2_fast(-lv), st[n].l);
+        a = fmaxf(row_a * ks, 0x1p-126f);
+        lv = __builtin_amdgcn_logf(vs);
+        iv = exp2_fast(-lv);
+        return __builtin_fmaf(most, a, lv);
     }
-    if (NR > 1) __builtin_amdgcn_s_setprio(1);
+};
+
+// Scores of 16 consecutive keys from `first` on that the row does not see (or that
+// have no place) become -infinity.  Scales of a group without any are 1 (they may be
+// anything there).
+template <class Get>
+__device__ inline void mask_scores(const AttnArgs& p, const Sees& sees, int32_t first, bool placed,
+                                   float& ks, float& vs, Get score)
+{
+    // of the 16 keys on those below x, as bits
+    auto below = [&](int32_t x) { return (1u << max(min(x - first, 16), 0)) - 1; };
+    uint32_t seen = below(sees.hi + 1) & (~below(sees.lo + 1) | below(p.sinks));
+    if (!placed) seen = 0;
+    if (seen == 0) ks = vs = 1.0f;
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt) {
-        v8h v[2];
-        value(dt, v);
-#pragma unroll
-        for (int n = 0; n < NR; ++n)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < N; ++e) st[n].acc[dt] = mfma(v[h], w[n][e][h], st[n].acc[dt]);
+    for (int i = 0; i < 16; ++i) {
+        const int keep = __builtin_amdgcn_sbfe((int)seen, i, 1);  // all ones or 0
+        const float y = score(i);
+        const int x = __builtin_bit_cast(int, y);
+        score(i, __builtin_bit_cast(float, (x & keep) | ((int)0xff800000u & ~keep)));
     }
-    if (NR > 1) __builtin_amdgcn_s_setprio(0);
 }
+
+// Weight i (of 8 of an operand) as N fp16 numbers; sum: of the lane's, not of the
+// rounded ones (a weight by a small value scale may be below fp16 and still count
+// there).
+template <int N>
+__device__ inline void weigh(const Weigh& f, float score, int i, v8h (&w)[N], float& sum)
+{
+    const float x = exp2_fast(__builtin_fmaf(score, f.a, f.b));
+    const _Float16 h = (_Float16)x;
+    w[0][i] = h;
+    if constexpr (N == 2) w[1][i] = (_Float16)(x - (float)h);
+    sum += x;
+}
+
+// Least value scale that is told apart (its inverse times weights stays finite).
+__device__ inline float value_scale(float vs) { return fmaxf(vs, 0x1p-67f); }
 
 // 1 / l; 0 for a row that sees nothing.
 __device__ inline float out_unit(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
@@ -415,13 +419,12 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
 {
     const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Sees sees[1] = {row.sees};
-    Rows<KS, ND, N> st[1];
-    st[0].clear();
+    Rows<KS, ND, N> st;
+    st.clear();
     int32_t i = i0 + wave;
     if (i < i1) {
         Pages pg = load_pages(p, tile, tile.block(i));
-        load_queries(p, row, st[0]);
+        load_queries(p, row, st);
         // values are read a block ahead; keys too where there are registers for them,
         // else once the block before has its scores
         constexpr bool kAhead = KS <= 2;
@@ -460,20 +463,65 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
             read_values(next);
             __builtin_amdgcn_sched_barrier(0);
             // (what is read without registers to spare goes into the keys just used)
-            const float ks = now.ks, vs = now.vs;
+            float ks = now.ks, vs = now.vs;
             const bool placed = now.placed;
-            attend_block<KS, ND, N, 1>(
-                p, st, sees, blk, tile.full(p, blk), placed, ks, vs,
-                [&](int j, int s, v8h (&k)[2]) { to_half((kAhead ? now : buf[0]).k[j][s], k); },
-                [&](int dt, v8h (&v)[2]) { to_half(now.v[dt], v); },
-                [&]() {
-                    if constexpr (!kAhead) {
-                        read_keys(buf[0]);
-                        next.ks = buf[0].ks;
-                        next.vs = buf[0].vs;
-                        next.placed = buf[0].placed;
-                    }
-                });
+            // scores of keys 16 g + 4 j + i
+            v4f c[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    v8h k[2];
+                    to_half((kAhead ? now : buf[0]).k[j][s], k);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int e = 0; e < N; ++e)
+                            c[j] = mfma(k[h], st.q[e][s][h],
+                                        s + h + e ? c[j] : v4f{0.0f, 0.0f, 0.0f, 0.0f});
+                }
+            if constexpr (!kAhead) {
+                read_keys(buf[0]);
+                next.ks = buf[0].ks;
+                next.vs = buf[0].vs;
+                next.placed = buf[0].placed;
+            }
+            if (!tile.full(p, blk) || __ballot(!placed) != 0) {
+                struct {
+                    v4f (&c)[4];
+                    __device__ float operator()(int i) const { return c[i >> 2][i & 3]; }
+                    __device__ void operator()(int i, float x) const { c[i >> 2][i & 3] = x; }
+                } score{c};
+                mask_scores(p, row.sees, blk * kBlk + 16 * g, placed, ks, vs, score);
+            }
+            float m = c[0][0];
+#pragma unroll
+            for (int x = 1; x < 16; ++x) m = fmaxf(m, c[x >> 2][x & 3]);
+            Weigh f;
+            m = row_max(f.top(st.a, ks, value_scale(vs), m));
+            if (__ballot(m > st.m + kLag) != 0) {
+                m = fmaxf(m, st.m);
+                const float down = exp2_fast(st.m - m);
+                st.l *= down;
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt) st.acc[dt] *= down;
+                st.m = m;
+            }
+            f.b = f.lv + (kTop - st.m);
+            v8h w[2][N];
+            float sum = 0.0f;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) weigh(f, c[x >> 2][x & 3], x & 7, w[x >> 3], sum);
+            st.l = __builtin_fmaf(sum, f.iv, st.l);
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) {
+                v8h v[2];
+                to_half(now.v[dt], v);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < N; ++e) st.acc[dt] = mfma(v[h], w[h][e], st.acc[dt]);
+            }
         };
         for (; i < i1; i += W) {
             block(buf[0], buf[1]);
@@ -484,14 +532,14 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
     }
     float* lm = lds + W * 4 * ND * 64;  // [wave][row]
     float* ll = lm + W * kRows;
-    const float l = row_sum(st[0].l);
+    const float l = row_sum(st.l);
     if (g == 0) {
-        lm[wave * kRows + r] = st[0].m;
+        lm[wave * kRows + r] = st.m;
         ll[wave * kRows + r] = l;
     }
     v4f* acc = reinterpret_cast<v4f*>(lds);  // [wave][tile][lane]
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt) acc[(wave * ND + dt) * 64 + lane] = st[0].acc[dt];
+    for (int dt = 0; dt < ND; ++dt) acc[(wave * ND + dt) * 64 + lane] = st.acc[dt];
     __syncthreads();
     float m = kNone;
 #pragma unroll
@@ -525,114 +573,225 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
     }
 }
 
-// Every wave has sets of its own; all walk over blocks [i0, i1), whose codes the
-// four together put into LDS as fp16, in the order of the lanes: keys (j, s), then
-// values, two halves of 1 KB each.  The next block's codes are read during this one
-// and converted once for all waves (by every wave for itself: 228 us instead of
-// WAVEFIG for 500 tokens over 16000, 32 heads of 128 on 8).
-template <int KS, int ND>
-constexpr int kStage = (4 * KS + ND) * 2048;
-template <int KS, int ND, int N>
+// Where many rows share keys: a wave has 32 rows on the 32 x 32 x 16 instructions.
+// Vector arithmetic (290 instructions a block, 32 of them exponentials) and products
+// (32 of 32 cycles) add up: 500 tokens over 16000, 32 heads of 128 on 8, take 167 us, two
+// sets of 16 rows on the smaller instructions the same, and so with the products of the
+// next block's scores between this one's exponentials.
+// Scores C[key][row] of 32 keys, the keys of tile t of a block in the order 32 t + 16
+// ((r >> 2) & 1) + 4 (r >> 3) + (r & 3): a lane holds row lane & 31 and the 16
+// consecutive keys of group 2 t + (lane >> 5), outputs in O[d][row].
+struct Wide {
+    int lane, r, hh;
+    __device__ Wide()
+    {
+        lane = threadIdx.x & 63;
+        r = lane & 31;
+        hh = lane >> 5;
+    }
+};
+typedef float v16f __attribute__((ext_vector_type(16)));
+__device__ inline v16f mfma32(v8h a, v8h b, v16f c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// All four waves walk over blocks [i0, i1), whose codes they put into LDS as fp16, in
+// the order of the lanes: keys (t, u) and values (t, u) of 32 channels u, two halves
+// of 1 KB each.  A block's codes are read during the block before and converted once
+// for all waves (by every wave for itself: 228 us instead of 167).
+template <int DT>
+constexpr int kStage = 4 * DT * 2048;
+template <int DT, int N>
 __device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g0, int32_t i0,
                                   int32_t i1, int split, MQ_LDS int8_t* lds)
 {
-    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const Wide at;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    constexpr int NR = kSets<KS, N>;
-    RowAt row[NR];
-    Sees sees[NR];
-    Rows<KS, ND, N> st[NR];
+    const RowAt row(p, tile, tile.row0 + 32 * wave, g0, at.r);
+    v16f acc[DT];
 #pragma unroll
-    for (int n = 0; n < NR; ++n) {
-        row[n] = RowAt(p, tile, tile.row0 + kRows * (NR * wave + n), g0);
-        sees[n] = row[n].sees;
-        st[n].clear();
-    }
+    for (int u = 0; u < DT; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[u][i] = 0.0f;
+    float m = kNone, l = 0.0f;
     if (i0 < i1) {
-        Pages pg = load_pages(p, tile, tile.block(i0));
-        float ks = 0.0f, vs = 0.0f;
-        bool placed = false;
-        // the wave's share: key tile j = wave, every fourth value tile
-        constexpr int NV = (ND + 3) / 4;
-        v4i kf[KS], vf[NV];
-        auto read = [&](int32_t blk) {
-            const Addr at(p, tile, g0, blk, pg);
-            ks = p.k_scale[at.scale];
-            vs = p.v_scale[at.scale];
-            placed = at.placed;
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-                kf[s] = *reinterpret_cast<const MQ_GLOBAL v4i*>(
-                    at.k + (4 * wave * p.kv.D + key_chunk(p, s)));
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                vf[i] = *reinterpret_cast<const MQ_GLOBAL v4i*>(at.v + value_tile(p, 4 * i + wave));
+        // waves 0 and 1 stage the keys of a tile, 2 and 3 the values
+        const int t = wave & 1;
+        const bool values = wave >= 2;
+        const int32_t group = 2 * t + (values ? at.hh : (at.r >> 2) & 1);
+        const uint32_t D = (uint32_t)p.kv.D, mask = (1u << p.kv.shift) - 1;
+        // from the first slot of the group's 16: a key and its channels, or a
+        // channel's 16 tokens; channels past the head read its first ones (queries are 0
+        // there, such outputs are dropped)
+        const uint32_t lane_at = values ? 16 * at.r : (4 * (at.r >> 3) + (at.r & 3)) * D + 16 * at.hh;
+        const uint32_t step = values ? 512 : 32;
+        const uint32_t last = (DT - 1) * step,
+                       back = (values ? 32 * (DT - 1) + at.r : 32 * (DT - 1) + 16 * at.hh) < (int)D
+                                  ? last
+                                  : 0u - (values ? 16 * at.r : 16 * at.hh);
+        const MQ_GLOBAL int8_t* const base =
+            (const MQ_GLOBAL int8_t*)(values ? p.kv.v : p.kv.k) +
+            (((uint32_t)g0 << p.kv.shift) * D + lane_at);
+        const int32_t* const list = p.kv.table + (int64_t)tile.b * p.kv.ld;
+        struct Entries {
+            int32_t stage, scale[2];
         };
-        auto put = [&](MQ_LDS int8_t* to) {
-            to += lane * 16;
-            v8h h[2];
+        auto entries = [&](int32_t i) {
+            const int32_t blk = tile.block(min(i, i1 - 1));
+            return Entries{list[min(entry_of(p, blk, group), tile.last)],
+                           {list[min(entry_of(p, blk, at.hh), tile.last)],
+                            list[min(entry_of(p, blk, 2 + at.hh), tile.last)]}};
+        };
+        struct Scales {
+            float k[2], v[2];
+            bool placed[2];
+        };
+        v4i raw[DT];
+        Entries pg = entries(i0);
+        auto read = [&](int32_t i, Scales& s) {
+            const int32_t blk = tile.block(min(i, i1 - 1));
+            const uint32_t page = is_page(p, tile, blk, group, pg.stage) ? (uint32_t)pg.stage : 0;
+            const uint32_t slot = (uint32_t)(blk * kBlk + 16 * group) & mask;
+            const MQ_GLOBAL int8_t* x = base + ((uint64_t)page * (uint32_t)p.page_bytes + slot * D);
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                to_half(kf[s], h);
-                *reinterpret_cast<MQ_LDS v8h*>(to + (wave * KS + s) * 2048) = h[0];
-                *reinterpret_cast<MQ_LDS v8h*>(to + (wave * KS + s) * 2048 + 1024) = h[1];
+            for (int u = 0; u < DT - 1; ++u)
+                raw[u] = *reinterpret_cast<const MQ_GLOBAL v4i*>(x + u * step);
+            raw[DT - 1] = *reinterpret_cast<const MQ_GLOBAL v4i*>(x + (int32_t)back);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int32_t g = 2 * j + at.hh;
+                s.placed[j] = is_page(p, tile, blk, g, pg.scale[j]);
+                const uint32_t sp = s.placed[j] ? (uint32_t)pg.scale[j] : 0;
+                const uint64_t e =
+                    (uint64_t)sp * ((uint32_t)p.kv.G << (p.kv.shift - p.bshift)) +
+                    ((((uint32_t)g0 << p.kv.shift) + ((uint32_t)(blk * kBlk + 16 * g) & mask)) >>
+                     p.bshift);
+                s.k[j] = p.k_scale[e];
+                s.v[j] = p.v_scale[e];
             }
+            pg = entries(i + 1);
+        };
+        MQ_LDS int8_t* const mine = lds + ((values ? 2 : 0) + t) * DT * 2048 + at.lane * 16;
+        auto put = [&](int buf) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int dt = 4 * i + wave;
-                if (ND % 4 != 0 && dt >= ND) break;
-                to_half(vf[i], h);
-                *reinterpret_cast<MQ_LDS v8h*>(to + (4 * KS + dt) * 2048) = h[0];
-                *reinterpret_cast<MQ_LDS v8h*>(to + (4 * KS + dt) * 2048 + 1024) = h[1];
+            for (int u = 0; u < DT; ++u) {
+                v8h h[2];
+                to_half(raw[u], h);
+                MQ_LDS int8_t* to = mine + buf * kStage<DT> + u * 2048;
+                *reinterpret_cast<MQ_LDS v8h*>(to) = h[0];
+                *reinterpret_cast<MQ_LDS v8h*>(to + 1024) = h[1];
             }
         };
-        read(tile.block(i0));
-        pg = load_pages(p, tile, tile.block(min(i0 + 1, i1 - 1)));
-#pragma unroll
-        for (int n = 0; n < NR; ++n) load_queries(p, row[n], st[n]);
-        put(lds);
+        // (fp32 rows of more than 224 channels leave no registers for the next block)
+        constexpr bool kLate = DT == 8 && N == 2;
+        Scales now, next;
+        read(i0, now);
+        v8h q[N][DT][2];
+        const float qa = load_queries32<DT, N>(p, row, q);
+        put(0);
         __syncthreads();
         for (int32_t i = i0; i < i1; ++i) {
             const int32_t blk = tile.block(i);
             const int buf = (i - i0) & 1;
-            const float ks0 = ks, vs0 = vs;
-            const bool placed0 = placed;
-            read(tile.block(min(i + 1, i1 - 1)));
-            pg = load_pages(p, tile, tile.block(min(i + 2, i1 - 1)));
-            const MQ_LDS int8_t* at = lds + buf * kStage<KS, ND> + lane * 16;
-            attend_block<KS, ND, N, NR>(
-                p, st, sees, blk, tile.full(p, blk), placed0, ks0, vs0,
-                [&](int j, int s, v8h (&k)[2]) {
-                    k[0] = *reinterpret_cast<const MQ_LDS v8h*>(at + (j * KS + s) * 2048);
-                    k[1] = *reinterpret_cast<const MQ_LDS v8h*>(at + (j * KS + s) * 2048 + 1024);
-                },
-                [&](int dt, v8h (&v)[2]) {
-                    v[0] = *reinterpret_cast<const MQ_LDS v8h*>(at + (4 * KS + dt) * 2048);
-                    v[1] = *reinterpret_cast<const MQ_LDS v8h*>(at + (4 * KS + dt) * 2048 + 1024);
-                },
-                []() {});
-            put(lds + (buf ^ 1) * kStage<KS, ND>);
+            if (!kLate) read(i + 1, next);
+            const MQ_LDS int8_t* from = lds + buf * kStage<DT> + at.lane * 16;
+            v16f c[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) c[j][x] = 0.0f;
+#pragma unroll
+            for (int u = 0; u < DT; ++u)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const v8h k = *reinterpret_cast<const MQ_LDS v8h*>(
+                            from + (j * DT + u) * 2048 + h * 1024);
+#pragma unroll
+                        for (int e = 0; e < N; ++e) c[j] = mfma32(k, q[e][u][h], c[j]);
+                    }
+            if (!tile.full(p, blk) || __ballot(!(now.placed[0] && now.placed[1])) != 0) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    struct {
+                        v16f& c;
+                        __device__ float operator()(int i) const { return c[i]; }
+                        __device__ void operator()(int i, float x) const { c[i] = x; }
+                    } score{c[j]};
+                    mask_scores(p, row.sees, blk * kBlk + 32 * j + 16 * at.hh, now.placed[j],
+                                now.k[j], now.v[j], score);
+                }
+            }
+            Weigh f[2];
+            float most = -__builtin_inff();
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float x = c[j][0];
+#pragma unroll
+                for (int e = 1; e < 16; ++e) x = fmaxf(x, c[j][e]);
+                most = fmaxf(most, f[j].top(qa, now.k[j], value_scale(now.v[j]), x));
+            }
+            uint32_t o;
+            const uint32_t own = swap32(__builtin_bit_cast(uint32_t, most), o);
+            most = fmaxf(__builtin_bit_cast(float, own), __builtin_bit_cast(float, o));
+            if (__ballot(most > m + kLag) != 0) {
+                most = fmaxf(most, m);
+                const float down = exp2_fast(m - most);
+                l *= down;
+#pragma unroll
+                for (int u = 0; u < DT; ++u) acc[u] *= down;
+                m = most;
+            }
+            v8h w[2][2][N];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                f[j].b = f[j].lv + (kTop - m);
+                float sum = 0.0f;
+#pragma unroll
+                for (int x = 0; x < 16; ++x) weigh(f[j], c[j][x], x & 7, w[j][x >> 3], sum);
+                l = __builtin_fmaf(sum, f[j].iv, l);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int u = 0; u < DT; ++u) {
+                        const v8h v = *reinterpret_cast<const MQ_LDS v8h*>(
+                            from + ((2 + j) * DT + u) * 2048 + h * 1024);
+#pragma unroll
+                        for (int e = 0; e < N; ++e) acc[u] = mfma32(v, w[j][h][e], acc[u]);
+                    }
+            if (kLate) read(i + 1, next);
+            put(buf ^ 1);
+            now = next;
             __syncthreads();
         }
     }
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-        const float l = row_sum(st[n].l);
-        if (!row[n].have) continue;
-        const int64_t part = (row[n].t * p.H + row[n].head) * p.splits + split;
-        if (p.splits > 1 && g == 0) {
-            p.ml[2 * part] = st[n].m;
-            p.ml[2 * part + 1] = l;
-        }
-        const float unit = out_unit(l);
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt) {
-            if (16 * dt >= p.kv.D) break;
-            const int32_t d = 16 * dt + 4 * g;
-            if (p.splits > 1) *reinterpret_cast<v4f*>(p.sums + part * p.kv.D + d) = st[n].acc[dt];
-            else store_four(p, row[n].t, row[n].head, d, st[n].acc[dt] * unit);
-        }
+    {
+        uint32_t o;
+        const uint32_t own = swap32(__builtin_bit_cast(uint32_t, l), o);
+        l = __builtin_bit_cast(float, own) + __builtin_bit_cast(float, o);
     }
+    if (!row.have) return;
+    const int64_t part = (row.t * p.H + row.head) * p.splits + split;
+    if (p.splits > 1 && at.hh == 0) {
+        p.ml[2 * part] = m;
+        p.ml[2 * part + 1] = l;
+    }
+    const float unit = out_unit(l);
+#pragma unroll
+    for (int u = 0; u < DT; ++u)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int32_t d = 32 * u + 8 * x + 4 * at.hh;
+            if (d >= p.kv.D) break;
+            const v4f v = {acc[u][4 * x], acc[u][4 * x + 1], acc[u][4 * x + 2], acc[u][4 * x + 3]};
+            if (p.splits > 1) *reinterpret_cast<v4f*>(p.sums + part * p.kv.D + d) = v;
+            else store_four(p, row.t, row.head, d, v * unit);
+        }
 }
 
 // The parts of a call's rows: every sequence's tiles of 16 rows, its blocks split
@@ -766,16 +925,16 @@ __global__ __launch_bounds__(64 * W, KS <= 2 ? 2 : 1) void attn_blocks_rows_kern
 // One work-group per tile of rows, cache head and split; a sequence's last 16 rows
 // or fewer are split among the waves.
 template <int KS, int ND, int N>
-__global__ __launch_bounds__(256, KS <= 2 ? 2 : 1) void attn_blocks_tile_kernel(AttnArgs p,
-                                                                                int64_t tiles)
+__global__ __launch_bounds__(256, KS <= (N == 2 ? 1 : 2) ? 2 : 1) void attn_blocks_tile_kernel(
+    AttnArgs p, int64_t tiles)
 {
-    constexpr int kJoin = kJoinFloats<ND, kWaves> * 4;
-    constexpr int kBytes = 2 * kStage<KS, ND> > kJoin ? 2 * kStage<KS, ND> : kJoin;
+    constexpr int DT = ND / 2, kJoin = kJoinFloats<ND, kWaves> * 4;
+    constexpr int kBytes = 2 * kStage<DT> > kJoin ? 2 * kStage<DT> : kJoin;
     __shared__ __attribute__((aligned(1024))) int8_t lds[kBytes];
     const Place w = place_of(p, blockIdx.x, tiles);
     const int32_t g0 = w.part % p.kv.G, split = w.part / p.kv.G;
     Tile tile;
-    if (w.tile >= tiles || !find_tile<kTile<KS, N>, kBlk>(p, w.tile, tile)) return;
+    if (w.tile >= tiles || !find_tile<kTile, kBlk>(p, w.tile, tile)) return;
     int32_t i0, i1;
     split_range(p, tile, split, i0, i1);
     if (tile.rows - tile.row0 <= kRows) {
@@ -783,7 +942,7 @@ __global__ __launch_bounds__(256, KS <= 2 ? 2 : 1) void attn_blocks_tile_kernel(
         const PartAt part{p.splits == 1, (row.t * p.H + row.head) * p.splits + split};
         split_rows<KS, ND, N, kWaves>(p, tile, g0, i0, i1, row, part, reinterpret_cast<float*>(lds));
     } else {
-        share_keys<KS, ND, N>(p, tile, g0, i0, i1, split, (MQ_LDS int8_t*)lds);
+        share_keys<DT, N>(p, tile, g0, i0, i1, split, (MQ_LDS int8_t*)lds);
     }
 }
 
@@ -903,7 +1062,7 @@ Split choose_split(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D, int64_
     ws_bytes = std::min<int64_t>(ws_bytes, MQ_ATTN_MAX_WORKSPACE);
     if (tiled(T, B, grp)) {
         // at least a block per wave in each
-        const int64_t groups = std::max(T * grp / kTile<1, 1>, std::min(B, T)) * G;
+        const int64_t groups = std::max(T * grp / kTile, std::min(B, T)) * G;
         int64_t s = (D > 128 ? kCUs : 2 * kCUs) / std::max<int64_t>(groups, 1);
         s = std::min(s, (blocks + kWaves - 1) / kWaves);
         s = std::min<int64_t>(s, ws_bytes / (T * H * row));
@@ -949,7 +1108,7 @@ hipError_t launch_main(const AttnArgs& p, const Split& c, hipStream_t s)
         return launch_rows<ND, N, 4>(p, s);
     }
     const int64_t parts = (int64_t)p.kv.G * p.splits;
-    const int64_t tiles = row_tiles(p.T, p.kv.B, p.grp, kTile<KS, N>);
+    const int64_t tiles = row_tiles(p.T, p.kv.B, p.grp, kTile);
     // (see place_of)
     const int64_t n = parts % 8 != 0 && 8 % parts == 0
                           ? 8 * ((tiles + 8 / parts - 1) / (8 / parts))

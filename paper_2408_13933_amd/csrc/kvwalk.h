@@ -85,17 +85,23 @@ __device__ inline bool find_tile(const Args& p, int64_t index, RowTile<BLK>& t)
     return true;
 }
 
-// Row lane & 15 of the 16 from `first` on: token row, query head, what it sees.
+// A row, by default lane & 15 of the 16 from `first` on: token row, query head, what it
+// sees.
 struct RowAt {
     bool have;
     int64_t t;
     int32_t head;
     Sees sees;
-    RowAt() = default;
     template <class Args, int BLK>
     __device__ RowAt(const Args& p, const RowTile<BLK>& tile, uint32_t first, int32_t g0)
+        : RowAt(p, tile, first, g0, threadIdx.x & 15)
     {
-        const uint32_t x = first + (threadIdx.x & 15);  // no overflow: rows below 2^32 - 64
+    }
+    // row r from `first` on
+    template <class Args, int BLK>
+    __device__ RowAt(const Args& p, const RowTile<BLK>& tile, uint32_t first, int32_t g0, uint32_t r)
+    {
+        const uint32_t x = first + r;  // no overflow: rows below 2^32 - 64
         have = x < tile.rows;
         const uint32_t row = have ? x : tile.rows - 1, tok = row / (uint32_t)p.grp;
         t = (int64_t)tile.s0 + tok;
