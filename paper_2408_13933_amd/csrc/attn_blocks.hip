@@ -21,6 +21,7 @@
 // outputs to the sum of two; statistics and outputs are fp32.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "kvblocks.h"
 #include "kvwalk.h"
@@ -35,6 +36,7 @@ namespace mq {
 namespace {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef int v2i __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
@@ -80,20 +82,29 @@ __device__ inline v4f mfma(v8h a, v8h b, v4f c)
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-// 16 codes as fp16, exact: the byte c + 128 in the low bits of 1024 is 1152 + c.
-__device__ inline void to_half(const v4i& x, v8h (&h)[2])
+// Eight codes as fp16, exact: the byte c + 128 in the low bits of 1024 is 1152 + c.
+__device__ inline v8h to_half(int32_t x, int32_t y)
 {
     const v2h off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+    const uint32_t b[2] = {(uint32_t)x ^ 0x80808080u, (uint32_t)y ^ 0x80808080u};
+    v8h h;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t b = (uint32_t)x[i] ^ 0x80808080u;
-        const v2h lo = __builtin_bit_cast(v2h, __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u)) + off;
-        const v2h hi = __builtin_bit_cast(v2h, __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u)) + off;
-        h[i >> 1][4 * (i & 1)] = lo[0];
-        h[i >> 1][4 * (i & 1) + 1] = lo[1];
-        h[i >> 1][4 * (i & 1) + 2] = hi[0];
-        h[i >> 1][4 * (i & 1) + 3] = hi[1];
+    for (int i = 0; i < 2; ++i) {
+        const v2h lo =
+            __builtin_bit_cast(v2h, __builtin_amdgcn_perm(0x64646464u, b[i], 0x04010400u)) + off;
+        const v2h hi =
+            __builtin_bit_cast(v2h, __builtin_amdgcn_perm(0x64646464u, b[i], 0x04030402u)) + off;
+        h[4 * i] = lo[0];
+        h[4 * i + 1] = lo[1];
+        h[4 * i + 2] = hi[0];
+        h[4 * i + 3] = hi[1];
     }
+    return h;
+}
+__device__ inline void to_half(const v4i& x, v8h (&h)[2])
+{
+    h[0] = to_half(x[0], x[1]);
+    h[1] = to_half(x[2], x[3]);
 }
 
 // Over the four lanes of a row.
@@ -127,8 +138,8 @@ __device__ inline float row_sum(float v)
     return over_row(v, [](float a, float b) { return a + b; });
 }
 
-// A set of 16 rows: KS steps of 64 channels, ND tiles of 16 output channels, N
-// fp16 terms of queries and of weights.
+// A set of 16 rows: KS steps of 64 channels (the last one of 32 where the number of 32
+// is odd), ND tiles of 16 output channels, N fp16 terms of queries and of weights.
 template <int KS, int ND, int N>
 struct Rows {
     v8h q[N][KS][2];
@@ -144,21 +155,6 @@ struct Rows {
     }
 };
 
-template <int TYPE>
-__device__ inline void load16(const AttnArgs& p, int64_t i, float (&x)[16])
-{
-    constexpr int E = TYPE == MQ_F32 ? 4 : 2;
-    if (p.vec_q) {
-        Raw<TYPE, 16> r;
-        r.load(static_cast<const int8_t*>(p.q) + i * E);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) x[j] = r[j];
-    } else {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) x[j] = load_elem<TYPE>(p.q, i + j);
-    }
-}
-
 // A row's queries from bits of its largest magnitude: times a power of two, as N
 // fp16 terms; returns the factor of its products, in units of log2.  2^e <= most <
 // 2^(e + 1): the row times 2^(14 - e).  A row that is not finite becomes NaN
@@ -172,31 +168,66 @@ struct Scaled {
         a = p.tau * __builtin_bit_cast(float, (e - 14u) << 23);
     }
 };
+// N == 2: fp32 queries.
 template <int N>
-__device__ inline void load16_any(const AttnArgs& p, int64_t i, float (&x)[16])
+__device__ inline void load8_any(const AttnArgs& p, int64_t i, float* x)
 {
-    if constexpr (N == 2) load16<MQ_F32>(p, i, x);
-    else if (p.type == MQ_BF16) load16<MQ_BF16>(p, i, x);
-    else load16<MQ_F16>(p, i, x);
+    auto load = [&](auto type) {
+        constexpr int TYPE = decltype(type)::value;
+        constexpr int E = TYPE == MQ_F32 ? 4 : 2;
+        if (p.vec_q) {
+            Raw<TYPE, 8> r;
+            r.load(static_cast<const int8_t*>(p.q) + i * E);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = r[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = load_elem<TYPE>(p.q, i + j);
+        }
+    };
+    if constexpr (N == 2) load(std::integral_constant<int, MQ_F32>{});
+    else if (p.type == MQ_BF16) load(std::integral_constant<int, MQ_BF16>{});
+    else load(std::integral_constant<int, MQ_F16>{});
 }
 
-// N == 2: fp32 queries.  Channels past the head and rows past the tile are 0.
+// The first channel of a lane's eight of operand (s, h) of a set's products.
+template <int ND>
+__device__ inline int operand_channel(int s, int h)
+{
+    constexpr int KS = (ND + 3) / 4;
+    const int g = (threadIdx.x & 63) >> 4;
+    return (ND / 2) % 2 == 1 && s == KS - 1 ? 64 * s + 8 * g : 64 * s + 16 * g + 8 * h;
+}
+// Operands of step s.
+template <int ND>
+constexpr int halves(int s)
+{
+    return (ND / 2) % 2 == 1 && s == (ND + 3) / 4 - 1 ? 1 : 2;
+}
+
+// Channels past the head and rows past the tile are 0.  All lanes read (those the row's
+// first channels; a row past the tile is its last one): where loads depended on the lane,
+// the compiler (HIP 7.2) moved registers of all lanes to accumulators with part of the
+// lanes off, and lost what the others held.
 template <int KS, int ND, int N>
 __device__ inline void load_queries(const AttnArgs& p, const RowAt& row, Rows<KS, ND, N>& st)
 {
-    const int g = (threadIdx.x & 63) >> 4;
     const int64_t at = row.t * p.ldq + (int64_t)row.head * p.kv.D;
-    float x[KS][16];
+    float x[KS][2][8];
     uint32_t most = 0;  // as bits: NaN and infinities are the largest
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-        const int d = 64 * s + 16 * g;
+    for (int s = 0; s < KS; ++s)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) x[s][j] = 0.0f;
-        if (row.have && d < p.kv.D) load16_any<N>(p, at + d, x[s]);
+        for (int h = 0; h < halves<ND>(s); ++h) {
+            const int d = operand_channel<ND>(s, h);
+            const bool have = row.have && d < p.kv.D;
+            load8_any<N>(p, at + (have ? d : 0), x[s][h]);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) most = max(most, abs_bits(x[s][j]));
-    }
+            for (int j = 0; j < 8; ++j) {
+                x[s][h][j] = have ? x[s][h][j] : 0.0f;
+                most = max(most, abs_bits(x[s][h][j]));
+            }
+        }
     uint32_t o;
     most = swap16(most, o);
     most = max(most, o);
@@ -207,12 +238,14 @@ __device__ inline void load_queries(const AttnArgs& p, const RowAt& row, Rows<KS
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const float v = x[s][j] * sc.up;
-            const _Float16 h = (_Float16)v;
-            st.q[0][s][j >> 3][j & 7] = h;
-            if constexpr (N == 2) st.q[1][s][j >> 3][j & 7] = (_Float16)(v - (float)h);
-        }
+        for (int h = 0; h < halves<ND>(s); ++h)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float v = x[s][h][j] * sc.up;
+                const _Float16 f = (_Float16)v;
+                st.q[0][s][h][j] = f;
+                if constexpr (N == 2) st.q[1][s][h][j] = (_Float16)(v - (float)f);
+            }
 }
 // The same for 32 rows: channels 32 u + 16 (lane >> 5) on; in two passes over the row,
 // whose channels do not all fit beside the rest.
@@ -224,9 +257,11 @@ __device__ inline float load_queries32(const AttnArgs& p, const RowAt& row, v8h 
     uint32_t most = 0;
     auto chunk = [&](int u, float (&x)[16]) {
         const int d = 32 * u + 16 * hh;
+        const bool have = row.have && d < p.kv.D;
+        load8_any<N>(p, at + (have ? d : 0), x);
+        load8_any<N>(p, at + (have ? d : 0) + 8, x + 8);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) x[j] = 0.0f;
-        if (row.have && d < p.kv.D) load16_any<N>(p, at + d, x);
+        for (int j = 0; j < 16; ++j) x[j] = have ? x[j] : 0.0f;
     };
 #pragma unroll
     for (int u = 0; u < DT; ++u) {
@@ -313,15 +348,13 @@ struct Addr {
 };
 
 // Channels past the head dimension: the scores read the head's first ones again
-// (the queries are 0 there), the outputs of such a tile are dropped.
+// (the queries are 0 there), the outputs of such a tile are dropped.  Offset of a
+// lane's channels of step s from its first address (channel 16 g).
+template <int ND>
 __device__ inline int32_t key_chunk(const AttnArgs& p, int s)
 {
-    const int32_t c = 16 * ((threadIdx.x & 63) >> 4);
-    return 64 * s + c < p.kv.D ? 64 * s : -c;
-}
-__device__ inline int32_t value_tile(const AttnArgs& p, int dt)
-{
-    return 16 * dt < p.kv.D ? 256 * dt : 0;
+    const int32_t d = operand_channel<ND>(s, 0), c = 16 * (((int)threadIdx.x & 63) >> 4);
+    return (d < p.kv.D ? d : 0) - c;
 }
 
 // How 16 scores of a lane become weights, 2^(a c + b); lv, iv: log2 and inverse of
@@ -442,14 +475,21 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int s = 0; s < KS; ++s)
-                    x.k[j][s] = *reinterpret_cast<const MQ_GLOBAL v4i*>(
-                        at.k + (4 * j * p.kv.D + key_chunk(p, s)));
+                for (int s = 0; s < KS; ++s) {
+                    const MQ_GLOBAL int8_t* from = at.k + (4 * j * p.kv.D + key_chunk<ND>(p, s));
+                    if (halves<ND>(s) == 2) {
+                        x.k[j][s] = *reinterpret_cast<const MQ_GLOBAL v4i*>(from);
+                    } else {
+                        const v2i h = *reinterpret_cast<const MQ_GLOBAL v2i*>(from);
+                        x.k[j][s] = v4i{h[0], h[1], 0, 0};
+                    }
+                }
         };
         auto read_values = [&](Block& x) {
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt)
-                x.v[dt] = *reinterpret_cast<const MQ_GLOBAL v4i*>(at.v + value_tile(p, dt));
+                if (dt < ND - 1 || 16 * dt < p.kv.D)
+                    x.v[dt] = *reinterpret_cast<const MQ_GLOBAL v4i*>(at.v + 256 * dt);
         };
         auto ahead = [&](int32_t x) { return tile.block(min(x, i1 - 1)); };
         read_keys(buf[0]);
@@ -471,14 +511,15 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int s = 0; s < KS; ++s) {
-                    v8h k[2];
-                    to_half((kAhead ? now : buf[0]).k[j][s], k);
+                    const v4i& x = (kAhead ? now : buf[0]).k[j][s];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                    for (int h = 0; h < halves<ND>(s); ++h) {
+                        const v8h k = to_half(x[2 * h], x[2 * h + 1]);
 #pragma unroll
                         for (int e = 0; e < N; ++e)
-                            c[j] = mfma(k[h], st.q[e][s][h],
+                            c[j] = mfma(k, st.q[e][s][h],
                                         s + h + e ? c[j] : v4f{0.0f, 0.0f, 0.0f, 0.0f});
+                    }
                 }
             if constexpr (!kAhead) {
                 read_keys(buf[0]);
@@ -515,6 +556,7 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
             st.l = __builtin_fmaf(sum, f.iv, st.l);
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) {
+                if (dt == ND - 1 && 16 * dt >= p.kv.D) break;
                 v8h v[2];
                 to_half(now.v[dt], v);
 #pragma unroll
@@ -1092,8 +1134,10 @@ hipError_t launch_rows(const AttnArgs& p, hipStream_t s)
 {
     constexpr int KS = (ND + 3) / 4;
     const dim3 grid((unsigned)p.slots, (unsigned)p.kv.G);
-    if (p.kv.B <= kPlanned) attn_blocks_rows_kernel<KS, ND, N, W, true><<<grid, 64 * W, 0, s>>>(p);
-    else attn_blocks_rows_kernel<KS, ND, N, W, false><<<grid, 64 * W, 0, s>>>(p);
+    if (p.kv.B <= kPlanned)
+        attn_blocks_rows_kernel<KS, ND, N, W, true><<<grid, 64 * W, 0, s>>>(p);
+    else
+        attn_blocks_rows_kernel<KS, ND, N, W, false><<<grid, 64 * W, 0, s>>>(p);
     return hipGetLastError();
 }
 
@@ -1103,7 +1147,7 @@ hipError_t launch_main(const AttnArgs& p, const Split& c, hipStream_t s)
     constexpr int KS = (ND + 3) / 4;
     if (c.waves > 0) {
         if (c.slots * p.kv.G >= kMaxBlocks / 2) return hipErrorInvalidConfiguration;
-        if constexpr (KS <= 2)
+        if constexpr (ND <= 8)
             if (c.waves == 8) return launch_rows<ND, N, 8>(p, s);
         return launch_rows<ND, N, 4>(p, s);
     }

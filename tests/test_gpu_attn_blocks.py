@@ -133,6 +133,34 @@ def test_long_sequences_split(H, G, D, type):
     _check(rng, H, G, D, 128, 64, [40, 2], [5000, 3000], type, max_len=5000)
 
 
+@pytest.mark.parametrize("D", range(16, 257, 16))
+@pytest.mark.parametrize("type", TYPES)
+def test_every_head_size_in_parts(D, type):
+    """Workspaces that held anything; tiles of many rows, of one to sixteen left over,
+    and rows of their own."""
+    import torch
+
+    import paper_2408_13933_amd as mq
+    for H, new, lens in ((8, [1, 17, 33, 20], [200, 317, 1350, 64]), (2, [1, 2, 8], [3000, 700, 9])):
+        n = mq.mq_paged_attn_blocks_workspace_bytes(sum(new) + 2, len(new), H, 1, D, 3008)
+        ws = torch.full((n // 4,), float("nan"), device="cuda").view(torch.uint8)
+        _check(np.random.default_rng(D), H, 1, D, 64, 32, new, lens, type, ws=ws)
+
+
+@pytest.mark.parametrize("B", [64, 65, 130, 256, 257, 400])
+@pytest.mark.parametrize("H,G,D,type", [(4, 2, 64, "bfloat16"), (2, 2, 32, "float32"),
+                                        (8, 1, 144, "float16")])
+def test_many_sequences(B, H, G, D, type):
+    """Of all lengths, some without new tokens or with several; one long."""
+    rng = np.random.default_rng(B)
+    new = rng.choice([0, 1, 1, 1, 1, 1, 2, 3], B)
+    lens = rng.integers(4, 200, B)
+    _check(rng, H, G, D, 16, 16, list(new), list(lens), type)
+    _check(rng, H, G, D, 16, 16, list(new), list(lens), type, window=50, sinks=3)
+    lens[B // 2] = 9000
+    _check(rng, H, G, D, 16, 16, list(new), list(lens), type)
+
+
 def test_sharp_and_flat_logits():
     for spread in (0.0, 1e-20, 30.0, 200.0):
         _check(np.random.default_rng(3), 4, 2, 64, 32, 16, [1, 20], [900, 300], "float32",
