@@ -1,12 +1,11 @@
 // Penalties for words that a sequence holds, biases and grammar masks, on logits
 // where they lie.
 //
-// A work-group takes a row's range of kWords words: it walks over the row's whole
-// history and counts the words of its range in LDS, so that order does not matter
-// and a word's penalties, bias and mask meet in one thread.  Only words that
-// change are read or written.  Latency bounds it for few rows (row lengths, the
-// history, the logits: three round trips), the history and the -infinities that
-// masks write for many.
+// A work-group takes a row's range of words: it walks over the row's whole history
+// and counts the words of its range in LDS, so that order does not matter and a
+// word's penalties, bias and mask meet in one thread.  Only groups of eight words
+// with one that changes are read or written.  Latency bounds it: row lengths and the
+// history's first words in one round trip, then biases, logits and bias values.
 #include <algorithm>
 
 #include "adjust.h"
@@ -17,139 +16,236 @@ namespace mq {
 namespace {
 
 constexpr int kThreads = 512;
-constexpr int kEach = 8;  // consecutive words of a thread
-constexpr int kWords = kThreads * kEach;
 
-// A word's entry: how often the sequence holds it past its prompt, and kPrompt if
-// the prompt does.
-constexpr uint32_t kPrompt = 0x80000000u;
+// A word's state in LDS.  Packed: an entry of the bias list + 1 in the upper bits, then
+// whether the prompt holds the word, then how often the sequence does past its prompt;
+// 8192 words are a work-group's, so that 200 rows of 32000 fit the chip at once.  Else
+// two numbers of 32 bits, 4096 words.
+template <bool PACKED, int EACH>
+struct State {
+    static constexpr int kWords = kThreads * EACH;  // consecutive ones of a thread
+    static constexpr int kEntry = PACKED ? 15 : 0;  // its lowest bit
+    static constexpr uint32_t kPrompt = PACKED ? 1u << 14 : 1u << 31;
+    __attribute__((aligned(16))) uint32_t count[kWords];
+    __attribute__((aligned(16))) uint32_t own[PACKED ? 4 : kWords];
+    __device__ uint32_t* entry() { return PACKED ? count : own; }
+};
+constexpr int64_t kPackedCols = (1 << 14) - 1, kPackedBias = (1 << 17) - 2;
 
+template <int TYPE>
+constexpr uint32_t kMinusInf = TYPE == MQ_F32 ? 0xff800000u : TYPE == MQ_BF16 ? 0xff80u : 0xfc00u;
+
+// Eight logits as they lie in memory.
+template <int TYPE>
+struct Eight {
+    static constexpr int kDwords = TYPE == MQ_F32 ? 8 : 4;
+    uint32_t d[kDwords];
+    __device__ void load(const void* x, int64_t i)
+    {
+        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const int8_t*>(x) +
+                                                        i * (TYPE == MQ_F32 ? 4 : 2));
+#pragma unroll
+        for (int j = 0; j < kDwords / 4; ++j) {
+            const uint4 v = p[j];
+            d[4 * j] = v.x, d[4 * j + 1] = v.y, d[4 * j + 2] = v.z, d[4 * j + 3] = v.w;
+        }
+    }
+    __device__ void store(void* x, int64_t i) const
+    {
+        uint4* p =
+            reinterpret_cast<uint4*>(static_cast<int8_t*>(x) + i * (TYPE == MQ_F32 ? 4 : 2));
+#pragma unroll
+        for (int j = 0; j < kDwords / 4; ++j)
+            p[j] = make_uint4(d[4 * j], d[4 * j + 1], d[4 * j + 2], d[4 * j + 3]);
+    }
+    __device__ float get(int i) const
+    {
+        if constexpr (TYPE == MQ_F32) return __builtin_bit_cast(float, d[i]);
+        else return half_of<TYPE>(d[i >> 1], i & 1);
+    }
+    __device__ void put(int i, uint32_t b)
+    {
+        if constexpr (TYPE == MQ_F32) d[i] = b;
+        else d[i >> 1] = (i & 1) ? (d[i >> 1] & 0xffffu) | b << 16 : (d[i >> 1] & 0xffff0000u) | b;
+    }
+};
+template <int TYPE>
+__device__ inline uint32_t bits_of(float x)
+{
+    if constexpr (TYPE == MQ_F32) return __builtin_bit_cast(uint32_t, x);
+    else return pack2<TYPE>(x, 0.0f) & 0xffffu;
+}
 template <int TYPE>
 __device__ inline void store_bits(void* x, int64_t i, uint32_t b)
 {
     if constexpr (TYPE == MQ_F32) static_cast<uint32_t*>(x)[i] = b;
     else static_cast<uint16_t*>(x)[i] = (uint16_t)b;
 }
-template <int TYPE>
-constexpr uint32_t kMinusInf = TYPE == MQ_F32 ? 0xff800000u : TYPE == MQ_BF16 ? 0xff80u : 0xfc00u;
 
-template <int TYPE, bool BIAS>
+template <int TYPE, bool PACKED, int kEach>
 __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs p, int32_t ranges, bool vec_x,
                                                           bool vec_h)
 {
 #pragma clang fp contract(off)
-    __shared__ __attribute__((aligned(16))) uint32_t count[kWords];
-    __shared__ __attribute__((aligned(16))) uint32_t entry[BIAS ? kWords : 4];  // of the bias list, + 1
+    using S = State<PACKED, kEach>;
+    constexpr int kWords = S::kWords;
+    __shared__ S st;
     const int tid = threadIdx.x;
     const int64_t m = blockIdx.x / ranges;
     const int32_t w0 = (int32_t)(blockIdx.x - m * ranges) * kWords;
     const int32_t V = (int32_t)p.V, first = w0 + tid * kEach;
     const int32_t words = min(kWords, V - w0);
 
-    // the mask's byte of this thread's words (words past the row: allowed)
-    uint32_t allowed = 0xff;
-    if (p.mask && first < V) {
-        allowed = (p.mask[m * p.ldm + (first >> 5)] >> (first & 31)) & 0xff;
-        if (first + kEach > V) allowed |= 0xff << (V - first);
+    // everything that depends on the row alone, the first words of its history too (they
+    // are there up to `cols`, counted or not)
+    int32_t n = 0, prompt = 0;
+    const int32_t* h = nullptr;
+    int4 ahead = make_int4(0, 0, 0, 0);
+    if (p.history) {
+        n = (int32_t)min((int64_t)p.hist_lens[m], p.cols);
+        prompt = p.prompt_lens ? p.prompt_lens[m] : 0;
+        h = p.history + m * p.ldh;
+        if (vec_h && tid * 4 < p.cols) ahead = reinterpret_cast<const int4*>(h)[tid];
     }
     const float rep = p.repetition ? p.repetition[m] : 1.0f;
     const float pres = p.presence ? p.presence[m] : 0.0f;
     const float freq = p.frequency ? p.frequency[m] : 0.0f;
-    // (x / 1, x - 0 and x - 0 * n change no bit)
-    const bool penal = p.history && !(rep == 1.0f && pres == 0.0f && freq == 0.0f);
     int32_t b0 = 0, b1 = 0;
-    if constexpr (BIAS) {
+    if (p.bias_starts) {
         b0 = max(p.bias_starts[m], 0);
         b1 = (int32_t)min((int64_t)p.bias_starts[m + 1], p.bias_n);
     }
-    if (penal || b0 < b1) {
-        const uint4 zero = make_uint4(0, 0, 0, 0);
-        for (int i = tid; i < kWords / 4; i += kThreads) {
-            reinterpret_cast<uint4*>(count)[i] = zero;
-            if constexpr (BIAS) reinterpret_cast<uint4*>(entry)[i] = zero;
-        }
-        __syncthreads();
+    // the mask's bits of this thread's words (words past the row: allowed)
+    constexpr uint32_t kAll = (1u << kEach) - 1;
+    uint32_t allowed = kAll;
+    if (p.mask && first < V) {
+        allowed = (p.mask[m * p.ldm + (first >> 5)] >> (first & 31)) & kAll;
+        if (first + kEach > V) allowed |= kAll & (kAll << (V - first));
     }
-    if (penal) {
-        const int32_t n = (int32_t)min((int64_t)p.hist_lens[m], p.cols);
-        const int32_t prompt = p.prompt_lens ? p.prompt_lens[m] : 0;
-        const int32_t* h = p.history + m * p.ldh;
-        auto add = [&](int32_t i, int32_t word) {
-            const uint32_t at = (uint32_t)word - (uint32_t)w0;
-            if (at >= (uint32_t)words) return;
-            if (i < prompt) atomicOr(&count[at], kPrompt);
-            else atomicAdd(&count[at], 1u);
-        };
-        if (vec_h) {
-            for (int32_t i = tid * 4; i < n; i += kThreads * 4) {
-                const int4 v = *reinterpret_cast<const int4*>(h + i);  // (whole fours of a row)
-                add(i, v.x);
-                if (i + 1 < n) add(i + 1, v.y);
-                if (i + 2 < n) add(i + 2, v.z);
-                if (i + 3 < n) add(i + 3, v.w);
-            }
-        } else {
-            for (int32_t i = tid; i < n; i += kThreads) add(i, h[i]);
-        }
-    }
-    if constexpr (BIAS) {
-        for (int32_t i = b0 + tid; i < b1; i += kThreads) {
-            const uint32_t at = (uint32_t)p.bias_tokens[i] - (uint32_t)w0;
-            // of equal words the last one
-            if (at < (uint32_t)words) atomicMax(&entry[at], (uint32_t)i + 1);
-        }
-    }
+    // (x / 1, x - 0 and x - 0 * n change no bit)
+    const bool penal = n > 0 && !(rep == 1.0f && pres == 0.0f && freq == 0.0f);
     uint32_t c[kEach] = {}, e[kEach] = {}, touched = 0;
     if (penal || b0 < b1) {
+        int32_t word = b0 + tid < b1 ? p.bias_tokens[b0 + tid] : -1;
+        const uint4 zero = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < kEach / 4; ++i) {
+            reinterpret_cast<uint4*>(st.count)[i * kThreads + tid] = zero;
+            if constexpr (!PACKED) reinterpret_cast<uint4*>(st.own)[i * kThreads + tid] = zero;
+        }
+        __syncthreads();
+        for (int32_t i = b0 + tid; i < b1; i += kThreads) {
+            if (i != b0 + tid) word = p.bias_tokens[i];
+            const uint32_t at = (uint32_t)word - (uint32_t)w0;
+            // of equal words the last one
+            if (at < (uint32_t)words) atomicMax(&st.entry()[at], ((uint32_t)i + 1) << S::kEntry);
+        }
+        if (PACKED && b0 < b1) __syncthreads();  // (the maxima are of entries alone)
+        if (penal) {
+            auto add = [&](int32_t i, int32_t word) {
+                const uint32_t at = (uint32_t)word - (uint32_t)w0;
+                if (i >= n || at >= (uint32_t)words) return;
+                if (i < prompt) atomicOr(&st.count[at], S::kPrompt);
+                else atomicAdd(&st.count[at], 1u);
+            };
+            auto add_four = [&](int32_t i, const int4& v) {
+                add(i, v.x);
+                add(i + 1, v.y);
+                add(i + 2, v.z);
+                add(i + 3, v.w);
+            };
+            if (vec_h) {
+                add_four(tid * 4, ahead);
+                for (int32_t i = (kThreads + tid) * 4; i < n; i += kThreads * 4)
+                    add_four(i, *reinterpret_cast<const int4*>(h + i));  // (whole fours of a row)
+            } else {
+                for (int32_t i = tid; i < n; i += kThreads) add(i, h[i]);
+            }
+        }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            c[i] = count[tid * kEach + i];
-            if constexpr (BIAS) e[i] = entry[tid * kEach + i];
+            c[i] = st.count[tid * kEach + i];
+            if constexpr (PACKED) {
+                e[i] = c[i] >> S::kEntry;
+                c[i] &= (1u << S::kEntry) - 1;
+            } else {
+                e[i] = st.own[tid * kEach + i];
+            }
             if (c[i] | e[i]) touched |= 1u << i;
         }
     }
     if (first >= V) return;
     touched &= allowed;
-    if (touched == 0 && allowed == 0xff) return;
+    if (touched == 0 && allowed == kAll) return;
     const int64_t at = m * p.ld + first;
+    float bias[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        bias[i] = 0.0f;
+        if (e[i] && ((touched >> i) & 1)) bias[i] = p.bias_values[e[i] - 1];
+    }
     auto value = [&](int i, float x) {
         if (c[i]) {
             x = x > 0.0f ? x / rep : x * rep;
-            if (const uint32_t n = c[i] & ~kPrompt) {
-                x = x - freq * (float)n;
+            if (const uint32_t k = c[i] & ~S::kPrompt) {
+                x = x - freq * (float)k;
                 x = x - pres;
             }
         }
-        if (BIAS && e[i]) x = x + p.bias_values[e[i] - 1];
+        if (e[i]) x = x + bias[i];
         return x;
     };
-    if (allowed == 0 && vec_x && first + kEach <= V) {
-        constexpr uint32_t b = TYPE == MQ_F32 ? kMinusInf<TYPE> : kMinusInf<TYPE> * 0x10001u;
-        uint4* y = reinterpret_cast<uint4*>(static_cast<int8_t*>(p.x) + at * (TYPE == MQ_F32 ? 4 : 2));
-        y[0] = make_uint4(b, b, b, b);
-        if constexpr (TYPE == MQ_F32) y[1] = make_uint4(b, b, b, b);
+    if (vec_x && first + kEach <= V) {
+        Eight<TYPE> x[kEach / 8];
+#pragma unroll
+        for (int j = 0; j < kEach / 8; ++j)
+            if (((touched >> (8 * j)) & 0xff) != 0 ||
+                (((allowed >> (8 * j)) & 0xff) != 0xff && ((allowed >> (8 * j)) & 0xff) != 0))
+                x[j].load(p.x, at + 8 * j);
+#pragma unroll
+        for (int j = 0; j < kEach / 8; ++j) {
+            const uint32_t ok = (allowed >> (8 * j)) & 0xff, to = (touched >> (8 * j)) & 0xff;
+            if (to == 0 && ok == 0xff) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (!((ok >> i) & 1)) x[j].put(i, kMinusInf<TYPE>);
+                else if ((to >> i) & 1) x[j].put(i, bits_of<TYPE>(value(8 * j + i, x[j].get(i))));
+            }
+            x[j].store(p.x, at + 8 * j);
+        }
         return;
     }
+    float x[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) x[i] = (touched >> i) & 1 ? load_elem<TYPE>(p.x, at + i) : 0.0f;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         if (!((allowed >> i) & 1)) store_bits<TYPE>(p.x, at + i, kMinusInf<TYPE>);
-        else if ((touched >> i) & 1)
-            store_elem<TYPE>(p.x, at + i, value(i, load_elem<TYPE>(p.x, at + i)));
+        else if ((touched >> i) & 1) store_bits<TYPE>(p.x, at + i, bits_of<TYPE>(value(i, x[i])));
     }
 }
 
-template <int TYPE>
-hipError_t launch(const AdjustArgs& p, hipStream_t s)
+template <int TYPE, bool PACKED, int EACH>
+hipError_t launch_p(const AdjustArgs& p, hipStream_t s)
 {
+    constexpr int kWords = State<PACKED, EACH>::kWords;
     const int64_t ranges = (p.V + kWords - 1) / kWords;
     if (p.M * ranges >= kMaxBlocks / 2) return hipErrorInvalidConfiguration;  // of 512 threads
     const bool vec_x = (uintptr_t)p.x % 16 == 0 && p.ld * type_bytes(TYPE) % 16 == 0;
     const bool vec_h = (uintptr_t)p.history % 16 == 0 && p.ldh % 4 == 0 && p.cols % 4 == 0;
-    const unsigned n = (unsigned)(p.M * ranges);
-    if (p.bias_starts) adjust_kernel<TYPE, true><<<n, kThreads, 0, s>>>(p, (int32_t)ranges, vec_x, vec_h);
-    else adjust_kernel<TYPE, false><<<n, kThreads, 0, s>>>(p, (int32_t)ranges, vec_x, vec_h);
+    adjust_kernel<TYPE, PACKED, EACH>
+        <<<(unsigned)(p.M * ranges), kThreads, 0, s>>>(p, (int32_t)ranges, vec_x, vec_h);
     return hipGetLastError();
+}
+template <int TYPE>
+hipError_t launch(const AdjustArgs& p, hipStream_t s)
+{
+    const bool fits = (!p.history || p.cols <= kPackedCols) &&
+                      (!p.bias_starts || p.bias_n <= kPackedBias);
+    if (!fits) return launch_p<TYPE, false, 8>(p, s);
+    return p.M * p.V < (int64_t)kThreads * 8 * 512 ? launch_p<TYPE, true, 8>(p, s)
+                                                   : launch_p<TYPE, true, 16>(p, s);
 }
 
 }  // namespace

@@ -80,6 +80,22 @@ def test_adjust(M, V, pad, hist, nbias, mask, type):
     _check(x, d, V)
 
 
+@pytest.mark.parametrize("type", TYPES)
+@pytest.mark.parametrize("M,V", [(3, 9000), (2, 40), (70, 5003)])
+@pytest.mark.parametrize("hist,nbias", [(16383, None), (16384, 5), (20000, 300), (40, 131070),
+                                        (40, 131071), (None, 140000)])
+def test_long_histories_and_bias_lists(M, V, hist, nbias, type):
+    """Around the most words and entries that counts of a few bits hold; all of a
+    row's history the same word."""
+    rng = np.random.default_rng(V)
+    M = M if (nbias or 0) < 1000 else 1
+    x, d = _inputs(rng, M, V, hist, nbias, V > 9, type)
+    if hist is not None:
+        d["history"][0] = V // 2
+        d["prompts"][0] = 0
+    _check(x, d, V)
+
+
 @pytest.mark.parametrize("left", ["prompts", "repetition", "presence", "frequency"])
 def test_parts_left_out(left):
     x, d = _inputs(np.random.default_rng(1), 4, 3000, 400, None, False, "float32")
