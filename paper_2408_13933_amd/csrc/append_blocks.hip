@@ -166,17 +166,26 @@ __device__ inline void rotate_queries(const AppendArgs& p, int64_t id)
     if (head >= p.per_turn) return;
     Angles a;
     if (p.angles) a.load(p.angles + pos * D + 2 * i);
-    for (int32_t h = (int32_t)(id - t * p.waves) * p.per_turn + head; h < p.H;
-         h += p.waves * p.per_turn) {
-        Four<TYPE, VEC> u, w;
-        const int64_t at = t * p.ldq + (int64_t)h * D + i;
-        u.load(p.q, at);
-        w.load(p.q, at + D / 2);
-        float r[8];
-        turn(u, w, a, p.angles != nullptr, r);
-        const int64_t to = t * p.ldo + (int64_t)h * D + i;
-        store_four<TYPE, VEC>(p.q_out, to, r);
-        store_four<TYPE, VEC>(p.q_out, to + D / 2, r + 4);
+    constexpr int U = 4;  // turns whose reads are under way together
+    const int32_t step = p.waves * p.per_turn;
+    for (int32_t h0 = (int32_t)(id - t * p.waves) * p.per_turn + head; h0 < p.H; h0 += U * step) {
+        Four<TYPE, VEC> u[U], w[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int64_t at = t * p.ldq + (int64_t)min(h0 + j * step, p.H - 1) * D + i;
+            u[j].load(p.q, at);
+            w[j].load(p.q, at + D / 2);
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int32_t h = h0 + j * step;
+            if (h >= p.H) break;
+            float r[8];
+            turn(u[j], w[j], a, p.angles != nullptr, r);
+            const int64_t to = t * p.ldo + (int64_t)h * D + i;
+            store_four<TYPE, VEC>(p.q_out, to, r);
+            store_four<TYPE, VEC>(p.q_out, to + D / 2, r + 4);
+        }
     }
 }
 
