@@ -50,6 +50,7 @@ constexpr int kMaxParts = 512;
 constexpr int kPlanRegs = 4, kPlanned = 64 * kPlanRegs;
 constexpr float kNone = -1e30f;           // running maximum of a row that has seen nothing
 constexpr float kTop = 8.0f, kLag = 7.0f; // weights up to 2^(kTop + kLag)
+constexpr float kHuge = 0x1p21f;          // maxima from here on round by more than that leaves
 using Tile = RowTile<kBlk>;
 
 struct AttnArgs {
@@ -372,6 +373,13 @@ struct Weigh {
     }
 };
 
+// Exponent of a weight, where a maximum's rounding could push it past fp16 (NaN stays).
+__device__ inline float limited(const Weigh& f, float score)
+{
+    const float x = __builtin_fmaf(score, f.a, f.b);
+    return x > kTop + kLag ? kTop + kLag : x;
+}
+
 // Scores of 16 consecutive keys from `first` on that the row does not see (or that
 // have no place) become -infinity.  Scales of a group without any are 1 (they may be
 // anything there).
@@ -549,6 +557,12 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
                 st.m = m;
             }
             f.b = f.lv + (kTop - st.m);
+            if (__ballot(fabsf(st.m) >= kHuge) != 0) {
+#pragma unroll
+                for (int x = 0; x < 16; ++x) c[x >> 2][x & 3] = limited(f, c[x >> 2][x & 3]);
+                f.a = 1.0f;
+                f.b = 0.0f;
+            }
             v8h w[2][N];
             float sum = 0.0f;
 #pragma unroll
@@ -790,6 +804,12 @@ __device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 f[j].b = f[j].lv + (kTop - m);
+                if (__ballot(fabsf(m) >= kHuge) != 0) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) c[j][x] = limited(f[j], c[j][x]);
+                    f[j].a = 1.0f;
+                    f[j].b = 0.0f;
+                }
                 float sum = 0.0f;
 #pragma unroll
                 for (int x = 0; x < 16; ++x) weigh(f[j], c[j][x], x & 7, w[j][x >> 3], sum);

@@ -175,14 +175,17 @@ def attn_bound(size, most, count, D, bits, vs_log2):
     and the maximum (numbers up to X + |log2 vs| + 8: four roundings); a weight
     takes its exp2 (2^-22) and its rounding (2^-11 for 16-bit types, else 2^-22);
     numerator and denominator each sum `count` terms over steps of 64 ((count /
-    16 + 64) u); every relative error of a weight counts in both.  Weights too
+    16 + 64) u); every relative error of a weight counts in both: weights w r with r
+    from 2^-e to 2^e have a mean R of that range, and sum w (r / R - 1) v is at most
+    2^(2 e) - 1 of sum w |v| (from e = 400 on, where 64 bits may not hold the other
+    weights, nothing is said).  Weights too
     small for fp16 are short of 2^-25 of 2^1 at least (the largest is >= 2): count
     * 2^-26 of the values."""
     u, X = 2.0 ** -24, most * 1.4426950408889634
     logit = (2 * D * u + 2.0 ** -22 + 4 * u) * X + 4 * u * (X + vs_log2 + 8)
     weight = 2.0 ** -22 + (2.0 ** -11 if bits == 16 else 2.0 ** -22)
-    rel = 2 * (0.6931471805599453 * logit + weight + (count / 16 + 64) * u)
-    return size * rel * 1.01, count * 2.0 ** -26
+    rel = np.exp2(np.minimum(2 * logit, 999)) - 1 + 2 * (weight + (count / 16 + 64) * u)
+    return np.where(logit < 400, size * rel * 1.01, np.inf), count * 2.0 ** -26
 
 
 def adjust_logits(x, history=None, lens=None, prompts=None, repetition=None, presence=None,

@@ -47,7 +47,9 @@ def _compare(got, q, cache, batch, scale, type, D, window, sinks):
     vs = vs[np.isfinite(vs) & (vs > 0)]
     rel, small = rs.attn_bound(size, most, count, D, 32 if type == "float32" else 16,
                                np.abs(np.log2(vs)).max())
-    tol = rel + small * vs.max() * 127
+    # (a context is a mean of values, whatever the weights are)
+    far = 127 * float(vs.max())
+    tol = np.minimum(rel, 2 * far * (1 + 2.0 ** -10)) + small * far
     want, got = want.reshape(T, H, D), got.astype(np.float64).reshape(T, H, D)
     tol = np.broadcast_to(tol[:, :, None], want.shape)
     # past the type's largest number the nearest one is infinite (from half a step
@@ -166,6 +168,18 @@ def test_sharp_and_flat_logits():
         _check(np.random.default_rng(3), 4, 2, 64, 32, 16, [1, 20], [900, 300], "float32",
                spread=spread)
         _check(np.random.default_rng(4), 4, 2, 64, 32, 16, [1, 20], [900, 300], "bfloat16",
+               spread=spread)
+
+
+@pytest.mark.parametrize("type,spread", [("float32", 1e5), ("float32", 1e7), ("float32", 1e20),
+                                         ("bfloat16", 1e5), ("bfloat16", 1e12),
+                                         ("float16", 5000.0)])
+@pytest.mark.parametrize("D", [32, 96, 256])
+def test_huge_logits(type, spread, D):
+    """Maxima whose last place is larger than a weight's range (one key has all the
+    weight, as far as 32 bits tell)."""
+    for new in (1, 40):
+        _check(np.random.default_rng(5), 4, 2, D, 32, 16, [new, new], [900, 70], type,
                spread=spread)
 
 
