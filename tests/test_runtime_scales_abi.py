@@ -207,4 +207,4 @@ def test_adjust_nothing_to_do_and_too_much():
     assert adjust(M=0, x=None) == 0
     assert adjust(h=None, bs=None, m=None) == 0
     assert adjust(M=1 << 23) == UNSUPPORTED
-    assert adjust(M=1 << 13, V=1 << 22, ld=1 << 22, ldm=1 << 17) == UNSUPPORTED
+    assert adjust(M=1 << 14, V=1 << 22, ld=1 << 22, ldm=1 << 17) == UNSUPPORTED
