@@ -5,7 +5,9 @@
 // and counts the words of its range in LDS, so that order does not matter and a
 // word's penalties, bias and mask meet in one thread.  Only groups of eight words
 // with one that changes are read or written.  Latency bounds it: row lengths and the
-// history's first words in one round trip, then biases, logits and bias values.
+// history's first words in one round trip, then biases, logits and bias values: one
+// row of 256000 fp32 words, 9000 of history and 300 biases 6.9 us, 200 rows of 32000
+// bf16 ones with 1500 of history and masks 12.9 (8 MB).
 #include <algorithm>
 
 #include "adjust.h"
@@ -244,6 +246,8 @@ hipError_t launch(const AdjustArgs& p, hipStream_t s)
     const bool fits = (!p.history || p.cols <= kPackedCols) &&
                       (!p.bias_starts || p.bias_n <= kPackedBias);
     if (!fits) return launch_p<TYPE, false, 8>(p, s);
+    // (small ranges until there are two work-groups per CU: one row of 256000 words 7.0 us,
+    // 9.1 with large ones; 200 rows of 32000 13.8, 18.1 with small ones)
     return p.M * p.V < (int64_t)kThreads * 8 * 512 ? launch_p<TYPE, true, 8>(p, s)
                                                    : launch_p<TYPE, true, 16>(p, s);
 }

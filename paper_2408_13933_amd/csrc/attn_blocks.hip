@@ -631,9 +631,10 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
 
 // Where many rows share keys: a wave has 32 rows on the 32 x 32 x 16 instructions.
 // Vector arithmetic (290 instructions a block, 32 of them exponentials) and products
-// (32 of 32 cycles) add up: 500 tokens over 16000, 32 heads of 128 on 8, take 167 us, two
-// sets of 16 rows on the smaller instructions the same, and so with the products of the
-// next block's scores between this one's exponentials.
+// (32 of 32 cycles) add up: 500 tokens over 16000, 32 heads of 128 on 8, take 160 us
+// and a join of 8, 0.77 PFLOP/s; two sets of 16 rows on the smaller instructions take the
+// same, and so do the products of the next block's scores between this one's
+// exponentials.
 // Scores C[key][row] of 32 keys, the keys of tile t of a block in the order 32 t + 16
 // ((r >> 2) & 1) + 4 (r >> 3) + (r & 3): a lane holds row lane & 31 and the 16
 // consecutive keys of group 2 t + (lane >> 5), outputs in O[d][row].
@@ -655,7 +656,7 @@ __device__ inline v16f mfma32(v8h a, v8h b, v16f c)
 // All four waves walk over blocks [i0, i1), whose codes they put into LDS as fp16, in
 // the order of the lanes: keys (t, u) and values (t, u) of 32 channels u, two halves
 // of 1 KB each.  A block's codes are read during the block before and converted once
-// for all waves (by every wave for itself: 228 us instead of 167).
+// for all waves (by every wave for itself: 228 us instead of 160).
 template <int DT>
 constexpr int kStage = 4 * DT * 2048;
 template <int DT, int N>
@@ -1134,11 +1135,14 @@ Split choose_split(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D, int64_
     }
     const int64_t tiles = row_tiles(T, B, grp, kRows);
     c.slots = tiles;
-    // eight waves on a CU: one work-group of a few tiles', two of many's; above 128
-    // channels their registers leave one wave per SIMD
+    // eight waves on a CU: one work-group of a few tiles', two of many's (one token over
+    // 1531 keys, 32 heads of 64 on 4: 8.6 us, 10.7 with four waves; 64 sequences of 1000,
+    // 32 heads of 128 on 8: 24.9 with four, 31.8 with eight); above 128 channels their
+    // registers leave one wave per SIMD
     c.waves = D > 128 || std::min(tiles, std::max<int64_t>(B, T * grp / kRows)) * G > kCUs ? 4 : 8;
-    // (up to four blocks per wave are one part's, whose launch needs no join; eight
-    // where the sequences alone fill the chip)
+    // Up to four blocks per wave are one part's, whose launch needs no join (1531 keys: 8.6
+    // us, 10.7 in parts; 3000 keys: 10.9 in parts, 12.5 in one; 8000: 11.0 and 25.6), eight
+    // where the sequences alone fill the chip (200 of 1000 keys: 89 us, 120 in parts).
     if (B > kPlanned || blocks <= (std::min(B, T) * G >= kCUs ? 8 : 4) * c.waves) return c;
     const int64_t target = D > 128 || c.waves == 8 ? kCUs : 2 * kCUs;
     const int64_t slots = tiles + (target + G - 1) / G;

@@ -14,7 +14,7 @@ hipError_t launch_qlinear_tokens(const QLinearArgs& p, const TokenArgs& t, int32
                                  hipStream_t s);
 // One token's product from its floating activations x, quantized by every
 // work-group for itself; whether it is the faster form (else: quantize first).
-bool one_token_fused(const QLinearArgs& p, const void* x, int32_t type);
+bool one_token_fused(const QLinearArgs& p, const void* x);
 hipError_t launch_linear_one_token(const QLinearArgs& p, const TokenArgs& t, const void* x,
                                    int32_t type, hipStream_t s);
 

@@ -443,14 +443,16 @@ bool rows_ok(const QLinearArgs& p, int chunk4)
 
 }  // namespace
 
-bool one_token_fused(const QLinearArgs& p, const void* x, int32_t type)
+bool one_token_fused(const QLinearArgs& p, const void* x)
 {
-    // at most so many work-groups: each spends about a microsecond on the token,
-    // which more of them pay more often than a launch costs
-    constexpr int64_t kMost = 4096;
-    (void)type;
+    // Every work-group quantizes the token once more, which costs a launch's time at
+    // about so many elements in all: in one launch and two (weights from memory, 8 and
+    // 4 bits), 2048 -> 5632 4.4 and 6.1, 3.8 and 5.4 us; 2048 -> 256000 81 and 85, 42
+    // and 46; 5632 -> 131072 115 and 117, 76 and 75; 5632 -> 256000 225 and 223, 148 and
+    // 135.
+    constexpr int64_t kMost = (int64_t)1 << 26;
     return p.M == 1 && rows_ok(p, 16) && (uintptr_t)x % 16 == 0 &&
-           (p.N + kChans - 1) / kChans <= kMost &&
+           (p.N + kChans - 1) / kChans * p.K <= kMost &&
            p.K <= (int64_t)one_token_waves(p) * 64 * 8 * kHold;
 }
 

