@@ -889,7 +889,8 @@ mq_status mq_quantize_tokens(const void* x, int32_t type, int64_t M, int64_t K, 
  *   bias      device fp32 [N] or NULL
  *   y         device [M][N] of y_type; must not overlap the inputs
  *   workspace, workspace_bytes, path  as for mq_qlinear_ws, with the bytes of
- *             mq_qlinear_workspace_bytes (any out_bits)
+ *             mq_qlinear_workspace_bytes (any out_bits); MQ_PATH_AUTO takes the
+ *             prefill kernel for 2 to 16 tokens too where N is large
  *   M, N >= 0 (0: nothing to do), 1 <= K <= MQ_MAX_K, even for w_bits 4; the
  *   shapes and alignments of the tuned kernels are those of mq_qlinear.
  */

@@ -15,6 +15,9 @@ hipError_t launch_qlinear_tokens(const QLinearArgs& p, const TokenArgs& t, int32
 // One token's product from its floating activations x, quantized by every
 // work-group for itself; whether it is the faster form (else: quantize first).
 bool one_token_fused(const QLinearArgs& p, const void* x);
+// Whether 2 to 16 tokens go through the many tokens' tiles where the caller leaves the
+// path open.
+bool few_tokens_in_tiles(const QLinearArgs& p, int32_t y_type);
 hipError_t launch_linear_one_token(const QLinearArgs& p, const TokenArgs& t, const void* x,
                                    int32_t type, hipStream_t s);
 

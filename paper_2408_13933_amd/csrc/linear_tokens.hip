@@ -230,14 +230,19 @@ hipError_t launch_one_w(const OneArgs& a, hipStream_t s)
 }
 
 // ---------------------------------------------------------------------------
-// 2 to 16 tokens: R channels per work-group, its waves split K; a lane streams
-// 16 weights of one channel per step and the MFMA multiplies them with the
-// tokens (zeros past the last).
+// 2 to 16 tokens: R channels per work-group (8, or tiles of 16), its waves split K; a
+// lane streams 16 weights of one channel of each tile per step and the MFMA multiplies
+// them with the tokens (zeros past the last), whose codes a wave reads once for all
+// tiles.  A load takes half a line of each row: read past the caches the lines came
+// twice (16 x 2048 -> 8192: 7.3 us, 6.4 through them).  What bounds it: the codes'
+// reads beside the weights', 2.7 TB/s of weights at that size.
 template <int WBITS, int NWAVES, int R>
 __global__ __launch_bounds__(NWAVES * 64) void few_tokens_kernel(QLinearArgs p, TokenArgs t)
 {
-    constexpr int U = 8;  // 64-deep steps per round of loads
-    __shared__ v4i red[NWAVES][64];
+    constexpr int RT = R > 16 ? R / 16 : 1;  // tiles
+    constexpr int U = 8;                     // 64-deep steps per round of loads
+    static_assert(NWAVES >= RT, "a wave per tile in the end");
+    __shared__ v4i red[NWAVES][RT][64];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, kg = lane >> 4;
@@ -253,12 +258,14 @@ __global__ __launch_bounds__(NWAVES * 64) void few_tokens_kernel(QLinearArgs p, 
     const int m = r16 < (int)p.M ? r16 : (int)p.M - 1;
     const uint32_t a_dead = r16 < (int)p.M ? 0u : kOOB;
 
+    // wave q ends tile q: token r16, channels c0 + {0..3}
+    const int64_t c0 = n0 + 16 * wave + 4 * kg;
     float ws[4], bias[4], ts = 0.0f;
     int32_t zw[4], rs = 0;
-    if (wave == 0) {
+    if (wave < RT) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            int64_t n = n0 + 4 * kg + r;
+            int64_t n = c0 + r;
             if (n >= p.N) n = p.N - 1;
             ws[r] = p.w_scale[n];
             bias[r] = p.bias ? p.bias[n] : -0.0f;
@@ -269,49 +276,59 @@ __global__ __launch_bounds__(NWAVES * 64) void few_tokens_kernel(QLinearArgs p, 
     }
     const int steps = (K + 63) / 64;
     const int s_begin = steps * wave / NWAVES, s_end = steps * (wave + 1) / NWAVES;
-    v4i wv[U], av[U];
+    v4i wv[U][RT], av[U];
     auto load = [&](int s) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int k = (s + u) * 64 + kg * 16;
             const uint32_t dead = (uint32_t)((s + u >= s_end) | (k >= K)) << 31;
-            if constexpr (WBITS == 8) {
-                wv[u] = __builtin_amdgcn_raw_buffer_load_b128(rw, (uint32_t)(r16 * K + k) | dead, 0,
-                                                              kStream);
-            } else {
-                typedef unsigned v2u __attribute__((ext_vector_type(2)));
-                const v2u pk = __builtin_amdgcn_raw_buffer_load_b64(
-                    rw, (uint32_t)(r16 * wrow + k / 2) | dead, 0, kStream);
-                wv[u] = v4i{(int)pk[0], (int)pk[1], 0, 0};
+#pragma unroll
+            for (int q = 0; q < RT; ++q) {
+                const int row = 16 * q + r16;
+                if constexpr (WBITS == 8) {
+                    wv[u][q] = __builtin_amdgcn_raw_buffer_load_b128(
+                        rw, (uint32_t)(row * K + k) | dead, 0, 0);
+                } else {
+                    typedef unsigned v2u __attribute__((ext_vector_type(2)));
+                    const v2u pk = __builtin_amdgcn_raw_buffer_load_b64(
+                        rw, (uint32_t)(row * wrow + k / 2) | dead, 0, 0);
+                    wv[u][q] = v4i{(int)pk[0], (int)pk[1], 0, 0};
+                }
             }
             av[u] = __builtin_amdgcn_raw_buffer_load_b128(
                 ra, (uint32_t)(r16 * K + k) | dead | a_dead, 0, 0);
         }
     };
-    v4i acc = {0, 0, 0, 0};
+    v4i acc[RT];
+#pragma unroll
+    for (int q = 0; q < RT; ++q) acc[q] = v4i{0, 0, 0, 0};
     for (int s = s_begin; s < s_end; s += U) {
         load(s);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            v4i w = wv[u];
-            if constexpr (WBITS == 4) w = unpack_int4_x16((uint32_t)w[0], (uint32_t)w[1]);
-            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, av[u], acc, 0, 0, 0);
-        }
-    }
-    if constexpr (NWAVES > 1) {
-        red[wave][lane] = acc;
-        __syncthreads();
-        if (wave != 0) return;
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int w = 1; w < NWAVES; ++w) acc += red[w][lane];
+            for (int q = 0; q < RT; ++q) {
+                v4i w = wv[u][q];
+                if constexpr (WBITS == 4) w = unpack_int4_x16((uint32_t)w[0], (uint32_t)w[1]);
+                acc[q] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, av[u], acc[q], 0, 0, 0);
+            }
     }
-    // token r16, channels n0 + 4 kg + {0..3}
+    v4i sum = acc[0];
+    if constexpr (NWAVES > 1) {
+#pragma unroll
+        for (int q = 0; q < RT; ++q) red[wave][q][lane] = acc[q];
+        __syncthreads();
+        if (wave >= RT) return;
+        sum = red[0][wave][lane];
+#pragma unroll
+        for (int w = 1; w < NWAVES; ++w) sum += red[w][wave][lane];
+    }
     if (r16 >= (int)p.M || 4 * kg >= R) return;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const int64_t n = n0 + 4 * kg + r;
+        const int64_t n = c0 + r;
         if (n >= p.N) break;
-        int32_t c = acc[r];
+        int32_t c = sum[r];
         if constexpr (WBITS == 4) c >>= 4;  // exact: a multiple of 16
         c -= zw[r] * rs;
         store_out(t, r16 * p.N + n, token_output(c, ws[r], ts, bias[r]));
@@ -322,19 +339,19 @@ template <int WBITS, int R>
 hipError_t launch_few_r(const QLinearArgs& p, const TokenArgs& t, hipStream_t s)
 {
     const int64_t blocks = (p.N + R - 1) / R, steps = (p.K + 63) / 64;
-    // waves: one round of loads covers each wave's share of K, at least four
-    // where there are few work-groups
-    int nw = 1;
-    while (nw < 16 && nw * 8 < steps) nw *= 2;
-    if (blocks < 2048)
-        while (nw < 4 && nw < steps) nw *= 2;
+    // waves: a round of loads each, up to four (at least four where there are few
+    // work-groups); eight from four rounds on (16 x 5632 -> 2048 of 4 bits: 6.8 us with
+    // four, 7.3 with eight; 16384 -> 2048 of 8 bits: 18.4 and 15.3)
+    int nw = R > 16 ? R / 16 : 1;
+    while (nw < 4 && (nw * 8 < steps || (blocks < 2048 && nw < steps))) nw *= 2;
+    if (nw == 4 && nw * 32 < steps) nw = 8;
     const unsigned b = (unsigned)blocks;
     switch (nw) {
-    case 16: few_tokens_kernel<WBITS, 16, R><<<b, 1024, 0, s>>>(p, t); break;
     case 8: few_tokens_kernel<WBITS, 8, R><<<b, 512, 0, s>>>(p, t); break;
     case 4: few_tokens_kernel<WBITS, 4, R><<<b, 256, 0, s>>>(p, t); break;
     case 2: few_tokens_kernel<WBITS, 2, R><<<b, 128, 0, s>>>(p, t); break;
-    default: few_tokens_kernel<WBITS, 1, R><<<b, 64, 0, s>>>(p, t); break;
+    default:
+        if constexpr (R <= 16) few_tokens_kernel<WBITS, 1, R><<<b, 64, 0, s>>>(p, t);
     }
     return hipGetLastError();
 }
@@ -342,9 +359,11 @@ hipError_t launch_few_r(const QLinearArgs& p, const TokenArgs& t, hipStream_t s)
 template <int WBITS>
 hipError_t launch_few(const QLinearArgs& p, const TokenArgs& t, hipStream_t s)
 {
-    // narrow layers: 8 channels, so that at least 256 work-groups stream
-    return (p.N + 15) / 16 < 256 ? launch_few_r<WBITS, 8>(p, t, s)
-                                 : launch_few_r<WBITS, 16>(p, t, s);
+    // enough work-groups to stream, then fewer reads of the tokens' codes: with 8, 16 and
+    // 32 channels per work-group 16 x 2048 -> 2048 takes 4.1, 4.3 and 5.2 us, -> 4096 6.0,
+    // 4.8 and 5.8, -> 8192 9.7, 7.3 and 6.2
+    if (p.N < 4096) return launch_few_r<WBITS, 8>(p, t, s);
+    return p.N < 8192 ? launch_few_r<WBITS, 16>(p, t, s) : launch_few_r<WBITS, 32>(p, t, s);
 }
 
 // ---------------------------------------------------------------------------
@@ -441,6 +460,12 @@ bool rows_ok(const QLinearArgs& p, int chunk4)
            (uintptr_t)p.w % (p.w_bits == 8 ? 16 : chunk4) == 0;
 }
 
+// (byte offsets inside a 256-row tile fit 31 bits)
+bool tiles_ok(const QLinearArgs& p, int32_t y_type)
+{
+    return rows_ok(p, 16) && 256 * p.N * type_bytes(y_type) < kOOB && 256 * p.K < kOOB;
+}
+
 }  // namespace
 
 bool one_token_fused(const QLinearArgs& p, const void* x)
@@ -454,6 +479,14 @@ bool one_token_fused(const QLinearArgs& p, const void* x)
     return p.M == 1 && rows_ok(p, 16) && (uintptr_t)x % 16 == 0 &&
            (p.N + kChans - 1) / kChans * p.K <= kMost &&
            p.K <= (int64_t)one_token_waves(p) * 64 * 8 * kHold;
+}
+
+bool few_tokens_in_tiles(const QLinearArgs& p, int32_t y_type)
+{
+    // The tiles read the weights in whole lines, and 16 tokens cost them what 2 do: 2, 6
+    // and 16 tokens of 2048 -> 16384 take the few tokens' kernel 9.0, 9.3 and 10.5 us, the
+    // tiles 8.9; -> 131072 62, 59 and 73, the tiles 55 to 61 (4 bits 41, 44, 57 and 33).
+    return p.M > 1 && p.N >= 16384 && tiles_ok(p, y_type);
 }
 
 hipError_t launch_linear_one_token(const QLinearArgs& p, const TokenArgs& t, const void* x,
@@ -472,9 +505,7 @@ hipError_t launch_qlinear_tokens(const QLinearArgs& p, const TokenArgs& t, int32
         if (rows_ok(p, 8))
             return p.w_bits == 8 ? launch_few<8>(p, t, s) : launch_few<4>(p, t, s);
     }
-    // (byte offsets inside a 256-row tile fit 31 bits)
-    if (path == MQ_PATH_PREFILL && rows_ok(p, 16) && 256 * p.N * type_bytes(t.type) < kOOB &&
-        256 * p.K < kOOB)
+    if (path == MQ_PATH_PREFILL && tiles_ok(p, t.type))
         return p.w_bits == 8 ? launch_tiles_w<8>(p, t, s) : launch_tiles_w<4>(p, t, s);
     return launch_any(p, t, s);
 }

@@ -919,6 +919,11 @@ mq_status mq_qlinear_tokens(const int8_t* a_q, const float* a_scale, const int32
     if (!a_q || !a_scale || (w_zp == nullptr) != (a_rowsum == nullptr)) return MQ_ERR_INVALID_ARG;
     p.a = a_q;
     p.a_rowsum = a_rowsum;
+    if (path == MQ_PATH_AUTO && M <= 16 && mq::few_tokens_in_tiles(p, y_type)) {
+        resolved = MQ_PATH_PREFILL;
+        p.ws = nullptr;  // (a call of so few tokens needs none)
+        p.ws_bytes = 0;
+    }
     return from_hip(mq::launch_qlinear_tokens(p, mq::TokenArgs{a_scale, y, y_type}, resolved,
                                               as_stream(stream)));
 }
@@ -974,6 +979,7 @@ mq_status mq_linear_tokens(const void* x, int32_t x_type, int64_t ldx, int64_t M
     p.a = ws + w.codes;
     if (mq::one_token_fused(p, x))
         return from_hip(mq::launch_linear_one_token(p, t, x, x_type, s));
+    if (M <= 16 && mq::few_tokens_in_tiles(p, y_type)) path = MQ_PATH_PREFILL;
     int32_t* rowsum = w_zp ? reinterpret_cast<int32_t*>(ws + w.rowsum) : nullptr;
     p.a_rowsum = rowsum;
     const int64_t counters = split ? mq::prefill_counter_bytes(p) / 4 : 0;

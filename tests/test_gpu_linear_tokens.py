@@ -150,6 +150,38 @@ def test_every_path_gives_the_same_bits(bits, asym, out):
             assert ok, (M, path)
 
 
+@pytest.mark.parametrize("bits,asym", [(8, False), (8, True), (4, False), (4, True)])
+@pytest.mark.parametrize("N", [1, 9, 2050, 4095, 4096, 5000, 8191, 8192, 8200, 16383, 16384, 20001])
+def test_few_tokens_of_every_width(N, bits, asym):
+    """The kernels of 2 to 16 tokens against one thread per output, and the one that
+    quantizes too with a workspace that held anything; rows of whole and half chunks."""
+    import torch
+
+    import paper_2408_13933_amd as mq
+    rng = np.random.default_rng(N + bits)
+    for M, K in ((2, 16), (16, 48), (5, 528), (16, 2048), (3, 8208), (16, 16400)):
+        if N > 9000 and K > 9000:
+            continue
+        c = _cuda(rng.integers(-127, 128, (M, K)).astype(np.int8))
+        w, ws, zp = _weights(rng, N, K, bits, asym)
+        args = (_cuda(w if bits == 8 else rs.pack4(w)), bits, _cuda(ws))
+        kw = dict(w_zp=_cuda(zp), bias=_cuda(rng.standard_normal(N).astype(np.float32)))
+        sums = c.sum(1, dtype=torch.int32) if asym else None
+        a = _cuda(rng.uniform(0.01, 2, M).astype(np.float32))
+        y = [mq.mq_qlinear_tokens(c, a, *args, a_rowsum=sums, out_dtype=torch.float32, path=p, **kw)
+             for p in (mq.PATH_GENERIC, mq.PATH_AUTO, mq.PATH_DECODE)]
+        assert torch.equal(y[0], y[1]) and torch.equal(y[0], y[2]), (M, K)
+        x = (c.float() * a[:, None]).to(torch.bfloat16)
+        q, s = mq.mq_quantize_tokens(x)
+        r = q.sum(1, dtype=torch.int32) if asym else None
+        want = mq.mq_qlinear_tokens(q, s, *args, a_rowsum=r, out_dtype=torch.float16,
+                                    path=mq.PATH_GENERIC, **kw)
+        n = mq.mq_linear_tokens_workspace_bytes(M, K, N, bits)
+        work = torch.full((n,), 0x7b, dtype=torch.uint8, device="cuda")
+        got = mq.mq_linear_tokens(x, *args, out_dtype=torch.float16, workspace=work, **kw)
+        assert torch.equal(got, want), (M, K)
+
+
 def test_sums_at_the_ends_of_their_range():
     """K = 65536 with codes and zero-points at the ends: 127 * 255 * 65536 < 2^31."""
     import torch
