@@ -903,7 +903,7 @@ mq_status mq_qlinear_tokens(const int8_t* a_q, const float* a_scale, const int32
 /*
  * mq_linear_tokens -- mq_quantize_tokens and mq_qlinear_tokens of its result
  * in one call, bit for bit: a linear layer from floating activations to
- * floating outputs.  One token over few channels takes one launch.
+ * floating outputs.  One token takes one launch at most sizes.
  *   x          device, of x_type, row m at x + m * ldx; 0 <= M < 2^24
  *   workspace  device, 256-byte aligned, any contents, overwritten (codes,
  *              scales, row sums, the K split's parts); at least the bytes of
@@ -1053,12 +1053,13 @@ typedef struct mq_logit_rules {
  *   x = (x - frequency[m] * n) - presence[m]            where n > 0
  * then, for a word with a bias, x = x + bias; a word that the mask forbids
  * becomes -infinity.  Each step is rounded once in fp32, the result once to x's
- * type.  Other words are not touched, nor read.
+ * type.  Other words keep their bits (up to eight that lie together are read and
+ * written at once).
  *   x      device, of `type` (fp32 for mq_sample), row m at x + m * ld
  *   rules  host struct
  *   0 <= M < 2^31; 1 <= V <= MQ_SAMPLE_MAX_V; V <= ld < 2^40; cols >= 0,
  *   cols <= ldh < 2^40; ceil(V / 32) <= ldm < 2^40; 0 <= bias_n < 2^31.  A call
- *   that takes 2^23 work-groups or more, M * ceil(V / 4096), is
+ *   that takes 2^23 work-groups or more, at most M * ceil(V / 4096), is
  *   MQ_ERR_UNSUPPORTED.
  */
 mq_status mq_adjust_logits(void* x, int32_t type, int64_t M, int64_t V, int64_t ld,

@@ -112,10 +112,11 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs p, int32_t 
     const float rep = p.repetition ? p.repetition[m] : 1.0f;
     const float pres = p.presence ? p.presence[m] : 0.0f;
     const float freq = p.frequency ? p.frequency[m] : 0.0f;
-    int32_t b0 = 0, b1 = 0;
+    // (unsigned: what threads add to them stays below 2^32)
+    uint32_t b0 = 0, b1 = 0;
     if (p.bias_starts) {
-        b0 = max(p.bias_starts[m], 0);
-        b1 = (int32_t)min((int64_t)p.bias_starts[m + 1], p.bias_n);
+        b1 = (uint32_t)min((int64_t)max(p.bias_starts[m + 1], 0), p.bias_n);
+        b0 = min((uint32_t)max(p.bias_starts[m], 0), b1);
     }
     // the mask's bits of this thread's words (words past the row: allowed)
     constexpr uint32_t kAll = (1u << kEach) - 1;
@@ -136,21 +137,21 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs p, int32_t 
             if constexpr (!PACKED) reinterpret_cast<uint4*>(st.own)[i * kThreads + tid] = zero;
         }
         __syncthreads();
-        for (int32_t i = b0 + tid; i < b1; i += kThreads) {
+        for (uint32_t i = b0 + tid; i < b1; i += kThreads) {
             if (i != b0 + tid) word = p.bias_tokens[i];
             const uint32_t at = (uint32_t)word - (uint32_t)w0;
             // of equal words the last one
-            if (at < (uint32_t)words) atomicMax(&st.entry()[at], ((uint32_t)i + 1) << S::kEntry);
+            if (at < (uint32_t)words) atomicMax(&st.entry()[at], (i + 1) << S::kEntry);
         }
         if (PACKED && b0 < b1) __syncthreads();  // (the maxima are of entries alone)
         if (penal) {
-            auto add = [&](int32_t i, int32_t word) {
+            auto add = [&](uint32_t i, int32_t word) {
                 const uint32_t at = (uint32_t)word - (uint32_t)w0;
-                if (i >= n || at >= (uint32_t)words) return;
-                if (i < prompt) atomicOr(&st.count[at], S::kPrompt);
+                if (i >= (uint32_t)n || at >= (uint32_t)words) return;
+                if ((int32_t)i < prompt) atomicOr(&st.count[at], S::kPrompt);
                 else atomicAdd(&st.count[at], 1u);
             };
-            auto add_four = [&](int32_t i, const int4& v) {
+            auto add_four = [&](uint32_t i, const int4& v) {
                 add(i, v.x);
                 add(i + 1, v.y);
                 add(i + 2, v.z);
@@ -158,10 +159,10 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs p, int32_t 
             };
             if (vec_h) {
                 add_four(tid * 4, ahead);
-                for (int32_t i = (kThreads + tid) * 4; i < n; i += kThreads * 4)
+                for (uint32_t i = (kThreads + tid) * 4; i < (uint32_t)n; i += kThreads * 4)
                     add_four(i, *reinterpret_cast<const int4*>(h + i));  // (whole fours of a row)
             } else {
-                for (int32_t i = tid; i < n; i += kThreads) add(i, h[i]);
+                for (uint32_t i = tid; i < (uint32_t)n; i += kThreads) add(i, h[i]);
             }
         }
         __syncthreads();

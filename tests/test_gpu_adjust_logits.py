@@ -124,6 +124,14 @@ def test_bias_starts_out_of_range():
     _check(x, d, 100)
 
 
+@pytest.mark.parametrize("starts", [(2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, 0, 9),
+                                    (-2 ** 31, -2 ** 31, 2 ** 31 - 1, -1, 2 ** 31 - 1)])
+def test_bias_starts_at_the_ends_of_their_range(starts):
+    x, d = _inputs(np.random.default_rng(7), 4, 100, 50, 10, False, "float32")
+    d["bias"] = (np.array(starts, np.int64).astype(np.int32),) + d["bias"][1:]
+    _check(x, d, 100)
+
+
 @pytest.mark.parametrize("type", TYPES)
 def test_largest_vocabulary_and_row_offsets(type):
     """2^22 words; rows that begin past 2^32 elements."""
