@@ -21,7 +21,6 @@
 // outputs to the sum of two; statistics and outputs are fp32.
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 
 #include "kvblocks.h"
 #include "kvwalk.h"
@@ -169,27 +168,80 @@ struct Scaled {
         a = p.tau * __builtin_bit_cast(float, (e - 14u) << 23);
     }
 };
-// N == 2: fp32 queries.
+// Eight consecutive queries as they lie in memory (N == 2: fp32, else 16 bits).  One
+// form for both types of 16 bits, which are told apart when they become numbers: a load
+// and a conversion per type made three quarters of a kernel of 160 KB.
+typedef unsigned short v2us __attribute__((ext_vector_type(2)));
 template <int N>
-__device__ inline void load8_any(const AttnArgs& p, int64_t i, float* x)
-{
-    auto load = [&](auto type) {
-        constexpr int TYPE = decltype(type)::value;
-        constexpr int E = TYPE == MQ_F32 ? 4 : 2;
+struct Eight {
+    uint32_t d[4 * N];
+    __device__ void load(const AttnArgs& p, int64_t i)
+    {
         if (p.vec_q) {
-            Raw<TYPE, 8> r;
-            r.load(static_cast<const int8_t*>(p.q) + i * E);
+            const uint4* x = reinterpret_cast<const uint4*>(static_cast<const int8_t*>(p.q) +
+                                                            i * (2 * N));
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = r[j];
+            for (int j = 0; j < N; ++j) {
+                const uint4 v = x[j];
+                d[4 * j] = v.x, d[4 * j + 1] = v.y, d[4 * j + 2] = v.z, d[4 * j + 3] = v.w;
+            }
+        } else if constexpr (N == 2) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) d[j] = static_cast<const uint32_t*>(p.q)[i + j];
         } else {
+            const uint16_t* x = static_cast<const uint16_t*>(p.q) + i;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = load_elem<TYPE>(p.q, i + j);
+            for (int j = 0; j < 4; ++j) d[j] = x[2 * j] | (uint32_t)x[2 * j + 1] << 16;
         }
-    };
-    if constexpr (N == 2) load(std::integral_constant<int, MQ_F32>{});
-    else if (p.type == MQ_BF16) load(std::integral_constant<int, MQ_BF16>{});
-    else load(std::integral_constant<int, MQ_F16>{});
-}
+    }
+    __device__ void keep(bool have)
+    {
+#pragma unroll
+        for (int j = 0; j < 4 * N; ++j) d[j] = have ? d[j] : 0;
+    }
+    // Magnitudes as bits, NaN and infinities the largest: of two numbers of 16 bits in one.
+    __device__ uint32_t most(uint32_t m) const
+    {
+#pragma unroll
+        for (int j = 0; j < 4 * N; ++j) {
+            if constexpr (N == 2)
+                m = max(m, d[j] & 0x7fffffffu);
+            else
+                m = __builtin_bit_cast(
+                    uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2us, m),
+                                                        __builtin_bit_cast(v2us, d[j] & 0x7fff7fffu)));
+        }
+        return m;
+    }
+    // Bits of the fp32 number of what `most` found.
+    static __device__ uint32_t bits(const AttnArgs& p, uint32_t m)
+    {
+        if constexpr (N == 2) return m;
+        m = max(m & 0xffffu, m >> 16);
+        return p.type == MQ_BF16 ? m << 16
+                                 : __builtin_bit_cast(
+                                       uint32_t, (float)__builtin_bit_cast(_Float16, (uint16_t)m));
+    }
+    // Times `up`, as N fp16 terms.
+    __device__ void terms(const AttnArgs& p, float up, v8h& a, v8h* b) const
+    {
+        auto put = [&](auto number) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float v = number(j) * up;
+                const _Float16 h = (_Float16)v;
+                a[j] = h;
+                if constexpr (N == 2) (*b)[j] = (_Float16)(v - (float)h);
+            }
+        };
+        if constexpr (N == 2)
+            put([&](int j) { return __builtin_bit_cast(float, d[j]); });
+        else if (p.type == MQ_BF16)
+            put([&](int j) { return half_of<MQ_BF16>(d[j >> 1], j & 1); });
+        else
+            put([&](int j) { return half_of<MQ_F16>(d[j >> 1], j & 1); });
+    }
+};
 
 // The first channel of a lane's eight of operand (s, h) of a set's products.
 template <int ND>
@@ -214,23 +266,20 @@ template <int KS, int ND, int N>
 __device__ inline void load_queries(const AttnArgs& p, const RowAt& row, Rows<KS, ND, N>& st)
 {
     const int64_t at = row.t * p.ldq + (int64_t)row.head * p.kv.D;
-    float x[KS][2][8];
-    uint32_t most = 0;  // as bits: NaN and infinities are the largest
+    Eight<N> x[KS][2];
+    uint32_t most = 0;
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int h = 0; h < halves<ND>(s); ++h) {
             const int d = operand_channel<ND>(s, h);
             const bool have = row.have && d < p.kv.D;
-            load8_any<N>(p, at + (have ? d : 0), x[s][h]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                x[s][h][j] = have ? x[s][h][j] : 0.0f;
-                most = max(most, abs_bits(x[s][h][j]));
-            }
+            x[s][h].load(p, at + (have ? d : 0));
+            x[s][h].keep(have);
+            most = x[s][h].most(most);
         }
     uint32_t o;
-    most = swap16(most, o);
+    most = swap16(Eight<N>::bits(p, most), o);
     most = max(most, o);
     most = swap32(most, o);
     most = max(most, o);
@@ -240,52 +289,42 @@ __device__ inline void load_queries(const AttnArgs& p, const RowAt& row, Rows<KS
     for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int h = 0; h < halves<ND>(s); ++h)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float v = x[s][h][j] * sc.up;
-                const _Float16 f = (_Float16)v;
-                st.q[0][s][h][j] = f;
-                if constexpr (N == 2) st.q[1][s][h][j] = (_Float16)(v - (float)f);
-            }
+            x[s][h].terms(p, sc.up, st.q[0][s][h], &st.q[N - 1][s][h]);
 }
-// The same for 32 rows: channels 32 u + 16 (lane >> 5) on; in two passes over the row,
+// The same for 32 rows: channels 32 u + 16 (lane >> 5) on; in two passes over fp32 rows,
 // whose channels do not all fit beside the rest.
 template <int DT, int N>
 __device__ inline float load_queries32(const AttnArgs& p, const RowAt& row, v8h (&q)[N][DT][2])
 {
     const int hh = (threadIdx.x & 63) >> 5;
     const int64_t at = row.t * p.ldq + (int64_t)row.head * p.kv.D;
+    Eight<N> x[N == 2 ? 1 : DT][2];
     uint32_t most = 0;
-    auto chunk = [&](int u, float (&x)[16]) {
+    auto read = [&](int u, Eight<N> (&e)[2]) {
         const int d = 32 * u + 16 * hh;
         const bool have = row.have && d < p.kv.D;
-        load8_any<N>(p, at + (have ? d : 0), x);
-        load8_any<N>(p, at + (have ? d : 0) + 8, x + 8);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) x[j] = have ? x[j] : 0.0f;
+        for (int h = 0; h < 2; ++h) {
+            e[h].load(p, at + (have ? d : 0) + 8 * h);
+            e[h].keep(have);
+        }
     };
 #pragma unroll
     for (int u = 0; u < DT; ++u) {
-        float x[16];
-        chunk(u, x);
+        read(u, x[N == 2 ? 0 : u]);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) most = max(most, abs_bits(x[j]));
+        for (int h = 0; h < 2; ++h) most = x[N == 2 ? 0 : u][h].most(most);
     }
     uint32_t o;
-    most = swap32(most, o);
+    most = swap32(Eight<N>::bits(p, most), o);
     most = max(most, o);
     const Scaled sc(p, most);
 #pragma unroll
     for (int u = 0; u < DT; ++u) {
-        float x[16];
-        chunk(u, x);
+        if constexpr (N == 2) read(u, x[0]);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const float v = x[j] * sc.up;
-            const _Float16 h = (_Float16)v;
-            q[0][u][j >> 3][j & 7] = h;
-            if constexpr (N == 2) q[1][u][j >> 3][j & 7] = (_Float16)(v - (float)h);
-        }
+        for (int h = 0; h < 2; ++h)
+            x[N == 2 ? 0 : u][h].terms(p, sc.up, q[0][u][h], &q[N - 1][u][h]);
     }
     return sc.a;
 }
@@ -1009,11 +1048,13 @@ __global__ __launch_bounds__(256, KS <= (N == 2 ? 1 : 2) ? 2 : 1) void attn_bloc
     }
 }
 
-// Joins the planned parts of a row and head, a work-group per 64 channels: 16 lanes
-// have four channels each of four parts at once, the four waves take turns; up to
-// 128 parts' reads are under way together.
+// Joins the parts of a row and head (PLAN: make_plan's, else the splits of tiles), a
+// work-group per 64 channels: 16 lanes have four channels each of four parts at once,
+// the four waves take turns; up to 128 parts' reads are under way together.
+template <bool PLAN>
 __global__ __launch_bounds__(256) void attn_blocks_join_kernel(AttnArgs p, int plan_waves)
 {
+    constexpr int kStep = PLAN ? kRows : 1;  // rows from a part's to the next one's
     __shared__ float f[kMaxParts];
     __shared__ __attribute__((aligned(16))) v4f sums[4][64];
     const int lane = threadIdx.x & 63;
@@ -1021,18 +1062,26 @@ __global__ __launch_bounds__(256) void attn_blocks_join_kernel(AttnArgs p, int p
     const int64_t t = blockIdx.x / p.H;
     const int32_t head = (int32_t)(blockIdx.x - t * p.H), D = p.kv.D;
     const int32_t g0 = head / p.grp, h = head - g0 * p.grp;
-    const Plan w = make_plan(p, plan_waves, 0, t, h);
-    if (w.b < 0 || w.parts <= 1) return;  // rows of no sequence, or done
-    const int32_t parts = w.parts, r = (int32_t)(((t - w.s0) * p.grp + h) & (kRows - 1));
-    const int64_t at = ((int64_t)g0 * p.slots + w.first) * kRows + r;
+    int32_t parts;
+    int64_t at;
+    if constexpr (PLAN) {
+        const Plan w = make_plan(p, plan_waves, 0, t, h);
+        if (w.b < 0 || w.parts <= 1) return;  // rows of no sequence, or done
+        parts = w.parts;
+        at = ((int64_t)g0 * p.slots + w.first) * kRows + (((t - w.s0) * p.grp + h) & (kRows - 1));
+    } else {
+        if (t < p.kv.starts[0] || t >= p.kv.starts[p.kv.B]) return;
+        parts = p.splits;
+        at = (t * p.H + head) * parts;
+    }
     const float* ml = p.ml + 2 * at;
     constexpr int kRegs = kMaxParts / 64;
     float m[kRegs], l[kRegs], most = kNone;
 #pragma unroll
     for (int i = 0; i < kRegs; ++i) {
         const int s = lane + 64 * i;
-        m[i] = s < parts ? ml[2 * kRows * s] : kNone;
-        l[i] = s < parts ? ml[2 * kRows * s + 1] : 0.0f;
+        m[i] = s < parts ? ml[2 * kStep * s] : kNone;
+        l[i] = s < parts ? ml[2 * kStep * s + 1] : 0.0f;
     }
     const int32_t which = 4 * wave + (lane >> 4), d = 64 * (int32_t)blockIdx.y + 4 * (lane & 15);
     const float* x = p.sums + at * D + min(d, D - 4);
@@ -1042,7 +1091,7 @@ __global__ __launch_bounds__(256) void attn_blocks_join_kernel(AttnArgs p, int p
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int32_t s = min(s0 + 16 * u + which, parts - 1);
-            v[u] = *reinterpret_cast<const v4f*>(x + (int64_t)s * kRows * D);
+            v[u] = *reinterpret_cast<const v4f*>(x + (int64_t)s * kStep * D);
         }
     };
     load(0);
@@ -1125,8 +1174,12 @@ Split choose_split(int64_t T, int64_t B, int32_t H, int32_t G, int32_t D, int64_
     ws_bytes = std::min<int64_t>(ws_bytes, MQ_ATTN_MAX_WORKSPACE);
     if (tiled(T, B, grp)) {
         // at least a block per wave in each
-        const int64_t groups = std::max(T * grp / kTile, std::min(B, T)) * G;
-        int64_t s = (D > 128 ? kCUs : 2 * kCUs) / std::max<int64_t>(groups, 1);
+        // (tiles as of sequences with as many rows each; work-groups of one round: 240 rows
+        // of two sequences over 15000 keys of 256 channels in 272 work-groups 119 us, in 256
+        // 72)
+        const int64_t seqs = std::min(B, T);
+        const int64_t groups = seqs * ((T * grp + seqs * kTile - 1) / (seqs * kTile)) * G;
+        int64_t s = (D > 128 ? kCUs : 2 * kCUs) / groups;
         s = std::min(s, (blocks + kWaves - 1) / kWaves);
         s = std::min<int64_t>(s, ws_bytes / (T * H * row));
         c.splits = std::max<int64_t>(1, std::min<int64_t>(s, kMaxParts));
@@ -1252,9 +1305,13 @@ hipError_t launch_attn_blocks(const BlockCache& c, const void* q, int64_t ldq, i
     if (err != hipSuccess || split.bytes == 0) return err;
     // (T * H is far below the number of work-groups of a launch: two parts of every row
     // fit the workspace)
+    const dim3 grid((unsigned)(T * H), (unsigned)((c.kv.D + 63) / 64));
     if (split.target > 0) {
-        const dim3 grid((unsigned)(T * H), (unsigned)((c.kv.D + 63) / 64));
-        attn_blocks_join_kernel<<<grid, 256, 0, s>>>(p, split.waves);
+        attn_blocks_join_kernel<true><<<grid, 256, 0, s>>>(p, split.waves);
+    } else if (T * H * (c.kv.D / 4) <= kCUs * 256) {
+        // (a lane's splits in turn where the rows fill the chip: 128 rows of 64 splits of 256
+        // channels 4.7 us, 25 in turn; 1920 of 16 splits 10.8 in turn, 17.6)
+        attn_blocks_join_kernel<false><<<grid, 256, 0, s>>>(p, 0);
     } else {
         const int64_t n = (T * H * (c.kv.D / 4) + 255) / 256;
         attn_blocks_join_tiles_kernel<<<(unsigned)n, 256, 0, s>>>(p);
