@@ -459,27 +459,44 @@ __device__ inline float value_scale(float vs) { return fmaxf(vs, 0x1p-67f); }
 // 1 / l; 0 for a row that sees nothing.
 __device__ inline float out_unit(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 
-__device__ inline void store_one(const AttnArgs& p, int64_t t, int32_t head, int32_t d, float v)
+// Element of a row's first output, and four outputs from channel d on (N == 2: fp32).
+__device__ inline int64_t out_at(const AttnArgs& p, int64_t t, int32_t head)
 {
-    const int64_t at = t * p.ldy + (int64_t)head * p.kv.D + d;
-    if (p.type == MQ_F32) store_elem<MQ_F32>(p.y, at, v);
-    else if (p.type == MQ_BF16) store_elem<MQ_BF16>(p.y, at, v);
-    else store_elem<MQ_F16>(p.y, at, v);
+    return t * p.ldy + (int64_t)head * p.kv.D;
 }
-__device__ inline void store_four(const AttnArgs& p, int64_t t, int32_t head, int32_t d, v4f v)
+template <int N>
+__device__ inline void store_four(const AttnArgs& p, int64_t row, int32_t d, v4f v)
 {
-    const int64_t at = t * p.ldy + (int64_t)head * p.kv.D + d;
-    if (!p.vec_y) {
+    if constexpr (N == 2) {
+        float* y = static_cast<float*>(p.y) + row + d;
+        if (p.vec_y) {
+            *reinterpret_cast<v4f*>(y) = v;
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) store_one(p, t, head, d + i, v[i]);
-    } else if (p.type == MQ_F32) {
-        *reinterpret_cast<v4f*>(static_cast<float*>(p.y) + at) = v;
+            for (int i = 0; i < 4; ++i) y[i] = v[i];
+        }
     } else {
-        const uint2 h = p.type == MQ_BF16
-                            ? make_uint2(pack2<MQ_BF16>(v[0], v[1]), pack2<MQ_BF16>(v[2], v[3]))
-                            : make_uint2(pack2<MQ_F16>(v[0], v[1]), pack2<MQ_F16>(v[2], v[3]));
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.y) + at) = h;
+        uint16_t* y = static_cast<uint16_t*>(p.y) + row + d;
+        uint32_t h[2];
+        if (p.type == MQ_BF16) {
+            h[0] = pack2<MQ_BF16>(v[0], v[1]);
+            h[1] = pack2<MQ_BF16>(v[2], v[3]);
+        } else {
+            h[0] = pack2<MQ_F16>(v[0], v[1]);
+            h[1] = pack2<MQ_F16>(v[2], v[3]);
+        }
+        if (p.vec_y) {
+            *reinterpret_cast<uint2*>(y) = make_uint2(h[0], h[1]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = (uint16_t)(h[i >> 1] >> (16 * (i & 1)));
+        }
     }
+}
+__device__ inline void store_four(const AttnArgs& p, int64_t row, int32_t d, v4f v)
+{
+    if (p.type == MQ_F32) store_four<2>(p, row, d, v);
+    else store_four<1>(p, row, d, v);
 }
 
 // Where a part's state goes: sums + at D and ml + 2 at, row r's 16 rows on; or,
@@ -651,6 +668,7 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
         p.ml[2 * part.at + 1] = sum;
     }
     const float unit = out_unit(sum);
+    const int64_t out = out_at(p, row.t, row.head);
 #pragma unroll
     for (int i = 0; i < (ND + W - 1) / W; ++i) {
         const int dt = W * i + wave;
@@ -664,7 +682,7 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
             for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(f[w], x[e], v[e]);
         }
         if (!part.only) *reinterpret_cast<v4f*>(p.sums + part.at * p.kv.D + d) = v;
-        else store_four(p, row.t, row.head, d, v * unit);
+        else store_four<N>(p, out, d, v * unit);
     }
 }
 
@@ -884,6 +902,7 @@ __device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g
         p.ml[2 * part + 1] = l;
     }
     const float unit = out_unit(l);
+    const int64_t out = out_at(p, row.t, row.head);
 #pragma unroll
     for (int u = 0; u < DT; ++u)
 #pragma unroll
@@ -892,7 +911,7 @@ __device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g
             if (d >= p.kv.D) break;
             const v4f v = {acc[u][4 * x], acc[u][4 * x + 1], acc[u][4 * x + 2], acc[u][4 * x + 3]};
             if (p.splits > 1) *reinterpret_cast<v4f*>(p.sums + part * p.kv.D + d) = v;
-            else store_four(p, row.t, row.head, d, v * unit);
+            else store_four<N>(p, out, d, v * unit);
         }
 }
 
@@ -1127,7 +1146,7 @@ __global__ __launch_bounds__(256) void attn_blocks_join_kernel(AttnArgs p, int p
     acc = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc += sums[i >> 2][16 * (i & 3) + lane];
-    store_four(p, t, head, d, acc * out_unit(sum));
+    store_four(p, out_at(p, t, head), d, acc * out_unit(sum));
 }
 
 // Joins the splits of tiles, a lane per four channels of a row and head.
@@ -1150,7 +1169,7 @@ __global__ __launch_bounds__(256) void attn_blocks_join_tiles_kernel(AttnArgs p)
 #pragma unroll
         for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(f, v[c], acc[c]);
     }
-    store_four(p, t, (int32_t)(row - t * p.H), d, acc * out_unit(l));
+    store_four(p, out_at(p, t, (int32_t)(row - t * p.H)), d, acc * out_unit(l));
 }
 
 // Whether the sequences have more rows than a set, on average.
