@@ -163,6 +163,17 @@ def test_many_sequences(B, H, G, D, type):
     _check(rng, H, G, D, 16, 16, list(new), list(lens), type)
 
 
+@pytest.mark.parametrize("B", [65, 300])
+@pytest.mark.parametrize("type", ["float32", "float16"])
+def test_many_prompts(B, type):
+    """Tiles of many sequences, with none to forty new tokens each."""
+    rng = np.random.default_rng(B)
+    new = rng.integers(0, 41, B)
+    lens = new + rng.integers(0, 150, B)
+    _check(rng, 2, 1, 32, 16, 16, list(new), list(lens), type)
+    _check(rng, 2, 1, 32, 16, 16, list(new), list(lens), type, window=30, sinks=2)
+
+
 def test_sharp_and_flat_logits():
     for spread in (0.0, 1e-20, 30.0, 200.0):
         _check(np.random.default_rng(3), 4, 2, 64, 32, 16, [1, 20], [900, 300], "float32",
