@@ -49,7 +49,7 @@ constexpr int kMaxParts = 512;
 constexpr int kPlanRegs = 4, kPlanned = 64 * kPlanRegs;
 constexpr float kNone = -1e30f;           // running maximum of a row that has seen nothing
 constexpr float kTop = 8.0f, kLag = 7.0f; // weights up to 2^(kTop + kLag)
-constexpr float kHuge = 0x1p21f;          // maxima from here on round by more than that leaves
+constexpr float kHuge = 0x1p21f;          // maxima from here on: far_exponent
 using Tile = RowTile<kBlk>;
 
 struct AttnArgs {
@@ -412,11 +412,15 @@ struct Weigh {
     }
 };
 
-// Exponent of a weight, where a maximum's rounding could push it past fp16 (NaN stays).
-__device__ inline float limited(const Weigh& f, float score)
+// Exponent of a weight in a wave with rows whose maximum's last place is as large as a
+// weight's range.  Theirs comes from the very number that the maximum was taken over, so
+// that the largest weight is 2^kTop up to 2^(kTop + kLag) there too.  (By f.b the two differ
+// by half a last place of the maximum, which from 2^29 on left fp16 nothing of any weight.)
+// The other rows keep their bits.
+__device__ inline float far_exponent(const Weigh& f, float score, float m)
 {
-    const float x = __builtin_fmaf(score, f.a, f.b);
-    return x > kTop + kLag ? kTop + kLag : x;
+    return fabsf(m) >= kHuge ? (__builtin_fmaf(score, f.a, f.lv) - m) + kTop
+                             : __builtin_fmaf(score, f.a, f.b);
 }
 
 // Scores of 16 consecutive keys from `first` on that the row does not see (or that
@@ -604,7 +608,7 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
             for (int x = 1; x < 16; ++x) m = fmaxf(m, c[x >> 2][x & 3]);
             Weigh f;
             m = row_max(f.top(st.a, ks, value_scale(vs), m));
-            if (__ballot(m > st.m + kLag) != 0) {
+            if (__ballot(m - st.m > kLag) != 0) {  // (the sum could round up)
                 m = fmaxf(m, st.m);
                 const float down = exp2_fast(st.m - m);
                 st.l *= down;
@@ -615,7 +619,8 @@ __device__ inline void split_rows(const AttnArgs& p, const Tile& tile, int32_t g
             f.b = f.lv + (kTop - st.m);
             if (__ballot(fabsf(st.m) >= kHuge) != 0) {
 #pragma unroll
-                for (int x = 0; x < 16; ++x) c[x >> 2][x & 3] = limited(f, c[x >> 2][x & 3]);
+                for (int x = 0; x < 16; ++x)
+                    c[x >> 2][x & 3] = far_exponent(f, c[x >> 2][x & 3], st.m);
                 f.a = 1.0f;
                 f.b = 0.0f;
             }
@@ -850,7 +855,7 @@ __device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g
             uint32_t o;
             const uint32_t own = swap32(__builtin_bit_cast(uint32_t, most), o);
             most = fmaxf(__builtin_bit_cast(float, own), __builtin_bit_cast(float, o));
-            if (__ballot(most > m + kLag) != 0) {
+            if (__ballot(most - m > kLag) != 0) {  // (the sum could round up)
                 most = fmaxf(most, m);
                 const float down = exp2_fast(m - most);
                 l *= down;
@@ -864,7 +869,7 @@ __device__ inline void share_keys(const AttnArgs& p, const Tile& tile, int32_t g
                 f[j].b = f[j].lv + (kTop - m);
                 if (__ballot(fabsf(m) >= kHuge) != 0) {
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) c[j][x] = limited(f[j], c[j][x]);
+                    for (int x = 0; x < 16; ++x) c[j][x] = far_exponent(f[j], c[j][x], m);
                     f[j].a = 1.0f;
                     f[j].b = 0.0f;
                 }

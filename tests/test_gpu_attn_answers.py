@@ -1,0 +1,35 @@
+"""Attention over the cache with block scales: answers that are known without a softmax
+where logits are huge."""
+import numpy as np
+import pytest
+
+from tests import attn_answers as aa
+from tests import runtime_scales as rs
+
+pytestmark = pytest.mark.gpu
+
+TYPES = ["float32", "bfloat16", "float16"]
+
+
+def _run(q, cache, batch, scale, type):
+    import torch
+
+    import paper_2408_13933_amd as mq
+    kc, ks, vc, vs = cache
+    g = [torch.from_numpy(np.ascontiguousarray(a)).cuda() for a in (kc, ks, rs.v_layout(vc), vs)]
+    i = [torch.from_numpy(np.ascontiguousarray(a)).cuda() for a in batch]
+    x = torch.from_numpy(q).to(getattr(torch, type)).cuda()
+    return mq.mq_paged_attn_blocks(x, *g, *i, scale).float().cpu().numpy()
+
+
+# (a winner's logit is 127 * 2^exponent; from 2^21 on it has a place of its own in the
+# kernels, from 2^29 on its last place in fp32 is more than a weight's range in fp16)
+@pytest.mark.parametrize("exponent", [15, 23, 33, 110])
+@pytest.mark.parametrize("type", TYPES)
+@pytest.mark.parametrize("D", [32, 96, 256])
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("keys", [1, 2])
+def test_winners_of_huge_logits(keys, new, D, type, exponent):
+    k = aa.Known(D + new + exponent, D, new, exponent, keys)
+    off = k.off(_run(k.q, k.cache, k.batch, k.scale, type), type)
+    assert not off.any(), (off.mean(), np.argwhere(off)[:3])
