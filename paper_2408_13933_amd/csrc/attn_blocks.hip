@@ -47,7 +47,7 @@ constexpr int kTile = 32 * kWaves;        // rows per work-group where the waves
 constexpr int kMaxParts = 512;
 // sequences of a call whose parts are planned on the device, 64 per lane register
 constexpr int kPlanRegs = 4, kPlanned = 64 * kPlanRegs;
-constexpr float kNone = -1e30f;           // running maximum of a row that has seen nothing
+constexpr float kNone = -0x1.fffffep127f; // running maximum of a row that has seen nothing
 constexpr float kTop = 8.0f, kLag = 7.0f; // weights up to 2^(kTop + kLag)
 constexpr float kHuge = 0x1p21f;          // maxima from here on: far_exponent
 using Tile = RowTile<kBlk>;

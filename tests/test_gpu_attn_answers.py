@@ -22,8 +22,8 @@ def _run(q, cache, batch, scale, type):
     return mq.mq_paged_attn_blocks(x, *g, *i, scale).float().cpu().numpy()
 
 
-# (a winner's logit is 127 * 2^exponent; from 2^21 on it has a place of its own in the
-# kernels, from 2^29 on its last place in fp32 is more than a weight's range in fp16)
+# (a winner's logit is 127 * 2^exponent: from 2^21 on, in units of log2, the exponents have a
+# path of their own, from 2^29 on a last place in fp32 is more than a weight's range in fp16)
 @pytest.mark.parametrize("exponent", [15, 23, 33, 110])
 @pytest.mark.parametrize("type", TYPES)
 @pytest.mark.parametrize("D", [32, 96, 256])
@@ -31,5 +31,16 @@ def _run(q, cache, batch, scale, type):
 @pytest.mark.parametrize("keys", [1, 2])
 def test_winners_of_huge_logits(keys, new, D, type, exponent):
     k = aa.Known(D + new + exponent, D, new, exponent, keys)
+    off = k.off(_run(k.q, k.cache, k.batch, k.scale, type), type)
+    assert not off.any(), (off.mean(), np.argwhere(off)[:3])
+
+
+@pytest.mark.parametrize("exponent", [20, 60, 105])
+@pytest.mark.parametrize("type", TYPES)
+@pytest.mark.parametrize("D", [32, 256])
+@pytest.mark.parametrize("new", [1, 40])
+def test_all_logits_far_below_zero(new, D, type, exponent):
+    """Down to -2^112: a row that sees keys has their values, whatever their logits are."""
+    k = aa.Known(D + new + exponent, D, new, exponent, low=True)
     off = k.off(_run(k.q, k.cache, k.batch, k.scale, type), type)
     assert not off.any(), (off.mean(), np.argwhere(off)[:3])
