@@ -983,11 +983,14 @@ mq_status mq_rope_append_blocks(const void* q, int64_t ldq, const void* k, int64
  * (j > pos - window or j < sinks) that have a place in the cache, and its output is
  *   y_d = sum_j w_j v_jd v_scale[j] / sum_j w_j,
  *   w_j = exp(logit_scale * k_scale[j] * sum_d q_d k_jd)
- * with sums, maxima and weights in fp32.  Products take fp16 operands: codes and
- * bf16 and fp16 queries exactly, fp32 queries to 22 bits; weights to 11 bits (22
- * for fp32) of their own.  A row that sees nothing gets 0; a row of q that holds
- * an infinity or NaN gets NaN.  What lies in places that no row sees, scales
- * included, changes nothing.
+ * with sums, maxima and weights in fp32.  Products take fp16 operands: codes
+ * exactly; queries of 16 bits exactly, fp32 ones to 22 bits, but none closer
+ * than 2^-39 of the largest magnitude in its row and head; products w_j v_scale[j]
+ * to 11 bits (22 for fp32), but none closer than 2^-33 of the row's largest.
+ * Logits in units of log2, log2 of the value scale added, are rounded to fp32; a
+ * row with one past fp32's range may get NaN.  A row that sees nothing gets 0; a
+ * row of q that holds an infinity or NaN gets NaN.  What lies in places that no
+ * row sees, scales included, changes nothing.
  *   q      device, of `type`, row t at q + t * ldq: H heads of D
  *   y      device, of `type`, row t at y + t * ldy; must not overlap q or the
  *          cache

@@ -5,8 +5,9 @@
 // share a cache head lie next to each other) per set and walks over blocks of 64
 // key positions.  Both products run on the fp16 matrix instructions with fp32
 // sums: codes are exact in fp16, the queries of a row are scaled by a power of
-// two to below 2^15, which leaves bf16 and fp16 queries exact, fp32 ones as the
-// sum of two fp16 numbers (22 bits).  Scores come out transposed,
+// two to below 2^15, which leaves those of 16 bits exact down to 2^-31 of the row's
+// largest (below, as for all, a step is 2^-24), fp32 ones as the sum of two fp16
+// numbers (22 bits).  Scores come out transposed,
 //   C[key][row] = K[key][d] * Q[row][d],
 // a lane holding one row (lane & 15) and, the 16 keys of tile j being taken in
 // the order 16 (r >> 2) + 4 j + (r & 3), the 16 consecutive keys of one group: the
@@ -18,7 +19,8 @@
 // lane's weights by 1 / vs once per 16 keys.  The running maximum m is that of x +
 // log2 vs; it moves only when exceeded by 2^7, so weights stay below 2^15.
 // Weights are rounded to fp16 (11 bits, the outputs have 8 or 11), for fp32
-// outputs to the sum of two; statistics and outputs are fp32.
+// outputs to the sum of two (500 tokens over 16000: 293 us with two terms of queries
+// and weights, 171 with one); statistics and outputs are fp32.
 #include <algorithm>
 #include <cmath>
 

@@ -1,5 +1,6 @@
 """Attention over the cache with block scales: answers that are known without a softmax
-where logits are huge."""
+where logits are huge, errors of fp32 calls that only two fp16 terms keep small, rows of a
+wide range."""
 import numpy as np
 import pytest
 
@@ -44,3 +45,25 @@ def test_all_logits_far_below_zero(new, D, type, exponent):
     k = aa.Known(D + new + exponent, D, new, exponent, low=True)
     off = k.off(_run(k.q, k.cache, k.batch, k.scale, type), type)
     assert not off.any(), (off.mean(), np.argwhere(off)[:3])
+
+
+@pytest.mark.parametrize("D,new,L", [(64, 1, 700), (64, 1, 9011), (64, 40, 700), (144, 40, 700),
+                                     (176, 1, 900), (208, 40, 300), (240, 1, 700), (256, 1, 700),
+                                     (256, 40, 700), (256, 1, 20011), (256, 2, 20011),
+                                     (256, 24, 5000)])
+def test_fp32_rows_have_two_terms(D, new, L):
+    """Rows of their own, parts of them, tiles and their splits: errors as of 22 bits."""
+    q, cache, batch, scale = aa.spread_inputs(D, new, L)
+    want, _, _, _ = rs.attn_blocks(q, *cache, *batch, scale)
+    got = _run(q, cache, batch, scale, "float32")
+    off = aa.spread(got, want, aa.noise(q, *cache, *batch, scale))
+    assert off < aa.SPREAD, off
+
+
+@pytest.mark.parametrize("type", TYPES)
+@pytest.mark.parametrize("new", [1, 40])
+def test_rows_of_a_wide_range(new, type):
+    w = aa.Wide(type, new)
+    got = _run(w.q, w.cache, w.batch, w.scale, type)
+    off = np.abs(got - w.want) / w.tolerance(type)
+    assert (off <= 1).all(), off.max()
