@@ -1249,7 +1249,8 @@ hipError_t launch_main(const AttnArgs& p, const Split& c, hipStream_t s)
 {
     constexpr int KS = (ND + 3) / 4;
     if (c.waves > 0) {
-        if (c.slots * p.kv.G >= kMaxBlocks / 2) return hipErrorInvalidConfiguration;
+        // (kMaxBlocks is of 256 threads)
+        if (c.slots * p.kv.G * (c.waves / 4) >= kMaxBlocks) return hipErrorInvalidConfiguration;
         if constexpr (ND <= 8)
             if (c.waves == 8) return launch_rows<ND, N, 8>(p, s);
         return launch_rows<ND, N, 4>(p, s);
