@@ -1003,6 +1003,8 @@ mq_status mq_rope_append_blocks(const void* q, int64_t ldq, const void* k, int64
  *   sizes as in mq_paged_attn.  A call that takes 2^24 work-groups or more is
  *   MQ_ERR_UNSUPPORTED: at most T * (H / G) / 64 + B of them per cache head, or,
  *   with T * (H / G) <= 16 B, T * (H / G) / 16 + B per cache head.
+ *   One kernel serves a call, chosen by its rows per sequence on average: many
+ *   sequences of a token each and long chunks are faster in calls of their own.
  */
 mq_status mq_paged_attn_blocks(const void* q, int64_t ldq, int32_t type, int64_t T, int32_t H,
                                const mq_block_cache* cache, const mq_kv_batch* batch,

@@ -5,9 +5,10 @@
 // and counts the words of its range in LDS, so that order does not matter and a
 // word's penalties, bias and mask meet in one thread.  Only groups of eight words
 // with one that changes are read or written.  Latency bounds it: row lengths and the
-// history's first words in one round trip, then biases, logits and bias values: one
-// row of 256000 fp32 words, 9000 of history and 300 biases 6.9 us, 200 rows of 32000
-// bf16 ones with 1500 of history and masks 12.9 (8 MB).
+// history's first 2048 words in one round trip, a trip for each of the words that a thread
+// counts past them, then bias values and logits: one row of 256000 fp32 words, 9000 of
+// history and 300 biases 7.1 us, 200 rows of 32000 bf16 ones with 1500 of history and
+// masks 13.8 (8 MB).
 #include <algorithm>
 
 #include "adjust.h"
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs p, int32_t 
             if (vec_h) {
                 add_four(tid * 4, ahead);
                 for (uint32_t i = (kThreads + tid) * 4; i < (uint32_t)n; i += kThreads * 4)
-                    add_four(i, *reinterpret_cast<const int4*>(h + i));  // (whole fours of a row)
+                    add_four(i, *reinterpret_cast<const int4*>(h + i));  // (read word by word)
             } else {
                 for (uint32_t i = tid; i < (uint32_t)n; i += kThreads) add(i, h[i]);
             }
@@ -247,7 +248,7 @@ hipError_t launch(const AdjustArgs& p, hipStream_t s)
     const bool fits = (!p.history || p.cols <= kPackedCols) &&
                       (!p.bias_starts || p.bias_n <= kPackedBias);
     if (!fits) return launch_p<TYPE, false, 8>(p, s);
-    // (small ranges until there are two work-groups per CU: one row of 256000 words 7.0 us,
+    // (small ranges until there are two work-groups per CU: one row of 256000 words 7.1 us,
     // 9.1 with large ones; 200 rows of 32000 13.8, 18.1 with small ones)
     return p.M * p.V < (int64_t)kThreads * 8 * 512 ? launch_p<TYPE, true, 8>(p, s)
                                                    : launch_p<TYPE, true, 16>(p, s);

@@ -234,8 +234,10 @@ hipError_t launch_one_w(const OneArgs& a, hipStream_t s)
 // lane streams 16 weights of one channel of each tile per step and the MFMA multiplies
 // them with the tokens (zeros past the last), whose codes a wave reads once for all
 // tiles.  A load takes half a line of each row: read past the caches the lines came
-// twice (16 x 2048 -> 8192: 7.3 us, 6.4 through them).  What bounds it: the codes'
-// reads beside the weights', 2.7 TB/s of weights at that size.
+// twice (16 x 2048 -> 8192: 7.3 us, 6.4 through them).  What bounds it: reads, 2.7 TB/s of
+// weights at that size, whose waves have one round of loads; where there are more, a way
+// to memory for each, since a round is asked for behind the products of the one before
+// (16 x 5632 -> 2048 of 4 bits, three rounds: 7.1 us; 16384 -> 2048 of 8 bits, four: 14.4).
 template <int WBITS, int NWAVES, int R>
 __global__ __launch_bounds__(NWAVES * 64) void few_tokens_kernel(QLinearArgs p, TokenArgs t)
 {
